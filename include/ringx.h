@@ -12,8 +12,8 @@
  *  Layout     Tensors are contiguous [B, H, N, d] (d fastest), the scaled_dot_product_attention
  *             convention (Sec. VI calls RingX a drop-in for it).  lse and part_lse are fp32
  *             [.., B, H, Nq], natural logarithm of sum_j exp(scale * q_i . k_j).
- *  Semantics  Non-causal, no mask, no dropout.  Scores are scale * q . k (scale is an explicit
- *             argument; the paper's Eqs. (1)/(4) print no scale).
+ *  Semantics  Non-causal, no mask; dropout in the entry points named _drop alone.  Scores are
+ *             scale * q . k (scale is an explicit argument; the paper's Eqs. (1)/(4) print no scale).
  *  dtype      RINGX_BF16: q, k, v, out, dout are bf16; products on bf16 MFMA with fp32
  *             accumulation; softmax statistics, merge, lse and gradients in fp32.
  *             RINGX_FP32: every tensor fp32, fp32 arithmetic throughout.
@@ -68,7 +68,9 @@ typedef enum ringx_status RINGX_ENUM_BASE {
   RINGX_E_WORKSPACE = 6,   /* backward workspace missing or smaller than required            */
   RINGX_E_HIP = 7,         /* a HIP launch failed                                            */
   RINGX_E_ALIAS = 8,       /* an output overlaps an input                                    */
-  RINGX_E_SCRATCH = 9      /* B*H*Nq above RINGX_NOALLOC_MAX_ROWS (ringx_attn_bwd_noalloc)   */
+  RINGX_E_SCRATCH = 9,     /* B*H*Nq above RINGX_NOALLOC_MAX_ROWS (ringx_attn_bwd_noalloc)   */
+  RINGX_E_DROPOUT = 10,    /* dropout rate or mask position out of range (the _drop entries) */
+  RINGX_E_ROPE = 11        /* rotated sections, strides, position or eps (ringx_qkv_norm_rope) */
 } ringx_status;
 
 typedef enum ringx_dtype RINGX_ENUM_BASE { RINGX_FP32 = 0, RINGX_BF16 = 1 } ringx_dtype;
@@ -304,6 +306,115 @@ ringx_status ringx_attn_bwd_gqa(const void* q, const void* k, const void* v, con
                                 int64_t Nk, int64_t d, int64_t R, float scale, ringx_dtype dtype,
                                 int accumulate_dkv, void* workspace, size_t workspace_bytes,
                                 hipStream_t stream);
+
+/*
+ * Attention with dropout on its probabilities, forward and recompute backward (Sec. VI names RingX a
+ * drop-in for scaled_dot_product_attention, whose dropout_p this is):
+ *   out_i = sum_j (m_ij / kappa) P_ij v_j with P the softmax and lse its log-sum-exp, both as without
+ *   dropout;  dP_ij = (m_ij / kappa) dout_i . v_j;  D_i = dout_i . out_i;  dS_ij = P_ij (dP_ij - D_i);
+ *   dV_j = sum_i (m_ij / kappa) P_ij dout_i;  dK_j = scale sum_i dS_ij q_i;  dQ_i = scale sum_j dS_ij k_j.
+ * The mask m in {0, 1} is never stored: it is a function of the generator's state and of a score's
+ * place, formed again wherever it is needed, bitwise the same in every call, launch and ring step.
+ *   p     rate.  A score is dropped with probability T / 256, T = p 256 rounded to nearest (even), and
+ *         kappa = 1 - T / 256, so that out keeps its expectation at the rate used.  RINGX_E_DROPOUT
+ *         unless 0 <= p, T <= 255, and T > 0 where p > 0 (a rate that would round to none).
+ *   rng   two uint64 in device memory, 8-byte aligned: the seed and an offset (taken mod 2^32) that
+ *         tells draws apart (layers, steps).  Read by the kernels when they run: a captured graph
+ *         draws another mask once the memory holds other values; the backward needs the forward's.
+ *   q0    index of the first query on the mask's query axis, 0 <= q0, q0 + Nq <= 2^32;
+ *   key0  index of the first key on its key axis, a multiple of 32 from 0 to 2^36 - 32 - Nk.
+ *         Ranks or steps that hold parts of one sequence pass their parts' places.  Errors:
+ *         RINGX_E_DROPOUT.
+ * Mask: Philox4x32 with 7 rounds (Salmon et al., SC'11), key = the seed's low and high 32 bits, counter
+ * = (2 J + h, q0 + i, b H + head, offset).  Byte e of result word m is that of key 32 J + 8 m + 4 h + e
+ * (m, e < 4; h < 2; J counts 32-key blocks of the key axis); the score is kept iff it is >= T.
+ * Everything else as ringx_attn_fwd_gqa and ringx_attn_bwd_gqa (Hkv = H for multi-head attention),
+ * whose chunk count has no part here: keys are visited in blocks of 32 from the first, and p = 0 gives
+ * their results to rounding.
+ */
+ringx_status ringx_attn_fwd_drop(const void* q, const void* k, const void* v, void* out, float* lse,
+                                 int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                                 float scale, ringx_dtype dtype, float p, const uint64_t* rng,
+                                 int64_t q0, int64_t key0, hipStream_t stream);
+
+/* Backward of ringx_attn_fwd_drop, with its p, rng values, q0 and key0.  Workspace as ringx_attn_bwd
+ * (ringx_bwd_workspace_bytes with R = 1). */
+ringx_status ringx_attn_bwd_drop(const void* q, const void* k, const void* v, const void* out,
+                                 const void* dout, const float* lse, float* dq, float* dk, float* dv,
+                                 int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                                 float scale, ringx_dtype dtype, float p, const uint64_t* rng,
+                                 int64_t q0, int64_t key0, int accumulate_dkv, void* workspace,
+                                 size_t workspace_bytes, hipStream_t stream);
+
+/* ringx_attn_fwd_step and ringx_attn_bwd_step with dropout; key0 is the chunk's place on the mask's
+ * key axis.  delta [2,B,H,Nq] is that of ringx_bwd_preprocess_drop with the same p. */
+ringx_status ringx_attn_fwd_step_drop(const void* q, const void* k, const void* v, float* out_acc,
+                                      float* lse_acc, int64_t B, int64_t H, int64_t Nq, int64_t Nk,
+                                      int64_t d, float scale, ringx_dtype dtype, int first, float p,
+                                      const uint64_t* rng, int64_t q0, int64_t key0,
+                                      hipStream_t stream);
+ringx_status ringx_attn_bwd_step_drop(const void* q, const void* k, const void* v, const void* dout,
+                                      const float* lse, const float* delta, float* dq_acc, float* dk,
+                                      float* dv, int64_t B, int64_t H, int64_t Nq, int64_t Nk,
+                                      int64_t d, float scale, ringx_dtype dtype, int accumulate_dq,
+                                      int accumulate_dkv, float p, const uint64_t* rng, int64_t q0,
+                                      int64_t key0, hipStream_t stream);
+
+/* ringx_bwd_preprocess for the steps with dropout: delta[0] = kappa D_i, delta[1] = nl_i. */
+ringx_status ringx_bwd_preprocess_drop(const void* out, const void* dout, const float* lse,
+                                       float* delta, int64_t B, int64_t H, int64_t Nq, int64_t d,
+                                       ringx_dtype dtype, float p, hipStream_t stream);
+
+/*
+ * From a packed projection to the attention's operands in one pass: RMS norm of every query and key
+ * head, rotation of its dims by the token's position, and the layout [B, heads, N, d].
+ *   qkv   [B, N, (H + 2 Hkv) d] (dtype): of every token H query heads, Hkv key heads, Hkv value heads.
+ *         Token n of batch b starts at element b batch_stride + n token_stride (the stride of a
+ *         dimension of size 1 is not looked at; neither is negative); the row itself is contiguous.
+ *   q [B,H,N,d], k, v [B,Hkv,N,d] (dtype), contiguous -- outputs.
+ *   norm: y_i = x_i r w_i, r = (mean_i x_i^2 + eps)^(-1/2) over the head's d dims; q_weight and
+ *         k_weight w [d] fp32, either or both NULL for 1.  eps > 0.  fp32 arithmetic; the squares'
+ *         sum has to stay in fp32's range.
+ *   rotation: axes = 1 .. 3 consecutive sections of rot[a] dims (even, >= 0, together <= d); in the
+ *         section of n = rot[a] / 2 pairs from dim o on, dims o + i and o + n + i become
+ *           y_{o+i} cos t - y_{o+n+i} sin t  and  y_{o+n+i} cos t + y_{o+i} sin t,
+ *         t = position_a f_i; the dims after the sections are left as they are.  freqs: the f_i in
+ *         radians of all sections, one after the other, fp64.  Angles are formed in 64 bits.
+ *   pos   [N, axes] int32 shared by the batch (pos_batch_stride = 0) or [B, N, axes]
+ *         (pos_batch_stride = N axes); NULL with axes = 1: positions pos0 + n, |pos0| <= 2^40.
+ *   v is copied.
+ * d as the attention takes it (bf16: 64, 128; fp32: 1 .. 128); Hkv divides H.  bf16 strides are
+ * multiples of 8 elements (RINGX_E_ALIGN); fp32 takes any.  Outputs overlap no input.
+ */
+ringx_status ringx_qkv_norm_rope(const void* qkv, int64_t batch_stride, int64_t token_stride,
+                                 const float* q_weight, const float* k_weight, const double* freqs,
+                                 const int32_t* pos, int64_t pos_batch_stride, int64_t pos0,
+                                 int64_t axes, const int64_t* rot, void* q, void* k, void* v,
+                                 int64_t B, int64_t N, int64_t H, int64_t Hkv, int64_t d, float eps,
+                                 ringx_dtype dtype, hipStream_t stream);
+
+/*
+ * Backward of ringx_qkv_norm_rope.  dq [B,H,N,d], dk, dv [B,Hkv,N,d] fp32, contiguous: the gradients of
+ * its outputs, as the attention's backward gives them.  With g the gradient turned back by the angle:
+ *   dqkv [B, N, (H + 2 Hkv) d] (dtype), contiguous: dx_i = r (g_i w_i - x_i r mean_j(g_j w_j x_j r));
+ *   dq_weight, dk_weight [d] fp32: sum over batch, tokens and heads of g_i x_i r; each is given iff
+ *   its weight is (RINGX_E_NULLPTR otherwise).
+ * All overwritten, bitwise reproducible.  workspace: ringx_qkv_norm_rope_bwd_workspace_bytes(...) bytes,
+ * 16-byte aligned, contents ignored; not needed without weights.
+ */
+ringx_status ringx_qkv_norm_rope_bwd(const void* qkv, int64_t batch_stride, int64_t token_stride,
+                                     const float* dq, const float* dk, const float* dv,
+                                     const float* q_weight, const float* k_weight,
+                                     const double* freqs, const int32_t* pos,
+                                     int64_t pos_batch_stride, int64_t pos0, int64_t axes,
+                                     const int64_t* rot, void* dqkv, float* dq_weight,
+                                     float* dk_weight, int64_t B, int64_t N, int64_t H, int64_t Hkv,
+                                     int64_t d, float eps, ringx_dtype dtype, void* workspace,
+                                     size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of its workspace (0 if the arguments are invalid).  Host only. */
+size_t ringx_qkv_norm_rope_bwd_workspace_bytes(int64_t B, int64_t N, int64_t H, int64_t Hkv, int64_t d,
+                                               ringx_dtype dtype);
 
 /*
  * One fidelity mode of the Turbulence Transformer's multi-fidelity input (Sec. III-B: the

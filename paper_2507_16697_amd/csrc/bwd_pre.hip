@@ -19,7 +19,7 @@ template <int D>
 __global__ __launch_bounds__(kPreThreads) void bwd_pre_bf16_kernel(
     const __bf16* __restrict__ out, const __bf16* __restrict__ dout,
     const float* __restrict__ lse, float* __restrict__ delta, float* __restrict__ nl,
-    int64_t rows) {
+    int64_t rows, float d_factor) {
   constexpr int kTpr = D / 8;
   const int64_t idx = (int64_t)blockIdx.x * kPreThreads + threadIdx.x;
   const int64_t row = idx / kTpr;
@@ -37,7 +37,7 @@ __global__ __launch_bounds__(kPreThreads) void bwd_pre_bf16_kernel(
 #pragma unroll
   for (int off = kTpr / 2; off > 0; off >>= 1) s += __shfl_xor(s, off, kTpr);
   if (row < rows && part == 0) {
-    delta[row] = s;
+    delta[row] = s * d_factor;
     nl[row] = lse[row] * -kLog2e;
   }
 }
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kPreThreads) void bwd_pre_bf16_kernel(
 constexpr int kF32Tpr = 16;
 __global__ __launch_bounds__(kPreThreads) void bwd_pre_f32_kernel(
     const float* __restrict__ out, const float* __restrict__ dout, const float* __restrict__ lse,
-    float* __restrict__ delta, float* __restrict__ nl, int64_t rows, int d) {
+    float* __restrict__ delta, float* __restrict__ nl, int64_t rows, int d, float d_factor) {
   const int part = threadIdx.x % kF32Tpr;
   for (int64_t row0 = (int64_t)blockIdx.x * (kPreThreads / kF32Tpr); row0 < rows;
        row0 += (int64_t)gridDim.x * (kPreThreads / kF32Tpr)) {
@@ -58,7 +58,7 @@ __global__ __launch_bounds__(kPreThreads) void bwd_pre_f32_kernel(
 #pragma unroll
     for (int off = kF32Tpr / 2; off > 0; off >>= 1) s += __shfl_xor(s, off, kF32Tpr);
     if (row < rows && part == 0) {
-      delta[row] = s;
+      delta[row] = s * d_factor;
       nl[row] = lse[row] * -kLog2e;
     }
   }
@@ -74,18 +74,18 @@ hipError_t launch_bwd_pre(const BwdArgs& a, bool bf16) {
     if (a.d == 128)
       hipLaunchKernelGGL(bwd_pre_bf16_kernel<128>, grid, dim3(kPreThreads), 0, a.stream,
                          (const __bf16*)a.out, (const __bf16*)a.dout, a.lse, a.delta, a.nl,
-                         rows);
+                         rows, a.d_factor);
     else
       hipLaunchKernelGGL(bwd_pre_bf16_kernel<64>, grid, dim3(kPreThreads), 0, a.stream,
                          (const __bf16*)a.out, (const __bf16*)a.dout, a.lse, a.delta, a.nl,
-                         rows);
+                         rows, a.d_factor);
   } else {
     // at most 2^22 workgroups (2^30 threads); they take further rows beyond that
     const int64_t wgs = (rows * kF32Tpr + kPreThreads - 1) / kPreThreads;
     const dim3 grid((uint32_t)(wgs < (1 << 22) ? wgs : 1 << 22));
     hipLaunchKernelGGL(bwd_pre_f32_kernel, grid, dim3(kPreThreads), 0, a.stream,
                        (const float*)a.out, (const float*)a.dout, a.lse, a.delta, a.nl, rows,
-                       (int)a.d);
+                       (int)a.d, a.d_factor);
   }
   return hipGetLastError();
 }

@@ -1,0 +1,76 @@
+// Dropout of attention probabilities by a counter-based generator: the mask of a score is a function
+// of its place and of the generator's state (seed, offset), so it is never stored: the backward, a
+// ring step and a launch that is cut another way form the same bits again.
+//
+// Generator: Philox4x32 (J. K. Salmon, M. A. Moraes, R. O. Dror, D. E. Shaw, "Parallel random
+// numbers: as easy as 1, 2, 3", SC'11) with 7 rounds, the fewest that pass the paper's whole test
+// battery.  Key: the seed.  Counter: (16-key group, query, query head of B * H, offset mod 2^32).
+// A group is half of a 32-key block: group 2 J + h holds keys 32 J + 8 m + 4 h + e, m, e < 4, and
+// byte e of result word m is the score's.  These are the 16 keys of a 32 x 32 score tile that one
+// lane holds for its query, so that in the query-stationary kernels a lane's 16 scores take one
+// generator call and no exchange.  A score is kept iff its byte is at least thr = round(256 p), so
+// the rate is a multiple of 1/256: a byte per score makes the generator a quarter of the vector work
+// of a score; 16 bits would double that.
+#pragma once
+
+#include "ringx_device.h"
+#include "ringx_kernels.h"
+
+#include <type_traits>
+
+namespace ringx {
+
+struct NoDrop {};   // kernels without dropout
+
+// The fields, 0 without dropout.
+__device__ __forceinline__ const uint64_t* drop_rng(const NoDrop&) { return nullptr; }
+__device__ __forceinline__ const uint64_t* drop_rng(const Drop& d) { return d.rng; }
+__device__ __forceinline__ uint32_t drop_q0(const NoDrop&) { return 0; }
+__device__ __forceinline__ uint32_t drop_q0(const Drop& d) { return d.q0; }
+__device__ __forceinline__ uint32_t drop_kb0(const NoDrop&) { return 0; }
+__device__ __forceinline__ uint32_t drop_kb0(const Drop& d) { return d.kb0; }
+__device__ __forceinline__ float drop_inv_keep(const NoDrop&) { return 1.f; }
+__device__ __forceinline__ float drop_inv_keep(const Drop& d) { return d.inv_keep; }
+
+template <class DROP>
+constexpr bool kHasDrop = !std::is_same_v<DROP, NoDrop>;
+
+// The generator's state as the kernels hold it (wave-uniform).
+struct DropKey {
+  uint32_t k0 = 0, k1 = 0, off = 0;
+  __device__ __forceinline__ explicit DropKey(const uint64_t* rng) {
+    if (!rng) return;
+    k0 = __builtin_amdgcn_readfirstlane((uint32_t)rng[0]);
+    k1 = __builtin_amdgcn_readfirstlane((uint32_t)(rng[0] >> 32));
+    off = __builtin_amdgcn_readfirstlane((uint32_t)rng[1]);
+  }
+};
+
+__device__ __forceinline__ u32x4 drop_bytes(uint32_t group, uint32_t query, uint32_t head,
+                                            const DropKey& key) {
+  uint32_t c0 = group, c1 = query, c2 = head, c3 = key.off, k0 = key.k0, k1 = key.k1;
+#pragma unroll
+  for (int r = 0; r < 7; ++r) {
+    const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+    c1 = (uint32_t)b;
+    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    c3 = (uint32_t)a;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return u32x4{c0, c1, c2, c3};
+}
+
+// Word m of four.
+__device__ __forceinline__ uint32_t drop_word(const u32x4& w, uint32_t m) {
+  const uint32_t lo = m & 1 ? w[1] : w[0], hi = m & 1 ? w[3] : w[2];
+  return m & 2 ? hi : lo;
+}
+
+// Whether score i (0 .. 15, in the order of the tile's registers) is kept.
+__device__ __forceinline__ bool drop_keep(const u32x4& w, int i, uint32_t thr) {
+  return ((w[i >> 2] >> (8 * (i & 3))) & 255u) >= thr;
+}
+
+}  // namespace ringx

@@ -86,6 +86,10 @@ const char* ringx_status_str(int status) {
     case RINGX_E_SCRATCH:
       return "B * H * Nq exceeds the fixed scratch of ringx_attn_bwd_noalloc "
              "(RINGX_NOALLOC_MAX_ROWS rows)";
+    case RINGX_E_DROPOUT:
+      return "dropout rate not in {0} or [1/512, 511/512], or mask position out of range or not a "
+             "multiple of 32 keys";
+    case RINGX_E_ROPE: return "invalid rotated sections, strides, position or eps";
   }
   return "unknown status";
 }
@@ -686,6 +690,349 @@ ringx_status ringx_attn_bwd_noalloc(const void* q, const void* k, const void* v,
   static_assert(RINGX_NOALLOC_MAX_ROWS % 64 == 0, "whole 256-byte blocks");
   return bwd_impl(q, k, v, out, dout, lse, dq, dk, dv, B, H, H, Nq, Nk, d, R, scale, dtype,
                   accumulate_dkv, ws, sizeof(float) * 2 * (size_t)RINGX_NOALLOC_MAX_ROWS, stream);
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------------------------------------
+// Attention with dropout
+
+namespace {
+
+// The launch's view of the dropout arguments.
+ringx_status make_drop(float p, const uint64_t* rng, int64_t q0, int64_t key0, int64_t Nq, int64_t Nk,
+                       ringx::Drop* out) {
+  if (!rng) return RINGX_E_NULLPTR;
+  if ((reinterpret_cast<uintptr_t>(rng) & 7u) != 0) return RINGX_E_ALIGN;
+  if (!(p >= 0.f && p < 1.f)) return RINGX_E_DROPOUT;
+  const long thr = std::lrint(256.0 * (double)p);
+  if (thr > 255 || (thr == 0 && p > 0.f)) return RINGX_E_DROPOUT;
+  // query and key-group indices of the generator are 32-bit
+  if (q0 < 0 || q0 > (int64_t(1) << 32) - Nq) return RINGX_E_DROPOUT;
+  if (key0 < 0 || key0 % 32 != 0 || key0 > (int64_t(1) << 36) - 32 - Nk) return RINGX_E_DROPOUT;
+  out->rng = rng, out->thr = (uint32_t)thr, out->inv_keep = (float)(256.0 / (double)(256 - thr));
+  out->q0 = (uint32_t)q0, out->kb0 = (uint32_t)(key0 / 32);
+  return RINGX_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+ringx_status ringx_attn_fwd_drop(const void* q, const void* k, const void* v, void* out, float* lse,
+                                 int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                                 float scale, ringx_dtype dtype, float p, const uint64_t* rng,
+                                 int64_t q0, int64_t key0, hipStream_t stream) {
+  if (!q || !k || !v || !out || !lse) return RINGX_E_NULLPTR;
+  if (Hkv < 1 || H < 1 || H % Hkv != 0) return RINGX_E_SHAPE;
+  ringx_status st = check_dims(B, H, Nq, Nk, d, 1, scale, dtype);
+  if (st != RINGX_OK) return st;
+  ringx::Drop drop;
+  st = make_drop(p, rng, q0, key0, Nq, Nk, &drop);
+  if (st != RINGX_OK) return st;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(lse))
+    return RINGX_E_ALIGN;
+  const int64_t es = esize(dtype), bh = B * H, bkv = B * Hkv;
+  const Span ins[] = {span(q, bh * Nq * d * es), span(k, bkv * Nk * d * es),
+                      span(v, bkv * Nk * d * es), span(rng, 16)};
+  const Span so = span(out, bh * Nq * d * es), sl = span(lse, bh * Nq * 4);
+  for (const Span& i : ins)
+    if (overlap(so, i) || overlap(sl, i)) return RINGX_E_ALIAS;
+  if (overlap(so, sl)) return RINGX_E_ALIAS;
+  ringx::FwdArgs a;
+  a.q = q, a.k = k, a.v = v, a.out = out, a.lse = lse;
+  a.BH = bh, a.Nq = Nq, a.Nk = Nk, a.d = d, a.R = 1, a.scale = scale, a.stream = stream;
+  a.H = H, a.G = H / Hkv;
+  return hip_status(dtype == RINGX_BF16
+                        ? ringx::launch_fwd_drop_bf16(a, ringx::FwdMode::kFused, drop)
+                        : ringx::launch_fwd_drop_f32(a, ringx::FwdMode::kFused, drop));
+}
+
+ringx_status ringx_attn_fwd_step_drop(const void* q, const void* k, const void* v, float* out_acc,
+                                      float* lse_acc, int64_t B, int64_t H, int64_t Nq, int64_t Nk,
+                                      int64_t d, float scale, ringx_dtype dtype, int first, float p,
+                                      const uint64_t* rng, int64_t q0, int64_t key0,
+                                      hipStream_t stream) {
+  if (!q || !k || !v || !out_acc || !lse_acc) return RINGX_E_NULLPTR;
+  ringx_status st = check_dims(B, H, Nq, Nk, d, 1, scale, dtype);
+  if (st != RINGX_OK) return st;
+  ringx::Drop drop;
+  st = make_drop(p, rng, q0, key0, Nq, Nk, &drop);
+  if (st != RINGX_OK) return st;
+  for (const void* x : {q, k, v, (const void*)out_acc, (const void*)lse_acc})
+    if (!aligned16(x)) return RINGX_E_ALIGN;
+  const int64_t es = esize(dtype), bh = B * H;
+  const Span ins[] = {span(q, bh * Nq * d * es), span(k, bh * Nk * d * es),
+                      span(v, bh * Nk * d * es), span(rng, 16)};
+  const Span so = span(out_acc, bh * Nq * d * 4), sl = span(lse_acc, bh * Nq * 4);
+  for (const Span& i : ins)
+    if (overlap(so, i) || overlap(sl, i)) return RINGX_E_ALIAS;
+  if (overlap(so, sl)) return RINGX_E_ALIAS;
+  ringx::FwdArgs a;
+  a.q = q, a.k = k, a.v = v, a.acc_out = out_acc, a.acc_lse = lse_acc, a.first = first != 0;
+  a.BH = bh, a.Nq = Nq, a.Nk = Nk, a.d = d, a.R = 1, a.scale = scale, a.stream = stream;
+  a.H = H, a.G = 1;
+  return hip_status(dtype == RINGX_BF16
+                        ? ringx::launch_fwd_drop_bf16(a, ringx::FwdMode::kStep, drop)
+                        : ringx::launch_fwd_drop_f32(a, ringx::FwdMode::kStep, drop));
+}
+
+ringx_status ringx_bwd_preprocess_drop(const void* out, const void* dout, const float* lse,
+                                       float* delta, int64_t B, int64_t H, int64_t Nq, int64_t d,
+                                       ringx_dtype dtype, float p, hipStream_t stream) {
+  if (!out || !dout || !lse || !delta) return RINGX_E_NULLPTR;
+  ringx_status st = check_dims(B, H, Nq, 1, d, 1, 1.0f, dtype);
+  if (st != RINGX_OK) return st;
+  ringx::Drop drop;
+  const uint64_t unused[2] = {0, 0};
+  st = make_drop(p, unused, 0, 0, Nq, 1, &drop);
+  if (st != RINGX_OK) return st;
+  for (const void* x : {out, dout, (const void*)lse, (const void*)delta})
+    if (!aligned16(x)) return RINGX_E_ALIGN;
+  const int64_t es = esize(dtype), bh = B * H;
+  const Span sd = span(delta, 2 * bh * Nq * 4);
+  if (overlap(sd, span(out, bh * Nq * d * es)) || overlap(sd, span(dout, bh * Nq * d * es)) ||
+      overlap(sd, span(lse, bh * Nq * 4)))
+    return RINGX_E_ALIAS;
+  ringx::BwdArgs a;
+  a.out = out, a.dout = dout, a.lse = lse, a.delta = delta, a.nl = delta + bh * Nq;
+  a.BH = bh, a.Nq = Nq, a.Nk = 1, a.d = d, a.R = 1, a.stream = stream, a.H = H, a.G = 1;
+  a.d_factor = (float)(256 - drop.thr) / 256.f;
+  return hip_status(ringx::launch_bwd_pre(a, dtype == RINGX_BF16));
+}
+
+}  // extern "C"
+
+namespace {
+
+// The stages after the preprocess.
+hipError_t launch_bwd_drop(const ringx::BwdArgs& a, bool bf16, const ringx::Drop& drop) {
+  if (!bf16) return ringx::launch_bwd_drop_f32(a, drop);
+  const hipError_t e = ringx::launch_bwd_dkdv_drop_bf16(a, drop);
+  return e != hipSuccess ? e : ringx::launch_bwd_dq_drop_bf16(a, drop);
+}
+
+}  // namespace
+
+extern "C" {
+
+ringx_status ringx_attn_bwd_drop(const void* q, const void* k, const void* v, const void* out,
+                                 const void* dout, const float* lse, float* dq, float* dk, float* dv,
+                                 int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
+                                 float scale, ringx_dtype dtype, float p, const uint64_t* rng,
+                                 int64_t q0, int64_t key0, int accumulate_dkv, void* workspace,
+                                 size_t workspace_bytes, hipStream_t stream) {
+  if (!q || !k || !v || !out || !dout || !lse || !dq || !dk || !dv) return RINGX_E_NULLPTR;
+  if (Hkv < 1 || H < 1 || H % Hkv != 0) return RINGX_E_SHAPE;
+  ringx_status st = check_dims(B, H, Nq, Nk, d, 1, scale, dtype);
+  if (st != RINGX_OK) return st;
+  ringx::Drop drop;
+  st = make_drop(p, rng, q0, key0, Nq, Nk, &drop);
+  if (st != RINGX_OK) return st;
+  const size_t need = ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, 1, dtype);
+  if (!workspace || workspace_bytes < need) return RINGX_E_WORKSPACE;
+  for (const void* x : {q, k, v, out, dout, (const void*)lse, (const void*)dq, (const void*)dk,
+                        (const void*)dv, (const void*)workspace})
+    if (!aligned16(x)) return RINGX_E_ALIGN;
+  const int64_t es = esize(dtype), bh = B * H, bkv = B * Hkv;
+  const Span ins[] = {span(q, bh * Nq * d * es),    span(k, bkv * Nk * d * es),
+                      span(v, bkv * Nk * d * es),   span(out, bh * Nq * d * es),
+                      span(dout, bh * Nq * d * es), span(lse, bh * Nq * 4), span(rng, 16)};
+  const Span outs[] = {span(dq, bh * Nq * d * 4), span(dk, bkv * Nk * d * 4),
+                       span(dv, bkv * Nk * d * 4), span(workspace, (int64_t)need)};
+  for (int i = 0; i < 4; ++i) {
+    for (const Span& x : ins)
+      if (overlap(outs[i], x)) return RINGX_E_ALIAS;
+    for (int j = i + 1; j < 4; ++j)
+      if (overlap(outs[i], outs[j])) return RINGX_E_ALIAS;
+  }
+  float* delta = static_cast<float*>(workspace);
+  ringx::BwdArgs a;
+  a.q = q, a.k = k, a.v = v, a.out = out, a.dout = dout, a.lse = lse;
+  a.dq = dq, a.dk = dk, a.dv = dv, a.delta = delta, a.nl = delta + bh * Nq;
+  a.BH = bh, a.Nq = Nq, a.Nk = Nk, a.d = d, a.R = 1, a.scale = scale;
+  a.H = H, a.G = H / Hkv;
+  a.accumulate_dkv = accumulate_dkv != 0, a.stream = stream;
+  a.d_factor = (float)(256 - drop.thr) / 256.f;
+  const bool bf16 = dtype == RINGX_BF16;
+  if (ringx::launch_bwd_pre(a, bf16) != hipSuccess) return RINGX_E_HIP;
+  return hip_status(launch_bwd_drop(a, bf16, drop));
+}
+
+ringx_status ringx_attn_bwd_step_drop(const void* q, const void* k, const void* v, const void* dout,
+                                      const float* lse, const float* delta, float* dq_acc, float* dk,
+                                      float* dv, int64_t B, int64_t H, int64_t Nq, int64_t Nk,
+                                      int64_t d, float scale, ringx_dtype dtype, int accumulate_dq,
+                                      int accumulate_dkv, float p, const uint64_t* rng, int64_t q0,
+                                      int64_t key0, hipStream_t stream) {
+  if (!dq_acc || !dk || !dv) return RINGX_E_NULLPTR;
+  const int64_t bh = B * H;
+  const std::initializer_list<Span> outs = {span(dq_acc, bh * Nq * d * 4), span(dk, bh * Nk * d * 4),
+                                            span(dv, bh * Nk * d * 4)};
+  ringx_status st = check_bwd_stage(q, k, v, dout, lse, delta, outs, B, H, Nq, Nk, d, 1, scale, dtype);
+  if (st != RINGX_OK) return st;
+  ringx::Drop drop;
+  st = make_drop(p, rng, q0, key0, Nq, Nk, &drop);
+  if (st != RINGX_OK) return st;
+  for (const Span& o : outs)
+    if (overlap(o, span(rng, 16))) return RINGX_E_ALIAS;
+  ringx::BwdArgs a;
+  a.q = q, a.k = k, a.v = v, a.dout = dout, a.lse = lse, a.delta = const_cast<float*>(delta);
+  a.nl = const_cast<float*>(delta) + bh * Nq;
+  a.dq = dq_acc, a.dk = dk, a.dv = dv;
+  a.BH = bh, a.Nq = Nq, a.Nk = Nk, a.d = d, a.R = 1, a.scale = scale, a.H = H, a.G = 1;
+  a.accumulate_dkv = accumulate_dkv != 0, a.accumulate_dq = accumulate_dq != 0, a.stream = stream;
+  return hip_status(launch_bwd_drop(a, dtype == RINGX_BF16, drop));
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------------------------------------
+// Norm and rotation between a packed projection and the attention's operands
+
+namespace {
+
+// What both directions check; fills everything but the tensors of one direction.
+ringx_status make_rope(const void* qkv, int64_t batch_stride, int64_t token_stride,
+                       const float* q_weight, const float* k_weight, const double* freqs,
+                       const int32_t* pos, int64_t pos_batch_stride, int64_t pos0, int64_t axes,
+                       const int64_t* rot, int64_t B, int64_t N, int64_t H, int64_t Hkv, int64_t d,
+                       float eps, ringx_dtype dtype, hipStream_t stream, ringx::RopeArgs* a,
+                       Span* sx) {
+  if (!qkv || !rot) return RINGX_E_NULLPTR;
+  if (B < 1 || N < 1 || H < 1 || Hkv < 1 || H % Hkv != 0 || H > (1 << 20)) return RINGX_E_SHAPE;
+  if (dtype != RINGX_BF16 && dtype != RINGX_FP32) return RINGX_E_UNSUPPORTED;
+  if (dtype == RINGX_BF16 && d != 64 && d != 128) return RINGX_E_UNSUPPORTED;
+  if (d < 1 || d > 128) return RINGX_E_UNSUPPORTED;
+  const int64_t cols = (H + 2 * Hkv) * d;
+  int64_t rows, x;
+  if (!mul_ok(B, N, &rows) || !mul_ok(rows, cols, &x)) return RINGX_E_SHAPE;
+  if (axes < 1 || axes > 3) return RINGX_E_ROPE;
+  int64_t turned = 0;
+  for (int64_t i = 0; i < axes; ++i) {
+    if (rot[i] < 0 || rot[i] > d || rot[i] % 2 != 0) return RINGX_E_ROPE;
+    turned += rot[i];
+  }
+  if (turned > d) return RINGX_E_ROPE;
+  if (turned > 0 && !freqs) return RINGX_E_NULLPTR;
+  if (!(std::isfinite(eps) && eps > 0.f)) return RINGX_E_ROPE;
+  if (token_stride < 0 || batch_stride < 0) return RINGX_E_ROPE;
+  int64_t tb = 0, tt = 0;
+  if ((B > 1 && !mul_ok(B - 1, batch_stride, &tb)) || (N > 1 && !mul_ok(N - 1, token_stride, &tt)))
+    return RINGX_E_SHAPE;
+  if (!pos && axes != 1) return RINGX_E_NULLPTR;
+  if (pos0 < -(int64_t(1) << 40) || pos0 > (int64_t(1) << 40)) return RINGX_E_ROPE;
+  if (pos && pos_batch_stride != 0 && pos_batch_stride != N * axes) return RINGX_E_ROPE;
+  if (!aligned16(qkv) || !aligned16(q_weight) || !aligned16(k_weight) || !aligned16(freqs) ||
+      !aligned16(pos))
+    return RINGX_E_ALIGN;
+  const int64_t es = esize(dtype);
+  const bool pieces = d * es % 16 == 0 && (N == 1 || token_stride * es % 16 == 0) &&
+                      (B == 1 || batch_stride * es % 16 == 0);
+  if (dtype == RINGX_BF16 && !pieces) return RINGX_E_ALIGN;
+  *sx = span(qkv, (tb + tt + cols) * es);
+  a->x = qkv, a->bs = B > 1 ? batch_stride : 0, a->ts = N > 1 ? token_stride : 0;
+  a->qw = q_weight, a->kw = k_weight, a->freqs = freqs;
+  a->pos = pos, a->pos_bs = pos_batch_stride, a->pos0 = pos0;
+  a->B = B, a->N = N, a->H = (int)H, a->Hkv = (int)Hkv, a->d = (int)d;
+  a->axes = (int)axes;
+  for (int64_t i = 0; i < axes; ++i) a->rot[i] = (int)rot[i];
+  a->eps = eps, a->bf16 = dtype == RINGX_BF16, a->vec = pieces, a->stream = stream;
+  return RINGX_OK;
+}
+
+// Inputs besides the projection that an output must not touch.
+bool overlaps_small_inputs(Span o, const ringx::RopeArgs& a) {
+  int64_t turned = 0;
+  for (int i = 0; i < a.axes; ++i) turned += a.rot[i];
+  return (a.qw && overlap(o, span(a.qw, 4 * a.d))) || (a.kw && overlap(o, span(a.kw, 4 * a.d))) ||
+         (turned > 0 && overlap(o, span(a.freqs, 4 * turned))) ||
+         (a.pos && overlap(o, span(a.pos, ((a.pos_bs ? a.B : 1) * a.N) * a.axes * 4)));
+}
+
+}  // namespace
+
+extern "C" {
+
+ringx_status ringx_qkv_norm_rope(const void* qkv, int64_t batch_stride, int64_t token_stride,
+                                 const float* q_weight, const float* k_weight, const double* freqs,
+                                 const int32_t* pos, int64_t pos_batch_stride, int64_t pos0,
+                                 int64_t axes, const int64_t* rot, void* q, void* k, void* v,
+                                 int64_t B, int64_t N, int64_t H, int64_t Hkv, int64_t d, float eps,
+                                 ringx_dtype dtype, hipStream_t stream) {
+  if (!q || !k || !v) return RINGX_E_NULLPTR;
+  ringx::RopeArgs a;
+  Span sx{};
+  const ringx_status st =
+      make_rope(qkv, batch_stride, token_stride, q_weight, k_weight, freqs, pos, pos_batch_stride,
+                pos0, axes, rot, B, N, H, Hkv, d, eps, dtype, stream, &a, &sx);
+  if (st != RINGX_OK) return st;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return RINGX_E_ALIGN;
+  const int64_t row = B * N * d * esize(dtype);
+  const Span outs[] = {span(q, H * row), span(k, Hkv * row), span(v, Hkv * row)};
+  for (int i = 0; i < 3; ++i) {
+    if (overlap(outs[i], sx) || overlaps_small_inputs(outs[i], a)) return RINGX_E_ALIAS;
+    for (int j = i + 1; j < 3; ++j)
+      if (overlap(outs[i], outs[j])) return RINGX_E_ALIAS;
+  }
+  a.q = q, a.k = k, a.v = v;
+  return hip_status(ringx::launch_norm_rope(a, false));
+}
+
+size_t ringx_qkv_norm_rope_bwd_workspace_bytes(int64_t B, int64_t N, int64_t H, int64_t Hkv, int64_t d,
+                                               ringx_dtype dtype) {
+  if (B < 1 || N < 1 || H < 1 || Hkv < 1 || H % Hkv != 0 || H > (1 << 20)) return 0;
+  if (dtype != RINGX_BF16 && dtype != RINGX_FP32) return 0;
+  if (d < 1 || d > 128 || (dtype == RINGX_BF16 && d != 64 && d != 128)) return 0;
+  int64_t rows, x;
+  if (!mul_ok(B, N, &rows) || !mul_ok(rows, (H + 2 * Hkv) * d, &x)) return 0;
+  const int lanes = ringx::rope_lanes(d, dtype == RINGX_BF16);
+  const ringx::RopeGrid g = ringx::rope_grid(rows, (int)(H + 2 * Hkv), 64 / lanes, true);
+  return static_cast<size_t>((g.x * g.y * 2 * d * 4 + 255) / 256 * 256);
+}
+
+ringx_status ringx_qkv_norm_rope_bwd(const void* qkv, int64_t batch_stride, int64_t token_stride,
+                                     const float* dq, const float* dk, const float* dv,
+                                     const float* q_weight, const float* k_weight,
+                                     const double* freqs, const int32_t* pos,
+                                     int64_t pos_batch_stride, int64_t pos0, int64_t axes,
+                                     const int64_t* rot, void* dqkv, float* dq_weight,
+                                     float* dk_weight, int64_t B, int64_t N, int64_t H, int64_t Hkv,
+                                     int64_t d, float eps, ringx_dtype dtype, void* workspace,
+                                     size_t workspace_bytes, hipStream_t stream) {
+  if (!dq || !dk || !dv || !dqkv) return RINGX_E_NULLPTR;
+  // a weight and its gradient come together
+  if (!q_weight != !dq_weight || !k_weight != !dk_weight) return RINGX_E_NULLPTR;
+  ringx::RopeArgs a;
+  Span sx{};
+  const ringx_status st =
+      make_rope(qkv, batch_stride, token_stride, q_weight, k_weight, freqs, pos, pos_batch_stride,
+                pos0, axes, rot, B, N, H, Hkv, d, eps, dtype, stream, &a, &sx);
+  if (st != RINGX_OK) return st;
+  const bool weights = q_weight || k_weight;
+  const size_t need =
+      weights ? ringx_qkv_norm_rope_bwd_workspace_bytes(B, N, H, Hkv, d, dtype) : 0;
+  if (weights && (!workspace || workspace_bytes < need)) return RINGX_E_WORKSPACE;
+  for (const void* x : {(const void*)dq, (const void*)dk, (const void*)dv, (const void*)dqkv,
+                        (const void*)dq_weight, (const void*)dk_weight,
+                        (const void*)(weights ? workspace : nullptr)})
+    if (!aligned16(x)) return RINGX_E_ALIGN;
+  const int64_t row = B * N * d * 4;
+  const Span ins[] = {sx, span(dq, H * row), span(dk, Hkv * row), span(dv, Hkv * row)};
+  const Span outs[] = {span(dqkv, B * N * (H + 2 * Hkv) * d * esize(dtype)),
+                       span(dq_weight, dq_weight ? 4 * d : 0), span(dk_weight, dk_weight ? 4 * d : 0),
+                       span(workspace, (int64_t)need)};
+  for (int i = 0; i < 4; ++i) {
+    if (outs[i].lo == outs[i].hi) continue;
+    for (const Span& x : ins)
+      if (overlap(outs[i], x)) return RINGX_E_ALIAS;
+    if (overlaps_small_inputs(outs[i], a)) return RINGX_E_ALIAS;
+    for (int j = i + 1; j < 4; ++j)
+      if (outs[j].lo != outs[j].hi && overlap(outs[i], outs[j])) return RINGX_E_ALIAS;
+  }
+  a.dq = dq, a.dk = dk, a.dv = dv, a.dx = dqkv, a.dqw = dq_weight, a.dkw = dk_weight;
+  a.part = weights ? static_cast<float*>(workspace) : nullptr;
+  return hip_status(ringx::launch_norm_rope(a, true));
 }
 
 }  // extern "C"

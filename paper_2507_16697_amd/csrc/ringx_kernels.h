@@ -188,6 +188,15 @@ struct FwdArgs {
   hipStream_t stream = nullptr;
 };
 
+// Dropout of the attention probabilities, as its kernels are told of it (dropout.h).
+struct Drop {
+  const uint64_t* rng = nullptr;   // seed, offset (device memory)
+  uint32_t thr = 0;                // a score is dropped iff its random byte is below
+  float inv_keep = 1.f;            // 256 / (256 - thr)
+  uint32_t q0 = 0;                 // generator's index of the launch's first query
+  uint32_t kb0 = 0;                // and of its first 32-key block
+};
+
 struct MergeArgs {
   const float* part_out = nullptr;
   const float* part_lse = nullptr;
@@ -213,6 +222,7 @@ struct BwdArgs {
   int64_t BH = 0, Nq = 0, Nk = 0, d = 0, R = 1;   // BH = B * H query heads
   int64_t H = 1, G = 1;         // query heads per batch; query heads per K/V head (GQA)
   float scale = 1.f;
+  float d_factor = 1.f;         // preprocess: D is stored times this
   bool accumulate_dkv = false;  // dk, dv += instead of =
   bool accumulate_dq = false;   // dq += instead of =
   char* ds = nullptr;           // store mode of the dK/dV kernel: -dS of every score, bf16
@@ -263,6 +273,48 @@ struct TokArgs {
   hipStream_t stream = nullptr;
 };
 
+// Norm, rotation and layout change between a packed projection and the attention's operands
+// (norm_rope.hip).
+struct RopeArgs {
+  const void* x = nullptr;       // [B, N, (H + 2 Hkv) d], batch and token strides bs, ts (elements)
+  int64_t bs = 0, ts = 0;
+  void *q = nullptr, *k = nullptr, *v = nullptr;               // forward: outputs
+  const float *dq = nullptr, *dk = nullptr, *dv = nullptr;     // backward: inputs
+  void* dx = nullptr;            // backward: [B, N, (H + 2 Hkv) d]
+  const float *qw = nullptr, *kw = nullptr;                    // [d] or null
+  float *dqw = nullptr, *dkw = nullptr;                        // backward: [d] or null
+  float* part = nullptr;         // backward: the workgroups' parts of dqw, dkw; null without weights
+  const double* freqs = nullptr;
+  const int32_t* pos = nullptr;  // [.., N, axes], null: pos0 + n
+  int64_t pos_bs = 0, pos0 = 0;
+  int64_t B = 0, N = 0;
+  int H = 1, Hkv = 1, d = 0;
+  int axes = 1, rot[3] = {0, 0, 0};
+  float eps = 0.f;
+  bool bf16 = false, vec = true; // vec: rows in 16-byte pieces
+  hipStream_t stream = nullptr;
+};
+// lanes that hold a row
+inline int rope_lanes(int64_t d, bool bf16) {
+  if (bf16) return (int)(d / 8);
+  int l = 1;
+  while (4 * l < d) l *= 2;
+  return l;
+}
+// Workgroups: along tokens, along heads.
+struct RopeGrid {
+  int64_t x, y;
+};
+inline RopeGrid rope_grid(int64_t rows, int heads, int tokens_per_wave, bool bwd) {
+  RopeGrid g;
+  (void)bwd;
+  const int64_t groups = (rows + 4 * tokens_per_wave - 1) / (4 * tokens_per_wave);
+  g.y = 1;
+  while (g.y < heads && groups * g.y < 2048) ++g.y;
+  g.x = groups < 2048 ? groups : 2048;
+  return g;
+}
+
 hipError_t launch_fwd_bf16(const FwdArgs& a, FwdMode mode);
 hipError_t launch_fwd_f32(const FwdArgs& a, FwdMode mode);
 hipError_t launch_lse_merge(const MergeArgs& a);
@@ -276,6 +328,15 @@ hipError_t launch_bwd_dkdv_f32(const BwdArgs& a);
 hipError_t launch_bwd_dq_f32(const BwdArgs& a);
 hipError_t launch_bwd_f32(const BwdArgs& a);      // both halves of the fp32 backward
 hipError_t launch_bwd_dq_ds(const DsArgs& a);   // d = 128, bf16 dS (bwd_dq_ds.hip)
+
+// with dropout (R = 1; fused and step mode; D of the preprocess times 1 - p)
+hipError_t launch_fwd_drop_bf16(const FwdArgs& a, FwdMode mode, const Drop& drop);
+hipError_t launch_fwd_drop_f32(const FwdArgs& a, FwdMode mode, const Drop& drop);
+hipError_t launch_bwd_dkdv_drop_bf16(const BwdArgs& a, const Drop& drop);
+hipError_t launch_bwd_dq_drop_bf16(const BwdArgs& a, const Drop& drop);
+hipError_t launch_bwd_drop_f32(const BwdArgs& a, const Drop& drop);
+
+hipError_t launch_norm_rope(const RopeArgs& a, bool bwd);
 
 hipError_t launch_tt_tokenize(const TokArgs& a);
 

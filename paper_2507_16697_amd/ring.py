@@ -10,6 +10,12 @@ orders streams).  Streams keep the default priority.
 
     out, lse = ring_forward(q, k_chunks, v_chunks)
     dq, dk_chunks, dv_chunks = ring_backward(q, k_chunks, v_chunks, out, dout, lse)
+
+With dropout=(p, rng) both run the steps with dropout (rng: the generator's seed and offset on the
+device, the same values in both directions); q0 is the first query's place in the whole sequence.
+Chunk r lies on the mask's key axis after the r chunks before it, each rounded up to whole blocks of
+32 keys: for chunks of whole blocks that is its place in the sequence, and the mask is that of one
+call over all keys.
 """
 
 from __future__ import annotations
@@ -74,7 +80,16 @@ def _check_chunks(q, k_chunks, v_chunks):
             raise ValueError("chunks must have q's dtype")
 
 
-def ring_forward(q, k_chunks, v_chunks, scale=None, out_dtype=None, overlap=True):
+def mask_places(lengths):
+    """key0 of every chunk: where it starts on the mask's key axis."""
+    places, at = [], 0
+    for n in lengths:
+        places.append(at)
+        at += (n + 31) // 32 * 32
+    return places
+
+
+def ring_forward(q, k_chunks, v_chunks, scale=None, out_dtype=None, overlap=True, dropout=None, q0=0):
     """Attention of q over the concatenated chunks, one ring step per chunk.
 
     Returns (out, lse): out in out_dtype (q's dtype by default), lse fp32 natural log."""
@@ -85,6 +100,7 @@ def ring_forward(q, k_chunks, v_chunks, scale=None, out_dtype=None, overlap=True
     copy, pp = _start(torch, compute, overlap, k_chunks[0], max(k.shape[2] for k in k_chunks))
     out_acc = torch.empty((B, H, Nq, d), dtype=torch.float32, device=q.device)
     lse_acc = torch.empty((B, H, Nq), dtype=torch.float32, device=q.device)
+    places = mask_places([k.shape[2] for k in k_chunks])
     pp.fill(torch, copy, 0, k_chunks[0], v_chunks[0])
     for r in range(len(k_chunks)):
         slot = r % 2
@@ -92,14 +108,20 @@ def ring_forward(q, k_chunks, v_chunks, scale=None, out_dtype=None, overlap=True
             pp.fill(torch, copy, 1 - slot, k_chunks[r + 1], v_chunks[r + 1])
         compute.wait_event(pp.ready[slot])
         n = k_chunks[r].shape[2]
-        ringx.ringx_attn_fwd_step(q, pp.view("k", slot, n), pp.view("v", slot, n), out_acc,
-                                  lse_acc, first=(r == 0), scale=scale, stream=compute)
+        kr, vr = pp.view("k", slot, n), pp.view("v", slot, n)
+        if dropout is None:
+            ringx.ringx_attn_fwd_step(q, kr, vr, out_acc, lse_acc, first=(r == 0), scale=scale,
+                                      stream=compute)
+        else:
+            ringx.ringx_attn_fwd_step_drop(q, kr, vr, out_acc, lse_acc, r == 0, *dropout, places[r],
+                                           q0=q0, scale=scale, stream=compute)
         pp.free[slot].record(compute)
     return ringx.ringx_lse_merge(out_acc[None], lse_acc[None], out_dtype=out_dtype or q.dtype,
                                  stream=compute)
 
 
-def ring_backward(q, k_chunks, v_chunks, out, dout, lse, scale=None, overlap=True):
+def ring_backward(q, k_chunks, v_chunks, out, dout, lse, scale=None, overlap=True, dropout=None,
+                  q0=0):
     """Gradients with the merged lse, one ring step per chunk.
 
     Returns (dq, dk_chunks, dv_chunks), all fp32; dk_chunks[r], dv_chunks[r] are the gradients of
@@ -109,7 +131,11 @@ def ring_backward(q, k_chunks, v_chunks, out, dout, lse, scale=None, overlap=Tru
     B, H, Nq, d = q.shape
     compute = torch.cuda.current_stream()
     copy, pp = _start(torch, compute, overlap, k_chunks[0], max(k.shape[2] for k in k_chunks))
-    delta = ringx.ringx_bwd_preprocess(out, dout, lse, stream=compute)
+    if dropout is None:
+        delta = ringx.ringx_bwd_preprocess(out, dout, lse, stream=compute)
+    else:
+        delta = ringx.ringx_bwd_preprocess_drop(out, dout, lse, dropout[0], stream=compute)
+    places = mask_places([k.shape[2] for k in k_chunks])
     dq = torch.empty((B, H, Nq, d), dtype=torch.float32, device=q.device)
     dks = [torch.empty(k.shape, dtype=torch.float32, device=q.device) for k in k_chunks]
     dvs = [torch.empty_like(t) for t in dks]
@@ -120,8 +146,12 @@ def ring_backward(q, k_chunks, v_chunks, out, dout, lse, scale=None, overlap=Tru
             pp.fill(torch, copy, 1 - slot, k_chunks[r + 1], v_chunks[r + 1])
         compute.wait_event(pp.ready[slot])
         n = k_chunks[r].shape[2]
-        ringx.ringx_attn_bwd_step(q, pp.view("k", slot, n), pp.view("v", slot, n), dout, lse,
-                                  delta, dq, dks[r], dvs[r], accumulate_dq=(r > 0), scale=scale,
-                                  stream=compute)
+        kr, vr = pp.view("k", slot, n), pp.view("v", slot, n)
+        if dropout is None:
+            ringx.ringx_attn_bwd_step(q, kr, vr, dout, lse, delta, dq, dks[r], dvs[r],
+                                      accumulate_dq=(r > 0), scale=scale, stream=compute)
+        else:
+            ringx.ringx_attn_bwd_step_drop(q, kr, vr, dout, lse, delta, dq, dks[r], dvs[r], r > 0,
+                                           *dropout, places[r], q0=q0, scale=scale, stream=compute)
         pp.free[slot].record(compute)
     return dq, dks, dvs

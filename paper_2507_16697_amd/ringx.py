@@ -9,6 +9,8 @@ supplies device memory and the current HIP stream.  Function names follow the C 
     dq, dk, dv = ringx_attn_bwd(q, k, v, out, dout, lse, R)
     ringx_attn_fwd_step(q, k_r, v_r, out_acc, lse_acc, first=(r == 0))   # one ring step
     ringx_attn_bwd_step(q, k_r, v_r, dout, lse, delta, dq_acc, dk_r, dv_r, accumulate_dq=(r > 0))
+    q, k, v = ringx_qkv_norm_rope(qkv, H, Hkv, freqs, rot)     # from a packed projection
+    out, lse = ringx_attn_fwd_drop(q, k, v, p, rng)            # with dropout; rng: seed and offset
 
 The library must be built (``python -m paper_2507_16697_amd.build``); loading fails loudly if it
 is missing -- there is no fallback implementation.
@@ -30,7 +32,7 @@ RINGX_BF16 = 1
 STATUS_NAMES = {
     0: "RINGX_OK", 1: "RINGX_E_NULLPTR", 2: "RINGX_E_SHAPE", 3: "RINGX_E_CHUNKS",
     4: "RINGX_E_UNSUPPORTED", 5: "RINGX_E_ALIGN", 6: "RINGX_E_WORKSPACE", 7: "RINGX_E_HIP",
-    8: "RINGX_E_ALIAS", 9: "RINGX_E_SCRATCH",
+    8: "RINGX_E_ALIAS", 9: "RINGX_E_SCRATCH", 10: "RINGX_E_DROPOUT", 11: "RINGX_E_ROPE",
 }
 
 # rows (B * H * Nq) of the fixed device array behind ringx_attn_bwd_noalloc (RINGX_NOALLOC_MAX_ROWS)
@@ -42,7 +44,10 @@ EXPORTED = ("ringx_attn_fwd", "ringx_attn_fwd_partials", "ringx_lse_merge", "rin
             "ringx_attn_bwd_gqa", "ringx_tt_tokenize", "ringx_bwd_workspace_bytes",
             "ringx_chunk_bounds", "ringx_status_str", "ringx_attn_bwd_noalloc",
             "ringx_bwd_ds_bytes", "ringx_attn_bwd_dkdv_ds", "ringx_attn_bwd_dq_ds",
-            "ringx_attn_bwd_ds", "ringx_bwd_ds_workspace_bytes")
+            "ringx_attn_bwd_ds", "ringx_bwd_ds_workspace_bytes", "ringx_attn_fwd_drop",
+            "ringx_attn_bwd_drop", "ringx_attn_fwd_step_drop", "ringx_attn_bwd_step_drop",
+            "ringx_bwd_preprocess_drop", "ringx_qkv_norm_rope", "ringx_qkv_norm_rope_bwd",
+            "ringx_qkv_norm_rope_bwd_workspace_bytes")
 
 
 class RingxError(RuntimeError):
@@ -104,6 +109,19 @@ def lib() -> ctypes.CDLL:
         L.ringx_attn_bwd_dq_ds.argtypes = [_P, ctypes.c_size_t, _P, _P, _I, _I, _I, _I, _I, _I,
                                            _I, ctypes.c_float, ctypes.c_int, _I, _I, _P]
         L.ringx_attn_bwd_ds.argtypes = L.ringx_attn_bwd_gqa.argtypes
+        F, C = ctypes.c_float, ctypes.c_int
+        L.ringx_attn_fwd_drop.argtypes = [_P] * 5 + [_I] * 6 + [F, C, F, _P, _I, _I, _P]
+        L.ringx_attn_bwd_drop.argtypes = ([_P] * 9 + [_I] * 6 +
+                                          [F, C, F, _P, _I, _I, C, _P, ctypes.c_size_t, _P])
+        L.ringx_attn_fwd_step_drop.argtypes = [_P] * 5 + [_I] * 5 + [F, C, C, F, _P, _I, _I, _P]
+        L.ringx_attn_bwd_step_drop.argtypes = [_P] * 9 + [_I] * 5 + [F, C, C, C, F, _P, _I, _I, _P]
+        L.ringx_bwd_preprocess_drop.argtypes = [_P] * 4 + [_I] * 4 + [C, F, _P]
+        L.ringx_qkv_norm_rope.argtypes = ([_P, _I, _I, _P, _P, _P, _P, _I, _I, _I, _P, _P, _P, _P] +
+                                          [_I] * 5 + [F, C, _P])
+        L.ringx_qkv_norm_rope_bwd.argtypes = ([_P, _I, _I] + [_P] * 7 + [_I, _I, _I] + [_P] * 4 +
+                                              [_I] * 5 + [F, C, _P, ctypes.c_size_t, _P])
+        L.ringx_qkv_norm_rope_bwd_workspace_bytes.argtypes = [_I] * 5 + [C]
+        L.ringx_qkv_norm_rope_bwd_workspace_bytes.restype = ctypes.c_size_t
         L.ringx_chunk_bounds.argtypes = [_I, _I, _I, ctypes.POINTER(_I), ctypes.POINTER(_I)]
         L.ringx_status_str.argtypes = [ctypes.c_int]
         L.ringx_status_str.restype = ctypes.c_char_p
@@ -112,7 +130,10 @@ def lib() -> ctypes.CDLL:
                      "ringx_attn_bwd_dq", "ringx_attn_fwd_step", "ringx_attn_bwd_step",
                      "ringx_attn_fwd_gqa", "ringx_attn_bwd_gqa", "ringx_tt_tokenize",
                      "ringx_chunk_bounds", "ringx_attn_bwd_noalloc", "ringx_attn_bwd_dkdv_ds",
-                     "ringx_attn_bwd_dq_ds", "ringx_attn_bwd_ds"):
+                     "ringx_attn_bwd_dq_ds", "ringx_attn_bwd_ds", "ringx_attn_fwd_drop",
+                     "ringx_attn_bwd_drop", "ringx_attn_fwd_step_drop", "ringx_attn_bwd_step_drop",
+                     "ringx_bwd_preprocess_drop", "ringx_qkv_norm_rope",
+                     "ringx_qkv_norm_rope_bwd"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -581,3 +602,240 @@ def ringx_tt_tokenize(field, k: int, ratio: int, centre, p: int, sigma=None, out
                                  cy, cx, p, sigma, _dtype_code(tokens), _stream(stream))
     _check("ringx_tt_tokenize", st)
     return tokens
+
+
+# ---------------------------------------------------------------------------------------------
+# attention with dropout
+
+
+def _rng(rng, like):
+    """The generator's state: int64 or uint64 [2] on the device, seed and offset."""
+    torch = _T or _torch()
+    _dev(rng)
+    if rng.shape != (2,):
+        raise ValueError(f"rng: shape {tuple(rng.shape)}, expected (2,)")
+    if rng.dtype not in (torch.int64, torch.uint64):
+        raise TypeError(f"rng: dtype {rng.dtype}, expected int64 or uint64")
+    if rng.device != like.device:
+        raise ValueError(f"rng: on {rng.device}, expected {like.device}")
+    return rng.data_ptr()
+
+
+def ringx_attn_fwd_drop(q, k, v, p: float, rng, scale=None, q0: int = 0, key0: int = 0, out=None,
+                        lse=None, stream=None):
+    """Attention of q [B,H,Nq,d] to k, v [B,Hkv,Nk,d] with dropout of its probabilities at rate p (to
+    a multiple of 1/256).  rng: int64 [2] on the device, seed and offset, read when the kernels run.
+    q0, key0: the tensors' places on the mask's axes (key0 a multiple of 32).  Returns (out, lse)."""
+    torch = _T or _torch()
+    _dev(q, k, v)
+    B, H, Hkv, Nq, Nk, d = _qkv(q, k, v, heads_kv=True)
+    state = _rng(rng, q)
+    out = torch.empty_like(q) if out is None else _out("out", out, q.shape, q.dtype, q)
+    lse = _out("lse", lse, (B, H, Nq), torch.float32, q)
+    st = lib().ringx_attn_fwd_drop(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+                                   lse.data_ptr(), B, H, Hkv, Nq, Nk, d, _scale(scale, d),
+                                   _dtype_code(q), float(p), state, q0, key0, _stream(stream))
+    _check("ringx_attn_fwd_drop", st)
+    return out, lse
+
+
+def ringx_attn_bwd_drop(q, k, v, out, dout, lse, p: float, rng, scale=None, q0: int = 0,
+                        key0: int = 0, dq=None, dk=None, dv=None, accumulate_dkv=False,
+                        workspace=None, stream=None):
+    """Backward of ringx_attn_fwd_drop with its p, rng, q0 and key0: fp32 dq [B,H,Nq,d], dk, dv
+    [B,Hkv,Nk,d]."""
+    torch = _T or _torch()
+    _dev(q, k, v, out, dout, lse)
+    B, H, Hkv, Nq, Nk, d = _qkv(q, k, v, heads_kv=True)
+    _expect("out", out, q.shape, q.dtype, q.device)
+    _expect("dout", dout, q.shape, q.dtype, q.device)
+    _expect("lse", lse, (B, H, Nq), torch.float32, q.device)
+    state = _rng(rng, q)
+    dq = _out("dq", dq, (B, H, Nq, d), torch.float32, q)
+    dk = _grad_out("dk", dk, (B, Hkv, Nk, d), q, accumulate_dkv)
+    dv = _grad_out("dv", dv, (B, Hkv, Nk, d), q, accumulate_dkv)
+    code = _dtype_code(q)
+    workspace = _workspace(workspace, ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, 1, code), q)
+    st = lib().ringx_attn_bwd_drop(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+                                   dout.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(),
+                                   dv.data_ptr(), B, H, Hkv, Nq, Nk, d, _scale(scale, d), code,
+                                   float(p), state, q0, key0, 1 if accumulate_dkv else 0,
+                                   workspace.data_ptr(), _nbytes(workspace), _stream(stream))
+    _check("ringx_attn_bwd_drop", st)
+    return dq, dk, dv
+
+
+def _workspace(workspace, need, like):
+    """The caller's workspace, or a new one of `need` bytes."""
+    if workspace is None:
+        return _new(max(need, 16), _T.uint8, like)
+    _dev(workspace)
+    if workspace.device != like.device:
+        raise ValueError(f"workspace: on {workspace.device}, expected {like.device}")
+    return workspace
+
+
+def ringx_attn_fwd_step_drop(q, k, v, out_acc, lse_acc, first: bool, p: float, rng, key0: int,
+                             q0: int = 0, scale=None, stream=None):
+    """ringx_attn_fwd_step with dropout; key0: the chunk's place on the mask's key axis."""
+    torch = _T or _torch()
+    _dev(q, k, v, out_acc, lse_acc)
+    B, H, _, Nq, Nk, d = _qkv(q, k, v)
+    _expect("out_acc", out_acc, (B, H, Nq, d), torch.float32, q.device)
+    _expect("lse_acc", lse_acc, (B, H, Nq), torch.float32, q.device)
+    state = _rng(rng, q)
+    st = lib().ringx_attn_fwd_step_drop(q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                        out_acc.data_ptr(), lse_acc.data_ptr(), B, H, Nq, Nk, d,
+                                        _scale(scale, d), _dtype_code(q), 1 if first else 0,
+                                        float(p), state, q0, key0, _stream(stream))
+    _check("ringx_attn_fwd_step_drop", st)
+    return out_acc, lse_acc
+
+
+def ringx_attn_bwd_step_drop(q, k, v, dout, lse, delta, dq_acc, dk, dv, accumulate_dq: bool,
+                             p: float, rng, key0: int, q0: int = 0, accumulate_dkv: bool = False,
+                             scale=None, stream=None):
+    """ringx_attn_bwd_step with dropout; delta is that of ringx_bwd_preprocess_drop."""
+    torch = _T or _torch()
+    _dev(q, k, v, dout, lse, delta, dq_acc, dk, dv)
+    B, H, _, Nq, Nk, d = _qkv(q, k, v)
+    _check_grad_inputs(q, dout, lse, delta)
+    _expect("dq_acc", dq_acc, (B, H, Nq, d), torch.float32, q.device)
+    _expect("dk", dk, (B, H, Nk, d), torch.float32, q.device)
+    _expect("dv", dv, (B, H, Nk, d), torch.float32, q.device)
+    state = _rng(rng, q)
+    st = lib().ringx_attn_bwd_step_drop(q.data_ptr(), k.data_ptr(), v.data_ptr(), dout.data_ptr(),
+                                        lse.data_ptr(), delta.data_ptr(), dq_acc.data_ptr(),
+                                        dk.data_ptr(), dv.data_ptr(), B, H, Nq, Nk, d,
+                                        _scale(scale, d), _dtype_code(q), 1 if accumulate_dq else 0,
+                                        1 if accumulate_dkv else 0, float(p), state, q0, key0,
+                                        _stream(stream))
+    _check("ringx_attn_bwd_step_drop", st)
+    return dq_acc, dk, dv
+
+
+def ringx_bwd_preprocess_drop(out, dout, lse, p: float, delta=None, stream=None):
+    """ringx_bwd_preprocess for ringx_attn_bwd_step_drop: delta[0] = (1 - p) rowsum(dout * out),
+    delta[1] = -lse * log2(e)."""
+    torch = _T or _torch()
+    _dev(out, dout, lse)
+    if out.dim() != 4:
+        raise ValueError("out must be 4-D [B, H, Nq, d]")
+    _dtype_code(out)
+    B, H, Nq, d = out.shape
+    _expect("dout", dout, out.shape, out.dtype, out.device)
+    _expect("lse", lse, (B, H, Nq), torch.float32, out.device)
+    delta = _out("delta", delta, (2, B, H, Nq), torch.float32, out)
+    st = lib().ringx_bwd_preprocess_drop(out.data_ptr(), dout.data_ptr(), lse.data_ptr(),
+                                         delta.data_ptr(), B, H, Nq, d, _dtype_code(out), float(p),
+                                         _stream(stream))
+    _check("ringx_bwd_preprocess_drop", st)
+    return delta
+
+
+# ---------------------------------------------------------------------------------------------
+# norm and rotation between a packed projection and the attention's operands
+
+
+def ringx_qkv_norm_rope_bwd_workspace_bytes(B, N, H, Hkv, d, dtype) -> int:
+    return int(lib().ringx_qkv_norm_rope_bwd_workspace_bytes(B, N, H, Hkv, d, int(dtype)))
+
+
+def _rope_args(qkv, H, Hkv, freqs, rot, pos, q_weight, k_weight):
+    """Checks of what both directions read; (B, N, d, batch stride, token stride, rot array, axes,
+    position batch stride)."""
+    torch = _T or _torch()
+    if not qkv.is_cuda:
+        raise ValueError("tensors must live on the GPU")
+    if qkv.dim() != 3:
+        raise ValueError("qkv must be 3-D [B, N, (H + 2 Hkv) d]")
+    _dtype_code(qkv)
+    B, N, cols = qkv.shape
+    heads = H + 2 * Hkv
+    if qkv.stride(2) != 1:
+        raise ValueError("qkv: a token's columns must be contiguous")
+    if H < 1 or Hkv < 1 or cols == 0 or cols % heads:
+        raise ValueError(f"qkv: {cols} columns are not those of {H} + 2 * {Hkv} heads")
+    rot = tuple(int(r) for r in rot)
+    if not 1 <= len(rot) <= 3:
+        raise ValueError("rot: sections of 1 to 3 axes")
+    dev = qkv.device
+    _dev(freqs)
+    _expect("freqs", freqs, (sum(rot) // 2,), torch.float64, dev)
+    d = cols // heads
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _dev(w)
+            _expect(name, w, (d,), torch.float32, dev)
+    pos_bs = 0
+    if pos is not None:
+        _dev(pos)
+        if pos.dim() == 3:
+            pos_bs = N * len(rot)
+        _expect("pos", pos, (B, N, len(rot)) if pos.dim() == 3 else (N, len(rot)), torch.int32, dev)
+    elif len(rot) != 1:
+        raise ValueError("pos: needed for more than one axis")
+    return (B, N, d, qkv.stride(0), qkv.stride(1), (_I * len(rot))(*rot), len(rot), pos_bs)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def ringx_qkv_norm_rope(qkv, H: int, Hkv: int, freqs, rot, pos=None, pos0: int = 0, q_weight=None,
+                        k_weight=None, eps: float = 1e-6, q=None, k=None, v=None, stream=None):
+    """From a packed projection qkv [B, N, (H + 2 Hkv) d] (columns contiguous, rows with any stride) to
+    q [B,H,N,d], k, v [B,Hkv,N,d]: RMS norm of every query and key head (weights fp32 [d] or None)
+    and rotation by position.  rot: rotated dims of 1 to 3 axes; freqs: fp64 [sum(rot) / 2], radians
+    per position; pos: int32 [N, axes] or [B, N, axes], or None for pos0 + n."""
+    torch = _T or _torch()
+    B, N, d, bs, ts, sections, axes, pos_bs = _rope_args(qkv, H, Hkv, freqs, rot, pos, q_weight,
+                                                         k_weight)
+    q = _out("q", q, (B, H, N, d), qkv.dtype, qkv)
+    k = _out("k", k, (B, Hkv, N, d), qkv.dtype, qkv)
+    v = _out("v", v, (B, Hkv, N, d), qkv.dtype, qkv)
+    st = lib().ringx_qkv_norm_rope(qkv.data_ptr(), bs, ts, _ptr(q_weight), _ptr(k_weight),
+                                   _ptr(freqs), _ptr(pos), pos_bs, pos0, axes, sections,
+                                   q.data_ptr(), k.data_ptr(), v.data_ptr(), B, N, H, Hkv, d,
+                                   float(eps), _dtype_code(qkv), _stream(stream))
+    _check("ringx_qkv_norm_rope", st)
+    return q, k, v
+
+
+def ringx_qkv_norm_rope_bwd(qkv, dq, dk, dv, freqs, rot, pos=None, pos0: int = 0, q_weight=None,
+                            k_weight=None, eps: float = 1e-6, dqkv=None, dq_weight=None,
+                            dk_weight=None, workspace=None, stream=None):
+    """Backward of ringx_qkv_norm_rope from fp32 dq [B,H,N,d], dk, dv [B,Hkv,N,d] (what the attention's
+    backward gives).  Returns (dqkv [B, N, (H + 2 Hkv) d] in qkv's dtype, dq_weight, dk_weight [d]
+    fp32, None where there is no weight)."""
+    torch = _T or _torch()
+    _dev(dq, dk, dv)
+    if dq.dim() != 4 or dk.dim() != 4:
+        raise ValueError("dq, dk and dv must be 4-D [B, heads, N, d]")
+    H, Hkv = dq.shape[1], dk.shape[1]
+    B, N, d, bs, ts, sections, axes, pos_bs = _rope_args(qkv, H, Hkv, freqs, rot, pos, q_weight,
+                                                         k_weight)
+    for name, g, heads in (("dq", dq, H), ("dk", dk, Hkv), ("dv", dv, Hkv)):
+        _expect(name, g, (B, heads, N, d), torch.float32, qkv.device)
+    if (q_weight is None and dq_weight is not None) or (k_weight is None and dk_weight is not None):
+        raise ValueError("a weight's gradient without the weight")
+    dqkv = _out("dqkv", dqkv, (B, N, (H + 2 * Hkv) * d), qkv.dtype, qkv)
+    if q_weight is not None:
+        dq_weight = _out("dq_weight", dq_weight, (d,), torch.float32, qkv)
+    if k_weight is not None:
+        dk_weight = _out("dk_weight", dk_weight, (d,), torch.float32, qkv)
+    code = _dtype_code(qkv)
+    if q_weight is not None or k_weight is not None:
+        workspace = _workspace(
+            workspace, ringx_qkv_norm_rope_bwd_workspace_bytes(B, N, H, Hkv, d, code), qkv)
+    else:
+        workspace = None
+    st = lib().ringx_qkv_norm_rope_bwd(qkv.data_ptr(), bs, ts, dq.data_ptr(), dk.data_ptr(),
+                                       dv.data_ptr(), _ptr(q_weight), _ptr(k_weight), _ptr(freqs),
+                                       _ptr(pos), pos_bs, pos0, axes, sections, dqkv.data_ptr(),
+                                       _ptr(dq_weight), _ptr(dk_weight), B, N, H, Hkv, d, float(eps),
+                                       code, _ptr(workspace),
+                                       0 if workspace is None else _nbytes(workspace),
+                                       _stream(stream))
+    _check("ringx_qkv_norm_rope_bwd", st)
+    return dqkv, dq_weight, dk_weight
