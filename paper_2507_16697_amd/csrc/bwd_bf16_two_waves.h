@@ -223,14 +223,19 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
 
   const bool key_ok = 32 * kb + n < nvalid;
 
-  // Dropout: lane (n = 8 m + 4 h + e, g) makes the bytes of query 8 m + 4 g + e of a 32-query block for
-  // the 16 keys of half h of this wave's key block, and reads its own key's byte of the 16 queries
-  // that its accumulators hold.
+  // Dropout: lane (n = 8 m + 4 h + e, g) makes the 16 bytes of query 8 m + 4 g + e of a 32-query block
+  // for half h of this wave's 32 keys, and needs its own key's byte of the 16 queries that its
+  // accumulators hold.  Row i = 4 m + e of the g half of the wave's 1 KiB takes that query's words, those
+  // of the two halves alternating, so that byte c of the row's first 16 is that of key c and byte
+  // c of the others that of key 16 + c; transposed 8-byte reads (16 lanes: 8 rows of 16 bytes, each
+  // lane a column) turn them round.
   const DropKey dkey(drop_rng(drop));
+  const float dedge = drop_edge(drop);
   const uint32_t dgroup = 2 * (drop_kb0(drop) + (uint32_t)(k0 / 32) + kb) + ((n >> 2) & 1);
   const uint32_t dquery = drop_q0(drop) + 32 * qh + 8 * (n >> 3) + 4 * g + (n & 3);
-  char* const dx = lds + C::kLds + wave * 1024 + (g * 2 + ((n >> 2) & 1)) * 256;
-  const int dkeep_at = 4 * (n >> 3) + (n & 3);
+  char* const dx = lds + C::kLds + wave * 1024 + g * 512;
+  char* const dxw = dx + (4 * (n >> 3) + (n & 3)) * 32 + 4 * ((n >> 2) & 1);
+  const char* const dxr = dx + ((n & 15) >> 1) * 32 + (n & 1) * 8 + (n >> 4) * 16;
 
   f32x16 dvt[C::kCT], dkt[C::kCT];
 #pragma unroll
@@ -283,9 +288,23 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
     // S = Q K^T and D - dP = D + dO (-V)^T for this wave's 32 keys and kQW queries; the dP
     // accumulators start from D in accumulator order (element 4 rq + x is query 8 rq + 4 g + x)
     f32x16 sacc[C::kQB], pacc[C::kQB];
+    u32x4 dw[C::kQB];   // dropout: the mask's bytes in accumulator order
 #pragma unroll
     for (int b = 0; b < C::kQB; ++b) {
       sacc[b] = f32x16{};
+      if constexpr (kDrop) {
+        const u32x4 w =
+            drop_bytes(dgroup, dquery + (uint32_t)(q0 + 64 * b), (uint32_t)(qh0 + hc), dkey);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) *reinterpret_cast<uint32_t*>(dxw + 8 * m) = w[m];
+        typedef int i32x2 __attribute__((ext_vector_type(2)));
+        typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+        const i32x2 lo = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)dxr);
+        const i32x2 hi = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(dxr + 256));
+        dw[b] = u32x4{(uint32_t)lo[0], (uint32_t)lo[1], (uint32_t)hi[0], (uint32_t)hi[1]};
+        pacc[b] = f32x16{};   // D joins after the mask
+        continue;
+      }
       const float* db = reinterpret_cast<const float*>(cd) + 64 * b;
       const f32x4 d0 = *reinterpret_cast<const f32x4*>(db);
       const f32x4 d1 = *reinterpret_cast<const f32x4*>(db + 8);
@@ -316,25 +335,21 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
 #pragma unroll
     for (int b = 0; b < C::kQB; ++b) {
       float p[16], dsv[16];
-      if constexpr (kDrop)
-        *reinterpret_cast<u32x4*>(dx + 16 * dkeep_at) =
-            drop_bytes(dgroup, dquery + (uint32_t)(q0 + 64 * b), (uint32_t)(qh0 + hc), dkey);
 #pragma unroll
       for (int rq = 0; rq < 4; ++rq) {
         // nl of 4 consecutive queries 64 b + 32 qh + 8 rq + 4 g ..
         const f32x4 nl4 = *reinterpret_cast<const f32x4*>(cl + 4 * (64 * b + 8 * rq));
+        f32x4 d4 = {};
+        if constexpr (kDrop) d4 = *reinterpret_cast<const f32x4*>(cd + 4 * (64 * b + 8 * rq));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float pe = fast_exp2(__builtin_fmaf(sacc[b][4 * rq + e], c2, nl4[e]));
           p[4 * rq + e] = pe;
           if constexpr (kDrop) {
             // (1 - p) times the definition's: D arrives so scaled, and a dropped score has dP = 0
-            const uint8_t byte =
-                *reinterpret_cast<const uint8_t*>(dx + 16 * (4 * rq + e) + dkeep_at);
-            const bool keep = byte >= drop.thr;
-            const float dd = reinterpret_cast<const float*>(cd)[64 * b + 8 * rq + e];
-            dsv[4 * rq + e] = pe * (keep ? pacc[b][4 * rq + e] : dd);
-            p[4 * rq + e] = keep ? pe : 0.f;
+            const float w = drop_weight(dw[b], 4 * rq + e, dedge);
+            dsv[4 * rq + e] = pe * __builtin_fmaf(pacc[b][4 * rq + e], w, d4[e]);
+            p[4 * rq + e] = pe * w;
           } else {
             dsv[4 * rq + e] = pe * pacc[b][4 * rq + e];   // -dS
           }

@@ -182,6 +182,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void bwd_dq_kernel(
   const float nl = -lse[bh * Nq + qi] * kLog2e;
   const float dq_d = delta[bh * Nq + qi];
   const DropKey dkey(drop_rng(drop));
+  const float dedge = drop_edge(drop);
   const uint32_t dquery = drop_q0(drop) + (uint32_t)qi;
   // the dP accumulators start from -D (the same for every key of this lane's query), so that they
   // come out of the matrix cores as dP - D
@@ -240,11 +241,18 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void bwd_dq_kernel(
     const char* vbuf = lds_v;
     const int nvalid = (int)min<uint32_t>(C::kBK, ct.hi - ct.start);
 
+    // the mask's bytes, which need no score, beside the products
+    u32x4 dw[C::kKTiles];
+    if constexpr (kDrop) {
+#pragma unroll
+      for (int kt = 0; kt < C::kKTiles; ++kt)
+        dw[kt] = drop_bytes(2 * (drop.kb0 + ct.start / 32 + kt) + g, dquery, (uint32_t)bh, dkey);
+    }
     f32x16 sacc[C::kKTiles], pacc[C::kKTiles];
 #pragma unroll
     for (int kt = 0; kt < C::kKTiles; ++kt) {
       sacc[kt] = f32x16{};
-      pacc[kt] = pinit;
+      pacc[kt] = kDrop ? f32x16{} : pinit;   // with dropout D joins after the mask
     }
 #pragma unroll
     for (int s = 0; s < C::kDSteps; ++s) {
@@ -255,6 +263,15 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void bwd_dq_kernel(
         const bf16x8 av = *reinterpret_cast<const bf16x8*>(vbuf + off);
         sacc[kt] = mfma32(ak, qf[s], sacc[kt]);
         pacc[kt] = mfma32(av, of[s], pacc[kt]);
+      }
+    }
+    if constexpr (kDrop) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int i = 0; i < 2 * C::kDSteps * C::kKTiles; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
       }
     }
     if (nvalid < C::kBK) {
@@ -271,9 +288,6 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void bwd_dq_kernel(
     bf16x8 sf[C::kKSteps];
 #pragma unroll
     for (int kt = 0; kt < C::kKTiles; ++kt) {
-      u32x4 dw;
-      if constexpr (kDrop)
-        dw = drop_bytes(2 * (drop.kb0 + ct.start / 32 + kt) + g, dquery, (uint32_t)bh, dkey);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         u32x4 w;
@@ -285,8 +299,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void bwd_dq_kernel(
           float g0 = pacc[kt][r0], g1 = pacc[kt][r0 + 1];
           if constexpr (kDrop) {
             // (1 - p) times the definition's: D arrives so scaled, and a dropped score has dP = 0
-            g0 = drop_keep(dw, r0, drop.thr) ? g0 : -dq_d;
-            g1 = drop_keep(dw, r0 + 1, drop.thr) ? g1 : -dq_d;
+            g0 = __builtin_fmaf(g0, drop_weight(dw[kt], r0, dedge), -dq_d);
+            g1 = __builtin_fmaf(g1, drop_weight(dw[kt], r0 + 1, dedge), -dq_d);
           }
           w[e] = pack_bf16x2(p0 * g0, p1 * g1);
         }

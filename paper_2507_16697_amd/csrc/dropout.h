@@ -27,6 +27,10 @@ __device__ __forceinline__ const uint64_t* drop_rng(const NoDrop&) { return null
 __device__ __forceinline__ const uint64_t* drop_rng(const Drop& d) { return d.rng; }
 __device__ __forceinline__ uint32_t drop_q0(const NoDrop&) { return 0; }
 __device__ __forceinline__ uint32_t drop_q0(const Drop& d) { return d.q0; }
+__device__ __forceinline__ uint32_t drop_fill(const NoDrop&) { return 0; }
+__device__ __forceinline__ uint32_t drop_fill(const Drop& d) { return (255u - d.thr) * 0x01010101u; }
+__device__ __forceinline__ float drop_edge(const NoDrop&) { return 0.f; }
+__device__ __forceinline__ float drop_edge(const Drop& d) { return (float)(int)d.thr - 1.f; }
 __device__ __forceinline__ uint32_t drop_kb0(const NoDrop&) { return 0; }
 __device__ __forceinline__ uint32_t drop_kb0(const Drop& d) { return d.kb0; }
 __device__ __forceinline__ float drop_inv_keep(const NoDrop&) { return 1.f; }
@@ -46,15 +50,20 @@ struct DropKey {
   }
 };
 
+// a ^ b ^ c in one instruction (the truth table of three inputs)
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) {
+  return (uint32_t)__builtin_amdgcn_bitop3_b32((int)a, (int)b, (int)c, 0x96);
+}
+
 __device__ __forceinline__ u32x4 drop_bytes(uint32_t group, uint32_t query, uint32_t head,
                                             const DropKey& key) {
   uint32_t c0 = group, c1 = query, c2 = head, c3 = key.off, k0 = key.k0, k1 = key.k1;
 #pragma unroll
   for (int r = 0; r < 7; ++r) {
     const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
-    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+    c0 = xor3((uint32_t)(b >> 32), c1, k0);
     c1 = (uint32_t)b;
-    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    c2 = xor3((uint32_t)(a >> 32), c3, k1);
     c3 = (uint32_t)a;
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
@@ -68,9 +77,26 @@ __device__ __forceinline__ uint32_t drop_word(const u32x4& w, uint32_t m) {
   return m & 2 ? hi : lo;
 }
 
-// Whether score i (0 .. 15, in the order of the tile's registers) is kept.
-__device__ __forceinline__ bool drop_keep(const u32x4& w, int i, uint32_t thr) {
-  return ((w[i >> 2] >> (8 * (i & 3))) & 255u) >= thr;
+// Bit 7 of every byte: whether the byte is at least thr, the carry of adding 256 - thr, which the
+// average of four bytes at once, (a + b + 1) / 2, leaves there.  fill = 255 - thr in every byte.
+__device__ __forceinline__ u32x4 drop_flags(const u32x4& w, uint32_t fill) {
+  u32x4 f;
+#pragma unroll
+  for (int m = 0; m < 4; ++m) f[m] = __builtin_amdgcn_lerp(w[m], fill, 0x01010101u);
+  return f;
+}
+// The mask of scores i, i + 1 (i even) for their bf16 pair: all ones in the half of one that is kept.
+// The byte permute copies sign bits, of odd bytes only, so the even ones come from a shifted copy.
+__device__ __forceinline__ uint32_t drop_pair(const u32x4& f, int i) {
+  return __builtin_amdgcn_perm(f[i >> 2], f[i >> 2] << 8, i & 2 ? 0x0B0B0909u : 0x0A0A0808u);
+}
+// 1 where score i is kept, else 0, from its byte: the byte less thr - 1, clamped to [0, 1].  For the
+// kernels that need a mask of fp32 values: a conversion, and a subtraction that runs at the rate of
+// fp32 arithmetic, twice that of integer instructions, like the multiply-add and the multiply that take
+// it (all-ones words and bit selects instead: 2% slower; lane masks do not fit the scalar registers).
+__device__ __forceinline__ float drop_weight(const u32x4& w, int i, float edge) {
+  const float b = (float)((w[i >> 2] >> (8 * (i & 3))) & 255u);
+  return __builtin_amdgcn_fmed3f(b - edge, 0.f, 1.f);
 }
 
 }  // namespace ringx

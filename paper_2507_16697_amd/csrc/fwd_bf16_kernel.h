@@ -246,6 +246,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void fwd_bf16_kernel(
 
   // the generator's state, and its index of this lane's query
   const DropKey dkey(drop_rng(drop));
+  const uint32_t dfill = drop_fill(drop);
   const uint32_t dq0 = drop_q0(drop) + (uint32_t)(q0 + n);
 
   // Q fragments (B operand of S^T = K Q^T): query n of this wave, dims 16*ks + 8g .. +8.
@@ -284,6 +285,21 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void fwd_bf16_kernel(
   float m2 = -INFINITY;     // reference max of the row (exp2 domain)
   float lc = 0.f;           // this lane's share of the chunk's row sum, relative to m2
   float lse2m = -INFINITY;  // merged log2-sum-exp over finished chunks (Eq. (5))
+
+  // Dropout: the flags of the current tile's mask.  They need no score, so the next tile's are formed
+  // beside the P V products, where the vector ALU has nothing else to do.
+  constexpr int kMasks = kDrop ? C::kKTiles : 1;
+  u32x4 dw[kMasks];
+  uint32_t dgroup = 2 * (drop_kb0(drop) + t0.start / 32) + g;   // the tile's first 16-key group
+  auto next_mask = [&] {
+    if constexpr (kDrop) {
+#pragma unroll
+      for (int kt = 0; kt < C::kKTiles; ++kt)
+        dw[kt] = drop_flags(drop_bytes(dgroup + 2 * kt, dq0, (uint32_t)bh, dkey), dfill);
+      dgroup += 2 * KS * C::kKTiles;   // one chunk: the stream's tiles are evenly spaced
+    }
+  };
+  next_mask();
 
   f32x16 sa[C::kKTiles], sb[C::kKTiles];
   // S_0, once K_0 has landed
@@ -363,8 +379,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void fwd_bf16_kernel(
     wait_vmem_all();
     __syncthreads();
     // wdst counts as redefined here, so that the load slots' addresses are formed at each use
-    // (scalar adds) instead of being held in registers across the loop
-    asm volatile("" : "+s"(wdst));
+    // (scalar adds) instead of being held in registers across the loop (with dropout the generator's
+    // keys take the scalar registers, and the compiler fails on a scalar held so)
+    if constexpr (!kDrop) asm volatile("" : "+s"(wdst));
     if (t2.start < key_end)
       issue_tile<C>(kb, lk + P * C::kTileBytes, t2.start, t2.hi, goff, grow, wave, wdst);
     if (t1.start < key_end)
@@ -399,18 +416,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void fwd_bf16_kernel(
                          qf[s], nxt[kt]);
     // The row sums are those of the softmax; dropout takes its scores from the products with V alone
     // (and their weight 1 / (1 - p) is applied to the finished output).
-    u32x4 dw[C::kKTiles];
-    if constexpr (kDrop) {
-#pragma unroll
-      for (int kt = 0; kt < C::kKTiles; ++kt)
-        dw[kt] = drop_bytes(2 * (drop.kb0 + t0.start / 32 + kt) + g, dq0, (uint32_t)bh, dkey);
-    }
-    auto pack_kept = [&](int kt, int i, float p0, float p1) {
-      if constexpr (kDrop) {
-        p0 = drop_keep(dw[kt], i, drop.thr) ? p0 : 0.f;
-        p1 = drop_keep(dw[kt], i + 1, drop.thr) ? p1 : 0.f;
-      }
-      return pack_bf16x2(p0, p1);
+    auto pack_kept = [&](const u32x4& flags, int i, float p0, float p1) {
+      if constexpr (kDrop) return pack_bf16x2(p0, p1) & drop_pair(flags, i);
+      else return pack_bf16x2(p0, p1);
     };
     bf16x8 pf[C::kKSteps];
     float la = 0.f, lb = 0.f;
@@ -425,7 +433,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void fwd_bf16_kernel(
           const float p1 = fast_exp2(__builtin_fmaf(cur[kt][8 * h + 2 * e + 1], c2, -m2));
           la += p0;
           lb += p1;
-          w[e] = pack_kept(kt, 8 * h + 2 * e, p0, p1);
+          w[e] = pack_kept(dw[kt % kMasks], 8 * h + 2 * e, p0, p1);
         }
         pf[2 * kt + h] = __builtin_bit_cast(bf16x8, w);
       }
@@ -434,7 +442,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void fwd_bf16_kernel(
     // front-loaded them onto the first nine and ran 1.5% slower; three and five were 0.3% and
     // 1.1% slower); d = 64 has half as many products for the same vector work and takes eight
     // per product (2-4% faster than seven, nine or ten)
-    constexpr int kValuPerProduct = D == 128 ? 4 : 8;
+    // (with the masks' instructions half as many more; 4 .. 8 and 8 .. 16 measured the same)
+    constexpr int kValuPerProduct = kDrop ? (D == 128 ? 6 : 12) : D == 128 ? 4 : 8;
     __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
     for (int i = 0; i < C::kDSteps * C::kKTiles; ++i) {
@@ -474,7 +483,14 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void fwd_bf16_kernel(
             const float p1 = fast_exp2(__builtin_fmaf(cur[kt][8 * h + 2 * e + 1], c2, -m2));
             la += p0;
             lb += p1;
-            w[e] = pack_kept(kt, 8 * h + 2 * e, p0, p1);
+            if constexpr (kDrop) {
+              // by weights from the flags: the pairs' masks would be held in registers for this path
+              const u32x4& f = dw[kt % kMasks];
+              w[e] = pack_bf16x2(p0 * drop_weight(f, 8 * h + 2 * e, 127.f),
+                                 p1 * drop_weight(f, 8 * h + 2 * e + 1, 127.f));
+            } else {
+              w[e] = pack_bf16x2(p0, p1);
+            }
           }
           pf[2 * kt + h] = __builtin_bit_cast(bf16x8, w);
         }
@@ -483,6 +499,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void fwd_bf16_kernel(
 
     __builtin_amdgcn_s_setprio(0);
     // O += V_j^T P_j on the matrix cores
+    next_mask();
     const char* vbuf = my_v + P * C::kTileBytes;
 #pragma unroll
     for (int s = 0; s < C::kKSteps; ++s)
@@ -499,6 +516,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void fwd_bf16_kernel(
     for (int i = 0; i < C::kKSteps * C::kCT; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      if constexpr (kDrop) __builtin_amdgcn_sched_group_barrier(0x002, D == 128 ? 4 : 8, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
 
