@@ -301,17 +301,23 @@ inline int rope_lanes(int64_t d, bool bf16) {
   while (4 * l < d) l *= 2;
   return l;
 }
-// Workgroups: along tokens, along heads.
+// Workgroups of 4 waves along tokens and along heads.  A token's heads are split only to fill the chip,
+// since every workgroup forms its tokens' angles: up to 1024 workgroups forward and, where each also
+// leaves a part of the weights' gradients, about 512 backward.  Measured (us; 256, 512, 1024, 2048; 16 heads
+// of 128, the last 16/4 of 64):
+//              512 tokens             2048                   8192                   2 x 4097
+//   forward    7.2 6.6 7.2 9.2        18.9 12.8 11.4 15.2    35.5 35.0 33.0 33.0    18.1 13.5 14.5 17.5
+//   backward   12.3 11.6 13.6 16.8    30.6 22.1 22.9 27.0    78.4 78.4 79.6 82.6    30.8 23.1 29.0 30.8
+// Backward workgroups take further tokens beyond 2048, so that the parts stay few.
 struct RopeGrid {
   int64_t x, y;
 };
 inline RopeGrid rope_grid(int64_t rows, int heads, int tokens_per_wave, bool bwd) {
   RopeGrid g;
-  (void)bwd;
   const int64_t groups = (rows + 4 * tokens_per_wave - 1) / (4 * tokens_per_wave);
   g.y = 1;
-  while (g.y < heads && groups * g.y < 2048) ++g.y;
-  g.x = groups < 2048 ? groups : 2048;
+  while (g.y < heads && groups * (g.y + 1) <= (bwd ? 640 : 1024)) ++g.y;
+  g.x = bwd && groups > 2048 ? 2048 : groups;
   return g;
 }
 

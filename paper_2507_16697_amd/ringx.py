@@ -19,6 +19,7 @@ is missing -- there is no fallback implementation.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 
@@ -741,6 +742,14 @@ def ringx_qkv_norm_rope_bwd_workspace_bytes(B, N, H, Hkv, d, dtype) -> int:
     return int(lib().ringx_qkv_norm_rope_bwd_workspace_bytes(B, N, H, Hkv, d, int(dtype)))
 
 
+@functools.lru_cache(maxsize=64)
+def _sections(rot):
+    """(ctypes array, axes, rotated dims) of the section sizes."""
+    if not 1 <= len(rot) <= 3:
+        raise ValueError("rot: sections of 1 to 3 axes")
+    return (_I * len(rot))(*rot), len(rot), sum(rot)
+
+
 def _rope_args(qkv, H, Hkv, freqs, rot, pos, q_weight, k_weight):
     """Checks of what both directions read; (B, N, d, batch stride, token stride, rot array, axes,
     position batch stride)."""
@@ -749,33 +758,32 @@ def _rope_args(qkv, H, Hkv, freqs, rot, pos, q_weight, k_weight):
         raise ValueError("tensors must live on the GPU")
     if qkv.dim() != 3:
         raise ValueError("qkv must be 3-D [B, N, (H + 2 Hkv) d]")
-    _dtype_code(qkv)
     B, N, cols = qkv.shape
     heads = H + 2 * Hkv
-    if qkv.stride(2) != 1:
+    bs, ts, cs = qkv.stride()
+    if cs != 1:
         raise ValueError("qkv: a token's columns must be contiguous")
     if H < 1 or Hkv < 1 or cols == 0 or cols % heads:
         raise ValueError(f"qkv: {cols} columns are not those of {H} + 2 * {Hkv} heads")
-    rot = tuple(int(r) for r in rot)
-    if not 1 <= len(rot) <= 3:
-        raise ValueError("rot: sections of 1 to 3 axes")
-    dev = qkv.device
+    sections, axes, turned = _sections(tuple(map(int, rot)))
+    dev, d = qkv.device, cols // heads
     _dev(freqs)
-    _expect("freqs", freqs, (sum(rot) // 2,), torch.float64, dev)
-    d = cols // heads
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            _dev(w)
-            _expect(name, w, (d,), torch.float32, dev)
+    _expect("freqs", freqs, (turned // 2,), torch.float64, dev)
+    if q_weight is not None:
+        _dev(q_weight)
+        _expect("q_weight", q_weight, (d,), torch.float32, dev)
+    if k_weight is not None:
+        _dev(k_weight)
+        _expect("k_weight", k_weight, (d,), torch.float32, dev)
     pos_bs = 0
     if pos is not None:
         _dev(pos)
         if pos.dim() == 3:
-            pos_bs = N * len(rot)
-        _expect("pos", pos, (B, N, len(rot)) if pos.dim() == 3 else (N, len(rot)), torch.int32, dev)
-    elif len(rot) != 1:
+            pos_bs = N * axes
+        _expect("pos", pos, (B, N, axes) if pos_bs else (N, axes), torch.int32, dev)
+    elif axes != 1:
         raise ValueError("pos: needed for more than one axis")
-    return (B, N, d, qkv.stride(0), qkv.stride(1), (_I * len(rot))(*rot), len(rot), pos_bs)
+    return B, N, d, bs, ts, sections, axes, pos_bs
 
 
 def _ptr(t):
