@@ -33,6 +33,8 @@
 #include "ringx_device.h"
 #include "ringx_kernels.h"
 
+#include <type_traits>
+
 namespace ringx {
 namespace {
 
@@ -131,8 +133,9 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
     int64_t Nq, int64_t Nk, int R, int tiles_per_chunk, float c2, float scale, int accumulate, DROP drop) {
   using C = DkvCfg<D, NW, QB>;
   constexpr bool kDrop = kHasDrop<DROP>;
-  // with dropout, 1 KiB per wave more to turn the mask's bytes round in
-  __shared__ __attribute__((aligned(1024))) char lds[C::kLds + (kDrop ? C::kWaves * 1024 : 0)];
+  // with dropout, 1 KiB per wave and block more to turn the mask's bytes round in
+  constexpr int kMaskWave = 1024;
+  __shared__ __attribute__((aligned(1024))) char lds[C::kLds + (kDrop ? C::kWaves * C::kQB * kMaskWave : 0)];
   const uint32_t lbase = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
 
   const int t = threadIdx.x;
@@ -233,7 +236,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
   const float dedge = drop_edge(drop);
   const uint32_t dgroup = 2 * (drop_kb0(drop) + (uint32_t)(k0 / 32) + kb) + ((n >> 2) & 1);
   const uint32_t dquery = drop_q0(drop) + 32 * qh + 8 * (n >> 3) + 4 * g + (n & 3);
-  char* const dx = lds + C::kLds + wave * 1024 + g * 512;
+  char* const dx = lds + C::kLds + wave * C::kQB * kMaskWave + g * 512;
   char* const dxw = dx + (4 * (n >> 3) + (n & 3)) * 32 + 4 * ((n >> 2) & 1);
   const char* const dxr = dx + ((n & 15) >> 1) * 32 + (n & 1) * 8 + (n >> 4) * 16;
 
@@ -253,11 +256,40 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
   }
   __syncthreads();
 
+  // with dropout at d = 64 and two blocks to a tile the wave's K and V rows stay in registers
+  constexpr bool kHeldKV = kDrop && D == 64 && QB == 2;
+  constexpr int kKV = kHeldKV ? C::kDSteps : 1;
+  bf16x8 kf[kKV], vf[kKV];
+  if constexpr (kHeldKV) {
+#pragma unroll
+    for (int s = 0; s < kKV; ++s) {
+      kf[s] = *reinterpret_cast<const bf16x8*>(lds + kvo[s]);
+      vf[s] = *reinterpret_cast<const bf16x8*>(lds + (C::kOffV - C::kOffK) + kvo[s]);
+    }
+  }
+
   const int ntiles = grp * nqt;
   int q0 = 0;         // first row of the current tile within its head
   int qn = 0;         // first row of the next tile
   int64_t hn = 0;     // the offset (in rows) of the next tile's head
   int hc = 0;         // the current tile's head in the group
+  u32x4 dw[C::kQB];   // dropout: the bytes of the current tile's mask in accumulator order
+  auto next_mask = [&](int first, int head) {
+    if constexpr (kDrop) {
+      typedef int i32x2 __attribute__((ext_vector_type(2)));
+      typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+#pragma unroll
+      for (int b = 0; b < C::kQB; ++b) {
+        const u32x4 w = drop_bytes(dgroup, dquery + (uint32_t)(first + 64 * b), (uint32_t)(qh0 + head), dkey);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) *reinterpret_cast<uint32_t*>(dxw + b * kMaskWave + 8 * m) = w[m];
+        const i32x2 lo = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(dxr + b * kMaskWave));
+        const i32x2 hi = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(dxr + b * kMaskWave + 256));
+        dw[b] = u32x4{(uint32_t)lo[0], (uint32_t)lo[1], (uint32_t)hi[0], (uint32_t)hi[1]};
+      }
+    }
+  };
+  next_mask(0, 0);
   for (int it = 0; it < ntiles; ++it) {
     const int cur = it & 1;
     // next query tile in flight: Q, dO rows and their nl, D straight into LDS
@@ -285,26 +317,105 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
     const char* cl = lds + so;                   // so holds the nl array's base
     const char* cd = lds + so + (C::kOffD - C::kOffL);
 
+    if constexpr (kDrop) {
+      // A score carries 10 vector instructions here against 4 without dropout, as much time as its
+      // products, so with two blocks to a tile the vector work of one goes beside the products of the
+      // other, in four parts: scores of block 0; scores of block 1 beside P and dS of block 0;
+      // gradients of block 0 beside P and dS of block 1; gradients of block 1 beside the next tile's
+      // generator calls; and the wave's K and V rows stay in registers, which leaves the LDS a
+      // third fewer reads.  (All scores, then P and dS, then all gradients, as without dropout: 4% slower
+      // for the whole backward of 16 heads of 64, 16384 x 16384; instructions dealt out to the
+      // products one by one: 2%.)  What is left is bound by the vector ALU's issue: 157 instructions
+      // to the 16 products of a 32 x 32 block.
+      if (q0 + C::kBQ > nq) {
+        // queries past the end are clamped copies: without their dO and D they add nothing
+        cold_path();
+        const int tail = nq - q0;
+        char* const to = lds + C::kOffO + cur * C::kQTile;
+        for (int i = tail * C::kRowBytes + 16 * t; i < C::kQTile; i += 16 * C::kThreads)
+          *reinterpret_cast<u32x4*>(to + i) = u32x4{};
+        float* const td = reinterpret_cast<float*>(lds + C::kOffD) + cur * C::kBQ;
+        if (t >= tail && t < C::kBQ) td[t] = 0.f;
+        __syncthreads();
+      }
+      f32x16 sacc[C::kQB], pacc[C::kQB];
+      bf16x8 pf[2 * C::kQB], sf[2 * C::kQB];
+      auto scores = [&](int b) {
+        sacc[b] = f32x16{};
+        pacc[b] = f32x16{};   // -dP; D joins after the mask
+#pragma unroll
+        for (int s = 0; s < C::kDSteps; ++s) {
+          const int at = 64 * b * C::kRowBytes + qo[s];
+          const bf16x8 bk = kHeldKV ? kf[s % kKV] : *reinterpret_cast<const bf16x8*>(kt + kvo[s]);
+          const bf16x8 bv = kHeldKV ? vf[s % kKV] : *reinterpret_cast<const bf16x8*>(vt + kvo[s]);
+          sacc[b] = mfma32(*reinterpret_cast<const bf16x8*>(qt + at), bk, sacc[b]);
+          pacc[b] = mfma32(*reinterpret_cast<const bf16x8*>(ot + at), bv, pacc[b]);
+        }
+      };
+      // P and -dS; (1 - p) times the definition's: D arrives so scaled, and a dropped score has dP = 0
+      auto weights = [&](int b) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u32x4 wp, ws;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float p[2], ds[2];
+            const int rq = 2 * h + (e >> 1);
+            const f32x4 nl4 = *reinterpret_cast<const f32x4*>(cl + 4 * (64 * b + 8 * rq));
+            const f32x4 d4 = *reinterpret_cast<const f32x4*>(cd + 4 * (64 * b + 8 * rq));
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const int i = 8 * h + 2 * e + x;
+              const float w = drop_weight(dw[b], i, dedge);
+              const float pe = fast_exp2(__builtin_fmaf(sacc[b][i], c2, nl4[i & 3]));
+              ds[x] = pe * __builtin_fmaf(pacc[b][i], w, d4[i & 3]);
+              p[x] = pe * w;
+            }
+            wp[e] = pack_bf16x2(p[0], p[1]);
+            ws[e] = pack_bf16x2(ds[0], ds[1]);
+          }
+          pf[2 * b + h] = __builtin_bit_cast(bf16x8, wp);
+          sf[2 * b + h] = __builtin_bit_cast(bf16x8, ws);
+        }
+      };
+      auto grads = [&](int b) {
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) {
+          const int rowb = (64 * b + 16 * k2) * C::kRowBytes;
+#pragma unroll
+          for (int c = 0; c < C::kCT; ++c) {
+            const bf16x4 o0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(ot + rowb + tqo[0][c]));
+            const bf16x4 o1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(ot + rowb + tqo[1][c]));
+            const bf16x4 q0v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(qt + rowb + tqo[0][c]));
+            const bf16x4 q1v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(qt + rowb + tqo[1][c]));
+            dvt[c] = mfma32(__builtin_shufflevector(o0, o1, 0, 1, 2, 3, 4, 5, 6, 7), pf[2 * b + k2], dvt[c]);
+            dkt[c] = mfma32(__builtin_shufflevector(q0v, q1v, 0, 1, 2, 3, 4, 5, 6, 7), sf[2 * b + k2], dkt[c]);
+          }
+        }
+      };
+      __builtin_amdgcn_sched_barrier(0);
+      scores(0);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (C::kQB == 2) {
+        scores(1);
+        weights(0);
+        __builtin_amdgcn_sched_barrier(0);
+        grads(0);
+        weights(1);
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
+        weights(0);
+      }
+      grads(C::kQB - 1);
+      next_mask(qn, hc + (qn == 0 ? 1 : 0));
+      __builtin_amdgcn_sched_barrier(0);
+    } else {
     // S = Q K^T and D - dP = D + dO (-V)^T for this wave's 32 keys and kQW queries; the dP
     // accumulators start from D in accumulator order (element 4 rq + x is query 8 rq + 4 g + x)
     f32x16 sacc[C::kQB], pacc[C::kQB];
-    u32x4 dw[C::kQB];   // dropout: the mask's bytes in accumulator order
 #pragma unroll
     for (int b = 0; b < C::kQB; ++b) {
       sacc[b] = f32x16{};
-      if constexpr (kDrop) {
-        const u32x4 w =
-            drop_bytes(dgroup, dquery + (uint32_t)(q0 + 64 * b), (uint32_t)(qh0 + hc), dkey);
-#pragma unroll
-        for (int m = 0; m < 4; ++m) *reinterpret_cast<uint32_t*>(dxw + 8 * m) = w[m];
-        typedef int i32x2 __attribute__((ext_vector_type(2)));
-        typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
-        const i32x2 lo = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)dxr);
-        const i32x2 hi = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(dxr + 256));
-        dw[b] = u32x4{(uint32_t)lo[0], (uint32_t)lo[1], (uint32_t)hi[0], (uint32_t)hi[1]};
-        pacc[b] = f32x16{};   // D joins after the mask
-        continue;
-      }
       const float* db = reinterpret_cast<const float*>(cd) + 64 * b;
       const f32x4 d0 = *reinterpret_cast<const f32x4*>(db);
       const f32x4 d1 = *reinterpret_cast<const f32x4*>(db + 8);
@@ -339,20 +450,11 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
       for (int rq = 0; rq < 4; ++rq) {
         // nl of 4 consecutive queries 64 b + 32 qh + 8 rq + 4 g ..
         const f32x4 nl4 = *reinterpret_cast<const f32x4*>(cl + 4 * (64 * b + 8 * rq));
-        f32x4 d4 = {};
-        if constexpr (kDrop) d4 = *reinterpret_cast<const f32x4*>(cd + 4 * (64 * b + 8 * rq));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float pe = fast_exp2(__builtin_fmaf(sacc[b][4 * rq + e], c2, nl4[e]));
           p[4 * rq + e] = pe;
-          if constexpr (kDrop) {
-            // (1 - p) times the definition's: D arrives so scaled, and a dropped score has dP = 0
-            const float w = drop_weight(dw[b], 4 * rq + e, dedge);
-            dsv[4 * rq + e] = pe * __builtin_fmaf(pacc[b][4 * rq + e], w, d4[e]);
-            p[4 * rq + e] = pe * w;
-          } else {
-            dsv[4 * rq + e] = pe * pacc[b][4 * rq + e];   // -dS
-          }
+          dsv[4 * rq + e] = pe * pacc[b][4 * rq + e];   // -dS
         }
       }
       if (masked) {
@@ -400,6 +502,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
     for (int i = 0; i < 4 * C::kQB * C::kCT; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
     }
     // next tile landed (the only vector memory operations in flight); this tile's reads done
     wait_vmem_all();
