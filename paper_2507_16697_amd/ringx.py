@@ -605,6 +605,19 @@ def ringx_tt_tokenize(field, k: int, ratio: int, centre, p: int, sigma=None, out
     return tokens
 
 
+def _launch(name, like, stream, *args):
+    """Call an entry point whose last argument is the stream, with `like`'s device current."""
+    fn = getattr(lib(), name)
+    cuda = _T.cuda
+    if like.device.index == cuda.current_device():
+        st = fn(*args, _stream(stream))
+    else:
+        with cuda.device(like.device):
+            st = fn(*args, _stream(stream))
+    if st != 0:
+        _check(name, st)
+
+
 # ---------------------------------------------------------------------------------------------
 # attention with dropout
 
@@ -633,10 +646,9 @@ def ringx_attn_fwd_drop(q, k, v, p: float, rng, scale=None, q0: int = 0, key0: i
     state = _rng(rng, q)
     out = torch.empty_like(q) if out is None else _out("out", out, q.shape, q.dtype, q)
     lse = _out("lse", lse, (B, H, Nq), torch.float32, q)
-    st = lib().ringx_attn_fwd_drop(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-                                   lse.data_ptr(), B, H, Hkv, Nq, Nk, d, _scale(scale, d),
-                                   _dtype_code(q), float(p), state, q0, key0, _stream(stream))
-    _check("ringx_attn_fwd_drop", st)
+    _launch("ringx_attn_fwd_drop", q, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+            out.data_ptr(), lse.data_ptr(), B, H, Hkv, Nq, Nk, d, _scale(scale, d), _dtype_code(q),
+            float(p), state, q0, key0)
     return out, lse
 
 
@@ -657,12 +669,10 @@ def ringx_attn_bwd_drop(q, k, v, out, dout, lse, p: float, rng, scale=None, q0: 
     dv = _grad_out("dv", dv, (B, Hkv, Nk, d), q, accumulate_dkv)
     code = _dtype_code(q)
     workspace = _workspace(workspace, ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, 1, code), q)
-    st = lib().ringx_attn_bwd_drop(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-                                   dout.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(),
-                                   dv.data_ptr(), B, H, Hkv, Nq, Nk, d, _scale(scale, d), code,
-                                   float(p), state, q0, key0, 1 if accumulate_dkv else 0,
-                                   workspace.data_ptr(), _nbytes(workspace), _stream(stream))
-    _check("ringx_attn_bwd_drop", st)
+    _launch("ringx_attn_bwd_drop", q, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+            out.data_ptr(), dout.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(),
+            dv.data_ptr(), B, H, Hkv, Nq, Nk, d, _scale(scale, d), code, float(p), state, q0, key0,
+            1 if accumulate_dkv else 0, workspace.data_ptr(), _nbytes(workspace))
     return dq, dk, dv
 
 
@@ -685,11 +695,9 @@ def ringx_attn_fwd_step_drop(q, k, v, out_acc, lse_acc, first: bool, p: float, r
     _expect("out_acc", out_acc, (B, H, Nq, d), torch.float32, q.device)
     _expect("lse_acc", lse_acc, (B, H, Nq), torch.float32, q.device)
     state = _rng(rng, q)
-    st = lib().ringx_attn_fwd_step_drop(q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                        out_acc.data_ptr(), lse_acc.data_ptr(), B, H, Nq, Nk, d,
-                                        _scale(scale, d), _dtype_code(q), 1 if first else 0,
-                                        float(p), state, q0, key0, _stream(stream))
-    _check("ringx_attn_fwd_step_drop", st)
+    _launch("ringx_attn_fwd_step_drop", q, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+            out_acc.data_ptr(), lse_acc.data_ptr(), B, H, Nq, Nk, d, _scale(scale, d),
+            _dtype_code(q), 1 if first else 0, float(p), state, q0, key0)
     return out_acc, lse_acc
 
 
@@ -705,13 +713,10 @@ def ringx_attn_bwd_step_drop(q, k, v, dout, lse, delta, dq_acc, dk, dv, accumula
     _expect("dk", dk, (B, H, Nk, d), torch.float32, q.device)
     _expect("dv", dv, (B, H, Nk, d), torch.float32, q.device)
     state = _rng(rng, q)
-    st = lib().ringx_attn_bwd_step_drop(q.data_ptr(), k.data_ptr(), v.data_ptr(), dout.data_ptr(),
-                                        lse.data_ptr(), delta.data_ptr(), dq_acc.data_ptr(),
-                                        dk.data_ptr(), dv.data_ptr(), B, H, Nq, Nk, d,
-                                        _scale(scale, d), _dtype_code(q), 1 if accumulate_dq else 0,
-                                        1 if accumulate_dkv else 0, float(p), state, q0, key0,
-                                        _stream(stream))
-    _check("ringx_attn_bwd_step_drop", st)
+    _launch("ringx_attn_bwd_step_drop", q, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+            dout.data_ptr(), lse.data_ptr(), delta.data_ptr(), dq_acc.data_ptr(), dk.data_ptr(),
+            dv.data_ptr(), B, H, Nq, Nk, d, _scale(scale, d), _dtype_code(q), 1 if accumulate_dq
+            else 0, 1 if accumulate_dkv else 0, float(p), state, q0, key0)
     return dq_acc, dk, dv
 
 
@@ -727,10 +732,8 @@ def ringx_bwd_preprocess_drop(out, dout, lse, p: float, delta=None, stream=None)
     _expect("dout", dout, out.shape, out.dtype, out.device)
     _expect("lse", lse, (B, H, Nq), torch.float32, out.device)
     delta = _out("delta", delta, (2, B, H, Nq), torch.float32, out)
-    st = lib().ringx_bwd_preprocess_drop(out.data_ptr(), dout.data_ptr(), lse.data_ptr(),
-                                         delta.data_ptr(), B, H, Nq, d, _dtype_code(out), float(p),
-                                         _stream(stream))
-    _check("ringx_bwd_preprocess_drop", st)
+    _launch("ringx_bwd_preprocess_drop", out, stream, out.data_ptr(), dout.data_ptr(),
+            lse.data_ptr(), delta.data_ptr(), B, H, Nq, d, _dtype_code(out), float(p))
     return delta
 
 
@@ -802,11 +805,9 @@ def ringx_qkv_norm_rope(qkv, H: int, Hkv: int, freqs, rot, pos=None, pos0: int =
     q = _out("q", q, (B, H, N, d), qkv.dtype, qkv)
     k = _out("k", k, (B, Hkv, N, d), qkv.dtype, qkv)
     v = _out("v", v, (B, Hkv, N, d), qkv.dtype, qkv)
-    st = lib().ringx_qkv_norm_rope(qkv.data_ptr(), bs, ts, _ptr(q_weight), _ptr(k_weight),
-                                   _ptr(freqs), _ptr(pos), pos_bs, pos0, axes, sections,
-                                   q.data_ptr(), k.data_ptr(), v.data_ptr(), B, N, H, Hkv, d,
-                                   float(eps), _dtype_code(qkv), _stream(stream))
-    _check("ringx_qkv_norm_rope", st)
+    _launch("ringx_qkv_norm_rope", qkv, stream, qkv.data_ptr(), bs, ts, _ptr(q_weight),
+            _ptr(k_weight), _ptr(freqs), _ptr(pos), pos_bs, pos0, axes, sections, q.data_ptr(),
+            k.data_ptr(), v.data_ptr(), B, N, H, Hkv, d, float(eps), _dtype_code(qkv))
     return q, k, v
 
 
@@ -838,12 +839,9 @@ def ringx_qkv_norm_rope_bwd(qkv, dq, dk, dv, freqs, rot, pos=None, pos0: int = 0
             workspace, ringx_qkv_norm_rope_bwd_workspace_bytes(B, N, H, Hkv, d, code), qkv)
     else:
         workspace = None
-    st = lib().ringx_qkv_norm_rope_bwd(qkv.data_ptr(), bs, ts, dq.data_ptr(), dk.data_ptr(),
-                                       dv.data_ptr(), _ptr(q_weight), _ptr(k_weight), _ptr(freqs),
-                                       _ptr(pos), pos_bs, pos0, axes, sections, dqkv.data_ptr(),
-                                       _ptr(dq_weight), _ptr(dk_weight), B, N, H, Hkv, d, float(eps),
-                                       code, _ptr(workspace),
-                                       0 if workspace is None else _nbytes(workspace),
-                                       _stream(stream))
-    _check("ringx_qkv_norm_rope_bwd", st)
+    _launch("ringx_qkv_norm_rope_bwd", qkv, stream, qkv.data_ptr(), bs, ts, dq.data_ptr(),
+            dk.data_ptr(), dv.data_ptr(), _ptr(q_weight), _ptr(k_weight), _ptr(freqs), _ptr(pos),
+            pos_bs, pos0, axes, sections, dqkv.data_ptr(), _ptr(dq_weight), _ptr(dk_weight), B, N,
+            H, Hkv, d, float(eps), code, _ptr(workspace), 0 if workspace is None else
+            _nbytes(workspace))
     return dqkv, dq_weight, dk_weight

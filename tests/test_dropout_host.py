@@ -153,3 +153,27 @@ def test_binding_refuses_a_wrong_generator_state():
     t = torch.zeros(2, dtype=torch.int64)
     with pytest.raises(ValueError, match="GPU"):
         ringx._rng(t, t)
+
+
+def test_calls_run_on_the_tensors_device(monkeypatch):
+    """An entry point is called with its tensors' device current and that device's current stream."""
+    import contextlib
+    import types
+    seen, current = [], [0]
+
+    @contextlib.contextmanager
+    def device(d):
+        old, current[0] = current[0], d.index
+        yield
+        current[0] = old
+
+    cuda = types.SimpleNamespace(current_device=lambda: current[0], device=device)
+    monkeypatch.setattr(ringx, "_T", types.SimpleNamespace(cuda=cuda))
+    monkeypatch.setattr(ringx, "_raw_stream", lambda d: 100 + d)
+    fake = types.SimpleNamespace(entry=lambda *a: seen.append((current[0], a)) or 0)
+    monkeypatch.setattr(ringx, "lib", lambda: fake)
+    for index in (0, 3):
+        like = types.SimpleNamespace(device=types.SimpleNamespace(index=index))
+        ringx._launch("entry", like, None, 7)
+        ringx._launch("entry", like, 55, 8)
+    assert seen == [(0, (7, 100)), (0, (8, 55)), (3, (7, 103)), (3, (8, 55))] and current == [0]
