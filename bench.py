@@ -389,13 +389,14 @@ MIX_KERNELS = [("fwd_bf16_kernel", (128, 0, 1, 8), "fwd_bf16_kernel<128, fused m
                ("bwd_dq_kernel", (64, 1, 8, 64), "bwd_dq_kernel<64>", 2),
                ("bwd_dq_kernel", (64, 1, 4, 32), "bwd_dq_kernel<64>, half-size", 3)]
 
+FWD_SOURCES = ["fwd_bf16.hip", "fwd_bf16_kernel.h", "ringx_device.h"]
 # kernel, template arguments -> (label in the summaries, traffic key, source files of its hash): the
 # forms that the full launches of the profiled workload take
 PROFILE_KERNELS = [
     ("fwd_bf16_kernel", (128, 0, 1, 8), "fwd_bf16_kernel<128, fused merge>", "fwd_bf16",
-     ["fwd_bf16.hip", "ringx_device.h"]),
+     FWD_SOURCES),
     ("fwd_bf16_kernel", (128, 1, 1, 8), "fwd_bf16_kernel<128, partials>", "fwd_bf16_partials",
-     ["fwd_bf16.hip", "ringx_device.h"]),
+     FWD_SOURCES),
     ("bwd_dkdv_kernel", (128, False), "bwd_dkdv_kernel<128>", "bwd_dkdv",
      ["bwd_bf16.hip", "ringx_device.h"]),
     ("bwd_dkdv_kernel", (128, True), "bwd_dkdv_kernel<128, dS stores>", "bwd_dkdv_store",
@@ -927,7 +928,7 @@ def main():
         "fwd_bf16_kernel": {"ms": fwd_ms, "flops": 2 * U, "work": "4*B*H*Nq*Nk*d (QK^T, PV)",
                             "tflops": tf(2 * U, fwd_ms),
                             "traffic": load_traffic("fwd_bf16", w.name,
-                                                    kernel_source_hash(["fwd_bf16.hip", "ringx_device.h"]))},
+                                                    kernel_source_hash(FWD_SOURCES))},
         # the backward's four algorithmic contractions (dV, dP, dK, dQ) are credited to the kernel
         # that computes them first: dP is part of the dK/dV pass, the dQ pass recomputes S and dP
         "bwd_dkdv_kernel": {"ms": dkdv_ms, "flops": 3 * U,

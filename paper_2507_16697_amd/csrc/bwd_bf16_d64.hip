@@ -20,8 +20,8 @@ namespace ringx {
 hipError_t launch_bwd_dkdv_bf16_d64(const BwdArgs& a) {
   const int64_t n = a.BH / a.G * a.R * ds_tiles_per_chunk(a.Nk, a.R);
   const bool ragged = n > 256 && n < 1024 && (n - 1) % 256 < 128;
-  if (n <= 128 || ragged) return launch<64, 4, 1, NoDrop>(a, NoDrop{});
-  return n <= 256 ? launch<64, 8, 2, NoDrop>(a, NoDrop{}) : launch<64, 8, 1, NoDrop>(a, NoDrop{});
+  if (n <= 128 || ragged) return launch<64, 4, 1>(a, NoDrop{});
+  return n <= 256 ? launch<64, 8, 2>(a, NoDrop{}) : launch<64, 8, 1>(a, NoDrop{});
 }
 
 }  // namespace ringx

@@ -124,8 +124,8 @@ __device__ __forceinline__ void issue_rowvals(const float* __restrict__ nlb,
 }
 
 // waves per SIMD: three 4-wave workgroups on a CU, two of 8 waves with 32 queries each
-template <int D, int NW, int QB, class DROP>
-__global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 : 1) void bwd_dkdv_kernel(
+template <int D, int NW, int QB>
+__global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 : 1) void RINGX_KERNEL(bwd_dkdv)(
     const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
     const __bf16* __restrict__ dout, const float* __restrict__ nl,
     const float* __restrict__ delta, float* __restrict__ dk, float* __restrict__ dv, int BHkv,
@@ -232,10 +232,10 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
   // of the two halves alternating, so that byte c of the row's first 16 is that of key c and byte
   // c of the others that of key 16 + c; transposed 8-byte reads (16 lanes: 8 rows of 16 bytes, each
   // lane a column) turn them round.
-  const DropKey dkey(drop_rng(drop));
-  const float dedge = drop_edge(drop);
-  const uint32_t dgroup = 2 * (drop_kb0(drop) + (uint32_t)(k0 / 32) + kb) + ((n >> 2) & 1);
-  const uint32_t dquery = drop_q0(drop) + 32 * qh + 8 * (n >> 3) + 4 * g + (n & 3);
+  const DropKey dkey(drop.rng);
+  const float dedge = (float)(int)drop.thr - 1.f;
+  const uint32_t dgroup = 2 * (drop.kb0 + (uint32_t)(k0 / 32) + kb) + ((n >> 2) & 1);
+  const uint32_t dquery = drop.q0 + 32 * qh + 8 * (n >> 3) + 4 * g + (n & 3);
   char* const dx = lds + C::kLds + wave * C::kQB * kMaskWave + g * 512;
   char* const dxw = dx + (4 * (n >> 3) + (n & 3)) * 32 + 4 * ((n >> 2) & 1);
   const char* const dxr = dx + ((n & 15) >> 1) * 32 + (n & 1) * 8 + (n >> 4) * 16;
@@ -561,13 +561,13 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
   }
 }
 
-template <int D, int NW, int QB, class DROP>
+template <int D, int NW, int QB>
 hipError_t launch(const BwdArgs& a, const DROP& drop) {
   using C = DkvCfg<D, NW, QB>;
   const int64_t max_chunk = (a.Nk + a.R - 1) / a.R;
   const int64_t tpc = (max_chunk + C::kBK - 1) / C::kBK;
   const int64_t nwg = a.BH / a.G * a.R * tpc;
-  hipLaunchKernelGGL((bwd_dkdv_kernel<D, NW, QB, DROP>), dim3((uint32_t)nwg), dim3(C::kThreads), 0,
+  hipLaunchKernelGGL((RINGX_KERNEL(bwd_dkdv)<D, NW, QB>), dim3((uint32_t)nwg), dim3(C::kThreads), 0,
                      a.stream, (const __bf16*)a.q, (const __bf16*)a.k, (const __bf16*)a.v,
                      (const __bf16*)a.dout, a.nl, a.delta, a.dk, a.dv, (int)(a.BH / a.G),
                      (int)a.H, (int)a.G, a.Nq, a.Nk,

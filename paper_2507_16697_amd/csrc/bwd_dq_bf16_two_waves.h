@@ -111,8 +111,8 @@ __device__ __forceinline__ void issue_tile(const char* __restrict__ kb,
 
 // With KS > 1 key streams, stream p of the workgroup takes every KS-th key tile, and the streams'
 // dQ^T meet in LDS at the end.
-template <int D, int KS, int NW, int BK, class DROP>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void bwd_dq_kernel(
+template <int D, int KS, int NW, int BK>
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(bwd_dq)(
     const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
     const __bf16* __restrict__ dout, const float* __restrict__ lse,
     const float* __restrict__ delta, float* __restrict__ dq, int BH, int H, int grp, int64_t Nq,
@@ -181,9 +181,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void bwd_dq_kernel(
   }
   const float nl = -lse[bh * Nq + qi] * kLog2e;
   const float dq_d = delta[bh * Nq + qi];
-  const DropKey dkey(drop_rng(drop));
-  const float dedge = drop_edge(drop);
-  const uint32_t dquery = drop_q0(drop) + (uint32_t)qi;
+  const DropKey dkey(drop.rng);
+  const float dedge = (float)(int)drop.thr - 1.f;
+  const uint32_t dquery = drop.q0 + (uint32_t)qi;
   // the dP accumulators start from -D (the same for every key of this lane's query), so that they
   // come out of the matrix cores as dP - D
   f32x16 pinit;
@@ -391,12 +391,12 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void bwd_dq_kernel(
   }
 }
 
-template <int D, int KS, int NW, int BK, class DROP>
+template <int D, int KS, int NW, int BK>
 hipError_t launch(const BwdArgs& a, const DROP& drop) {
   using C = DqCfg<D, KS, NW, BK>;
   const int64_t nqt = (a.Nq + C::kBQ - 1) / C::kBQ;
   const int64_t nwg = nqt * a.BH;
-  hipLaunchKernelGGL((bwd_dq_kernel<D, KS, NW, BK, DROP>), dim3((uint32_t)nwg), dim3(C::kThreads), 0,
+  hipLaunchKernelGGL((RINGX_KERNEL(bwd_dq)<D, KS, NW, BK>), dim3((uint32_t)nwg), dim3(C::kThreads), 0,
                      a.stream, (const __bf16*)a.q, (const __bf16*)a.k, (const __bf16*)a.v,
                      (const __bf16*)a.dout, a.lse, a.delta, a.dq, (int)a.BH, (int)a.H, (int)a.G,
                      a.Nq, a.Nk, (int)a.R, a.scale * kLog2e, a.scale, a.accumulate_dq ? 1 : 0, drop);

@@ -1,6 +1,7 @@
 // Recompute backward with dropout, dQ part, bf16: launches of the kernel in bwd_dq_bf16_two_waves.h
 // with it, at both head sizes.
 
+#define RINGX_DROPOUT
 #include "bwd_dq_bf16_two_waves.h"
 
 namespace ringx {

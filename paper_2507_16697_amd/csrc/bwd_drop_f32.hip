@@ -1,5 +1,6 @@
 // Recompute backward with dropout, fp32: launches of the kernel in bwd_f32_kernel.h with it.
 
+#define RINGX_DROPOUT
 #include "bwd_f32_kernel.h"
 
 namespace ringx {

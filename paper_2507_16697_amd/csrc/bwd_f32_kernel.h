@@ -76,7 +76,7 @@ __device__ __forceinline__ void store_rows(const AccF32<NS>& a, const F32Dims<NS
   }
 }
 
-template <int NS, int EDGE, class DROP>
+template <int NS, int EDGE>
 __device__ __forceinline__ void dkdv_tile(const BwdF32Args& A, const F32Dims<NS, EDGE>& D, int64_t tile,
                                           float* lds, int wave, const DROP& drop, const DropKey& dkey) {
   constexpr bool kDrop = kHasDrop<DROP>;
@@ -174,13 +174,13 @@ __device__ __forceinline__ void dkdv_tile(const BwdF32Args& A, const F32Dims<NS,
     reduce_parts(dv, D, lds, wave, kp, ks);
   }
   if (kp == 0 && active) {
-    const float f = drop_inv_keep(drop);
+    const float f = drop.inv_keep;
     store_rows(dk, D, A.dk + krow * d, A.scale * f, A.acc_kv);
     store_rows(dv, D, A.dv + krow * d, f, A.acc_kv);
   }
 }
 
-template <int NS, int EDGE, class DROP>
+template <int NS, int EDGE>
 __device__ __forceinline__ void dq_tile(const BwdF32Args& A, const F32Dims<NS, EDGE>& D, int64_t tile,
                                         float* lds, int wave, const DROP& drop, const DropKey& dkey) {
   constexpr bool kDrop = kHasDrop<DROP>;
@@ -238,12 +238,12 @@ __device__ __forceinline__ void dq_tile(const BwdF32Args& A, const F32Dims<NS, E
     dq.add(kc, ds);
   }
   if (ks > 1) reduce_parts(dq, D, lds, wave, kp, ks);
-  if (kp == 0 && active) store_rows(dq, D, A.dq + qrow * d, A.scale * drop_inv_keep(drop), A.acc_q);
+  if (kp == 0 && active) store_rows(dq, D, A.dq + qrow * d, A.scale * drop.inv_keep, A.acc_q);
 }
 
-template <int NS, int EDGE, class DROP>
-__global__ __launch_bounds__(kThreads, 2) void bwd_f32_kernel(BwdF32Args A, DROP drop) {
-  const DropKey dkey(drop_rng(drop));
+template <int NS, int EDGE>
+__global__ __launch_bounds__(kThreads, 2) void RINGX_KERNEL(bwd_f32)(BwdF32Args A, DROP drop) {
+  const DropKey dkey(drop.rng);
   __shared__ __attribute__((aligned(16))) float lds[kF32Waves * 16 * (16 * NS + 4)];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -254,7 +254,7 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_f32_kernel(BwdF32Args A, DROP
   }
 }
 
-template <int NS, int EDGE, class DROP>
+template <int NS, int EDGE>
 hipError_t launch_edge(const BwdArgs& a, bool want_kv, bool want_q, const DROP& drop) {
   BwdF32Args A;
   A.q = (const float*)a.q, A.k = (const float*)a.k, A.v = (const float*)a.v;
@@ -275,18 +275,17 @@ hipError_t launch_edge(const BwdArgs& a, bool want_kv, bool want_q, const DROP& 
   A.n_q = want_q ? A.tiles_q * a.BH : 0;
   // a workgroup takes further tiles when the grid's limit cuts it short
   const dim3 grid((uint32_t)std::min<int64_t>(A.n_kv + A.n_q, 1 << 22));
-  hipLaunchKernelGGL((bwd_f32_kernel<NS, EDGE, DROP>), grid, dim3(kThreads), 0, a.stream, A, drop);
+  hipLaunchKernelGGL((RINGX_KERNEL(bwd_f32)<NS, EDGE>), grid, dim3(kThreads), 0, a.stream, A, drop);
   return hipGetLastError();
 }
 
-template <int NS, class DROP>
+template <int NS>
 hipError_t launch(const BwdArgs& a, bool want_kv, bool want_q, const DROP& drop) {
   if (a.d == 16 * NS) return launch_edge<NS, kFull>(a, want_kv, want_q, drop);
   if (a.d % 4 == 0) return launch_edge<NS, kQuad>(a, want_kv, want_q, drop);
   return launch_edge<NS, kAny>(a, want_kv, want_q, drop);
 }
 
-template <class DROP>
 hipError_t launch_any(const BwdArgs& a, bool want_kv, bool want_q, const DROP& drop) {
   switch ((a.d + 15) / 16) {
     case 1: return launch<1>(a, want_kv, want_q, drop);

@@ -20,24 +20,27 @@
 
 namespace ringx {
 
-struct NoDrop {};   // kernels without dropout
+// The argument of kernels without dropout: Drop's fields, as constants.
+struct NoDrop {
+  static constexpr const uint64_t* rng = nullptr;
+  static constexpr uint32_t thr = 0, q0 = 0, kb0 = 0;
+  static constexpr float inv_keep = 1.f;
+};
 
-// The fields, 0 without dropout.
-__device__ __forceinline__ const uint64_t* drop_rng(const NoDrop&) { return nullptr; }
-__device__ __forceinline__ const uint64_t* drop_rng(const Drop& d) { return d.rng; }
-__device__ __forceinline__ uint32_t drop_q0(const NoDrop&) { return 0; }
-__device__ __forceinline__ uint32_t drop_q0(const Drop& d) { return d.q0; }
-__device__ __forceinline__ uint32_t drop_fill(const NoDrop&) { return 0; }
-__device__ __forceinline__ uint32_t drop_fill(const Drop& d) { return (255u - d.thr) * 0x01010101u; }
-__device__ __forceinline__ float drop_edge(const NoDrop&) { return 0.f; }
-__device__ __forceinline__ float drop_edge(const Drop& d) { return (float)(int)d.thr - 1.f; }
-__device__ __forceinline__ uint32_t drop_kb0(const NoDrop&) { return 0; }
-__device__ __forceinline__ uint32_t drop_kb0(const Drop& d) { return d.kb0; }
-__device__ __forceinline__ float drop_inv_keep(const NoDrop&) { return 1.f; }
-__device__ __forceinline__ float drop_inv_keep(const Drop& d) { return d.inv_keep; }
+template <class T>
+constexpr bool kHasDrop = !std::is_same_v<T, NoDrop>;
 
-template <class DROP>
-constexpr bool kHasDrop = !std::is_same_v<DROP, NoDrop>;
+// The attention kernels stand in headers and are compiled twice, by a source file without dropout and by
+// one with it, which defines RINGX_DROPOUT and so gives them this argument and names of their own.
+namespace {
+#ifdef RINGX_DROPOUT
+using DROP = Drop;
+#define RINGX_KERNEL(name) name##_drop_kernel
+#else
+using DROP = NoDrop;
+#define RINGX_KERNEL(name) name##_kernel
+#endif
+}  // namespace
 
 // The generator's state as the kernels hold it (wave-uniform).
 struct DropKey {

@@ -9,11 +9,11 @@ template <int D, int MODE>
 hipError_t launch_plan(const FwdArgs& a) {
   const FwdPlan p = fwd_plan((a.Nq + 255) / 256 * a.BH, a.Nk, a.R, D, MODE == (int)FwdMode::kPartials);
   if constexpr (D == 64)
-    if (p.cut.half) return launch<D, MODE, 1, 4, NoDrop>(a, p.rg, NoDrop{});
+    if (p.cut.half) return launch<D, MODE, 1, 4>(a, p.rg, NoDrop{});
   if constexpr (MODE != (int)FwdMode::kPartials)
-    if (p.cut.ks == 4) return launch<D, MODE, 4, 8, NoDrop>(a, p.rg, NoDrop{});
-  if (p.cut.ks == 2) return launch<D, MODE, 2, 8, NoDrop>(a, p.rg, NoDrop{});
-  return launch<D, MODE, 1, 8, NoDrop>(a, p.rg, NoDrop{});
+    if (p.cut.ks == 4) return launch<D, MODE, 4, 8>(a, p.rg, NoDrop{});
+  if (p.cut.ks == 2) return launch<D, MODE, 2, 8>(a, p.rg, NoDrop{});
+  return launch<D, MODE, 1, 8>(a, p.rg, NoDrop{});
 }
 
 template <int D>

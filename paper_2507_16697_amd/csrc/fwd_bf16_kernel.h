@@ -140,8 +140,8 @@ __device__ __forceinline__ void issue_tile(const char* __restrict__ base, uint32
 // partials mode only, where chunks are independent).  With KS > 1 key streams, stream p of the
 // workgroup takes every KS-th key tile of the range (the whole range in fused and step mode, one
 // chunk after the other in partials mode) and the streams merge through LDS at its end.
-template <int D, int MODE, int KS, int NW, class DROP>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void fwd_bf16_kernel(
+template <int D, int MODE, int KS, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(fwd_bf16)(
     const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
     __bf16* __restrict__ out, float* __restrict__ lse, float* __restrict__ part_out,
     float* __restrict__ part_lse, float* __restrict__ acc_out, float* __restrict__ acc_lse,
@@ -245,9 +245,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void fwd_bf16_kernel(
   }
 
   // the generator's state, and its index of this lane's query
-  const DropKey dkey(drop_rng(drop));
-  const uint32_t dfill = drop_fill(drop);
-  const uint32_t dq0 = drop_q0(drop) + (uint32_t)(q0 + n);
+  const DropKey dkey(drop.rng);
+  const uint32_t dfill = (255u - drop.thr) * 0x01010101u;
+  const uint32_t dq0 = drop.q0 + (uint32_t)(q0 + n);
 
   // Q fragments (B operand of S^T = K Q^T): query n of this wave, dims 16*ks + 8g .. +8.
   bf16x8 qf[C::kDSteps];
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void fwd_bf16_kernel(
   // beside the P V products, where the vector ALU has nothing else to do.
   constexpr int kMasks = kDrop ? C::kKTiles : 1;
   u32x4 dw[kMasks];
-  uint32_t dgroup = 2 * (drop_kb0(drop) + t0.start / 32) + g;   // the tile's first 16-key group
+  uint32_t dgroup = 2 * (drop.kb0 + t0.start / 32) + g;   // the tile's first 16-key group
   auto next_mask = [&] {
     if constexpr (kDrop) {
 #pragma unroll
@@ -667,11 +667,11 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void fwd_bf16_kernel(
   }
 }
 
-template <int D, int MODE, int KS, int NW, class DROP>
+template <int D, int MODE, int KS, int NW>
 hipError_t launch(const FwdArgs& a, int64_t RG, const DROP& drop) {
   using C = FwdCfg<D, KS, NW>;
   const int64_t nwg = (a.Nq + C::kBQ - 1) / C::kBQ * a.BH * RG;
-  hipLaunchKernelGGL((fwd_bf16_kernel<D, MODE, KS, NW, DROP>), dim3((uint32_t)nwg), dim3(C::kThreads), 0,
+  hipLaunchKernelGGL((RINGX_KERNEL(fwd_bf16)<D, MODE, KS, NW>), dim3((uint32_t)nwg), dim3(C::kThreads), 0,
                      a.stream, (const __bf16*)a.q, (const __bf16*)a.k, (const __bf16*)a.v,
                      (__bf16*)a.out, a.lse, a.part_out, a.part_lse, a.acc_out, a.acc_lse,
                      a.first ? 1 : 0, (int)a.BH, (int)a.H, (int)a.G, a.Nq, a.Nk, (int)a.R, (int)RG,

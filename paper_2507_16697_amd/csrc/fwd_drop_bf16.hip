@@ -1,5 +1,6 @@
 // Attention forward with dropout, bf16: launches of the kernel in fwd_bf16_kernel.h with it.
 
+#define RINGX_DROPOUT
 #include "fwd_bf16_kernel.h"
 
 namespace ringx {

@@ -1,5 +1,6 @@
 // Attention forward with dropout, fp32: launches of the kernel in fwd_f32_kernel.h with it.
 
+#define RINGX_DROPOUT
 #include "fwd_f32_kernel.h"
 
 namespace ringx {

@@ -37,13 +37,13 @@ namespace {
 
 constexpr int kThreads = 64 * kF32Waves;
 
-template <int NS, int EDGE, class DROP>
-__global__ __launch_bounds__(kThreads, 2) void fwd_f32_kernel(
+template <int NS, int EDGE>
+__global__ __launch_bounds__(kThreads, 2) void RINGX_KERNEL(fwd_f32)(
     const float* __restrict__ q, const float* __restrict__ k, const float* __restrict__ v,
     float* __restrict__ out, float* __restrict__ lse, int mode, int first, int64_t BH, int H,
     int grp, int64_t Nq, int64_t Nk, int64_t R, int d, float scale, int ks_log2, DROP drop) {
   constexpr bool kDrop = kHasDrop<DROP>;
-  const DropKey dkey(drop_rng(drop));
+  const DropKey dkey(drop.rng);
   // the key-split merge: per wave 16 queries x (16 NS dims, m, l)
   constexpr int kRow = 16 * NS + 4;
   __shared__ __attribute__((aligned(16))) float part[kF32Waves * 16 * kRow];
@@ -217,7 +217,7 @@ __global__ __launch_bounds__(kThreads, 2) void fwd_f32_kernel(
   }
 }
 
-template <int NS, int EDGE, class DROP>
+template <int NS, int EDGE>
 hipError_t launch_edge(const FwdArgs& a, FwdMode mode, const DROP& drop) {
   const bool partials = mode == FwdMode::kPartials;
   const int64_t blocks = (a.Nq + 15) / 16, chunks = partials ? a.R : 1;
@@ -228,21 +228,20 @@ hipError_t launch_edge(const FwdArgs& a, FwdMode mode, const DROP& drop) {
                   (uint32_t)std::min<int64_t>(chunks, 65535));
   float* out = partials ? a.part_out : mode == FwdMode::kStep ? a.acc_out : (float*)a.out;
   float* lse = partials ? a.part_lse : mode == FwdMode::kStep ? a.acc_lse : a.lse;
-  hipLaunchKernelGGL((fwd_f32_kernel<NS, EDGE, DROP>), grid, dim3(kThreads), 0, a.stream, (const float*)a.q,
+  hipLaunchKernelGGL((RINGX_KERNEL(fwd_f32)<NS, EDGE>), grid, dim3(kThreads), 0, a.stream, (const float*)a.q,
                      (const float*)a.k, (const float*)a.v, out, lse, (int)mode, a.first ? 1 : 0,
                      a.BH, (int)a.H, (int)a.G, a.Nq, a.Nk, a.R, (int)a.d, a.scale,
                      __builtin_ctz(ks), drop);
   return hipGetLastError();
 }
 
-template <int NS, class DROP>
+template <int NS>
 hipError_t launch(const FwdArgs& a, FwdMode mode, const DROP& drop) {
   if (a.d == 16 * NS) return launch_edge<NS, kFull>(a, mode, drop);
   if (a.d % 4 == 0) return launch_edge<NS, kQuad>(a, mode, drop);
   return launch_edge<NS, kAny>(a, mode, drop);
 }
 
-template <class DROP>
 hipError_t launch_any(const FwdArgs& a, FwdMode mode, const DROP& drop) {
   switch ((a.d + 15) / 16) {
     case 1: return launch<1>(a, mode, drop);
