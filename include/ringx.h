@@ -384,7 +384,8 @@ ringx_status ringx_bwd_preprocess_drop(const void* out, const void* dout, const 
  *         (pos_batch_stride = N axes); NULL with axes = 1: positions pos0 + n, |pos0| <= 2^40.
  *   v is copied.
  * d as the attention takes it (bf16: 64, 128; fp32: 1 .. 128); Hkv divides H.  bf16 strides are
- * multiples of 8 elements (RINGX_E_ALIGN); fp32 takes any.  Outputs overlap no input.
+ * multiples of 8 elements (RINGX_E_ALIGN); fp32 takes any.  Outputs overlap no input.  Tokens that one
+ * launch cannot take (B N of 2^28 and more at d = 128 in bf16, more where d is less): RINGX_E_SHAPE.
  */
 ringx_status ringx_qkv_norm_rope(const void* qkv, int64_t batch_stride, int64_t token_stride,
                                  const float* q_weight, const float* k_weight, const double* freqs,

@@ -967,6 +967,9 @@ ringx_status ringx_qkv_norm_rope(const void* qkv, int64_t batch_stride, int64_t 
       make_rope(qkv, batch_stride, token_stride, q_weight, k_weight, freqs, pos, pos_batch_stride,
                 pos0, axes, rot, B, N, H, Hkv, d, eps, dtype, stream, &a, &sx);
   if (st != RINGX_OK) return st;
+  // a launch has at most 2^32 threads
+  const int per_wave = 64 / ringx::rope_lanes(d, dtype == RINGX_BF16);
+  if (ringx::rope_grid(B * N, (int)(H + 2 * Hkv), per_wave, false).x >= (1 << 24)) return RINGX_E_SHAPE;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return RINGX_E_ALIGN;
   const int64_t row = B * N * d * esize(dtype);
   const Span outs[] = {span(q, H * row), span(k, Hkv * row), span(v, Hkv * row)};

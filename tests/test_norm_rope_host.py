@@ -106,6 +106,16 @@ def test_refusals_of_overlaps_and_weights():
 
 
 @needs_lib
+def test_refusal_of_more_tokens_than_a_launch_takes():
+    # 256 tokens to a workgroup of 2^24 - 1 at one dim per head; the last size that fits is refused for
+    # another reason here (an output on top of the projection)
+    most = ((1 << 24) - 1) * 256
+    one = dict(B=1, H=1, Hkv=1, d=1, dt=FP32, rot=(0,), pos=None, f=None, qw=None, kw=None, bs=0, ts=0)
+    assert fwd(N=most + 1, **one) == SHAPE
+    assert fwd(N=most, q=XP, **one) == ALIAS
+
+
+@needs_lib
 def test_workspace_sizes():
     ask = ringx.ringx_qkv_norm_rope_bwd_workspace_bytes
     assert ask(0, 1, 1, 1, 64, BF16) == 0 and ask(1, 1, 3, 2, 64, BF16) == 0
