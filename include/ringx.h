@@ -337,8 +337,10 @@ ringx_status ringx_attn_fwd_drop(const void* q, const void* k, const void* v, vo
                                  float scale, ringx_dtype dtype, float p, const uint64_t* rng,
                                  int64_t q0, int64_t key0, hipStream_t stream);
 
-/* Backward of ringx_attn_fwd_drop, with its p, rng values, q0 and key0.  Workspace as ringx_attn_bwd
- * (ringx_bwd_workspace_bytes with R = 1). */
+/* Backward of ringx_attn_fwd_drop, with its p, rng values, q0 and key0.  workspace:
+ * ringx_bwd_drop_workspace_bytes(...) bytes, 16-byte aligned, contents ignored.  Bitwise reproducible. */
+size_t ringx_bwd_drop_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
+                                      int64_t d, ringx_dtype dtype);
 ringx_status ringx_attn_bwd_drop(const void* q, const void* k, const void* v, const void* out,
                                  const void* dout, const float* lse, float* dq, float* dk, float* dv,
                                  int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,

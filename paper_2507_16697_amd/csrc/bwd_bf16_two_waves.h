@@ -146,7 +146,13 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
   const int kb = wave % C::kKB;     // key block of this wave
   const int qh = wave / C::kKB;     // parity of this wave's 32-query blocks
 
-  const uint32_t wg = xcd_remap(blockIdx.x, gridDim.x);
+  uint32_t wg = xcd_remap(blockIdx.x, gridDim.x);
+  uint32_t split = 0;
+  if constexpr (kDrop) {
+    const uint32_t per_split = gridDim.x / drop.splits;
+    split = wg / per_split;
+    wg -= split * per_split;
+  }
   const int64_t per_bh = (int64_t)R * tiles_per_chunk;
   const int64_t bh = wg / per_bh;   // K/V head (of B * H / G)
   const int r = (int)((wg % per_bh) / tiles_per_chunk);
@@ -163,14 +169,19 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
   // the grp query heads sharing this K/V head are swept one after the other: query tile it is
   // tile it % nqt of head qh0 + it / nqt
   const int64_t qh0 = (bh / (H / grp)) * H + (bh % (H / grp)) * grp;
-  const __bf16* qb = q + qh0 * Nq * D;
-  const __bf16* ob = dout + qh0 * Nq * D;
-  const float* nlb = nl + qh0 * Nq;
-  const float* deltab = delta + qh0 * Nq;
+  // with dropout a workgroup may sweep a part of every head's queries alone, never an empty one
+  static_assert(!kDrop || C::kBQ <= 128, "parts of at least 128 queries hold a tile");
+  const int64_t all_tiles = (Nq + C::kBQ - 1) / C::kBQ;
+  const int64_t from = kDrop ? split * all_tiles / drop.splits * C::kBQ : 0;
+  const int64_t to = kDrop ? min<int64_t>((split + 1) * all_tiles / drop.splits * C::kBQ, Nq) : Nq;
+  const __bf16* qb = q + (qh0 * Nq + from) * D;
+  const __bf16* ob = dout + (qh0 * Nq + from) * D;
+  const float* nlb = nl + qh0 * Nq + from;
+  const float* deltab = delta + qh0 * Nq + from;
 
   // query positions within a head are 32-bit (the library takes at most 2^31 - 128 queries
   // per head), so that the tile bookkeeping stays scalar instructions
-  const int nq = (int)Nq;
+  const int nq = (int)(to - from);
   const int nqt = (nq + C::kBQ - 1) / C::kBQ;
 
   // K and V tiles (kept for the whole sweep), then the first query tile
@@ -235,7 +246,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
   const DropKey dkey(drop.rng);
   const float dedge = (float)(int)drop.thr - 1.f;
   const uint32_t dgroup = 2 * (drop.kb0 + (uint32_t)(k0 / 32) + kb) + ((n >> 2) & 1);
-  const uint32_t dquery = drop.q0 + 32 * qh + 8 * (n >> 3) + 4 * g + (n & 3);
+  const uint32_t dquery = drop.q0 + (uint32_t)from + 32 * qh + 8 * (n >> 3) + 4 * g + (n & 3);
   char* const dx = lds + C::kLds + wave * C::kQB * kMaskWave + g * 512;
   char* const dxw = dx + (4 * (n >> 3) + (n & 3)) * 32 + 4 * ((n >> 2) & 1);
   const char* const dxr = dx + ((n & 15) >> 1) * 32 + (n & 1) * 8 + (n >> 4) * 16;
@@ -524,8 +535,9 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
   // the two waves of a key block add their dK^T / dV^T through LDS
   float* xch = reinterpret_cast<float*>(lds + C::kOffQ);
   const int64_t key = k0 + 32 * kb + n;
-  float* dkr = dk + (bh * Nk + key) * D;
-  float* dvr = dv + (bh * Nk + key) * D;
+  const int64_t row = (int64_t)split * BHkv * Nk + bh * Nk + key;
+  float* dkr = dk + row * D;
+  float* dvr = dv + row * D;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     f32x16* acc = which == 0 ? dkt : dvt;
@@ -566,7 +578,7 @@ hipError_t launch(const BwdArgs& a, const DROP& drop) {
   using C = DkvCfg<D, NW, QB>;
   const int64_t max_chunk = (a.Nk + a.R - 1) / a.R;
   const int64_t tpc = (max_chunk + C::kBK - 1) / C::kBK;
-  const int64_t nwg = a.BH / a.G * a.R * tpc;
+  const int64_t nwg = a.BH / a.G * a.R * tpc * drop.splits;
   hipLaunchKernelGGL((RINGX_KERNEL(bwd_dkdv)<D, NW, QB>), dim3((uint32_t)nwg), dim3(C::kThreads), 0,
                      a.stream, (const __bf16*)a.q, (const __bf16*)a.k, (const __bf16*)a.v,
                      (const __bf16*)a.dout, a.nl, a.delta, a.dk, a.dv, (int)(a.BH / a.G),

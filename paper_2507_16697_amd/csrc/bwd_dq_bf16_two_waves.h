@@ -133,21 +133,32 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(bwd_dq)
   const int g = lane >> 5;
 
   const int64_t nqt = (Nq + C::kBQ - 1) / C::kBQ;
-  const uint32_t wg = xcd_remap(blockIdx.x, gridDim.x);
+  uint32_t wg = xcd_remap(blockIdx.x, gridDim.x);
+  uint32_t split = 0;
+  if constexpr (kDrop) {
+    const uint32_t per_split = gridDim.x / drop.splits;
+    split = wg / per_split;
+    wg -= split * per_split;
+  }
   const int64_t bh = wg / nqt;
   const int64_t q0 = (wg % nqt) * C::kBQ + wave * C::kQW;
   if (bh >= BH) return;
 
+  // with dropout a workgroup may sweep a part of the keys alone, never an empty one
+  static_assert(!kDrop || C::kBK <= 256, "parts of at least 256 keys hold a tile");
+  const int64_t all_tiles = (Nk + C::kBK - 1) / C::kBK;
+  const int64_t from = kDrop ? split * all_tiles / drop.splits * C::kBK : 0;
+  const int64_t to = kDrop ? min<int64_t>((split + 1) * all_tiles / drop.splits * C::kBK, Nk) : Nk;
   const int64_t kvh = kv_head(bh, H, grp);
   const char* kb =
-      static_cast<const char*>(uniform_ptr(reinterpret_cast<const char*>(k + kvh * Nk * D)));
+      static_cast<const char*>(uniform_ptr(reinterpret_cast<const char*>(k + (kvh * Nk + from) * D)));
   const char* vb =
-      static_cast<const char*>(uniform_ptr(reinterpret_cast<const char*>(v + kvh * Nk * D)));
+      static_cast<const char*>(uniform_ptr(reinterpret_cast<const char*>(v + (kvh * Nk + from) * D)));
   int goff[C::kLoads], grow[C::kLoads];
   load_offsets<C>(goff, grow, wave, lane);
 
   // the chunked key sequence, one tile at a time (32-bit positions, no divisions)
-  const uint32_t nk = (uint32_t)Nk;
+  const uint32_t nk = (uint32_t)(to - from);
   ChunkWalk walk{nk, nk / (uint32_t)R, nk % (uint32_t)R, 0, (uint32_t)R};
   KeyTile ct = walk.first();
   // KS > 1: rounds of KS tiles (a chunk has ceil(len / kBK) tiles, len = Nk / R or, in Nk mod R of
@@ -183,6 +194,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(bwd_dq)
   const float dq_d = delta[bh * Nq + qi];
   const DropKey dkey(drop.rng);
   const float dedge = (float)(int)drop.thr - 1.f;
+  const uint32_t kb0 = drop.kb0 + (uint32_t)(from / 32);
   const uint32_t dquery = drop.q0 + (uint32_t)qi;
   // the dP accumulators start from -D (the same for every key of this lane's query), so that they
   // come out of the matrix cores as dP - D
@@ -246,7 +258,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(bwd_dq)
     if constexpr (kDrop) {
 #pragma unroll
       for (int kt = 0; kt < C::kKTiles; ++kt)
-        dw[kt] = drop_bytes(2 * (drop.kb0 + ct.start / 32 + kt) + g, dquery, (uint32_t)bh, dkey);
+        dw[kt] = drop_bytes(2 * (kb0 + ct.start / 32 + kt) + g, dquery, (uint32_t)bh, dkey);
     }
     f32x16 sacc[C::kKTiles], pacc[C::kKTiles];
 #pragma unroll
@@ -377,7 +389,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(bwd_dq)
 
   if constexpr (kDrop) scale *= drop.inv_keep;
   if (q_ok) {
-    float* dqr = dq + (bh * Nq + qi) * D;
+    float* dqr = dq + (((int64_t)split * BH + bh) * Nq + qi) * D;
 #pragma unroll
     for (int c = 0; c < C::kCT; ++c)
 #pragma unroll
@@ -395,7 +407,7 @@ template <int D, int KS, int NW, int BK>
 hipError_t launch(const BwdArgs& a, const DROP& drop) {
   using C = DqCfg<D, KS, NW, BK>;
   const int64_t nqt = (a.Nq + C::kBQ - 1) / C::kBQ;
-  const int64_t nwg = nqt * a.BH;
+  const int64_t nwg = nqt * a.BH * drop.splits;
   hipLaunchKernelGGL((RINGX_KERNEL(bwd_dq)<D, KS, NW, BK>), dim3((uint32_t)nwg), dim3(C::kThreads), 0,
                      a.stream, (const __bf16*)a.q, (const __bf16*)a.k, (const __bf16*)a.v,
                      (const __bf16*)a.dout, a.lse, a.delta, a.dq, (int)a.BH, (int)a.H, (int)a.G,

@@ -23,7 +23,7 @@ namespace ringx {
 // The argument of kernels without dropout: Drop's fields, as constants.
 struct NoDrop {
   static constexpr const uint64_t* rng = nullptr;
-  static constexpr uint32_t thr = 0, q0 = 0, kb0 = 0;
+  static constexpr uint32_t thr = 0, q0 = 0, kb0 = 0, splits = 1;
   static constexpr float inv_keep = 1.f;
 };
 

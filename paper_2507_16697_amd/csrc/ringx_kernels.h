@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 namespace ringx {
 
 // What the forward does with each chunk's local result (loc_out_r, loc_lse_r).
@@ -195,6 +197,66 @@ struct Drop {
   float inv_keep = 1.f;            // 256 / (256 - thr)
   uint32_t q0 = 0;                 // generator's index of the launch's first query
   uint32_t kb0 = 0;                // and of its first 32-key block
+  uint32_t splits = 1;             // parts of the sweep (dK/dV: of the queries, dQ: of the keys), each in
+                                   // workgroups of its own, with outputs [splits, ...]
+};
+
+// How the backward with dropout, bf16, splits its sweeps over workgroups of their own where heads and rows
+// are too few to fill the chip; the parts are summed by a launch more (split_sum.hip).
+//   dQ     w workgroups of query_cut's form, up to 128 of them: as many parts of at least 256 keys as one
+//          round of 256 holds, at most 32.  The whole backward (us), unsplit -> split: 2 heads of 64, 1873
+//          queries, 5265 keys (w = 60) 87 -> 62; 4/1 of 64, 1000 x 30000 (64) 309 -> 157; 2 of 128,
+//          4096 x 4096 (128) 174 -> 155; 1 of 64, 300 x 900 (5) 31.5 -> 28.3.  From w = 129 on it loses
+//          (192: 340 -> 361).
+//   dK/dV  n tiles of 128 keys, `sweep` query rows to each (those of all heads of the group).  Parts of at
+//          least 256 rows, 128 of a head (a tile of queries), at most 32, as the shorter sum of rounds of 256 workgroups and of what
+//          the parts cost says, where that is a tenth less: a workgroup takes 0.026 us a row at d = 128
+//          and 0.02 at 64, and 5 or 3 besides; a round's parts 17 or 8.4 to write and read, their launch 4;
+//          unsplit workgroups of 64 keys at d = 64 save 4.5.  Fitted to times like (one, two, three,
+//          four parts; n x sweep):
+//            d = 128  64 x 4096 187 143 123 120, 64 x 16384 539 344 294 276, 160 x 4096 212 242 213
+//                     233, 192 x 8192 419 439 461 427, 192 x 1024 78 103 120 120
+//            d = 64   16 x 1024 41 37 35 35, 84 x 1873 86 87 84 88, 128 x 2048 69 71 73 74
+//          Where at d = 64 few tiles are left for the last round, two parts, also three workgroups of 64
+//          keys to a CU: 320 x 6000 346 -> 320, 288 x 3000 190 -> 185.
+struct DropSplit {
+  int kv = 1, q = 1;
+};
+inline bool ragged_last_round(int64_t n) { return n > 256 && n < 1024 && (n - 1) % 256 < 128; }
+inline DropSplit drop_split(int64_t BHkv, int64_t BH, int64_t Nq, int64_t Nk, int64_t d) {
+  DropSplit s;
+  const QueryCut c = query_cut((Nq + 255) / 256 * BH, Nk, dq_cut_rule(d));
+  const int64_t w = (Nq + 256 / c.ks - 1) / (256 / c.ks) * BH;
+  if (w <= 128) s.q = (int)std::max<int64_t>(1, std::min<int64_t>({256 / w, Nk / 256, 32}));
+  const int64_t n = (Nk + 127) / 128 * BHkv, sweep = Nq * (BH / BHkv);
+  if (d == 64 && ragged_last_round(n)) {
+    s.kv = Nq >= 256 && sweep >= 2048 ? 2 : 1;
+  } else if (n < 1024) {
+    const double row = d == 64 ? 0.02 : 0.026, start = d == 64 ? 3 : 5, parts = d == 64 ? 8.4 : 17;
+    double best = 0;
+    for (int64_t k = 1; k <= 32 && k <= std::max<int64_t>(1, std::min(Nq / 128, sweep / 256)); ++k) {
+      double us = (double)((n * k + 255) / 256) * ((double)sweep / (double)k * row + start);
+      if (k > 1) us += (double)(n * k) / 256 * parts + 4;
+      else if (d == 64 && n <= 128) us -= 4.5;
+      if (k == 1 || us < best) {
+        if (k > 1) s.kv = (int)k;
+        best = k == 1 ? 0.9 * us : us;
+      }
+    }
+  }
+  return s;
+}
+
+// out = (out +) sum of `splits` parts of 4 n4 floats
+struct SplitSum {
+  const float* part = nullptr;
+  float* out = nullptr;
+  int64_t n4 = 0;
+  int splits = 1, accumulate = 0;
+};
+struct SplitSums {
+  SplitSum sum[3];
+  int count = 0;
 };
 
 struct MergeArgs {
@@ -324,6 +386,7 @@ inline RopeGrid rope_grid(int64_t rows, int heads, int tokens_per_wave, bool bwd
 hipError_t launch_fwd_bf16(const FwdArgs& a, FwdMode mode);
 hipError_t launch_fwd_f32(const FwdArgs& a, FwdMode mode);
 hipError_t launch_lse_merge(const MergeArgs& a);
+hipError_t launch_split_sums(const SplitSums& a, hipStream_t stream);
 hipError_t launch_bwd_pre(const BwdArgs& a, bool bf16);
 hipError_t launch_bwd_dkdv_bf16(const BwdArgs& a);
 hipError_t launch_bwd_dkdv_bf16_d64(const BwdArgs& a);   // d = 64 (bwd_bf16_d64.hip)

@@ -46,7 +46,8 @@ EXPORTED = ("ringx_attn_fwd", "ringx_attn_fwd_partials", "ringx_lse_merge", "rin
             "ringx_chunk_bounds", "ringx_status_str", "ringx_attn_bwd_noalloc",
             "ringx_bwd_ds_bytes", "ringx_attn_bwd_dkdv_ds", "ringx_attn_bwd_dq_ds",
             "ringx_attn_bwd_ds", "ringx_bwd_ds_workspace_bytes", "ringx_attn_fwd_drop",
-            "ringx_attn_bwd_drop", "ringx_attn_fwd_step_drop", "ringx_attn_bwd_step_drop",
+            "ringx_attn_bwd_drop", "ringx_bwd_drop_workspace_bytes", "ringx_attn_fwd_step_drop",
+            "ringx_attn_bwd_step_drop",
             "ringx_bwd_preprocess_drop", "ringx_qkv_norm_rope", "ringx_qkv_norm_rope_bwd",
             "ringx_qkv_norm_rope_bwd_workspace_bytes")
 
@@ -114,6 +115,8 @@ def lib() -> ctypes.CDLL:
         L.ringx_attn_fwd_drop.argtypes = [_P] * 5 + [_I] * 6 + [F, C, F, _P, _I, _I, _P]
         L.ringx_attn_bwd_drop.argtypes = ([_P] * 9 + [_I] * 6 +
                                           [F, C, F, _P, _I, _I, C, _P, ctypes.c_size_t, _P])
+        L.ringx_bwd_drop_workspace_bytes.argtypes = [_I] * 6 + [C]
+        L.ringx_bwd_drop_workspace_bytes.restype = ctypes.c_size_t
         L.ringx_attn_fwd_step_drop.argtypes = [_P] * 5 + [_I] * 5 + [F, C, C, F, _P, _I, _I, _P]
         L.ringx_attn_bwd_step_drop.argtypes = [_P] * 9 + [_I] * 5 + [F, C, C, C, F, _P, _I, _I, _P]
         L.ringx_bwd_preprocess_drop.argtypes = [_P] * 4 + [_I] * 4 + [C, F, _P]
@@ -652,6 +655,10 @@ def ringx_attn_fwd_drop(q, k, v, p: float, rng, scale=None, q0: int = 0, key0: i
     return out, lse
 
 
+def ringx_bwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, dtype) -> int:
+    return int(lib().ringx_bwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, int(dtype)))
+
+
 def ringx_attn_bwd_drop(q, k, v, out, dout, lse, p: float, rng, scale=None, q0: int = 0,
                         key0: int = 0, dq=None, dk=None, dv=None, accumulate_dkv=False,
                         workspace=None, stream=None):
@@ -668,7 +675,7 @@ def ringx_attn_bwd_drop(q, k, v, out, dout, lse, p: float, rng, scale=None, q0: 
     dk = _grad_out("dk", dk, (B, Hkv, Nk, d), q, accumulate_dkv)
     dv = _grad_out("dv", dv, (B, Hkv, Nk, d), q, accumulate_dkv)
     code = _dtype_code(q)
-    workspace = _workspace(workspace, ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, 1, code), q)
+    workspace = _workspace(workspace, ringx_bwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, code), q)
     _launch("ringx_attn_bwd_drop", q, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(),
             out.data_ptr(), dout.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(),
             dv.data_ptr(), B, H, Hkv, Nq, Nk, d, _scale(scale, d), code, float(p), state, q0, key0,

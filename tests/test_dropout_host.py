@@ -132,7 +132,7 @@ def test_refusals_of_overlaps_and_groups():
     assert fwd(o=QP) == ALIAS and fwd(l=OP) == ALIAS and fwd(o=RP) == ALIAS and fwd(l=RP) == ALIAS
     assert fstep(o=KP) == ALIAS and fstep(l=RP) == ALIAS
     assert fwd(Hkv=3) == SHAPE and bwd(Hkv=0) == SHAPE
-    need = ringx.ringx_bwd_workspace_bytes(1, 4, 100, 300, 64, 1, BF16)
+    need = ringx.ringx_bwd_drop_workspace_bytes(1, 4, 2, 100, 300, 64, BF16)
     assert bwd(ws=0) == WORKSPACE and bwd(wsb=need - 1) == WORKSPACE
     assert bwd(dq=QP) == ALIAS and bwd(dk=OP) == ALIAS and bwd(ws=RP) == ALIAS and bwd(dv=RP) == ALIAS
     assert bstep(dq=RP) == ALIAS and bstep(dk=OP) == ALIAS and bstep(dv=0) == NULLPTR
@@ -140,6 +140,24 @@ def test_refusals_of_overlaps_and_groups():
     assert pre(QP, KP, LP, LP, 1, 2, 100, 64, BF16, 0.1, None) == ALIAS
     assert pre(QP, KP, LP, OP, 1, 2, 100, 64, BF16, 1.0, None) == DROPOUT
     assert pre(QP, 0, LP, OP, 1, 2, 100, 64, BF16, 0.1, None) == NULLPTR
+
+
+@needs_lib
+def test_backward_workspace_holds_the_parts():
+    size, stats = ringx.ringx_bwd_drop_workspace_bytes, ringx.ringx_bwd_workspace_bytes
+    # enough workgroups: the statistics alone; fp32 never splits
+    for B, H, Hkv, Nq, Nk, d in ((1, 16, 16, 4096, 4096, 64), (1, 16, 16, 4096, 32768, 128),
+                                 (1, 1, 1, 1, 1, 64)):
+        assert size(B, H, Hkv, Nq, Nk, d, BF16) == stats(B, H, Nq, Nk, d, 1, BF16)
+    assert size(1, 2, 2, 4096, 4096, 128, FP32) == stats(1, 2, 4096, 4096, 128, 1, FP32)
+    # 2 heads, 4096 x 4096: four parts of dK and dV and two of dQ
+    assert (size(1, 2, 2, 4096, 4096, 128, BF16) - stats(1, 2, 4096, 4096, 128, 1, BF16)
+            == (4 * 2 + 2) * 2 * 4096 * 128 * 4)
+    # never more parts than 256 keys or query rows each allow, however few the heads
+    for n in (1, 100, 255, 256, 511, 4096, 100000):
+        extra = size(1, 1, 1, n, n, 64, BF16) - stats(1, 1, n, n, 64, 1, BF16)
+        assert 0 <= extra <= 3 * min(32, n // 256) * n * 64 * 4
+    assert size(1, 4, 3, 100, 300, 64, BF16) == 0 and size(1, 4, 2, 0, 300, 64, BF16) == 0
 
 
 @needs_lib

@@ -113,6 +113,32 @@ def test_forward_and_backward(store, B, H, Hkv, Nq, Nk, d, p):
     check(x, got, p, SEED, f32_scale(d), store)
 
 
+# few heads: sweeps in parts that are summed afterwards, on both sides, on one, with shared heads, and
+# with small workgroups in a ragged launch; the parts end inside tiles of the whole
+@pytest.mark.parametrize("B,H,Hkv,Nq,Nk,d", [
+    (1, 2, 2, 1111, 1333, 64), (1, 4, 1, 517, 2100, 128), (1, 1, 1, 300, 900, 64), (1, 1, 1, 1, 1030, 128),
+    (2, 3, 1, 2051, 77, 128), (1, 514, 257, 1030, 5, 64)])
+def test_split_sweeps(B, H, Hkv, Nq, Nk, d):
+    print(f"split B={B} H={H}/{Hkv} Nq={Nq} Nk={Nk} d={d}", flush=True)
+    args = (B, H, Hkv, Nq, Nk, d, ringx.RINGX_BF16)
+    need = ringx.ringx_bwd_drop_workspace_bytes(*args)
+    assert need > ringx.ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, 1, ringx.RINGX_BF16)
+    g, x = case(Nq + Nk, B, H, Hkv, Nq, Nk, d, "bf16")
+    p, scale, kw = 0.2, f32_scale(d), dict(q0=77, key0=64)
+    got = both(g, p, state(), scale, **kw)
+    check(x, got, p, SEED, scale, "bf16", **kw)
+    # what a workspace held before does not matter, nothing behind it is written, and a sum onto given
+    # gradients is the sum
+    ws = torch.full((need + 256,), 255, dtype=torch.uint8, device="cuda")
+    acc = {n: torch.randn_like(got[n]) for n in ("dk", "dv")}
+    old = {n: t.clone() for n, t in acc.items()}
+    dq, _, _ = ringx.ringx_attn_bwd_drop(g["q"], g["k"], g["v"], got["out"], g["do"], got["lse"], p, state(),
+                                         scale=scale, dk=acc["dk"], dv=acc["dv"], accumulate_dkv=True,
+                                         workspace=ws[:need], **kw)
+    assert torch.equal(dq, got["dq"]) and bool((ws[need:] == 255).all())
+    assert all(torch.equal(acc[n], old[n] + got[n]) for n in acc)
+
+
 @pytest.mark.parametrize("store,d", [("bf16", 128), ("bf16", 64), ("fp32", 40)])
 def test_places_on_the_mask_axes(store, d):
     """Parts of the queries and of the keys with their places draw the whole call's mask; places far out
@@ -253,7 +279,7 @@ def test_graph_draws_a_new_mask_when_the_state_moves():
     g, x = case(12, 1, 2, 2, 300, 520, 64, "bf16")
     p, scale, rng = 0.25, f32_scale(64), state()
     res = both(g, p, rng, scale)                      # the buffers, and a warm start
-    ws = torch.empty(ringx.ringx_bwd_workspace_bytes(1, 2, 300, 520, 64, 1, ringx.RINGX_BF16),
+    ws = torch.empty(ringx.ringx_bwd_drop_workspace_bytes(1, 2, 2, 300, 520, 64, ringx.RINGX_BF16),
                      dtype=torch.uint8, device="cuda")
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
