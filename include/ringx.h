@@ -335,7 +335,14 @@ ringx_status ringx_attn_bwd_gqa(const void* q, const void* k, const void* v, con
 ringx_status ringx_attn_fwd_drop(const void* q, const void* k, const void* v, void* out, float* lse,
                                  int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
                                  float scale, ringx_dtype dtype, float p, const uint64_t* rng,
-                                 int64_t q0, int64_t key0, hipStream_t stream);
+                                 int64_t q0, int64_t key0, void* workspace, size_t workspace_bytes,
+                                 hipStream_t stream);
+
+/* Bytes of its workspace (16-byte aligned, contents ignored): 0 where one pass fills the chip, and for
+ * invalid arguments; where heads and queries are few, room for the results of parts of the keys.
+ * Host only. */
+size_t ringx_fwd_drop_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
+                                      int64_t d, ringx_dtype dtype);
 
 /* Backward of ringx_attn_fwd_drop, with its p, rng values, q0 and key0.  workspace:
  * ringx_bwd_drop_workspace_bytes(...) bytes, 16-byte aligned, contents ignored.  Bitwise reproducible. */

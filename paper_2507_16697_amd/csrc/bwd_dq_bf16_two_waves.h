@@ -145,7 +145,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(bwd_dq)
   if (bh >= BH) return;
 
   // with dropout a workgroup may sweep a part of the keys alone, never an empty one
-  static_assert(!kDrop || C::kBK <= 256, "parts of at least 256 keys hold a tile");
+  static_assert(!kDrop || C::kBK <= 512, "parts of at least 512 keys hold a tile");
   const int64_t all_tiles = (Nk + C::kBK - 1) / C::kBK;
   const int64_t from = kDrop ? split * all_tiles / drop.splits * C::kBK : 0;
   const int64_t to = kDrop ? min<int64_t>((split + 1) * all_tiles / drop.splits * C::kBK, Nk) : Nk;

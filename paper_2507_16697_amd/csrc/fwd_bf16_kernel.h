@@ -167,12 +167,25 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(fwd_bf1
 
   const int64_t nqt = (Nq + C::kBQ - 1) / C::kBQ;
   uint32_t wg = xcd_remap(blockIdx.x, gridDim.x);
+  // with dropout a workgroup of step mode may take a part of the keys alone, never an empty one
+  constexpr bool kSplit = kDrop && kStep;
+  static_assert(!kSplit || C::kBK <= 512, "parts of at least 512 keys hold a tile");
+  uint32_t split = 0;
+  int64_t from = 0, to = Nk;
+  if constexpr (kSplit) {
+    const uint32_t per_split = gridDim.x / drop.splits;
+    split = wg / per_split;
+    wg -= split * per_split;
+    const int64_t all_tiles = (Nk + C::kBK - 1) / C::kBK;
+    from = split * all_tiles / drop.splits * C::kBK;
+    to = min<int64_t>((split + 1) * all_tiles / drop.splits * C::kBK, Nk);
+  }
   const int64_t q0 = (wg % nqt) * C::kBQ + wave * C::kQW;
   wg /= nqt;
   const int64_t bh = kPartials ? wg / RG : wg;
   if (bh >= BH) return;
 
-  const uint32_t nk = (uint32_t)Nk;
+  const uint32_t nk = (uint32_t)(to - from);
   // this workgroup's chunks and their keys [key_lo, key_hi)
   int r0 = 0;
   uint32_t key_lo = 0, key_hi = nk;
@@ -192,9 +205,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(fwd_bf1
   const int64_t kvh = kv_head(bh, H, grp);
   // wave-uniform bases in SGPRs, so that the per-tile load addresses are scalar arithmetic
   const char* kb =
-      static_cast<const char*>(uniform_ptr(reinterpret_cast<const char*>(k + kvh * Nk * D)));
+      static_cast<const char*>(uniform_ptr(reinterpret_cast<const char*>(k + (kvh * Nk + from) * D)));
   const char* vb =
-      static_cast<const char*>(uniform_ptr(reinterpret_cast<const char*>(v + kvh * Nk * D)));
+      static_cast<const char*>(uniform_ptr(reinterpret_cast<const char*>(v + (kvh * Nk + from) * D)));
   int goff[C::kLoads], grow[C::kLoads];
   load_offsets<C>(goff, grow, wave, lane);
 
@@ -290,7 +303,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(fwd_bf1
   // beside the P V products, where the vector ALU has nothing else to do.
   constexpr int kMasks = kDrop ? C::kKTiles : 1;
   u32x4 dw[kMasks];
-  uint32_t dgroup = 2 * (drop.kb0 + t0.start / 32) + g;   // the tile's first 16-key group
+  uint32_t dgroup = 2 * (drop.kb0 + (uint32_t)(from / 32) + t0.start / 32) + g;   // the tile's first 16-key group
   auto next_mask = [&] {
     if constexpr (kDrop) {
 #pragma unroll
@@ -322,10 +335,11 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(fwd_bf1
     // Eq. (5) with the running result: out_acc <- (out_acc a + loc_out b) / (a + b)
     const int64_t qi = q0 + n;
     if (qi < Nq) {
-      const int64_t row = bh * Nq + qi;
+      const int64_t row = ((int64_t)split * BH + bh) * Nq + qi;
       float* ao = acc_out + row * D;
       float inv = 1.0f / lrow;
-      if constexpr (kDrop) inv *= drop.inv_keep;
+      // a part of the keys may have scores of -inf alone: it adds 0, with a log-sum-exp of -inf
+      if constexpr (kDrop) inv = lrow == 0.f ? 0.f : inv * drop.inv_keep;
       float wa = 0.f, wb = inv;
       float lnew = lse2r;
       if (!first) {
@@ -462,9 +476,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(fwd_bf1
 #pragma unroll
         for (int rr = 0; rr < 16; ++rr) ma = fmaxf(ma, cur[kt][rr]);
       float mnew = fmaxf(m2, max_halves(ma) * c2);
-      // a stream may meet scores of -inf alone (keys masked by an infinite feature) that one stream
+      // a stream or part may meet scores of -inf alone (keys masked by an infinite feature) that one stream
       // over all keys would weigh at 0: a finite reference keeps its sums 0 instead of NaN
-      if constexpr (KS > 1) mnew = fmaxf(mnew, -3e38f);
+      if constexpr (KS > 1 || kSplit) mnew = fmaxf(mnew, -3e38f);
       const float alpha = fast_exp2(m2 - mnew);
       m2 = mnew;
       lc *= alpha;
@@ -670,7 +684,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(fwd_bf1
 template <int D, int MODE, int KS, int NW>
 hipError_t launch(const FwdArgs& a, int64_t RG, const DROP& drop) {
   using C = FwdCfg<D, KS, NW>;
-  const int64_t nwg = (a.Nq + C::kBQ - 1) / C::kBQ * a.BH * RG;
+  const int64_t nwg = (a.Nq + C::kBQ - 1) / C::kBQ * a.BH * RG * drop.splits;
   hipLaunchKernelGGL((RINGX_KERNEL(fwd_bf16)<D, MODE, KS, NW>), dim3((uint32_t)nwg), dim3(C::kThreads), 0,
                      a.stream, (const __bf16*)a.q, (const __bf16*)a.k, (const __bf16*)a.v,
                      (__bf16*)a.out, a.lse, a.part_out, a.part_lse, a.acc_out, a.acc_lse,

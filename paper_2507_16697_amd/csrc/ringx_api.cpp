@@ -699,6 +699,9 @@ ringx_status ringx_attn_bwd_noalloc(const void* q, const void* k, const void* v,
 
 namespace {
 
+// Floats of the parts of a split forward: outputs and log-sum-exps.
+int64_t fwd_drop_floats(int64_t parts, int64_t rows, int64_t d) { return parts * rows * (d + 1); }
+
 // The launch's view of the dropout arguments.
 ringx_status make_drop(float p, const uint64_t* rng, int64_t q0, int64_t key0, int64_t Nq, int64_t Nk,
                        ringx::Drop* out) {
@@ -719,10 +722,19 @@ ringx_status make_drop(float p, const uint64_t* rng, int64_t q0, int64_t key0, i
 
 extern "C" {
 
+size_t ringx_fwd_drop_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
+                                      int64_t d, ringx_dtype dtype) {
+  if (Hkv < 1 || H < 1 || H % Hkv != 0) return 0;
+  if (check_dims(B, H, Nq, Nk, d, 1, 1.0f, dtype) != RINGX_OK || dtype != RINGX_BF16) return 0;
+  const int64_t parts = ringx::drop_fwd_split(B * H, Nq, Nk, d);
+  return parts == 1 ? 0 : static_cast<size_t>(fwd_drop_floats(parts, B * H * Nq, d) * 4);
+}
+
 ringx_status ringx_attn_fwd_drop(const void* q, const void* k, const void* v, void* out, float* lse,
                                  int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t d,
                                  float scale, ringx_dtype dtype, float p, const uint64_t* rng,
-                                 int64_t q0, int64_t key0, hipStream_t stream) {
+                                 int64_t q0, int64_t key0, void* workspace, size_t workspace_bytes,
+                                 hipStream_t stream) {
   if (!q || !k || !v || !out || !lse) return RINGX_E_NULLPTR;
   if (Hkv < 1 || H < 1 || H % Hkv != 0) return RINGX_E_SHAPE;
   ringx_status st = check_dims(B, H, Nq, Nk, d, 1, scale, dtype);
@@ -730,22 +742,35 @@ ringx_status ringx_attn_fwd_drop(const void* q, const void* k, const void* v, vo
   ringx::Drop drop;
   st = make_drop(p, rng, q0, key0, Nq, Nk, &drop);
   if (st != RINGX_OK) return st;
-  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(lse))
-    return RINGX_E_ALIGN;
+  const size_t need = ringx_fwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, dtype);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return RINGX_E_WORKSPACE;
+  for (const void* x : {q, k, v, (const void*)out, (const void*)lse,
+                        (const void*)(need > 0 ? workspace : nullptr)})
+    if (!aligned16(x)) return RINGX_E_ALIGN;
   const int64_t es = esize(dtype), bh = B * H, bkv = B * Hkv;
   const Span ins[] = {span(q, bh * Nq * d * es), span(k, bkv * Nk * d * es),
                       span(v, bkv * Nk * d * es), span(rng, 16)};
   const Span so = span(out, bh * Nq * d * es), sl = span(lse, bh * Nq * 4);
+  const Span sw = span(workspace, (int64_t)need);
   for (const Span& i : ins)
-    if (overlap(so, i) || overlap(sl, i)) return RINGX_E_ALIAS;
-  if (overlap(so, sl)) return RINGX_E_ALIAS;
+    if (overlap(so, i) || overlap(sl, i) || (need > 0 && overlap(sw, i))) return RINGX_E_ALIAS;
+  if (overlap(so, sl) || (need > 0 && (overlap(sw, so) || overlap(sw, sl)))) return RINGX_E_ALIAS;
   ringx::FwdArgs a;
   a.q = q, a.k = k, a.v = v, a.out = out, a.lse = lse;
   a.BH = bh, a.Nq = Nq, a.Nk = Nk, a.d = d, a.R = 1, a.scale = scale, a.stream = stream;
   a.H = H, a.G = H / Hkv;
-  return hip_status(dtype == RINGX_BF16
-                        ? ringx::launch_fwd_drop_bf16(a, ringx::FwdMode::kFused, drop)
-                        : ringx::launch_fwd_drop_f32(a, ringx::FwdMode::kFused, drop));
+  if (dtype == RINGX_FP32)
+    return hip_status(ringx::launch_fwd_drop_f32(a, ringx::FwdMode::kFused, drop));
+  if (need == 0) return hip_status(ringx::launch_fwd_drop_bf16(a, ringx::FwdMode::kFused, drop));
+  // the parts as first steps, each with its own result, and their merge
+  drop.splits = (uint32_t)ringx::drop_fwd_split(bh, Nq, Nk, d);
+  a.acc_out = static_cast<float*>(workspace), a.first = true;
+  a.acc_lse = a.acc_out + (int64_t)drop.splits * bh * Nq * d;
+  if (ringx::launch_fwd_drop_bf16(a, ringx::FwdMode::kStep, drop) != hipSuccess) return RINGX_E_HIP;
+  ringx::MergeArgs m;
+  m.part_out = a.acc_out, m.part_lse = a.acc_lse, m.out = out, m.lse = lse;
+  m.R = drop.splits, m.BH = bh, m.Nq = Nq, m.d = d, m.out_bf16 = true, m.stream = stream;
+  return hip_status(ringx::launch_lse_merge(m));
 }
 
 ringx_status ringx_attn_fwd_step_drop(const void* q, const void* k, const void* v, float* out_acc,

@@ -201,19 +201,31 @@ struct Drop {
                                    // workgroups of its own, with outputs [splits, ...]
 };
 
+// Dropout, bf16: parts of the keys for a sweep of them in w workgroups.  Up to 128 workgroups, as many parts
+// of at least 512 keys as one round of 256 workgroups holds, at most 32: parts of 256 keys gain no more than
+// their launch costs (2 heads of 128, 200 x 700, launched one by one: 15 us whole, 19 in two parts).
+inline int key_parts(int64_t w, int64_t Nk) {
+  return w > 128 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({256 / w, Nk / 512, 32}));
+}
+// The forward, whose parts are merged by Eq. (5) in a launch more.  us, whole -> in parts: 2 heads of
+// 64, 1873 queries, 5265 keys (w = 60) 42 -> 27; 4/1 of 64, 1000 x 30000 (64) 181 -> 66; 1 of 64, 1 x 8192 (1)
+// 56 -> 24; 2 of 128, 4096 x 4096 (128) 51 -> 45; from w = 129 on it loses (160: 74 -> 81 .. 98).
+inline int drop_fwd_split(int64_t BH, int64_t Nq, int64_t Nk, int64_t d) {
+  const int ks = fwd_plan((Nq + 255) / 256 * BH, Nk, 1, d, false).cut.ks;
+  return key_parts((Nq + 256 / ks - 1) / (256 / ks) * BH, Nk);
+}
 // How the backward with dropout, bf16, splits its sweeps over workgroups of their own where heads and rows
 // are too few to fill the chip; the parts are summed by a launch more (split_sum.hip).
-//   dQ     w workgroups of query_cut's form, up to 128 of them: as many parts of at least 256 keys as one
-//          round of 256 holds, at most 32.  The whole backward (us), unsplit -> split: 2 heads of 64, 1873
-//          queries, 5265 keys (w = 60) 87 -> 62; 4/1 of 64, 1000 x 30000 (64) 309 -> 157; 2 of 128,
-//          4096 x 4096 (128) 174 -> 155; 1 of 64, 300 x 900 (5) 31.5 -> 28.3.  From w = 129 on it loses
-//          (192: 340 -> 361).
+//   dQ     key_parts of the workgroups of query_cut's form.  The whole backward (us), whole -> dQ in parts:
+//          2 heads of 64, 1873 queries, 5265 keys (w = 60) 87 -> 62; 4/1 of 64, 1000 x 30000 (64) 309 ->
+//          157; 2 of 128, 4096 x 4096 (128) 174 -> 155; 1 of 64, 1024 x 1024 (32) 41 -> 40.
+//          From w = 129 on it loses (192: 340 -> 361).
 //   dK/dV  n tiles of 128 keys, `sweep` query rows to each (those of all heads of the group).  Parts of at
-//          least 256 rows, 128 of a head (a tile of queries), at most 32, as the shorter sum of rounds of 256 workgroups and of what
-//          the parts cost says, where that is a tenth less: a workgroup takes 0.026 us a row at d = 128
-//          and 0.02 at 64, and 5 or 3 besides; a round's parts 17 or 8.4 to write and read, their launch 4;
-//          unsplit workgroups of 64 keys at d = 64 save 4.5.  Fitted to times like (one, two, three,
-//          four parts; n x sweep):
+//          least 256 rows, 128 of a head (a tile of queries), at most 32, as many as make the shortest
+//          sum of the rounds of 256 workgroups and of the parts' cost, where that is a tenth less than
+//          whole: a workgroup takes 0.026 us a row at d = 128 and 0.02 at 64, and 5 or 3 besides; a
+//          round's parts 17 or 8.4 to write and read, their launch 4; whole workgroups of 64 keys at
+//          d = 64 save 4.5.  Fitted to times like (one, two, three, four parts; n x sweep):
 //            d = 128  64 x 4096 187 143 123 120, 64 x 16384 539 344 294 276, 160 x 4096 212 242 213
 //                     233, 192 x 8192 419 439 461 427, 192 x 1024 78 103 120 120
 //            d = 64   16 x 1024 41 37 35 35, 84 x 1873 86 87 84 88, 128 x 2048 69 71 73 74
@@ -226,8 +238,7 @@ inline bool ragged_last_round(int64_t n) { return n > 256 && n < 1024 && (n - 1)
 inline DropSplit drop_split(int64_t BHkv, int64_t BH, int64_t Nq, int64_t Nk, int64_t d) {
   DropSplit s;
   const QueryCut c = query_cut((Nq + 255) / 256 * BH, Nk, dq_cut_rule(d));
-  const int64_t w = (Nq + 256 / c.ks - 1) / (256 / c.ks) * BH;
-  if (w <= 128) s.q = (int)std::max<int64_t>(1, std::min<int64_t>({256 / w, Nk / 256, 32}));
+  s.q = key_parts((Nq + 256 / c.ks - 1) / (256 / c.ks) * BH, Nk);
   const int64_t n = (Nk + 127) / 128 * BHkv, sweep = Nq * (BH / BHkv);
   if (d == 64 && ragged_last_round(n)) {
     s.kv = Nq >= 256 && sweep >= 2048 ? 2 : 1;

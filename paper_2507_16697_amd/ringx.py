@@ -46,9 +46,9 @@ EXPORTED = ("ringx_attn_fwd", "ringx_attn_fwd_partials", "ringx_lse_merge", "rin
             "ringx_chunk_bounds", "ringx_status_str", "ringx_attn_bwd_noalloc",
             "ringx_bwd_ds_bytes", "ringx_attn_bwd_dkdv_ds", "ringx_attn_bwd_dq_ds",
             "ringx_attn_bwd_ds", "ringx_bwd_ds_workspace_bytes", "ringx_attn_fwd_drop",
-            "ringx_attn_bwd_drop", "ringx_bwd_drop_workspace_bytes", "ringx_attn_fwd_step_drop",
-            "ringx_attn_bwd_step_drop",
-            "ringx_bwd_preprocess_drop", "ringx_qkv_norm_rope", "ringx_qkv_norm_rope_bwd",
+            "ringx_fwd_drop_workspace_bytes", "ringx_attn_bwd_drop", "ringx_bwd_drop_workspace_bytes",
+            "ringx_attn_fwd_step_drop", "ringx_attn_bwd_step_drop", "ringx_bwd_preprocess_drop",
+            "ringx_qkv_norm_rope", "ringx_qkv_norm_rope_bwd",
             "ringx_qkv_norm_rope_bwd_workspace_bytes")
 
 
@@ -112,7 +112,10 @@ def lib() -> ctypes.CDLL:
                                            _I, ctypes.c_float, ctypes.c_int, _I, _I, _P]
         L.ringx_attn_bwd_ds.argtypes = L.ringx_attn_bwd_gqa.argtypes
         F, C = ctypes.c_float, ctypes.c_int
-        L.ringx_attn_fwd_drop.argtypes = [_P] * 5 + [_I] * 6 + [F, C, F, _P, _I, _I, _P]
+        L.ringx_attn_fwd_drop.argtypes = ([_P] * 5 + [_I] * 6 +
+                                          [F, C, F, _P, _I, _I, _P, ctypes.c_size_t, _P])
+        L.ringx_fwd_drop_workspace_bytes.argtypes = [_I] * 6 + [C]
+        L.ringx_fwd_drop_workspace_bytes.restype = ctypes.c_size_t
         L.ringx_attn_bwd_drop.argtypes = ([_P] * 9 + [_I] * 6 +
                                           [F, C, F, _P, _I, _I, C, _P, ctypes.c_size_t, _P])
         L.ringx_bwd_drop_workspace_bytes.argtypes = [_I] * 6 + [C]
@@ -639,7 +642,7 @@ def _rng(rng, like):
 
 
 def ringx_attn_fwd_drop(q, k, v, p: float, rng, scale=None, q0: int = 0, key0: int = 0, out=None,
-                        lse=None, stream=None):
+                        lse=None, workspace=None, stream=None):
     """Attention of q [B,H,Nq,d] to k, v [B,Hkv,Nk,d] with dropout of its probabilities at rate p (to
     a multiple of 1/256).  rng: int64 [2] on the device, seed and offset, read when the kernels run.
     q0, key0: the tensors' places on the mask's axes (key0 a multiple of 32).  Returns (out, lse)."""
@@ -649,10 +652,18 @@ def ringx_attn_fwd_drop(q, k, v, p: float, rng, scale=None, q0: int = 0, key0: i
     state = _rng(rng, q)
     out = torch.empty_like(q) if out is None else _out("out", out, q.shape, q.dtype, q)
     lse = _out("lse", lse, (B, H, Nq), torch.float32, q)
+    code = _dtype_code(q)
+    need = ringx_fwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, code)
+    if workspace is not None or need:
+        workspace = _workspace(workspace, need, q)
     _launch("ringx_attn_fwd_drop", q, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(),
-            out.data_ptr(), lse.data_ptr(), B, H, Hkv, Nq, Nk, d, _scale(scale, d), _dtype_code(q),
-            float(p), state, q0, key0)
+            out.data_ptr(), lse.data_ptr(), B, H, Hkv, Nq, Nk, d, _scale(scale, d), code, float(p),
+            state, q0, key0, _ptr(workspace), 0 if workspace is None else _nbytes(workspace))
     return out, lse
+
+
+def ringx_fwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, dtype) -> int:
+    return int(lib().ringx_fwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, int(dtype)))
 
 
 def ringx_bwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, dtype) -> int:

@@ -14,7 +14,7 @@ needs_lib = pytest.mark.skipif(not os.path.exists(ringx.LIB_PATH), reason="libri
 OK, NULLPTR, SHAPE, CHUNKS, UNSUP, ALIGN, WORKSPACE, HIP, ALIAS, SCRATCH, DROPOUT, ROPE = range(12)
 BF16, FP32 = ringx.RINGX_BF16, ringx.RINGX_FP32
 GB = 1 << 30
-QP, KP, VP, OP, LP, RP = (0x10_0000_0000 + i * 64 * GB for i in range(6))   # never dereferenced
+QP, KP, VP, OP, LP, RP, WP = (0x10_0000_0000 + i * 64 * GB for i in range(7))   # never dereferenced
 
 
 def _words(counter, key, rounds):
@@ -89,9 +89,9 @@ def test_mask_places_of_chunks():
 
 
 def fwd(q=QP, k=KP, v=VP, o=OP, l=LP, B=1, H=4, Hkv=2, Nq=100, Nk=300, d=64, scale=0.125, dt=BF16,
-        p=0.1, rng=RP, q0=0, key0=0):
+        p=0.1, rng=RP, q0=0, key0=0, ws=None, wsb=0):
     return ringx.lib().ringx_attn_fwd_drop(q, k, v, o, l, B, H, Hkv, Nq, Nk, d, scale, dt, p, rng, q0,
-                                           key0, None)
+                                           key0, ws, wsb, None)
 
 
 def fstep(q=QP, k=KP, v=VP, o=OP, l=LP, B=1, H=4, Hkv=None, Nq=100, Nk=300, d=64, scale=0.125,
@@ -153,7 +153,16 @@ def test_backward_workspace_holds_the_parts():
     # 2 heads, 4096 x 4096: four parts of dK and dV and two of dQ
     assert (size(1, 2, 2, 4096, 4096, 128, BF16) - stats(1, 2, 4096, 4096, 128, 1, BF16)
             == (4 * 2 + 2) * 2 * 4096 * 128 * 4)
-    # never more parts than 256 keys or query rows each allow, however few the heads
+    # the forward's: the parts' outputs and log-sum-exps, here two of 2 heads of 4096 rows
+    need = ringx.ringx_fwd_drop_workspace_bytes
+    assert need(1, 2, 2, 4096, 4096, 128, BF16) == 2 * 2 * 4096 * 129 * 4
+    assert need(1, 2, 2, 4096, 4096, 128, FP32) == need(1, 16, 16, 4096, 4096, 64, BF16) == 0
+    big = dict(H=2, Hkv=2, Nq=4096, Nk=4096, d=128)
+    n = need(1, 2, 2, 4096, 4096, 128, BF16)
+    assert fwd(**big) == WORKSPACE and fwd(ws=WP, wsb=n - 1, **big) == WORKSPACE
+    assert fwd(ws=WP + 8, wsb=n, **big) == ALIGN
+    assert fwd(ws=QP, wsb=n, **big) == ALIAS and fwd(ws=OP, wsb=n, **big) == ALIAS
+    # never more parts than 512 keys and 256 query rows each allow, however few the heads
     for n in (1, 100, 255, 256, 511, 4096, 100000):
         extra = size(1, 1, 1, n, n, 64, BF16) - stats(1, 1, n, n, 64, 1, BF16)
         assert 0 <= extra <= 3 * min(32, n // 256) * n * 64 * 4

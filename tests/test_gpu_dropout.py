@@ -116,7 +116,7 @@ def test_forward_and_backward(store, B, H, Hkv, Nq, Nk, d, p):
 # few heads: sweeps in parts that are summed afterwards, on both sides, on one, with shared heads, and
 # with small workgroups in a ragged launch; the parts end inside tiles of the whole
 @pytest.mark.parametrize("B,H,Hkv,Nq,Nk,d", [
-    (1, 2, 2, 1111, 1333, 64), (1, 4, 1, 517, 2100, 128), (1, 1, 1, 300, 900, 64), (1, 1, 1, 1, 1030, 128),
+    (1, 2, 2, 1111, 1333, 64), (1, 4, 1, 517, 2100, 128), (1, 1, 1, 300, 1100, 64), (1, 1, 1, 1, 1030, 128),
     (2, 3, 1, 2051, 77, 128), (1, 514, 257, 1030, 5, 64)])
 def test_split_sweeps(B, H, Hkv, Nq, Nk, d):
     print(f"split B={B} H={H}/{Hkv} Nq={Nq} Nk={Nk} d={d}", flush=True)
@@ -130,6 +130,13 @@ def test_split_sweeps(B, H, Hkv, Nq, Nk, d):
     # what a workspace held before does not matter, nothing behind it is written, and a sum onto given
     # gradients is the sum
     ws = torch.full((need + 256,), 255, dtype=torch.uint8, device="cuda")
+    fwd_need = ringx.ringx_fwd_drop_workspace_bytes(*args)
+    if fwd_need:
+        fws = torch.full((fwd_need + 256,), 255, dtype=torch.uint8, device="cuda")
+        out, lse = ringx.ringx_attn_fwd_drop(g["q"], g["k"], g["v"], p, state(), scale=scale,
+                                             workspace=fws[:fwd_need], **kw)
+        assert torch.equal(out, got["out"]) and torch.equal(lse, got["lse"])
+        assert bool((fws[fwd_need:] == 255).all())
     acc = {n: torch.randn_like(got[n]) for n in ("dk", "dv")}
     old = {n: t.clone() for n, t in acc.items()}
     dq, _, _ = ringx.ringx_attn_bwd_drop(g["q"], g["k"], g["v"], got["out"], g["do"], got["lse"], p, state(),
@@ -157,6 +164,7 @@ def test_places_on_the_mask_axes(store, d):
 
 
 def test_no_rate_is_plain_attention():
+    # 700 keys: too few for parts of their own, so to the bit
     g, x = case(6, 1, 2, 2, 300, 700, 128, "bf16")
     o, l = ringx.ringx_attn_fwd_drop(g["q"], g["k"], g["v"], 0.0, state())
     ro, rl = ringx.ringx_attn_fwd(g["q"], g["k"], g["v"], 1)
@@ -273,6 +281,34 @@ def test_infinite_key_features_stay_where_they_are():
     # whose weights add up to at most 256 / (256 - T)
     most = 256 / (256 - od.threshold(0.2)) * float(g["v"].abs().max())
     assert float((out.float() - ref.float()).abs().max()) <= 4 * 2 ** -8 * most
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_parts_of_the_keys_without_a_finite_score(d):
+    """Few queries: the keys go to workgroups in parts, most of which hold scores of -inf alone; the
+    same for the chunks of a ring after the first."""
+    Nk, some = 2048, 200
+    g, _ = case(14, 1, 2, 2, 70, Nk, d, "bf16")
+    assert ringx.ringx_fwd_drop_workspace_bytes(1, 2, 2, 70, Nk, d, ringx.RINGX_BF16) > 0
+    g["q"][..., 0] = 1.0
+    g["k"][..., 0] = 0.0
+    g["k"][:, :, some:, 0] = -float("inf")
+    out, lse = ringx.ringx_attn_fwd_drop(g["q"], g["k"], g["v"], 0.2, state())
+    ref, rl = ringx.ringx_attn_fwd_drop(g["q"], g["k"][:, :, :some].contiguous(),
+                                        g["v"][:, :, :some].contiguous(), 0.2, state())
+    most = 256 / (256 - od.threshold(0.2)) * float(g["v"].abs().max())   # as above
+    assert torch.allclose(lse, rl, atol=1e-5, rtol=0)
+    assert float((out.float() - ref.float()).abs().max()) <= 4 * 2 ** -8 * most
+    dq = ringx.ringx_attn_bwd_drop(g["q"], g["k"], g["v"], out, g["do"], lse, 0.2, state())[0]
+    assert torch.isfinite(dq[..., 1:]).all()
+    acc = torch.empty((1, 2, 70, d), device="cuda")
+    al = torch.empty((1, 2, 70), device="cuda")
+    for i, lo in enumerate((0, 1024)):
+        ringx.ringx_attn_fwd_step_drop(g["q"], g["k"][:, :, lo:lo + 1024].contiguous(),
+                                       g["v"][:, :, lo:lo + 1024].contiguous(), acc, al, i == 0, 0.2,
+                                       state(), lo)
+    assert torch.allclose(al, rl, atol=1e-5, rtol=0)
+    assert float((acc - ref.float()).abs().max()) <= 4 * 2 ** -8 * most
 
 
 def test_graph_draws_a_new_mask_when_the_state_moves():
