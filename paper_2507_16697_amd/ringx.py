@@ -662,10 +662,12 @@ def ringx_attn_fwd_drop(q, k, v, p: float, rng, scale=None, q0: int = 0, key0: i
     return out, lse
 
 
+@functools.lru_cache(maxsize=256)   # a function of the sizes alone
 def ringx_fwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, dtype) -> int:
     return int(lib().ringx_fwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, int(dtype)))
 
 
+@functools.lru_cache(maxsize=256)   # a function of the sizes alone
 def ringx_bwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, dtype) -> int:
     return int(lib().ringx_bwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, int(dtype)))
 
@@ -759,6 +761,7 @@ def ringx_bwd_preprocess_drop(out, dout, lse, p: float, delta=None, stream=None)
 # norm and rotation between a packed projection and the attention's operands
 
 
+@functools.lru_cache(maxsize=256)   # a function of the sizes alone
 def ringx_qkv_norm_rope_bwd_workspace_bytes(B, N, H, Hkv, d, dtype) -> int:
     return int(lib().ringx_qkv_norm_rope_bwd_workspace_bytes(B, N, H, Hkv, d, int(dtype)))
 
