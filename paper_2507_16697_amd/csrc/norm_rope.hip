@@ -28,9 +28,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-// Rows of a lane at work, and in flight behind them, forward: 174 us over 32768 tokens of 48 heads of 128
-// (4.6 TB/s; without norm and rotation, the copy to the other layout alone took 180 in a form without
-// loads ahead).  Without loads ahead, four rows one after the other: 252.
+// Rows of a lane at work, and in flight behind them, forward: 165 us over 32768 tokens of 48 heads of 128
+// (4.9 TB/s; 174 through the caches; without norm and rotation, the copy to the other layout alone took
+// 180 in a form without loads ahead).  Without loads ahead, four rows one after the other: 252.
 constexpr int kBatch = 2;
 
 // Dims per lane: 16 bytes of the storage type.
@@ -38,11 +38,13 @@ template <class T>
 constexpr int kHeld = std::is_same_v<T, float> ? 4 : 8;
 
 // kHeld dims of a row as they are stored: 16-byte accesses (VEC), else one by one where dim < d.
-template <class T, bool VEC>
+// STREAM: past the caches, for tensors that they would not hold anyway.
+template <class T, bool VEC, bool STREAM>
 __device__ __forceinline__ u32x4 load_raw(const T* p, int dim, int d) {
   u32x4 w = {};
   if constexpr (VEC) {
-    if (dim < d) w = *reinterpret_cast<const u32x4*>(p + dim);
+    const u32x4* const x = reinterpret_cast<const u32x4*>(p + dim);
+    if (dim < d) w = STREAM ? __builtin_nontemporal_load(x) : *x;
   } else {
     static_assert(std::is_same_v<T, float>, "bf16 rows come in 16-byte pieces");
 #pragma unroll
@@ -62,17 +64,21 @@ __device__ __forceinline__ void unpack(const u32x4& w, float (&x)[kHeld<T>]) {
     }
   }
 }
-template <class T, bool VEC>
+template <class T, bool VEC, bool STREAM>
 __device__ __forceinline__ void store_raw(T* p, int dim, int d, const u32x4& w) {
   if constexpr (VEC) {
-    if (dim < d) *reinterpret_cast<u32x4*>(p + dim) = w;
+    u32x4* const x = reinterpret_cast<u32x4*>(p + dim);
+    if (dim < d) {
+      if constexpr (STREAM) __builtin_nontemporal_store(w, x);
+      else *x = w;
+    }
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (dim + j < d) p[dim + j] = __uint_as_float(w[j]);
   }
 }
-template <class T, bool VEC>
+template <class T, bool VEC, bool STREAM>
 __device__ __forceinline__ void store_row(T* p, int dim, int d, const float (&x)[kHeld<T>]) {
   u32x4 w;
 #pragma unroll
@@ -80,7 +86,7 @@ __device__ __forceinline__ void store_row(T* p, int dim, int d, const float (&x)
     if constexpr (std::is_same_v<T, float>) w[j] = __float_as_uint(x[j]);
     else w[j] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
   }
-  store_raw<T, VEC>(p, dim, d, w);
+  store_raw<T, VEC, STREAM>(p, dim, d, w);
 }
 
 // What rotation needs to know.  Once per workgroup, a word for every dim: the other dim of its pair,
@@ -217,7 +223,7 @@ __device__ __forceinline__ float row_sum(float x) {
 
 // A wave takes 64 / LPR tokens and the heads [h0, h1) of its share (blockIdx.y), kBatch rows of a lane
 // at a time while the next ones arrive.
-template <class T, int LPR, bool VEC>
+template <class T, int LPR, bool VEC, bool STREAM>
 __global__ __launch_bounds__(kThreads, 4) void norm_rope_kernel(RopeArgs a) {
   constexpr int E = kHeld<T>, kTok = 64 / LPR;
   __shared__ float lds[kWaves][kBatch * E * 64];
@@ -238,7 +244,7 @@ __global__ __launch_bounds__(kThreads, 4) void norm_rope_kernel(RopeArgs a) {
   u32x4 raw[kBatch];
 #pragma unroll
   for (int u = 0; u < kBatch; ++u)
-    raw[u] = load_raw<T, VEC>(src + (int64_t)min(h0 + u, h1 - 1) * a.d, dim, a.d);
+    raw[u] = load_raw<T, VEC, STREAM>(src + (int64_t)min(h0 + u, h1 - 1) * a.d, dim, a.d);
 
   rotation.fill(a);
   __syncthreads();
@@ -257,7 +263,7 @@ __global__ __launch_bounds__(kThreads, 4) void norm_rope_kernel(RopeArgs a) {
     u32x4 next[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
-      next[u] = load_raw<T, VEC>(src + (int64_t)min(hb + kBatch + u, h1 - 1) * a.d, dim, a.d);
+      next[u] = load_raw<T, VEC, STREAM>(src + (int64_t)min(hb + kBatch + u, h1 - 1) * a.d, dim, a.d);
     if (hb < turned) {
       float x[kBatch][E];
 #pragma unroll
@@ -276,14 +282,14 @@ __global__ __launch_bounds__(kThreads, 4) void norm_rope_kernel(RopeArgs a) {
       for (int u = 0; u < kBatch; ++u) {
         const int h = hb + u;
         if (live && h < h1 && h < turned)
-          store_row<T, VEC>(h < a.H ? q + h * head : k + (h - a.H) * head, dim, a.d, x[u]);
+          store_row<T, VEC, STREAM>(h < a.H ? q + h * head : k + (h - a.H) * head, dim, a.d, x[u]);
       }
     }
     if (hb + kBatch > turned) {
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
         const int h = hb + u;
-        if (live && h < h1 && h >= turned) store_raw<T, VEC>(v + (h - turned) * head, dim, a.d, raw[u]);
+        if (live && h < h1 && h >= turned) store_raw<T, VEC, STREAM>(v + (h - turned) * head, dim, a.d, raw[u]);
       }
     }
 #pragma unroll
@@ -292,13 +298,14 @@ __global__ __launch_bounds__(kThreads, 4) void norm_rope_kernel(RopeArgs a) {
 }
 
 // kHeld<T> dims of an fp32 gradient row
-template <class T, bool VEC>
+template <class T, bool VEC, bool STREAM>
 __device__ __forceinline__ void load_grad(const float* p, int dim, int d, float (&x)[kHeld<T>]) {
 #pragma unroll
   for (int j = 0; j < kHeld<T>; j += 4) {
     if constexpr (VEC) {
       f32x4 v = {};
-      if (dim + j < d) v = *reinterpret_cast<const f32x4*>(p + dim + j);
+      const f32x4* const y = reinterpret_cast<const f32x4*>(p + dim + j);
+      if (dim + j < d) v = STREAM ? __builtin_nontemporal_load(y) : *y;
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[j + i] = v[i];
     } else {
@@ -312,7 +319,7 @@ __device__ __forceinline__ void load_grad(const float* p, int dim, int d, float 
 // heads of 128 (5.0 TB/s; a copy of that size reaches 5.4).  Loading the next row ahead takes the
 // registers of a wave (326 us, and 87 against 79 over 8192 tokens, whose loads hit the caches), two rows at
 // a time too (340).
-template <class T, int LPR, bool VEC>
+template <class T, int LPR, bool VEC, bool STREAM>
 __global__ __launch_bounds__(kThreads, 4) void norm_rope_bwd_kernel(RopeArgs a) {
   constexpr int E = kHeld<T>, kTok = 64 / LPR;
   __shared__ float lds[kWaves][E * 64];
@@ -350,8 +357,8 @@ __global__ __launch_bounds__(kThreads, 4) void norm_rope_bwd_kernel(RopeArgs a) 
                       float (&dw)[E]) {
       for (int h = lo; h < hi; ++h) {
         float x[E], g[1][E];
-        load_grad<T, VEC>(gp + h * head, dim, a.d, g[0]);
-        unpack<T>(load_raw<T, VEC>(src + (int64_t)(first + h) * a.d, dim, a.d), x);
+        load_grad<T, VEC, STREAM>(gp + h * head, dim, a.d, g[0]);
+        unpack<T>(load_raw<T, VEC, STREAM>(src + (int64_t)(first + h) * a.d, dim, a.d), x);
         turn(g, c, s, partner, lane, xch, -1.f);
         float ss = 0.f, sg = 0.f;
 #pragma unroll
@@ -368,7 +375,7 @@ __global__ __launch_bounds__(kThreads, 4) void norm_rope_bwd_kernel(RopeArgs a) 
           dw[j] = __builtin_fmaf(g[0][j] * x[j], count, dw[j]);
           dx[j] = r * (g[0][j] * w[j]) - x[j] * r * m;
         }
-        if (live) store_row<T, VEC>(dst + (int64_t)(first + h) * a.d, dim, a.d, dx);
+        if (live) store_row<T, VEC, STREAM>(dst + (int64_t)(first + h) * a.d, dim, a.d, dx);
       }
     };
     normed(h0, min(h1, a.H), 0, a.dq + (b * a.H * a.N + n) * a.d, w[0], dw[0]);
@@ -378,8 +385,8 @@ __global__ __launch_bounds__(kThreads, 4) void norm_rope_bwd_kernel(RopeArgs a) 
 #pragma unroll 2
     for (int h = max(h0 - a.H - a.Hkv, 0); h < h1 - a.H - a.Hkv; ++h) {
       float g[E];
-      load_grad<T, VEC>(gv + h * head, dim, a.d, g);
-      if (live) store_row<T, VEC>(dst + (int64_t)(a.H + a.Hkv + h) * a.d, dim, a.d, g);
+      load_grad<T, VEC, STREAM>(gv + h * head, dim, a.d, g);
+      if (live) store_row<T, VEC, STREAM>(dst + (int64_t)(a.H + a.Hkv + h) * a.d, dim, a.d, g);
     }
   }
   // the workgroup's sums: over the tokens of a wave, then over the waves
@@ -405,58 +412,74 @@ __global__ __launch_bounds__(kThreads, 4) void norm_rope_bwd_kernel(RopeArgs a) 
   }
 }
 
-// Sums of the workgroups' parts [parts, 2, d] in their order: 32 columns x 32 groups of parts to a
-// workgroup.
+// Sums of the workgroups' parts [parts, 2, d] in their order: 16 columns x 64 groups of parts to a
+// workgroup, 16 loads of a thread in flight, since the loads' latency is all that it waits for.
+constexpr int kSumCols = 16, kSumGroups = 64;
 __global__ __launch_bounds__(1024) void weight_grad_kernel(const float* __restrict__ part, int parts,
                                                            int d, float* __restrict__ dqw,
                                                            float* __restrict__ dkw) {
-  __shared__ float lds[32][33];
-  const int cl = threadIdx.x & 31, grp = threadIdx.x >> 5;
-  const int col = blockIdx.x * 32 + cl;
-  const int per = (parts + 31) / 32;
+  __shared__ float lds[kSumGroups][kSumCols + 1];
+  const int cl = threadIdx.x % kSumCols, grp = threadIdx.x / kSumCols;
+  const int col = blockIdx.x * kSumCols + cl;
+  const int per = (parts + kSumGroups - 1) / kSumGroups;
   float t = 0.f;
   if (col < 2 * d) {
     const int hi = min(parts, (grp + 1) * per);
-#pragma unroll 8
-    for (int p = grp * per; p < hi; ++p) t += part[(int64_t)p * 2 * d + col];
+    for (int p = grp * per; p < hi; p += 16) {
+      float x[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) x[u] = part[(int64_t)min(p + u, hi - 1) * 2 * d + col];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) t += p + u < hi ? x[u] : 0.f;
+    }
   }
   lds[grp][cl] = t;
   __syncthreads();
   if (grp == 0 && col < 2 * d) {
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) s += lds[i][cl];
+    for (int i = 0; i < kSumGroups; ++i) s += lds[i][cl];
     if (col < d && dqw) dqw[col] = s;
     if (col >= d && dkw) dkw[col - d] = s;
   }
 }
 
-template <class T, int LPR, bool VEC>
+template <class T, int LPR, bool VEC, bool STREAM>
 hipError_t launch(const RopeArgs& a, bool bwd) {
   const RopeGrid g = rope_grid(a.B * a.N, a.H + 2 * a.Hkv, 64 / LPR, bwd);
   const dim3 grid((uint32_t)g.x, (uint32_t)g.y);
   if (!bwd) {
-    hipLaunchKernelGGL((norm_rope_kernel<T, LPR, VEC>), grid, dim3(kThreads), 0, a.stream, a);
+    hipLaunchKernelGGL((norm_rope_kernel<T, LPR, VEC, STREAM>), grid, dim3(kThreads), 0, a.stream, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((norm_rope_bwd_kernel<T, LPR, VEC>), grid, dim3(kThreads), 0, a.stream, a);
+  hipLaunchKernelGGL((norm_rope_bwd_kernel<T, LPR, VEC, STREAM>), grid, dim3(kThreads), 0, a.stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.part) return e;
-  hipLaunchKernelGGL(weight_grad_kernel, dim3((2 * a.d + 31) / 32), dim3(1024), 0, a.stream, a.part,
+  hipLaunchKernelGGL(weight_grad_kernel, dim3((2 * a.d + kSumCols - 1) / kSumCols), dim3(kSumCols * kSumGroups), 0, a.stream, a.part,
                      (int)(g.x * g.y), a.d, a.dqw, a.dkw);
   return hipGetLastError();
 }
 
+// From 384 MB on, half as much again as the memory-side cache holds, past the caches.  us, as is -> past
+// them: forward, 16 heads of 128, 8192 tokens (201 MB) 37 -> 41, 12288 (302) 66 -> 67, 16384 (403) 88 -> 82,
+// 32768 (805) 174 -> 165; backward, 16/4 heads of 64, 16384 tokens (201) 43 -> 45, 32768 (403) 85 -> 84, 65536
+// (805) 164 -> 157; 16 of 128, 32768 (1611) 324 -> 322.
+template <class T, int LPR>
+hipError_t launch_vec(const RopeArgs& a, bool bwd) {
+  const int64_t values = a.B * a.N * (a.H + 2 * a.Hkv) * a.d;
+  const int64_t bytes = values * (2 * (int64_t)sizeof(T) + (bwd ? 4 : 0));
+  return bytes >= 384000000 ? launch<T, LPR, true, true>(a, bwd) : launch<T, LPR, true, false>(a, bwd);
+}
+
 template <int LPR>
 hipError_t launch_f32(const RopeArgs& a, bool bwd) {
-  return a.vec ? launch<float, LPR, true>(a, bwd) : launch<float, LPR, false>(a, bwd);
+  return a.vec ? launch_vec<float, LPR>(a, bwd) : launch<float, LPR, false, false>(a, bwd);
 }
 
 }  // namespace
 
 hipError_t launch_norm_rope(const RopeArgs& a, bool bwd) {
-  if (a.bf16)
-    return a.d == 128 ? launch<__bf16, 16, true>(a, bwd) : launch<__bf16, 8, true>(a, bwd);
+  if (a.bf16) return a.d == 128 ? launch_vec<__bf16, 16>(a, bwd) : launch_vec<__bf16, 8>(a, bwd);
   switch (rope_lanes(a.d, false)) {
     case 1: return launch_f32<1>(a, bwd);
     case 2: return launch_f32<2>(a, bwd);

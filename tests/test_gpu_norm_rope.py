@@ -195,6 +195,38 @@ def test_strides(store, d):
     assert all(torch.equal(q[b], want[0][0]) for b in range(B))
 
 
+@pytest.mark.parametrize("store,H,d,N", [("bf16", 1, 64, 500_017), ("bf16", 1, 128, 250_009),
+                                         ("fp32", 2, 32, 375_013)])
+def test_large_calls_are_their_parts(store, H, d, N):
+    """Calls whose tensors outgrow the caches, by another form of the kernels, against calls on parts of
+    their tokens: every row to the bit, the weights' gradients to the rounding of their sums."""
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    dt = torch.float32 if store == "fp32" else torch.bfloat16
+    new = lambda *shape: torch.randn(shape, generator=gen, device="cuda")   # noqa: E731
+    a = {"qkv": new(1, N, (H + 2) * d).to(dt), "rot": (d // 2,), "pos": None, "pos0": -1000,
+         "freqs": torch.from_numpy(10000.0 ** (-np.arange(0, d // 2, 2) / (d // 2))).cuda(),
+         "qw": 1 + 0.2 * new(d), "kw": 1 + 0.2 * new(d)}
+    g = [new(1, h, N, d) for h in (H, 1, 1)]
+    whole, wholeg = forward(a, H, 1), backward(a, *g)
+    sums = [torch.zeros(d, dtype=torch.float64, device="cuda") for _ in range(2)]
+    size = [torch.zeros(d, dtype=torch.float64, device="cuda") for _ in range(2)]
+    for lo in range(0, N, 100_000):
+        hi = min(N, lo + 100_000)
+        part = dict(a, qkv=a["qkv"][:, lo:hi].contiguous(), pos0=lo - 1000)
+        for t, u in zip(whole, forward(part, H, 1)):
+            assert torch.equal(t[:, :, lo:hi], u)
+        dx, dqw, dkw = backward(part, *(t[:, :, lo:hi].contiguous() for t in g))
+        assert torch.equal(wholeg[0][:, lo:hi], dx)
+        for i, t in enumerate((dqw, dkw)):
+            sums[i] += t.double()
+            # |g| |x r| summed: at most 6 standard deviations of a gradient and of a normed row each
+            size[i] += 36.0 * (hi - lo) * (H if i == 0 else 1)
+    for i in range(2):
+        # up to 2048 workgroups' chains of N H / 8192 rows and then the parts' sums, on both sides
+        steps = 2 * (N * H / 8192 + 2048 / 32 + 64)
+        assert bool(((wholeg[1 + i].double() - sums[i]).abs() <= steps * E * size[i]).all())
+
+
 def test_buffers_behind_the_last_row_stay():
     a, _ = make(6, 1, 37, 2, 2, 64, (64,), "bf16", pos=0)
     n = 37 * 64
