@@ -20,7 +20,7 @@ LIB = os.path.join(PKG, "libringx.so")
 SOURCES = ["ringx_api.cpp", "fwd_bf16.hip", "fwd_f32.hip", "merge.hip", "bwd_pre.hip", "split_sum.hip",
            "bwd_bf16.hip", "bwd_bf16_d64.hip", "bwd_dq_bf16.hip",
            "bwd_dq_bf16_d64.hip", "bwd_dq_ds.hip", "bwd_f32.hip", "tt_tokenize.hip",
-           "fwd_drop_bf16.hip", "fwd_drop_f32.hip", "bwd_drop_bf16.hip", "bwd_dq_drop_bf16.hip",
+           "fwd_drop_bf16.hip", "fwd_drop_f32.hip", "bwd_drop_bf16.hip",
            "bwd_drop_f32.hip", "norm_rope.hip"]
 
 HIPCC_FLAGS = [

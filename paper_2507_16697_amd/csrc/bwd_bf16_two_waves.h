@@ -37,6 +37,9 @@
 
 namespace ringx {
 namespace {
+#ifdef RINGX_DROPOUT
+namespace dkdv {
+#endif
 
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
@@ -123,9 +126,20 @@ __device__ __forceinline__ void issue_rowvals(const float* __restrict__ nlb,
   }
 }
 
+// with dropout, 1 KiB per wave and 32-query block more to turn the mask's bytes round in
+constexpr int kMaskWave = 1024;
+template <int D, int NW, int QB>
+constexpr int kLdsBytes = DkvCfg<D, NW, QB>::kLds + (kHasDrop<DROP> ? NW * QB * kMaskWave : 0);
+
+#ifdef RINGX_DROPOUT
+template <int D, int NW, int QB>
+__device__ __forceinline__ void body(
+    char* const lds, const uint32_t block, const uint32_t blocks,
+#else
 // waves per SIMD: three 4-wave workgroups on a CU, two of 8 waves with 32 queries each
 template <int D, int NW, int QB>
-__global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 : 1) void RINGX_KERNEL(bwd_dkdv)(
+__global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 : 1) void bwd_dkdv_kernel(
+#endif
     const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
     const __bf16* __restrict__ dout, const float* __restrict__ nl,
     const float* __restrict__ delta, float* __restrict__ dk, float* __restrict__ dv, int BHkv,
@@ -133,9 +147,10 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
     int64_t Nq, int64_t Nk, int R, int tiles_per_chunk, float c2, float scale, int accumulate, DROP drop) {
   using C = DkvCfg<D, NW, QB>;
   constexpr bool kDrop = kHasDrop<DROP>;
-  // with dropout, 1 KiB per wave and block more to turn the mask's bytes round in
-  constexpr int kMaskWave = 1024;
-  __shared__ __attribute__((aligned(1024))) char lds[C::kLds + (kDrop ? C::kWaves * C::kQB * kMaskWave : 0)];
+#ifndef RINGX_DROPOUT
+  __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes<D, NW, QB>];
+  const uint32_t block = blockIdx.x, blocks = gridDim.x;
+#endif
   const uint32_t lbase = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
 
   const int t = threadIdx.x;
@@ -146,10 +161,10 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
   const int kb = wave % C::kKB;     // key block of this wave
   const int qh = wave / C::kKB;     // parity of this wave's 32-query blocks
 
-  uint32_t wg = xcd_remap(blockIdx.x, gridDim.x);
+  uint32_t wg = xcd_remap(block, blocks);
   uint32_t split = 0;
   if constexpr (kDrop) {
-    const uint32_t per_split = gridDim.x / drop.splits;
+    const uint32_t per_split = blocks / drop.splits;
     split = wg / per_split;
     wg -= split * per_split;
   }
@@ -573,13 +588,14 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
   }
 }
 
+#ifndef RINGX_DROPOUT
 template <int D, int NW, int QB>
 hipError_t launch(const BwdArgs& a, const DROP& drop) {
   using C = DkvCfg<D, NW, QB>;
   const int64_t max_chunk = (a.Nk + a.R - 1) / a.R;
   const int64_t tpc = (max_chunk + C::kBK - 1) / C::kBK;
-  const int64_t nwg = a.BH / a.G * a.R * tpc * drop.splits;
-  hipLaunchKernelGGL((RINGX_KERNEL(bwd_dkdv)<D, NW, QB>), dim3((uint32_t)nwg), dim3(C::kThreads), 0,
+  const int64_t nwg = a.BH / a.G * a.R * tpc;
+  hipLaunchKernelGGL((bwd_dkdv_kernel<D, NW, QB>), dim3((uint32_t)nwg), dim3(C::kThreads), 0,
                      a.stream, (const __bf16*)a.q, (const __bf16*)a.k, (const __bf16*)a.v,
                      (const __bf16*)a.dout, a.nl, a.delta, a.dk, a.dv, (int)(a.BH / a.G),
                      (int)a.H, (int)a.G, a.Nq, a.Nk,
@@ -587,5 +603,10 @@ hipError_t launch(const BwdArgs& a, const DROP& drop) {
   return hipGetLastError();
 }
 
+#endif
+
+#ifdef RINGX_DROPOUT
+}  // namespace dkdv
+#endif
 }  // namespace
 }  // namespace ringx

@@ -27,6 +27,9 @@
 
 namespace ringx {
 namespace {
+#ifdef RINGX_DROPOUT
+namespace dq {
+#endif
 
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
@@ -111,8 +114,14 @@ __device__ __forceinline__ void issue_tile(const char* __restrict__ kb,
 
 // With KS > 1 key streams, stream p of the workgroup takes every KS-th key tile, and the streams'
 // dQ^T meet in LDS at the end.
+#ifdef RINGX_DROPOUT
 template <int D, int KS, int NW, int BK>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(bwd_dq)(
+__device__ __forceinline__ void body(
+    char* const lds, const uint32_t block, const uint32_t blocks,
+#else
+template <int D, int KS, int NW, int BK>
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void bwd_dq_kernel(
+#endif
     const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
     const __bf16* __restrict__ dout, const float* __restrict__ lse,
     const float* __restrict__ delta, float* __restrict__ dq, int BH, int H, int grp, int64_t Nq,
@@ -120,7 +129,10 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(bwd_dq)
   using C = DqCfg<D, KS, NW, BK>;
   constexpr bool kDrop = kHasDrop<DROP>;
   // per stream two K buffers, then two V buffers
+#ifndef RINGX_DROPOUT
   __shared__ __attribute__((aligned(1024))) char lds[4 * KS * C::kTileBytes];
+  const uint32_t block = blockIdx.x, blocks = gridDim.x;
+#endif
 
   const int t = threadIdx.x;
   const int lane = t & 63;
@@ -133,10 +145,10 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(bwd_dq)
   const int g = lane >> 5;
 
   const int64_t nqt = (Nq + C::kBQ - 1) / C::kBQ;
-  uint32_t wg = xcd_remap(blockIdx.x, gridDim.x);
+  uint32_t wg = xcd_remap(block, blocks);
   uint32_t split = 0;
   if constexpr (kDrop) {
-    const uint32_t per_split = gridDim.x / drop.splits;
+    const uint32_t per_split = blocks / drop.splits;
     split = wg / per_split;
     wg -= split * per_split;
   }
@@ -403,17 +415,23 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(bwd_dq)
   }
 }
 
+#ifndef RINGX_DROPOUT
 template <int D, int KS, int NW, int BK>
 hipError_t launch(const BwdArgs& a, const DROP& drop) {
   using C = DqCfg<D, KS, NW, BK>;
   const int64_t nqt = (a.Nq + C::kBQ - 1) / C::kBQ;
-  const int64_t nwg = nqt * a.BH * drop.splits;
-  hipLaunchKernelGGL((RINGX_KERNEL(bwd_dq)<D, KS, NW, BK>), dim3((uint32_t)nwg), dim3(C::kThreads), 0,
+  const int64_t nwg = nqt * a.BH;
+  hipLaunchKernelGGL((bwd_dq_kernel<D, KS, NW, BK>), dim3((uint32_t)nwg), dim3(C::kThreads), 0,
                      a.stream, (const __bf16*)a.q, (const __bf16*)a.k, (const __bf16*)a.v,
                      (const __bf16*)a.dout, a.lse, a.delta, a.dq, (int)a.BH, (int)a.H, (int)a.G,
                      a.Nq, a.Nk, (int)a.R, a.scale * kLog2e, a.scale, a.accumulate_dq ? 1 : 0, drop);
   return hipGetLastError();
 }
 
+#endif
+
+#ifdef RINGX_DROPOUT
+}  // namespace dq
+#endif
 }  // namespace
 }  // namespace ringx

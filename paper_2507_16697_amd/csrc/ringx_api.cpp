@@ -830,43 +830,47 @@ ringx_status ringx_bwd_preprocess_drop(const void* out, const void* dout, const 
 
 namespace {
 
-// Floats of the parts that a split of the sweeps leaves.
+// Floats of the parts that a cut of the sweeps leaves.
 struct DropParts {
   int64_t kv, q;   // of dK (as many of dV) and of dQ
 };
-DropParts drop_parts(const ringx::DropSplit& s, int64_t BHkv, int64_t BH, int64_t Nq, int64_t Nk,
+DropParts drop_parts(const ringx::DropCut& c, int64_t BHkv, int64_t BH, int64_t Nq, int64_t Nk,
                      int64_t d) {
-  return {s.kv > 1 ? s.kv * BHkv * Nk * d : 0, s.q > 1 ? s.q * BH * Nq * d : 0};
+  return {c.kv > 1 ? c.kv * BHkv * Nk * d : 0, c.q > 1 ? c.q * BH * Nq * d : 0};
 }
 
-// The stages after the preprocess.  parts: room for those of a split, null without one.
+// The stages after the preprocess.  parts: room for those of a cut.
 hipError_t launch_bwd_drop(const ringx::BwdArgs& a, bool bf16, const ringx::Drop& drop,
-                           const ringx::DropSplit& split, float* parts) {
+                           const ringx::DropCut& cut, float* parts) {
   if (!bf16) return ringx::launch_bwd_drop_f32(a, drop);
   const int64_t bkv = a.BH / a.G;
-  const DropParts n = drop_parts(split, bkv, a.BH, a.Nq, a.Nk, a.d);
+  const DropParts n = drop_parts(cut, bkv, a.BH, a.Nq, a.Nk, a.d);
   ringx::SplitSums sums;
-  auto part_of = [&](float** out, int64_t part, int64_t floats, int parts_of, bool accumulate) {
-    sums.sum[sums.count++] = {parts, *out, floats / 4, parts_of, accumulate ? 1 : 0};
+  auto in_parts = [&](float** out, int64_t floats, int count, bool accumulate) {
+    sums.sum[sums.count++] = {parts, *out, floats / count / 4, count, accumulate ? 1 : 0};
     *out = parts;
-    parts += part;
+    parts += floats;
   };
   ringx::BwdArgs w = a;
   ringx::Drop dkv = drop, dq = drop;
-  if (split.kv > 1) {
-    dkv.splits = (uint32_t)split.kv;
-    part_of(&w.dk, n.kv, bkv * a.Nk * a.d, split.kv, a.accumulate_dkv);
-    part_of(&w.dv, n.kv, bkv * a.Nk * a.d, split.kv, a.accumulate_dkv);
+  if (cut.kv > 1) {
+    dkv.splits = (uint32_t)cut.kv;
+    in_parts(&w.dk, n.kv, cut.kv, a.accumulate_dkv);
+    in_parts(&w.dv, n.kv, cut.kv, a.accumulate_dkv);
     w.accumulate_dkv = false;
   }
-  if (split.q > 1) {
-    dq.splits = (uint32_t)split.q;
-    part_of(&w.dq, n.q, a.BH * a.Nq * a.d, split.q, a.accumulate_dq);
+  if (cut.q > 1) {
+    dq.splits = (uint32_t)cut.q;
+    in_parts(&w.dq, n.q, cut.q, a.accumulate_dq);
     w.accumulate_dq = false;
   }
-  hipError_t e = ringx::launch_bwd_dkdv_drop_bf16(w, dkv);
-  if (e == hipSuccess) e = ringx::launch_bwd_dq_drop_bf16(w, dq);
+  const hipError_t e = ringx::launch_bwd_drop_bf16(w, dkv, dq, cut.ks);
   return e != hipSuccess || sums.count == 0 ? e : ringx::launch_split_sums(sums, a.stream);
+}
+
+// Bytes of ringx_attn_bwd_drop's workspace: the statistics, then the parts.
+size_t bwd_drop_bytes(size_t stats, const DropParts& n) {
+  return stats + static_cast<size_t>(4 * (2 * n.kv + n.q));
 }
 
 }  // namespace
@@ -878,8 +882,8 @@ size_t ringx_bwd_drop_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t
   if (Hkv < 1 || H < 1 || H % Hkv != 0) return 0;
   const size_t stats = ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, 1, dtype);
   if (stats == 0 || dtype != RINGX_BF16) return stats;
-  const DropParts n = drop_parts(ringx::drop_split(B * Hkv, B * H, Nq, Nk, d), B * Hkv, B * H, Nq, Nk, d);
-  return stats + static_cast<size_t>(4 * (2 * n.kv + n.q));
+  const ringx::DropCut cut = ringx::drop_cut(B * Hkv, B * H, Nq, Nk, d, true);
+  return bwd_drop_bytes(stats, drop_parts(cut, B * Hkv, B * H, Nq, Nk, d));
 }
 
 ringx_status ringx_attn_bwd_drop(const void* q, const void* k, const void* v, const void* out,
@@ -895,7 +899,11 @@ ringx_status ringx_attn_bwd_drop(const void* q, const void* k, const void* v, co
   ringx::Drop drop;
   st = make_drop(p, rng, q0, key0, Nq, Nk, &drop);
   if (st != RINGX_OK) return st;
-  const size_t need = ringx_bwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, dtype);
+  const bool bf16 = dtype == RINGX_BF16;
+  const ringx::DropCut cut =
+      bf16 ? ringx::drop_cut(B * Hkv, B * H, Nq, Nk, d, true) : ringx::DropCut{};
+  const size_t stats = ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, 1, dtype);
+  const size_t need = bwd_drop_bytes(stats, drop_parts(cut, B * Hkv, B * H, Nq, Nk, d));
   if (!workspace || workspace_bytes < need) return RINGX_E_WORKSPACE;
   for (const void* x : {q, k, v, out, dout, (const void*)lse, (const void*)dq, (const void*)dk,
                         (const void*)dv, (const void*)workspace})
@@ -920,12 +928,8 @@ ringx_status ringx_attn_bwd_drop(const void* q, const void* k, const void* v, co
   a.H = H, a.G = H / Hkv;
   a.accumulate_dkv = accumulate_dkv != 0, a.stream = stream;
   a.d_factor = (float)(256 - drop.thr) / 256.f;
-  const bool bf16 = dtype == RINGX_BF16;
   if (ringx::launch_bwd_pre(a, bf16) != hipSuccess) return RINGX_E_HIP;
-  const ringx::DropSplit split =
-      bf16 ? ringx::drop_split(bkv, bh, Nq, Nk, d) : ringx::DropSplit{};
-  float* const parts = delta + ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, 1, dtype) / 4;
-  return hip_status(launch_bwd_drop(a, bf16, drop, split, parts));
+  return hip_status(launch_bwd_drop(a, bf16, drop, cut, delta + stats / 4));
 }
 
 ringx_status ringx_attn_bwd_step_drop(const void* q, const void* k, const void* v, const void* dout,
@@ -951,7 +955,10 @@ ringx_status ringx_attn_bwd_step_drop(const void* q, const void* k, const void* 
   a.dq = dq_acc, a.dk = dk, a.dv = dv;
   a.BH = bh, a.Nq = Nq, a.Nk = Nk, a.d = d, a.R = 1, a.scale = scale, a.H = H, a.G = 1;
   a.accumulate_dkv = accumulate_dkv != 0, a.accumulate_dq = accumulate_dq != 0, a.stream = stream;
-  return hip_status(launch_bwd_drop(a, dtype == RINGX_BF16, drop, {}, nullptr));
+  const bool bf16 = dtype == RINGX_BF16;
+  // without a workspace there is no room for parts
+  const ringx::DropCut cut = bf16 ? ringx::drop_cut(bh, bh, Nq, Nk, d, false) : ringx::DropCut{};
+  return hip_status(launch_bwd_drop(a, bf16, drop, cut, nullptr));
 }
 
 }  // extern "C"

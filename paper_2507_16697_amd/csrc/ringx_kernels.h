@@ -214,48 +214,71 @@ inline int drop_fwd_split(int64_t BH, int64_t Nq, int64_t Nk, int64_t d) {
   const int ks = fwd_plan((Nq + 255) / 256 * BH, Nk, 1, d, false).cut.ks;
   return key_parts((Nq + 256 / ks - 1) / (256 / ks) * BH, Nk);
 }
-// How the backward with dropout, bf16, splits its sweeps over workgroups of their own where heads and rows
-// are too few to fill the chip; the parts are summed by a launch more (split_sum.hip).
-//   dQ     key_parts of the workgroups of query_cut's form.  The whole backward (us), whole -> dQ in parts:
-//          2 heads of 64, 1873 queries, 5265 keys (w = 60) 87 -> 62; 4/1 of 64, 1000 x 30000 (64) 309 ->
-//          157; 2 of 128, 4096 x 4096 (128) 174 -> 155; 1 of 64, 1024 x 1024 (32) 41 -> 40.
-//          From w = 129 on it loses (192: 340 -> 361).
-//   dK/dV  n tiles of 128 keys, `sweep` query rows to each (those of all heads of the group).  Parts of at
-//          least 256 rows, 128 of a head (a tile of queries), at most 32, as many as make the shortest
-//          sum of the rounds of 256 workgroups and of the parts' cost, where that is a tenth less than
-//          whole: a workgroup takes 0.026 us a row at d = 128 and 0.02 at 64, and 5 or 3 besides; a
-//          round's parts 17 or 8.4 to write and read, their launch 4; whole workgroups of 64 keys at
-//          d = 64 save 4.5.  Fitted to times like (one, two, three, four parts; n x sweep):
-//            d = 128  64 x 4096 187 143 123 120, 64 x 16384 539 344 294 276, 160 x 4096 212 242 213
-//                     233, 192 x 8192 419 439 461 427, 192 x 1024 78 103 120 120
-//            d = 64   16 x 1024 41 37 35 35, 84 x 1873 86 87 84 88, 128 x 2048 69 71 73 74
-//          Where at d = 64 few tiles are left for the last round, two parts, also three workgroups of 64
-//          keys to a CU: 320 x 6000 346 -> 320, 288 x 3000 190 -> 185.
-struct DropSplit {
-  int kv = 1, q = 1;
+// How the backward with dropout, bf16, is cut: dQ's key streams in a workgroup, and where heads and rows are
+// few, parts of the dK/dV sweep over queries and of the dQ sweep over keys, whose results are summed by
+// a launch more (split_sum.hip).
+struct DropCut {
+  int ks = 1;         // a dQ workgroup takes 256 / ks queries
+  int kv = 1, q = 1;  // parts of at least 256 query rows (128 of a head, a tile) and of 512 keys
 };
-inline bool ragged_last_round(int64_t n) { return n > 256 && n < 1024 && (n - 1) % 256 < 128; }
-inline DropSplit drop_split(int64_t BHkv, int64_t BH, int64_t Nq, int64_t Nk, int64_t d) {
-  DropSplit s;
-  const QueryCut c = query_cut((Nq + 255) / 256 * BH, Nk, dq_cut_rule(d));
-  s.q = key_parts((Nq + 256 / c.ks - 1) / (256 / c.ks) * BH, Nk);
-  const int64_t n = (Nk + 127) / 128 * BHkv, sweep = Nq * (BH / BHkv);
-  if (d == 64 && ragged_last_round(n)) {
-    s.kv = Nq >= 256 && sweep >= 2048 ? 2 : 1;
-  } else if (n < 1024) {
-    const double row = d == 64 ? 0.02 : 0.026, start = d == 64 ? 3 : 5, parts = d == 64 ? 8.4 : 17;
-    double best = 0;
-    for (int64_t k = 1; k <= 32 && k <= std::max<int64_t>(1, std::min(Nq / 128, sweep / 256)); ++k) {
-      double us = (double)((n * k + 255) / 256) * ((double)sweep / (double)k * row + start);
-      if (k > 1) us += (double)(n * k) / 256 * parts + 4;
-      else if (d == 64 && n <= 128) us -= 4.5;
-      if (k == 1 || us < best) {
-        if (k > 1) s.kv = (int)k;
-        best = k == 1 ? 0.9 * us : us;
+// The cut with the shortest time by this model.  A dK/dV workgroup takes `row` us for every query row that it
+// sweeps, a dQ workgroup `key` us for every key of a stream, each 4 besides, where 256 of them run; fewer at
+// a time run 0.85 as long (a higher clock).  The launch lasts as long as its whole work does on 256 CUs,
+// or as its list of workgroups, dK/dV's first, on CUs that take the next one when they are free.  Parts
+// are written and read at 4 TB/s, and their launch takes 4.  Fitted to times like these (us; dQ streams, *
+// parts of dK/dV, + of dQ; model in brackets):
+//   heads    queries x keys   one          two         four         others
+//   16 d64   4096 x 4096      295 (285)    294 (291)
+//   12 d64   3000 x 3000      141 (129)    159 (134)   151 (134)    2* one 158 (155)
+//   8 d64    2048 x 2048      59 (53)      48 (44)     48 (46)      2* two 69 (65)
+//   32/8 d64 1500 x 5003      257 (259)    277 (264)   292 (281)    2* two 290 (293)
+//   4/1 d64  1000 x 30000                              301 (266)    4+ 149 (147), 8+ 153 (153), 2* 4+ 159 (166)
+//   8 d128   4096 x 4096      278 (271)    243 (236)
+//   5 d128   4096 x 4096      166 (152)    196 (163)   187 (176)    2* two 181 (177)
+//   3 d128   8192 x 8192      536 (528)    425 (392)   372 (386)    2* one 434 (443)
+//   2 d128   4096 x 4096                               118 (124)    2* 80 (83), 3* two 107 (100), 4* 110 (110)
+//   8/1 d128 2048 x 8192                               434 (469)    2* 254 (271), 2* two 259 (251)
+// dQ's workgroups first is even or slower in all cuts that it picks.
+inline DropCut drop_cut(int64_t BHkv, int64_t BH, int64_t Nq, int64_t Nk, int64_t d, bool parts) {
+  constexpr int kParts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+  const double row = d == 64 ? 0.020 : 0.033;
+  const int64_t sweep = Nq * (BH / BHkv), n1 = (Nk + 127) / 128 * BHkv;
+  // nk dK/dV workgroups of tk each, then nq dQ workgroups of tq
+  auto length = [](int64_t nk, double tk, int64_t nq, double tq) {
+    const int64_t full = nk / 256, rest = nk % 256;
+    double a = full * tk + tq, b = (full + 1) * tk + tq;   // next ends on the 256 - rest CUs, on the others
+    double t = 0;
+    for (int64_t done = 0; done < nq;) {
+      const bool late = rest > 0 && b <= a;
+      t = late ? b : a;
+      done += late ? rest : 256 - rest;
+      (late ? b : a) += tq;
+    }
+    return std::max(t, (full + (rest > 0)) * tk);
+  };
+  DropCut best;
+  double best_us = 0;
+  for (int kv : kParts) {
+    if (kv > 1 && (!parts || n1 >= 1024 || kv > std::min(Nq / 128, sweep / 256))) break;
+    const double tk = (double)sweep / kv * row;
+    for (int ks = 1; ks <= 4; ks *= 2) {
+      const int64_t n2 = (Nq + 256 / ks - 1) / (256 / ks) * BH;
+      if (ks > 1 && (Nk < 64 * ks || n2 / ks >= 1024)) break;
+      for (int q : kParts) {
+        if (q > 1 && (!parts || ks < 4 || n2 > 256 || q > Nk / 512)) break;
+        const double key = d == 64 ? (ks == 1 ? 0.0255 : ks == 2 ? 0.026 : 0.029)
+                                   : (ks == 1 ? 0.041 : ks == 2 ? 0.043 : 0.055);
+        const double tq = (double)Nk / (ks * q) * key;
+        double us = (double)(n1 * kv) * (tk + 4) / 256 + (double)(n2 * q) * (tq + 4) / 256;
+        us = std::max(us, length(n1 * kv, 0.85 * tk + 4, n2 * q, 0.85 * tq + 4));
+        if (kv > 1) us += (double)(kv * BHkv * Nk * d) * 16 / 4e6;
+        if (q > 1) us += (double)(q * BH * Nq * d) * 8 / 4e6;
+        if (kv > 1 || q > 1) us += 4;
+        if (best_us == 0 || us < best_us) best_us = us, best = {ks, kv, q};
       }
     }
   }
-  return s;
+  return best;
 }
 
 // out = (out +) sum of `splits` parts of 4 n4 floats
@@ -412,8 +435,8 @@ hipError_t launch_bwd_dq_ds(const DsArgs& a);   // d = 128, bf16 dS (bwd_dq_ds.h
 // with dropout (R = 1; fused and step mode; D of the preprocess times 1 - p)
 hipError_t launch_fwd_drop_bf16(const FwdArgs& a, FwdMode mode, const Drop& drop);
 hipError_t launch_fwd_drop_f32(const FwdArgs& a, FwdMode mode, const Drop& drop);
-hipError_t launch_bwd_dkdv_drop_bf16(const BwdArgs& a, const Drop& drop);
-hipError_t launch_bwd_dq_drop_bf16(const BwdArgs& a, const Drop& drop);
+// dK/dV and dQ, each in its parts, dQ in ks key streams
+hipError_t launch_bwd_drop_bf16(const BwdArgs& a, const Drop& drop_kv, const Drop& drop_q, int ks);
 hipError_t launch_bwd_drop_f32(const BwdArgs& a, const Drop& drop);
 
 hipError_t launch_norm_rope(const RopeArgs& a, bool bwd);

@@ -12,17 +12,12 @@ from test_build_isa import _asm, _resources, test_m0_only_feeds_direct_lds_loads
 pytestmark = pytest.mark.skipif(shutil.which("hipcc") is None and not os.path.exists("/opt/rocm/bin/hipcc"),
                                 reason="hipcc not available")
 
-DROP_BF16 = ["fwd_drop_bf16.hip", "bwd_drop_bf16.hip", "bwd_dq_drop_bf16.hip"]
+DROP_BF16 = ["fwd_drop_bf16.hip", "bwd_drop_bf16.hip"]
 # (part of the kernel's name, workgroups that share a CU, waves of one); every kernel matching keeps its
 # values in registers.  A wave of w per SIMD has 512 / w registers, in steps of 8; a CU has 160 KiB of LDS.
 NO_SCRATCH = {
     "fwd_drop_bf16.hip": [(r"fwd_bf16_drop_kernelILi64E", 1, 8)],
-    "bwd_drop_bf16.hip": [(r"bwd_dkdv_drop_kernelILi64ELi8ELi2E", 1, 8),
-                          (r"bwd_dkdv_drop_kernelILi64ELi4ELi1E", 3, 4),
-                          (r"bwd_dkdv_drop_kernelILi128ELi8E", 1, 8),
-                          (r"bwd_dkdv_drop_kernelILi128ELi4E", 1, 4)],
-    "bwd_dq_drop_bf16.hip": [(r"bwd_dq_drop_kernelILi64ELi[124]ELi8E", 1, 8),
-                             (r"bwd_dq_drop_kernelILi64ELi1ELi4E", 3, 4)],
+    "bwd_drop_bf16.hip": [(r"bwd_drop_kernelILi64E", 1, 8)],
     "fwd_drop_f32.hip": [(r"fwd_f32_drop_kernel", 1, 4)],
     "bwd_drop_f32.hip": [(r"bwd_f32_drop_kernelILi[1-5]E", 2, 4)],
     # the backward's measured splits count on 4 waves on a SIMD

@@ -150,9 +150,9 @@ def test_backward_workspace_holds_the_parts():
                                  (1, 1, 1, 1, 1, 64)):
         assert size(B, H, Hkv, Nq, Nk, d, BF16) == stats(B, H, Nq, Nk, d, 1, BF16)
     assert size(1, 2, 2, 4096, 4096, 128, FP32) == stats(1, 2, 4096, 4096, 128, 1, FP32)
-    # 2 heads, 4096 x 4096: four parts of dK and dV and two of dQ
+    # 2 heads, 4096 x 4096: two parts of dK and dV
     assert (size(1, 2, 2, 4096, 4096, 128, BF16) - stats(1, 2, 4096, 4096, 128, 1, BF16)
-            == (4 * 2 + 2) * 2 * 4096 * 128 * 4)
+            == 2 * 2 * 2 * 4096 * 128 * 4)
     # the forward's: the parts' outputs and log-sum-exps, here two of 2 heads of 4096 rows
     need = ringx.ringx_fwd_drop_workspace_bytes
     assert need(1, 2, 2, 4096, 4096, 128, BF16) == 2 * 2 * 4096 * 129 * 4
