@@ -8,9 +8,9 @@ namespace {
 
 template <int D, int MODE>
 hipError_t launch_plan(const FwdArgs& a, const Drop& drop) {
-  const FwdPlan p = fwd_plan((a.Nq + 255) / 256 * a.BH, a.Nk, 1, D, false);
-  if (p.cut.ks == 4) return launch<D, MODE, 4, 8>(a, 1, drop);
-  if (p.cut.ks == 2) return launch<D, MODE, 2, 8>(a, 1, drop);
+  const int ks = drop_fwd_streams(a.BH, a.Nq, a.Nk, D);
+  if (ks == 4) return launch<D, MODE, 4, 8>(a, 1, drop);
+  if (ks == 2) return launch<D, MODE, 2, 8>(a, 1, drop);
   return launch<D, MODE, 1, 8>(a, 1, drop);
 }
 

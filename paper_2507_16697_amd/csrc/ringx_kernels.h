@@ -201,6 +201,16 @@ struct Drop {
                                    // workgroups of its own, with outputs [splits, ...]
 };
 
+// Dropout, bf16: the forward's key streams, those of the plain forward, which has half-size workgroups for
+// ragged launches at d = 64.  With dropout these would spill the mask's registers, and two streams serve:
+// n workgroups whole, in two, four streams at 1024 x 4096 (us): 260 175 147 143, 320 175 147 148, 384 175 151
+// 178, 448 176 194 202, 512 183 200 231, 576 263 246 261, 640 263 254 287; whole and in two at 256, 512, 1024,
+// 2048 keys: 320 27 28, 36 35, 56 50, 95 82; 576 39 44, 53 56, 82 81, 142 135.
+inline int drop_fwd_streams(int64_t BH, int64_t Nq, int64_t Nk, int64_t d) {
+  const int64_t n = (Nq + 255) / 256 * BH;
+  if (d == 64 && n > 256 && (n - 1) % 256 < 128 && Nk >= (n <= 512 ? 512 : 2048) && n <= 768) return 2;
+  return fwd_plan(n, Nk, 1, d, false).cut.ks;
+}
 // Dropout, bf16: parts of the keys for a sweep of them in w workgroups.  Up to 128 workgroups, as many parts
 // of at least 512 keys as one round of 256 workgroups holds, at most 32: parts of 256 keys gain no more than
 // their launch costs (2 heads of 128, 200 x 700, launched one by one: 15 us whole, 19 in two parts).
@@ -211,7 +221,7 @@ inline int key_parts(int64_t w, int64_t Nk) {
 // 64, 1873 queries, 5265 keys (w = 60) 42 -> 27; 4/1 of 64, 1000 x 30000 (64) 181 -> 66; 1 of 64, 1 x 8192 (1)
 // 56 -> 24; 2 of 128, 4096 x 4096 (128) 51 -> 45; from w = 129 on it loses (160: 74 -> 81 .. 98).
 inline int drop_fwd_split(int64_t BH, int64_t Nq, int64_t Nk, int64_t d) {
-  const int ks = fwd_plan((Nq + 255) / 256 * BH, Nk, 1, d, false).cut.ks;
+  const int ks = drop_fwd_streams(BH, Nq, Nk, d);
   return key_parts((Nq + 256 / ks - 1) / (256 / ks) * BH, Nk);
 }
 // How the backward with dropout, bf16, is cut: dQ's key streams in a workgroup, and where heads and rows are

@@ -101,6 +101,7 @@ def f32_scale(d):
     ("bf16", 2, 6, 2, 300, 1000, 128, 0.15), ("bf16", 1, 3, 3, 64, 2049, 64, 0.9),
     ("bf16", 1, 36, 36, 513, 190, 64, 0.1), ("bf16", 1, 36, 36, 513, 190, 128, 0.1),
     ("bf16", 1, 70, 70, 1025, 130, 64, 0.2), ("bf16", 1, 70, 35, 1025, 130, 128, 0.2),
+    ("bf16", 1, 130, 26, 270, 515, 64, 0.2),
     ("bf16", 1, 130, 130, 520, 70, 64, 0.2), ("bf16", 1, 8, 4, 300, 4400, 64, 0.2),
     ("bf16", 1, 1, 1, 100, 100, 64, 0.0), ("bf16", 1, 1, 1, 100, 100, 128, 0.0),
     ("fp32", 1, 1, 1, 1, 1, 1, 0.5), ("fp32", 1, 2, 1, 17, 47, 3, 0.2),
