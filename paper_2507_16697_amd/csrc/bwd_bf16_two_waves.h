@@ -5,7 +5,8 @@
 // d = 128 kernel in bwd_bf16.hip runs one wave per SIMD on a fixed software-pipelined schedule).
 //
 // One workgroup = 8 (or 4) waves = one K/V head and a tile of 128 (64) keys inside one chunk (a key
-// tile never straddles a chunk boundary; the launch rule is at the end of the file).  With the
+// tile never straddles a chunk boundary; the launch rules are beside the launches: bwd_bf16_d64.hip, and
+// bwd_drop_bf16.hip for dropout, which takes this kernel at d = 128 too).  With the
 // merged log-sum-exp saved by the forward, every chunk's
 // gradients are independent (arXiv 2507.16697 Sec. III-A: K/V chunk gradients computed per
 // chunk), so the workgroup sweeps every query tile of 64 or 128 queries once -- of every query head

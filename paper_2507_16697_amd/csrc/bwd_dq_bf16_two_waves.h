@@ -4,7 +4,8 @@
 // two waves per SIMD (the d = 128 kernel in bwd_dq_bf16.hip runs one wave per SIMD on a fixed
 // software-pipelined schedule).
 // Where the launch has to be cut smaller (query_cut in ringx_kernels.h) this kernel also serves
-// d = 128, whose one-wave schedule has no room for a second key stream in LDS.
+// d = 128, whose one-wave schedule has no room for a second key stream in LDS.  With dropout it serves
+// every launch (bwd_drop_bf16.hip).
 //
 // Query-stationary, like the forward: one workgroup = 8 waves = one (b, h) and 256 queries (32
 // per wave).  The key/value sequence is streamed chunk by chunk (ring steps, arXiv 2507.16697

@@ -31,8 +31,8 @@ template <class T>
 constexpr bool kHasDrop = !std::is_same_v<T, NoDrop>;
 
 // The attention kernels stand in headers and are compiled twice, by a source file without dropout and by
-// one with it, which defines RINGX_DROPOUT and so gives them this argument and names of their own (the bf16
-// backward's two kernels: makes them functions, since with dropout one kernel runs both).
+// one with it.  The latter defines RINGX_DROPOUT and so gives them this argument and names of their own; the
+// two kernels of the bf16 backward become functions, since with dropout one kernel runs both.
 namespace {
 #ifdef RINGX_DROPOUT
 using DROP = Drop;
