@@ -476,9 +476,10 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(fwd_bf1
 #pragma unroll
         for (int rr = 0; rr < 16; ++rr) ma = fmaxf(ma, cur[kt][rr]);
       float mnew = fmaxf(m2, max_halves(ma) * c2);
-      // a stream or part may meet scores of -inf alone (keys masked by an infinite feature) that one stream
-      // over all keys would weigh at 0: a finite reference keeps its sums 0 instead of NaN
-      if constexpr (KS > 1 || kSplit) mnew = fmaxf(mnew, -3e38f);
+      // a stream, a part, a ring step or the first tiles may meet scores of -inf alone (keys masked by an
+      // infinite feature): a finite reference keeps their sums 0 instead of NaN, so that the row is that of its
+      // finite scores however the launch is cut
+      if constexpr (KS > 1 || kDrop) mnew = fmaxf(mnew, -3e38f);
       const float alpha = fast_exp2(m2 - mnew);
       m2 = mnew;
       lc *= alpha;
