@@ -344,12 +344,14 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void RINGX_KERNEL(fwd_bf1
       float lnew = lse2r;
       if (!first) {
         const float lold = acc_lse[row] * kLog2e;
-        const float M = fmaxf(lold, lse2r);
+        float M = fmaxf(lold, lse2r);
+        // neither has seen a finite score: 0 and -inf again
+        if constexpr (kDrop) M = fmaxf(M, -3e38f);
         const float a = fast_exp2(lold - M);
         const float b = fast_exp2(lse2r - M);
         const float den = a + b;
-        wa = a / den;
-        wb = b * inv / den;
+        wa = kDrop && den == 0.f ? 0.f : a / den;
+        wb = kDrop && den == 0.f ? 0.f : b * inv / den;
         lnew = M + fast_log2(den);
       }
 #pragma unroll
