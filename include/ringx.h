@@ -356,7 +356,8 @@ ringx_status ringx_attn_bwd_drop(const void* q, const void* k, const void* v, co
                                  size_t workspace_bytes, hipStream_t stream);
 
 /* ringx_attn_fwd_step and ringx_attn_bwd_step with dropout; key0 is the chunk's place on the mask's
- * key axis.  delta [2,B,H,Nq] is that of ringx_bwd_preprocess_drop with the same p. */
+ * key axis.  delta [2,B,H,Nq] is that of ringx_bwd_preprocess_drop with the same p.  A chunk all of whose
+ * scores are -inf in a row adds nothing to it; a row that has had no others yet is 0, its lse -inf. */
 ringx_status ringx_attn_fwd_step_drop(const void* q, const void* k, const void* v, float* out_acc,
                                       float* lse_acc, int64_t B, int64_t H, int64_t Nq, int64_t Nk,
                                       int64_t d, float scale, ringx_dtype dtype, int first, float p,

@@ -186,7 +186,8 @@ __global__ __launch_bounds__(kThreads, 2) void RINGX_KERNEL(fwd_f32)(
       if (kp != 0 || !active) continue;
 
       float inv = 1.0f / l;
-      if constexpr (kDrop) inv *= drop.inv_keep;
+      // a ring step may have scores of -inf alone: it adds 0, with a log-sum-exp of -inf
+      if constexpr (kDrop) inv = mode == (int)FwdMode::kStep && l == 0.f ? 0.f : inv * drop.inv_keep;
       const float lse_r = m + logf(l);
       const int64_t row = (partials ? r * BH * Nq : 0) + (int64_t)bh * Nq + qi;
       float* orow = out + row * d;
@@ -194,10 +195,12 @@ __global__ __launch_bounds__(kThreads, 2) void RINGX_KERNEL(fwd_f32)(
       if (mode == (int)FwdMode::kStep && !first) {
         // Eq. (5) with the running result
         const float lold = lse[row];
-        const float M = fmaxf(lold, lse_r);
+        float M = fmaxf(lold, lse_r);
+        // neither has seen a finite score: 0 and -inf again
+        if constexpr (kDrop) M = fmaxf(M, -3e38f);
         const float a = expf(lold - M), b = expf(lse_r - M);
-        wa = a / (a + b);
-        wb = b * inv / (a + b);
+        wa = kDrop && a + b == 0.f ? 0.f : a / (a + b);
+        wb = kDrop && a + b == 0.f ? 0.f : b * inv / (a + b);
         lnew = M + logf(a + b);
 #pragma unroll
         for (int t = 0; t < NS; ++t) {

@@ -51,7 +51,7 @@ def test_masked_keys_in_front(store, H, Nq, Nk, d, lo):
           store, key0=lo)
 
 
-@pytest.mark.parametrize("store,d", [("bf16", 64), ("bf16", 128)])
+@pytest.mark.parametrize("store,d", [("bf16", 64), ("bf16", 128), ("fp32", 64), ("fp32", 37)])
 def test_masked_ring_chunks(store, d):
     """Chunks without a finite score before the first one that has some, and after it."""
     lengths, Nq, p, scale = (64, 96, 160, 64), 130, 0.2, f32_scale(d)
