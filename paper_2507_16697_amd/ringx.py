@@ -227,6 +227,33 @@ def _new(shape, dtype, like):
     return _T.empty(shape, dtype=dtype, device=like.device)
 
 
+def _elsewhere(stream, like):
+    """`stream` as a torch stream where it is not the current one of like's device, else None."""
+    if stream is None:
+        return None
+    cuda, handle = _T.cuda, _stream(stream)
+    if handle == (_raw_stream(like.device.index) if _raw_stream is not None
+                  else cuda.current_stream(like.device).cuda_stream):
+        return None
+    return stream if isinstance(stream, cuda.Stream) else cuda.ExternalStream(handle, like.device)
+
+
+def _workspace(workspace, need, like, stream):
+    """The caller's workspace, or a new one of `need` bytes.  The new one is dropped when the call returns,
+    with its kernels still to run: it is memory of the stream that they run on, which goes to later work
+    of that stream alone."""
+    if workspace is None:
+        other = _elsewhere(stream, like)
+        if other is None:
+            return _new(max(need, 16), _T.uint8, like)
+        with _T.cuda.stream(other):
+            return _new(max(need, 16), _T.uint8, like)
+    _dev(workspace)
+    if workspace.device != like.device:
+        raise ValueError(f"workspace: on {workspace.device}, expected {like.device}")
+    return workspace
+
+
 def _out(name, t, shape, dtype, like):
     """The caller's output buffer, checked, or a new one on `like`'s device."""
     if t is None:
@@ -346,13 +373,8 @@ def ringx_attn_bwd(q, k, v, out, dout, lse, R: int, scale=None, dq=None, dk=None
     dk = _grad_out("dk", dk, (B, H, Nk, d), q, accumulate_dkv)
     dv = _grad_out("dv", dv, (B, H, Nk, d), q, accumulate_dkv)
     code = _dtype_code(q)
-    if workspace is None:
-        need = ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, R, code)
-        workspace = _new(max(need, 16), torch.uint8, q)
-    else:
-        _dev(workspace)
-        if workspace.device != q.device:
-            raise ValueError(f"workspace: on {workspace.device}, expected {q.device}")
+    need = 0 if workspace is not None else ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, R, code)
+    workspace = _workspace(workspace, need, q, stream)
     st = lib().ringx_attn_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                               dout.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(),
                               dv.data_ptr(), B, H, Nq, Nk, d, R, _scale(scale, d), code,
@@ -497,7 +519,7 @@ def ringx_attn_bwd_gqa(q, k, v, out, dout, lse, R: int, scale=None, dq=None, dk=
     dk = _grad_out("dk", dk, (B, Hkv, Nk, d), q, accumulate_dkv)
     dv = _grad_out("dv", dv, (B, Hkv, Nk, d), q, accumulate_dkv)
     nbytes = ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, R, _dtype_code(q))
-    ws = _new(max(nbytes, 256), torch.uint8, q)
+    ws = _workspace(None, nbytes, q, stream)
     st = lib().ringx_attn_bwd_gqa(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                                   dout.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(),
                                   dv.data_ptr(), B, H, Hkv, Nq, Nk, d, R, _scale(scale, d),
@@ -573,14 +595,11 @@ def ringx_attn_bwd_ds(q, k, v, out, dout, lse, R: int, scale=None, dq=None, dk=N
     dq = _out("dq", dq, (B, H, Nq, d), torch.float32, q)
     dk = _grad_out("dk", dk, (B, Hkv, Nk, d), q, accumulate_dkv)
     dv = _grad_out("dv", dv, (B, Hkv, Nk, d), q, accumulate_dkv)
+    need = 0
     if workspace is None:
-        nbytes = ringx_bwd_ds_workspace_bytes(B, H, Hkv, Nq, Nk, d, R,
-                                              max(1, min(int(kv_per_slab), B * Hkv)))
-        workspace = _new(max(nbytes, 256), torch.uint8, q)
-    else:
-        _dev(workspace)
-        if workspace.device != q.device:
-            raise ValueError(f"workspace: on {workspace.device}, expected {q.device}")
+        need = ringx_bwd_ds_workspace_bytes(B, H, Hkv, Nq, Nk, d, R,
+                                            max(1, min(int(kv_per_slab), B * Hkv)))
+    workspace = _workspace(workspace, need, q, stream)
     st = lib().ringx_attn_bwd_ds(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                                  dout.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(),
                                  dv.data_ptr(), B, H, Hkv, Nq, Nk, d, R, _scale(scale, d),
@@ -655,7 +674,7 @@ def ringx_attn_fwd_drop(q, k, v, p: float, rng, scale=None, q0: int = 0, key0: i
     code = _dtype_code(q)
     need = ringx_fwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, code)
     if workspace is not None or need:
-        workspace = _workspace(workspace, need, q)
+        workspace = _workspace(workspace, need, q, stream)
     _launch("ringx_attn_fwd_drop", q, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(),
             out.data_ptr(), lse.data_ptr(), B, H, Hkv, Nq, Nk, d, _scale(scale, d), code, float(p),
             state, q0, key0, _ptr(workspace), 0 if workspace is None else _nbytes(workspace))
@@ -688,22 +707,13 @@ def ringx_attn_bwd_drop(q, k, v, out, dout, lse, p: float, rng, scale=None, q0: 
     dk = _grad_out("dk", dk, (B, Hkv, Nk, d), q, accumulate_dkv)
     dv = _grad_out("dv", dv, (B, Hkv, Nk, d), q, accumulate_dkv)
     code = _dtype_code(q)
-    workspace = _workspace(workspace, ringx_bwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, code), q)
+    workspace = _workspace(workspace, ringx_bwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, code), q,
+                           stream)
     _launch("ringx_attn_bwd_drop", q, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(),
             out.data_ptr(), dout.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(),
             dv.data_ptr(), B, H, Hkv, Nq, Nk, d, _scale(scale, d), code, float(p), state, q0, key0,
             1 if accumulate_dkv else 0, workspace.data_ptr(), _nbytes(workspace))
     return dq, dk, dv
-
-
-def _workspace(workspace, need, like):
-    """The caller's workspace, or a new one of `need` bytes."""
-    if workspace is None:
-        return _new(max(need, 16), _T.uint8, like)
-    _dev(workspace)
-    if workspace.device != like.device:
-        raise ValueError(f"workspace: on {workspace.device}, expected {like.device}")
-    return workspace
 
 
 def ringx_attn_fwd_step_drop(q, k, v, out_acc, lse_acc, first: bool, p: float, rng, key0: int,
@@ -857,7 +867,7 @@ def ringx_qkv_norm_rope_bwd(qkv, dq, dk, dv, freqs, rot, pos=None, pos0: int = 0
     code = _dtype_code(qkv)
     if q_weight is not None or k_weight is not None:
         workspace = _workspace(
-            workspace, ringx_qkv_norm_rope_bwd_workspace_bytes(B, N, H, Hkv, d, code), qkv)
+            workspace, ringx_qkv_norm_rope_bwd_workspace_bytes(B, N, H, Hkv, d, code), qkv, stream)
     else:
         workspace = None
     _launch("ringx_qkv_norm_rope_bwd", qkv, stream, qkv.data_ptr(), bs, ts, dq.data_ptr(),
