@@ -12,6 +12,9 @@ supplies device memory and the current HIP stream.  Function names follow the C 
     q, k, v = ringx_qkv_norm_rope(qkv, H, Hkv, freqs, rot)     # from a packed projection
     out, lse = ringx_attn_fwd_drop(q, k, v, p, rng)            # with dropout; rng: seed and offset
 
+stream= is a torch stream or a handle, by default the current stream; the caller orders it against the
+current one, as for any work on two streams.  Buffers that a call makes are that stream's memory.
+
 The library must be built (``python -m paper_2507_16697_amd.build``); loading fails loudly if it
 is missing -- there is no fallback implementation.
 """
@@ -254,20 +257,48 @@ def _workspace(workspace, need, like, stream):
     return workspace
 
 
-def _out(name, t, shape, dtype, like):
+def _made_for(other, like, make):
+    """A tensor that a call on the stream `other` hands out: memory of that stream, whose earlier work may
+    still use it and which may write it long after the caller has dropped it, and in use by the current
+    stream until then."""
+    here = _T.cuda.current_stream(like.device)
+    with _T.cuda.stream(other):
+        t = make()
+    t.record_stream(here)
+    return t
+
+
+def _out(name, t, shape, dtype, like, stream=None):
     """The caller's output buffer, checked, or a new one on `like`'s device."""
     if t is None:
+        other = _elsewhere(stream, like)
+        if other is not None:
+            return _made_for(other, like, lambda: _new(shape, dtype, like))
         return _new(shape, dtype, like)
     _dev(t)
     _expect(name, t, shape, dtype, like.device)
     return t
 
 
-def _grad_out(name, t, shape, like, accumulate):
-    """An fp32 gradient buffer that the call overwrites, or adds to (then a new one starts at 0)."""
+def _out_like(name, t, like, stream=None):
+    """The caller's output buffer, checked, or a new one, of `like`'s shape and type."""
+    if t is None:
+        other = _elsewhere(stream, like)
+        if other is not None:
+            return _made_for(other, like, lambda: _T.empty_like(like))
+        return _T.empty_like(like)
+    return _out(name, t, like.shape, like.dtype, like, stream)
+
+
+def _grad_out(name, t, shape, like, accumulate, stream=None):
+    """An fp32 gradient buffer that the call overwrites, or adds to (then a new one starts at 0, on the
+    stream that adds)."""
     if t is None and accumulate:
+        other = _elsewhere(stream, like)
+        if other is not None:
+            return _made_for(other, like, lambda: _new(shape, _T.float32, like).zero_())
         return _new(shape, _T.float32, like).zero_()
-    return _out(name, t, shape, _T.float32, like)
+    return _out(name, t, shape, _T.float32, like, stream)
 
 
 def _qkv(q, k, v, heads_kv=None):
@@ -317,8 +348,8 @@ def ringx_attn_fwd(q, k, v, R: int, scale=None, out=None, lse=None, stream=None)
     torch = _T or _torch()
     _dev(q, k, v)
     B, H, _, Nq, Nk, d = _qkv(q, k, v)
-    out = torch.empty_like(q) if out is None else _out("out", out, q.shape, q.dtype, q)
-    lse = _out("lse", lse, (B, H, Nq), torch.float32, q)
+    out = _out_like("out", out, q, stream)
+    lse = _out("lse", lse, (B, H, Nq), torch.float32, q, stream)
     st = lib().ringx_attn_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                               lse.data_ptr(), B, H, Nq, Nk, d, R, _scale(scale, d),
                               _dtype_code(q), _stream(stream))
@@ -332,8 +363,8 @@ def ringx_attn_fwd_partials(q, k, v, R: int, scale=None, part_out=None, part_lse
     torch = _T or _torch()
     _dev(q, k, v)
     B, H, _, Nq, Nk, d = _qkv(q, k, v)
-    part_out = _out("part_out", part_out, (R, B, H, Nq, d), torch.float32, q)
-    part_lse = _out("part_lse", part_lse, (R, B, H, Nq), torch.float32, q)
+    part_out = _out("part_out", part_out, (R, B, H, Nq, d), torch.float32, q, stream)
+    part_lse = _out("part_lse", part_lse, (R, B, H, Nq), torch.float32, q, stream)
     st = lib().ringx_attn_fwd_partials(q.data_ptr(), k.data_ptr(), v.data_ptr(),
                                        part_out.data_ptr(), part_lse.data_ptr(), B, H, Nq, Nk, d,
                                        R, _scale(scale, d), _dtype_code(q), _stream(stream))
@@ -352,8 +383,8 @@ def ringx_lse_merge(part_out, part_lse, out_dtype=None, out=None, lse=None, stre
     _expect("part_out", part_out, (R, B, H, Nq, d), torch.float32, dev)
     _expect("part_lse", part_lse, (R, B, H, Nq), torch.float32, dev)
     out = _out("out", out, (B, H, Nq, d),
-               (out_dtype or torch.float32) if out is None else out.dtype, part_out)
-    lse = _out("lse", lse, (B, H, Nq), torch.float32, part_out)
+               (out_dtype or torch.float32) if out is None else out.dtype, part_out, stream)
+    lse = _out("lse", lse, (B, H, Nq), torch.float32, part_out, stream)
     st = lib().ringx_lse_merge(part_out.data_ptr(), part_lse.data_ptr(), out.data_ptr(),
                                lse.data_ptr(), R, B, H, Nq, d, _dtype_code(out), _stream(stream))
     _check("ringx_lse_merge", st)
@@ -369,9 +400,9 @@ def ringx_attn_bwd(q, k, v, out, dout, lse, R: int, scale=None, dq=None, dk=None
     _expect("out", out, q.shape, q.dtype, q.device)
     _expect("dout", dout, q.shape, q.dtype, q.device)
     _expect("lse", lse, (B, H, Nq), torch.float32, q.device)
-    dq = _out("dq", dq, (B, H, Nq, d), torch.float32, q)
-    dk = _grad_out("dk", dk, (B, H, Nk, d), q, accumulate_dkv)
-    dv = _grad_out("dv", dv, (B, H, Nk, d), q, accumulate_dkv)
+    dq = _out("dq", dq, (B, H, Nq, d), torch.float32, q, stream)
+    dk = _grad_out("dk", dk, (B, H, Nk, d), q, accumulate_dkv, stream)
+    dv = _grad_out("dv", dv, (B, H, Nk, d), q, accumulate_dkv, stream)
     code = _dtype_code(q)
     need = 0 if workspace is not None else ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, R, code)
     workspace = _workspace(workspace, need, q, stream)
@@ -418,7 +449,7 @@ def ringx_bwd_preprocess(out, dout, lse, delta=None, stream=None):
     B, H, Nq, d = out.shape
     _expect("dout", dout, out.shape, out.dtype, out.device)
     _expect("lse", lse, (B, H, Nq), torch.float32, out.device)
-    delta = _out("delta", delta, (2, B, H, Nq), torch.float32, out)
+    delta = _out("delta", delta, (2, B, H, Nq), torch.float32, out, stream)
     st = lib().ringx_bwd_preprocess(out.data_ptr(), dout.data_ptr(), lse.data_ptr(),
                                     delta.data_ptr(), B, H, Nq, d, _dtype_code(out),
                                     _stream(stream))
@@ -433,8 +464,8 @@ def ringx_attn_bwd_dkdv(q, k, v, dout, lse, delta, R: int, scale=None, dk=None, 
     _dev(q, k, v, dout, lse, delta)
     B, H, _, Nq, Nk, d = _qkv(q, k, v)
     _check_grad_inputs(q, dout, lse, delta)
-    dk = _grad_out("dk", dk, (B, H, Nk, d), q, accumulate_dkv)
-    dv = _grad_out("dv", dv, (B, H, Nk, d), q, accumulate_dkv)
+    dk = _grad_out("dk", dk, (B, H, Nk, d), q, accumulate_dkv, stream)
+    dv = _grad_out("dv", dv, (B, H, Nk, d), q, accumulate_dkv, stream)
     st = lib().ringx_attn_bwd_dkdv(q.data_ptr(), k.data_ptr(), v.data_ptr(), dout.data_ptr(),
                                    lse.data_ptr(), delta.data_ptr(), dk.data_ptr(), dv.data_ptr(),
                                    B, H, Nq, Nk, d, R, _scale(scale, d), _dtype_code(q),
@@ -449,7 +480,7 @@ def ringx_attn_bwd_dq(q, k, v, dout, lse, delta, R: int, scale=None, dq=None, st
     _dev(q, k, v, dout, lse, delta)
     B, H, _, Nq, Nk, d = _qkv(q, k, v)
     _check_grad_inputs(q, dout, lse, delta)
-    dq = _out("dq", dq, (B, H, Nq, d), torch.float32, q)
+    dq = _out("dq", dq, (B, H, Nq, d), torch.float32, q, stream)
     st = lib().ringx_attn_bwd_dq(q.data_ptr(), k.data_ptr(), v.data_ptr(), dout.data_ptr(),
                                  lse.data_ptr(), delta.data_ptr(), dq.data_ptr(), B, H, Nq, Nk, d,
                                  R, _scale(scale, d), _dtype_code(q), _stream(stream))
@@ -497,8 +528,8 @@ def ringx_attn_fwd_gqa(q, k, v, R: int, scale=None, out=None, lse=None, stream=N
     torch = _T or _torch()
     _dev(q, k, v)
     B, H, Hkv, Nq, Nk, d = _qkv(q, k, v, heads_kv=True)
-    out = torch.empty_like(q) if out is None else _out("out", out, q.shape, q.dtype, q)
-    lse = _out("lse", lse, (B, H, Nq), torch.float32, q)
+    out = _out_like("out", out, q, stream)
+    lse = _out("lse", lse, (B, H, Nq), torch.float32, q, stream)
     st = lib().ringx_attn_fwd_gqa(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                                   lse.data_ptr(), B, H, Hkv, Nq, Nk, d, R, _scale(scale, d),
                                   _dtype_code(q), _stream(stream))
@@ -515,9 +546,9 @@ def ringx_attn_bwd_gqa(q, k, v, out, dout, lse, R: int, scale=None, dq=None, dk=
     _expect("out", out, q.shape, q.dtype, q.device)
     _expect("dout", dout, q.shape, q.dtype, q.device)
     _expect("lse", lse, (B, H, Nq), torch.float32, q.device)
-    dq = _out("dq", dq, (B, H, Nq, d), torch.float32, q)
-    dk = _grad_out("dk", dk, (B, Hkv, Nk, d), q, accumulate_dkv)
-    dv = _grad_out("dv", dv, (B, Hkv, Nk, d), q, accumulate_dkv)
+    dq = _out("dq", dq, (B, H, Nq, d), torch.float32, q, stream)
+    dk = _grad_out("dk", dk, (B, Hkv, Nk, d), q, accumulate_dkv, stream)
+    dv = _grad_out("dv", dv, (B, Hkv, Nk, d), q, accumulate_dkv, stream)
     nbytes = ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, R, _dtype_code(q))
     ws = _workspace(None, nbytes, q, stream)
     st = lib().ringx_attn_bwd_gqa(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
@@ -542,12 +573,8 @@ def ringx_attn_bwd_dkdv_ds(q, k, v, dout, lse, delta, R: int, ds, kv_begin: int,
     _dev(q, k, v, dout, lse, delta, ds)
     B, H, Hkv, Nq, Nk, d = _qkv(q, k, v, heads_kv=True)
     _check_grad_inputs(q, dout, lse, delta)
-    f32 = dict(dtype=torch.float32, device=q.device)
-    dk = torch.zeros((B, Hkv, Nk, d), **f32) if dk is None else dk
-    dv = torch.zeros((B, Hkv, Nk, d), **f32) if dv is None else dv
-    _dev(dk, dv)
-    _expect("dk", dk, (B, Hkv, Nk, d), torch.float32, q.device)
-    _expect("dv", dv, (B, Hkv, Nk, d), torch.float32, q.device)
+    dk = _grad_out("dk", dk, (B, Hkv, Nk, d), q, True, stream)   # rows of other heads: 0
+    dv = _grad_out("dv", dv, (B, Hkv, Nk, d), q, True, stream)
     if ds.device != q.device:
         raise ValueError(f"ds: on {ds.device}, expected {q.device}")
     st = lib().ringx_attn_bwd_dkdv_ds(q.data_ptr(), k.data_ptr(), v.data_ptr(), dout.data_ptr(),
@@ -571,7 +598,7 @@ def ringx_attn_bwd_dq_ds(ds, k, q_shape, R: int, kv_begin: int, kv_count: int, s
     if k.dim() != 4 or k.shape[0] != B or k.shape[3] != d:
         raise ValueError(f"k: shape {tuple(k.shape)} does not match q_shape {tuple(q_shape)}")
     Hkv, Nk = int(k.shape[1]), int(k.shape[2])
-    dq = _out("dq", dq, (B, H, Nq, d), torch.float32, k)
+    dq = _out("dq", dq, (B, H, Nq, d), torch.float32, k, stream)
     if ds.device != k.device:
         raise ValueError(f"ds: on {ds.device}, expected {k.device}")
     st = lib().ringx_attn_bwd_dq_ds(ds.data_ptr(), _nbytes(ds), k.data_ptr(), dq.data_ptr(), B, H,
@@ -592,9 +619,9 @@ def ringx_attn_bwd_ds(q, k, v, out, dout, lse, R: int, scale=None, dq=None, dk=N
     _expect("out", out, q.shape, q.dtype, q.device)
     _expect("dout", dout, q.shape, q.dtype, q.device)
     _expect("lse", lse, (B, H, Nq), torch.float32, q.device)
-    dq = _out("dq", dq, (B, H, Nq, d), torch.float32, q)
-    dk = _grad_out("dk", dk, (B, Hkv, Nk, d), q, accumulate_dkv)
-    dv = _grad_out("dv", dv, (B, Hkv, Nk, d), q, accumulate_dkv)
+    dq = _out("dq", dq, (B, H, Nq, d), torch.float32, q, stream)
+    dk = _grad_out("dk", dk, (B, Hkv, Nk, d), q, accumulate_dkv, stream)
+    dv = _grad_out("dv", dv, (B, Hkv, Nk, d), q, accumulate_dkv, stream)
     need = 0
     if workspace is None:
         need = ringx_bwd_ds_workspace_bytes(B, H, Hkv, Nq, Nk, d, R,
@@ -621,7 +648,7 @@ def ringx_tt_tokenize(field, k: int, ratio: int, centre, p: int, sigma=None, out
     out_dtype = out_dtype or torch.float32
     L = (D // (ratio * k * p)) * (H // (ratio * k * p)) * (W // (ratio * k * p))
     tokens = _out("tokens", tokens, (L, C * p ** 3), out_dtype if tokens is None else tokens.dtype,
-                  field)
+                  field, stream)
     sigma = float(k) / 2.0 if sigma is None else float(sigma)
     cz, cy, cx = (int(c) for c in centre)
     st = lib().ringx_tt_tokenize(field.data_ptr(), tokens.data_ptr(), C, D, H, W, k, ratio, cz,
@@ -669,8 +696,8 @@ def ringx_attn_fwd_drop(q, k, v, p: float, rng, scale=None, q0: int = 0, key0: i
     _dev(q, k, v)
     B, H, Hkv, Nq, Nk, d = _qkv(q, k, v, heads_kv=True)
     state = _rng(rng, q)
-    out = torch.empty_like(q) if out is None else _out("out", out, q.shape, q.dtype, q)
-    lse = _out("lse", lse, (B, H, Nq), torch.float32, q)
+    out = _out_like("out", out, q, stream)
+    lse = _out("lse", lse, (B, H, Nq), torch.float32, q, stream)
     code = _dtype_code(q)
     need = ringx_fwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, code)
     if workspace is not None or need:
@@ -703,9 +730,9 @@ def ringx_attn_bwd_drop(q, k, v, out, dout, lse, p: float, rng, scale=None, q0: 
     _expect("dout", dout, q.shape, q.dtype, q.device)
     _expect("lse", lse, (B, H, Nq), torch.float32, q.device)
     state = _rng(rng, q)
-    dq = _out("dq", dq, (B, H, Nq, d), torch.float32, q)
-    dk = _grad_out("dk", dk, (B, Hkv, Nk, d), q, accumulate_dkv)
-    dv = _grad_out("dv", dv, (B, Hkv, Nk, d), q, accumulate_dkv)
+    dq = _out("dq", dq, (B, H, Nq, d), torch.float32, q, stream)
+    dk = _grad_out("dk", dk, (B, Hkv, Nk, d), q, accumulate_dkv, stream)
+    dv = _grad_out("dv", dv, (B, Hkv, Nk, d), q, accumulate_dkv, stream)
     code = _dtype_code(q)
     workspace = _workspace(workspace, ringx_bwd_drop_workspace_bytes(B, H, Hkv, Nq, Nk, d, code), q,
                            stream)
@@ -761,7 +788,7 @@ def ringx_bwd_preprocess_drop(out, dout, lse, p: float, delta=None, stream=None)
     B, H, Nq, d = out.shape
     _expect("dout", dout, out.shape, out.dtype, out.device)
     _expect("lse", lse, (B, H, Nq), torch.float32, out.device)
-    delta = _out("delta", delta, (2, B, H, Nq), torch.float32, out)
+    delta = _out("delta", delta, (2, B, H, Nq), torch.float32, out, stream)
     _launch("ringx_bwd_preprocess_drop", out, stream, out.data_ptr(), dout.data_ptr(),
             lse.data_ptr(), delta.data_ptr(), B, H, Nq, d, _dtype_code(out), float(p))
     return delta
@@ -833,9 +860,9 @@ def ringx_qkv_norm_rope(qkv, H: int, Hkv: int, freqs, rot, pos=None, pos0: int =
     torch = _T or _torch()
     B, N, d, bs, ts, sections, axes, pos_bs = _rope_args(qkv, H, Hkv, freqs, rot, pos, q_weight,
                                                          k_weight)
-    q = _out("q", q, (B, H, N, d), qkv.dtype, qkv)
-    k = _out("k", k, (B, Hkv, N, d), qkv.dtype, qkv)
-    v = _out("v", v, (B, Hkv, N, d), qkv.dtype, qkv)
+    q = _out("q", q, (B, H, N, d), qkv.dtype, qkv, stream)
+    k = _out("k", k, (B, Hkv, N, d), qkv.dtype, qkv, stream)
+    v = _out("v", v, (B, Hkv, N, d), qkv.dtype, qkv, stream)
     _launch("ringx_qkv_norm_rope", qkv, stream, qkv.data_ptr(), bs, ts, _ptr(q_weight),
             _ptr(k_weight), _ptr(freqs), _ptr(pos), pos_bs, pos0, axes, sections, q.data_ptr(),
             k.data_ptr(), v.data_ptr(), B, N, H, Hkv, d, float(eps), _dtype_code(qkv))
@@ -859,11 +886,11 @@ def ringx_qkv_norm_rope_bwd(qkv, dq, dk, dv, freqs, rot, pos=None, pos0: int = 0
         _expect(name, g, (B, heads, N, d), torch.float32, qkv.device)
     if (q_weight is None and dq_weight is not None) or (k_weight is None and dk_weight is not None):
         raise ValueError("a weight's gradient without the weight")
-    dqkv = _out("dqkv", dqkv, (B, N, (H + 2 * Hkv) * d), qkv.dtype, qkv)
+    dqkv = _out("dqkv", dqkv, (B, N, (H + 2 * Hkv) * d), qkv.dtype, qkv, stream)
     if q_weight is not None:
-        dq_weight = _out("dq_weight", dq_weight, (d,), torch.float32, qkv)
+        dq_weight = _out("dq_weight", dq_weight, (d,), torch.float32, qkv, stream)
     if k_weight is not None:
-        dk_weight = _out("dk_weight", dk_weight, (d,), torch.float32, qkv)
+        dk_weight = _out("dk_weight", dk_weight, (d,), torch.float32, qkv, stream)
     code = _dtype_code(qkv)
     if q_weight is not None or k_weight is not None:
         workspace = _workspace(

@@ -146,3 +146,44 @@ def test_hidden_workspaces_are_the_launch_streams(torch, name, stream):
     hidden = [t for t in torch.made if t.dtype == torch.uint8]
     assert launched == (HERE if stream in (None, HERE) else THERE)
     assert len(hidden) == 1 and hidden[0].pool == launched and torch.now == HERE
+
+
+ALL = dict(WITH_WORKSPACE, **{
+    "fwd": lambda o, **kw: ringx.ringx_attn_fwd(o.q, o.k, o.v, 4, **kw),
+    "fwd_partials": lambda o, **kw: ringx.ringx_attn_fwd_partials(o.q, o.k, o.v, 4, **kw),
+    "merge": lambda o, **kw: ringx.ringx_lse_merge(o.parts, o.part_lse, **kw),
+    "pre": lambda o, **kw: ringx.ringx_bwd_preprocess(o.out, o.do, o.lse, **kw),
+    "pre_drop": lambda o, **kw: ringx.ringx_bwd_preprocess_drop(o.out, o.do, o.lse, 0.1, **kw),
+    "dkdv": lambda o, **kw: ringx.ringx_attn_bwd_dkdv(o.q, o.k, o.v, o.do, o.lse, o.delta, 4, **kw),
+    "dq": lambda o, **kw: ringx.ringx_attn_bwd_dq(o.q, o.k, o.v, o.do, o.lse, o.delta, 4, **kw),
+    "fwd_gqa": lambda o, **kw: ringx.ringx_attn_fwd_gqa(o.q, o.k, o.v, 4, **kw),
+    "dkdv_ds": lambda o, **kw: ringx.ringx_attn_bwd_dkdv_ds(o.q, o.k, o.v, o.do, o.lse, o.delta, 4, o.ds, 0, 1,
+                                                            **kw),
+    "dq_ds": lambda o, **kw: ringx.ringx_attn_bwd_dq_ds(o.ds, o.k, o.q.shape, 4, 0, 1, **kw),
+    "rope": lambda o, **kw: ringx.ringx_qkv_norm_rope(o.qkv, o.H, o.H, o.freqs, (o.d,), **kw),
+    "tokenize": lambda o, **kw: ringx.ringx_tt_tokenize(o.field, 2, 1, (0, 0, 0), 4, **kw),
+    "bwd +=": lambda o, **kw: ringx.ringx_attn_bwd(o.q, o.k, o.v, o.out, o.do, o.lse, 4, accumulate_dkv=True,
+                                                   **kw),
+    "bwd_drop +=": lambda o, **kw: ringx.ringx_attn_bwd_drop(o.q, o.k, o.v, o.out, o.do, o.lse, 0.1, o.rng,
+                                                             accumulate_dkv=True, **kw),
+})
+
+
+@needs_lib
+@pytest.mark.parametrize("name", sorted(ALL))
+@pytest.mark.parametrize("stream", [None, HERE, THERE, "object"])
+def test_buffers_handed_out_are_the_launch_streams(torch, name, stream):
+    """Outputs that the caller does not give, and the zeros that gradients are added to."""
+    o = operands(torch)
+    o.parts, o.part_lse = torch.Tensor((4, 1, 2, 8, 64), torch.float32), torch.Tensor((4, 1, 2, 8), torch.float32)
+    o.field, o.ds = torch.Tensor((1, 16, 16, 16), torch.float32), torch.Tensor((1 << 20,), torch.uint8)
+    res = ALL[name](o, stream=Stream(THERE) if stream == "object" else stream)
+    res = [t for t in (res if isinstance(res, tuple) else (res,)) if t is not None]
+    (_, launched), = torch.calls
+    assert launched == (HERE if stream in (None, HERE) else THERE)
+    assert res and all(any(t is m for m in torch.made) for t in res) and torch.now == HERE
+    for t in torch.made:
+        assert t.pool == launched and all(f == launched for f in t.fills)
+    for t in res:     # the caller's stream goes on to use them
+        assert t.users == ([] if launched == HERE else [HERE])
+    assert sum(len(t.fills) for t in torch.made) == (2 if "+=" in name or name == "dkdv_ds" else 0)

@@ -81,3 +81,56 @@ def test_workspaces_of_calls_on_another_stream(name, form):
             assert all(bool((x == 255).all()) for x in junk)
             assert all(torch.equal(a, b) for a, b in zip(want, got))
             del junk
+
+
+CALLS_HANDING_OUT = dict(CALLS, **{
+    "fwd": lambda t, **kw: ringx.ringx_attn_fwd(t["q"], t["k"], t["v"], 4, **kw),
+    "fwd_partials": lambda t, **kw: ringx.ringx_attn_fwd_partials(t["q"], t["k"], t["v"], 4, **kw),
+    "rope": lambda t, **kw: ringx.ringx_qkv_norm_rope(t["qkv"], H, H, t["freqs"], (D,), **kw),
+    "bwd +=": lambda t, **kw: ringx.ringx_attn_bwd(t["q"], t["k"], t["v"], t["out"], t["do"], t["lse"], 4,
+                                                   accumulate_dkv=True, **kw),
+    "bwd_drop +=": lambda t, **kw: ringx.ringx_attn_bwd_drop(t["q"], t["k"], t["v"], t["out"], t["do"],
+                                                             t["lse"], 0.1, t["rng"], accumulate_dkv=True,
+                                                             **kw),
+})
+
+
+@pytest.mark.parametrize("name", sorted(CALLS_HANDING_OUT))
+def test_outputs_of_calls_on_another_stream(name):
+    """Outputs may be dropped before they are written; gradients are added to zeros, not to what the fill
+    has still to clear."""
+    print(name, flush=True)
+    call = CALLS_HANDING_OUT[name]
+    t = operands()
+    want = call(t)
+    sizes = [x.numel() * x.element_size() for x in want]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for keep in range(len(want)):
+        got = on_a_held_up_stream(side, lambda: call(t, stream=side)[keep])
+        junk = buffers_like(n for i, n in enumerate(sizes) if i != keep)
+        torch.cuda.synchronize()
+        assert all(bool((x == 255).all()) for x in junk) and torch.equal(got, want[keep])
+        del junk
+
+
+def test_a_call_on_another_stream_is_captured():
+    """The launch stream forked from a capturing one: its buffers belong to the graph."""
+    t = operands()
+    want = CALLS["fwd_drop"](t) + CALLS["bwd_drop"](t)
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+    main.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(main), torch.cuda.graph(graph, stream=main):
+        side.wait_stream(main)
+        got = CALLS["fwd_drop"](t, stream=side) + CALLS["bwd_drop"](t, stream=side)
+        main.wait_stream(side)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        graph.replay()
+        junk = buffers_like([BYTES["fwd_drop"](), BYTES["bwd_drop"]()])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+        assert all(bool((x == 255).all()) for x in junk)
+        for x in got:
+            x.zero_()
