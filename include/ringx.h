@@ -345,7 +345,9 @@ size_t ringx_fwd_drop_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t
                                       int64_t d, ringx_dtype dtype);
 
 /* Backward of ringx_attn_fwd_drop, with its p, rng values, q0 and key0.  workspace:
- * ringx_bwd_drop_workspace_bytes(...) bytes, 16-byte aligned, contents ignored.  Bitwise reproducible. */
+ * ringx_bwd_drop_workspace_bytes(...) bytes, 16-byte aligned, contents ignored.  Bitwise reproducible.
+ * bf16 heads that one launch cannot take (B Hkv ceil(Nk / 128) + B H ceil(Nq / 256) of 2^23 and more):
+ * RINGX_E_SHAPE, from ringx_attn_bwd_step_drop too. */
 size_t ringx_bwd_drop_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t Nk,
                                       int64_t d, ringx_dtype dtype);
 ringx_status ringx_attn_bwd_drop(const void* q, const void* k, const void* v, const void* out,

@@ -22,6 +22,7 @@ struct Forms {
   using Dq = dq::DqCfg<D, KS, 8, kBK>;
   static constexpr int kDkvLds = dkdv::kLdsBytes<D, 8, kQB>, kDqLds = 4 * KS * Dq::kTileBytes;
   static constexpr int kLds = kDkvLds > kDqLds ? kDkvLds : kDqLds;
+  static_assert(Dkv::kBK == 128 && Dq::kBQ == 256 / KS, "tiles of drop_bwd_workgroups");
 };
 
 // The first n_kv workgroups are dK/dV's, the others dQ's.

@@ -839,6 +839,18 @@ DropParts drop_parts(const ringx::DropCut& c, int64_t BHkv, int64_t BH, int64_t 
   return {c.kv > 1 ? c.kv * BHkv * Nk * d : 0, c.q > 1 ? c.q * BH * Nq * d : 0};
 }
 
+// The cut of the bf16 backward (fp32: none), or RINGX_E_SHAPE for more workgroups than its one launch takes:
+// 512 threads each, and a launch has fewer than 2^32.
+ringx_status make_cut(int64_t BHkv, int64_t BH, int64_t Nq, int64_t Nk, int64_t d, bool bf16, bool parts,
+                      ringx::DropCut* cut) {
+  constexpr int64_t kMost = (int64_t(1) << 23) - 1;
+  *cut = ringx::DropCut{};
+  if (!bf16) return RINGX_OK;
+  if (ringx::drop_bwd_workgroups(*cut, BHkv, BH, Nq, Nk) > kMost) return RINGX_E_SHAPE;
+  *cut = ringx::drop_cut(BHkv, BH, Nq, Nk, d, parts);
+  return ringx::drop_bwd_workgroups(*cut, BHkv, BH, Nq, Nk) > kMost ? RINGX_E_SHAPE : RINGX_OK;
+}
+
 // The stages after the preprocess.  parts: room for those of a cut.
 hipError_t launch_bwd_drop(const ringx::BwdArgs& a, bool bf16, const ringx::Drop& drop,
                            const ringx::DropCut& cut, float* parts) {
@@ -881,8 +893,9 @@ size_t ringx_bwd_drop_workspace_bytes(int64_t B, int64_t H, int64_t Hkv, int64_t
                                       int64_t d, ringx_dtype dtype) {
   if (Hkv < 1 || H < 1 || H % Hkv != 0) return 0;
   const size_t stats = ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, 1, dtype);
-  if (stats == 0 || dtype != RINGX_BF16) return stats;
-  const ringx::DropCut cut = ringx::drop_cut(B * Hkv, B * H, Nq, Nk, d, true);
+  ringx::DropCut cut;
+  if (stats == 0 || make_cut(B * Hkv, B * H, Nq, Nk, d, dtype == RINGX_BF16, true, &cut) != RINGX_OK)
+    return 0;
   return bwd_drop_bytes(stats, drop_parts(cut, B * Hkv, B * H, Nq, Nk, d));
 }
 
@@ -900,8 +913,9 @@ ringx_status ringx_attn_bwd_drop(const void* q, const void* k, const void* v, co
   st = make_drop(p, rng, q0, key0, Nq, Nk, &drop);
   if (st != RINGX_OK) return st;
   const bool bf16 = dtype == RINGX_BF16;
-  const ringx::DropCut cut =
-      bf16 ? ringx::drop_cut(B * Hkv, B * H, Nq, Nk, d, true) : ringx::DropCut{};
+  ringx::DropCut cut;
+  st = make_cut(B * Hkv, B * H, Nq, Nk, d, bf16, true, &cut);
+  if (st != RINGX_OK) return st;
   const size_t stats = ringx_bwd_workspace_bytes(B, H, Nq, Nk, d, 1, dtype);
   const size_t need = bwd_drop_bytes(stats, drop_parts(cut, B * Hkv, B * H, Nq, Nk, d));
   if (!workspace || workspace_bytes < need) return RINGX_E_WORKSPACE;
@@ -949,15 +963,16 @@ ringx_status ringx_attn_bwd_step_drop(const void* q, const void* k, const void* 
   if (st != RINGX_OK) return st;
   for (const Span& o : outs)
     if (overlap(o, span(rng, 16))) return RINGX_E_ALIAS;
+  const bool bf16 = dtype == RINGX_BF16;
+  ringx::DropCut cut;   // without a workspace there is no room for parts
+  st = make_cut(bh, bh, Nq, Nk, d, bf16, false, &cut);
+  if (st != RINGX_OK) return st;
   ringx::BwdArgs a;
   a.q = q, a.k = k, a.v = v, a.dout = dout, a.lse = lse, a.delta = const_cast<float*>(delta);
   a.nl = const_cast<float*>(delta) + bh * Nq;
   a.dq = dq_acc, a.dk = dk, a.dv = dv;
   a.BH = bh, a.Nq = Nq, a.Nk = Nk, a.d = d, a.R = 1, a.scale = scale, a.H = H, a.G = 1;
   a.accumulate_dkv = accumulate_dkv != 0, a.accumulate_dq = accumulate_dq != 0, a.stream = stream;
-  const bool bf16 = dtype == RINGX_BF16;
-  // without a workspace there is no room for parts
-  const ringx::DropCut cut = bf16 ? ringx::drop_cut(bh, bh, Nq, Nk, d, false) : ringx::DropCut{};
   return hip_status(launch_bwd_drop(a, bf16, drop, cut, nullptr));
 }
 

@@ -231,6 +231,10 @@ struct DropCut {
   int ks = 1;         // a dQ workgroup takes 256 / ks queries
   int kv = 1, q = 1;  // parts of at least 256 query rows (128 of a head, a tile) and of 512 keys
 };
+// Workgroups of its one launch: dK/dV's, each of 128 keys of a K/V head, and dQ's.
+inline int64_t drop_bwd_workgroups(const DropCut& c, int64_t BHkv, int64_t BH, int64_t Nq, int64_t Nk) {
+  return (Nk + 127) / 128 * BHkv * c.kv + (Nq + 256 / c.ks - 1) / (256 / c.ks) * BH * c.q;
+}
 // The cut with the shortest time by this model.  A dK/dV workgroup takes `row` us for every query row that it
 // sweeps, a dQ workgroup `key` us for every key of a stream, each 4 besides, where 256 of them run; fewer at
 // a time run 0.85 as long (a higher clock).  The launch lasts as long as its whole work does on 256 CUs,

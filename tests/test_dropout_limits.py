@@ -1,0 +1,28 @@
+"""Limits of the dropout entry points, on the host (pointers are never dereferenced)."""
+
+import pytest
+
+from paper_2507_16697_amd import ringx
+
+from test_dropout_host import BF16, SHAPE, WORKSPACE, bstep, bwd, needs_lib
+
+LAUNCH = 1 << 23      # workgroups of 512 threads: a launch has fewer than 2^32 threads
+
+
+@needs_lib
+@pytest.mark.parametrize("d", [64, 128])
+def test_backward_is_refused_where_one_launch_cannot_take_it(d):
+    """dK/dV's workgroups (128 keys of a K/V head) and dQ's (256 queries of a head) share a launch.  What fits
+    goes on to the next check, here that of the workspace."""
+    size = ringx.ringx_bwd_drop_workspace_bytes
+    half = LAUNCH // 2
+    for n, Hkv, H, Nq, Nk in ((LAUNCH, half, half, 1, 1), (LAUNCH - 2, half - 1, half - 1, 1, 1),
+                              (LAUNCH, 1, LAUNCH - 1, 1, 1), (LAUNCH - 1, 1, LAUNCH - 2, 1, 1),
+                              (LAUNCH, 4, half - 4, 257, 256)):
+        assert Hkv * ((Nk + 127) // 128) + H * ((Nq + 255) // 256) == n
+        got = bwd(B=1, H=H, Hkv=Hkv, Nq=Nq, Nk=Nk, d=d, wsb=16)
+        assert got == (SHAPE if n >= LAUNCH else WORKSPACE), (n, Hkv, H)
+        assert (size(1, H, Hkv, Nq, Nk, d, BF16) == 0) == (n >= LAUNCH)
+    assert bstep(B=2, H=LAUNCH // 4, Nq=1, Nk=1, d=d) == SHAPE
+    # far beyond: no time is spent on how such a launch would be cut
+    assert bwd(B=1, H=1 << 30, Hkv=1 << 30, Nq=1, Nk=1, d=d, wsb=16) == SHAPE
