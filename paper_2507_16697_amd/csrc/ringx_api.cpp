@@ -87,8 +87,8 @@ const char* ringx_status_str(int status) {
       return "B * H * Nq exceeds the fixed scratch of ringx_attn_bwd_noalloc "
              "(RINGX_NOALLOC_MAX_ROWS rows)";
     case RINGX_E_DROPOUT:
-      return "dropout rate not in {0} or [1/512, 511/512], or mask position out of range or not a "
-             "multiple of 32 keys";
+      return "dropout rate neither 0 nor between 1/512 and 511/512 (both excluded), or mask position out of "
+             "range or not a multiple of 32 keys";
     case RINGX_E_ROPE: return "invalid rotated sections, strides, position or eps";
   }
   return "unknown status";
