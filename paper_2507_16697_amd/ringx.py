@@ -232,8 +232,6 @@ def _new(shape, dtype, like):
 
 def _elsewhere(stream, like):
     """`stream` as a torch stream where it is not the current one of like's device, else None."""
-    if stream is None:
-        return None
     cuda, handle = _T.cuda, _stream(stream)
     if handle == (_raw_stream(like.device.index) if _raw_stream is not None
                   else cuda.current_stream(like.device).cuda_stream):
@@ -246,7 +244,7 @@ def _workspace(workspace, need, like, stream):
     with its kernels still to run: it is memory of the stream that they run on, which goes to later work
     of that stream alone."""
     if workspace is None:
-        other = _elsewhere(stream, like)
+        other = None if stream is None else _elsewhere(stream, like)
         if other is None:
             return _new(max(need, 16), _T.uint8, like)
         with _T.cuda.stream(other):
@@ -271,7 +269,7 @@ def _made_for(other, like, make):
 def _out(name, t, shape, dtype, like, stream=None):
     """The caller's output buffer, checked, or a new one on `like`'s device."""
     if t is None:
-        other = _elsewhere(stream, like)
+        other = None if stream is None else _elsewhere(stream, like)
         if other is not None:
             return _made_for(other, like, lambda: _new(shape, dtype, like))
         return _new(shape, dtype, like)
@@ -283,7 +281,7 @@ def _out(name, t, shape, dtype, like, stream=None):
 def _out_like(name, t, like, stream=None):
     """The caller's output buffer, checked, or a new one, of `like`'s shape and type."""
     if t is None:
-        other = _elsewhere(stream, like)
+        other = None if stream is None else _elsewhere(stream, like)
         if other is not None:
             return _made_for(other, like, lambda: _T.empty_like(like))
         return _T.empty_like(like)
@@ -294,7 +292,7 @@ def _grad_out(name, t, shape, like, accumulate, stream=None):
     """An fp32 gradient buffer that the call overwrites, or adds to (then a new one starts at 0, on the
     stream that adds)."""
     if t is None and accumulate:
-        other = _elsewhere(stream, like)
+        other = None if stream is None else _elsewhere(stream, like)
         if other is not None:
             return _made_for(other, like, lambda: _new(shape, _T.float32, like).zero_())
         return _new(shape, _T.float32, like).zero_()
