@@ -328,6 +328,7 @@ ringx_status ringx_attn_bwd_gqa(const void* q, const void* k, const void* v, con
  * Mask: Philox4x32 with 7 rounds (Salmon et al., SC'11), key = the seed's low and high 32 bits, counter
  * = (2 J + h, q0 + i, b H + head, offset).  Byte e of result word m is that of key 32 J + 8 m + 4 h + e
  * (m, e < 4; h < 2; J counts 32-key blocks of the key axis); the score is kept iff it is >= T.
+ * Heads count within the call: ranks that hold parts of the batch or of the heads take seeds of their own.
  * Everything else as ringx_attn_fwd_gqa and ringx_attn_bwd_gqa (Hkv = H for multi-head attention),
  * whose chunk count has no part here: keys are visited in blocks of 32 from the first, and p = 0 gives
  * their results to rounding.
@@ -391,7 +392,8 @@ ringx_status ringx_bwd_preprocess_drop(const void* out, const void* dout, const 
  *         section of n = rot[a] / 2 pairs from dim o on, dims o + i and o + n + i become
  *           y_{o+i} cos t - y_{o+n+i} sin t  and  y_{o+n+i} cos t + y_{o+i} sin t,
  *         t = position_a f_i; the dims after the sections are left as they are.  freqs: the f_i in
- *         radians of all sections, one after the other, fp64.  Angles are formed in 64 bits.
+ *         radians of all sections, one after the other, fp64.  Angles are formed in 64 bits; cos t and
+ *         sin t of such an angle are at most 2.2e-7 off (its fraction of a turn is rounded to fp32).
  *   pos   [N, axes] int32 shared by the batch (pos_batch_stride = 0) or [B, N, axes]
  *         (pos_batch_stride = N axes); NULL with axes = 1: positions pos0 + n, |pos0| <= 2^40.
  *   v is copied.

@@ -379,7 +379,8 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 1 : NW == 4 ? 3 : QB == 1 ? 4 :
           pacc[b] = mfma32(*reinterpret_cast<const bf16x8*>(ot + at), bv, pacc[b]);
         }
       };
-      // P and -dS; (1 - p) times the definition's: D arrives so scaled, and a dropped score has dP = 0
+      // P and -dS; (1 - p) times the definition's: D arrives so scaled, and a dropped score has dP = 0.  Both
+      // are rounded to bf16 for their products, 2^-8 of each at most, as without dropout.
       auto weights = [&](int b) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {

@@ -266,7 +266,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void bwd_dq_kernel(
     const char* vbuf = lds_v;
     const int nvalid = (int)min<uint32_t>(C::kBK, ct.hi - ct.start);
 
-    // the mask's bytes, which need no score, beside the products
+    // The mask's bytes, which need no score.  Built, the compiler moves them past the branch of the ragged
+    // last tile, so that they stand with the exponentials and the dQ products, and the S and dP products
+    // have no vector work beside them.
     u32x4 dw[C::kKTiles];
     if constexpr (kDrop) {
 #pragma unroll
@@ -323,7 +325,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 3) void bwd_dq_kernel(
           const float p1 = fast_exp2(__builtin_fmaf(sacc[kt][r0 + 1], c2, nl));
           float g0 = pacc[kt][r0], g1 = pacc[kt][r0 + 1];
           if constexpr (kDrop) {
-            // (1 - p) times the definition's: D arrives so scaled, and a dropped score has dP = 0
+            // (1 - p) times the definition's: D arrives so scaled, and a dropped score has dP = 0.  dS is
+            // rounded to bf16 for its product, 2^-8 of each at most, as without dropout.
             g0 = __builtin_fmaf(g0, drop_weight(dw[kt], r0, dedge), -dq_d);
             g1 = __builtin_fmaf(g1, drop_weight(dw[kt], r0 + 1, dedge), -dq_d);
           }

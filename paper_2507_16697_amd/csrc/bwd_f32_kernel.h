@@ -132,7 +132,8 @@ __device__ __forceinline__ void dkdv_tile(const BwdF32Args& A, const F32Dims<NS,
     for (int r = 0; r < 4; ++r) {
       p[r] = expf(__builtin_fmaf(s[r], A.scale, -ls[r]));
       if constexpr (kDrop) {
-        // (1 - p) times the definition's: D arrives so scaled, and a dropped score has dP = 0
+        // (1 - p) times the definition's: D arrives so scaled, and a dropped score has dP = 0.  A lane holds
+        // one key, so it takes one byte of each call: 256 calls for a 16 x 16 tile, of which 32 differ.
         const uint32_t k16 = (uint32_t)key & 31u;
         const u32x4 w = drop_bytes(2 * (drop.kb0 + (uint32_t)(key >> 5)) + ((k16 >> 2) & 1),
                                    drop.q0 + (uint32_t)(i0 + 4 * D.g + r), (uint32_t)head, dkey);
@@ -221,6 +222,7 @@ __device__ __forceinline__ void dq_tile(const BwdF32Args& A, const F32Dims<NS, E
     for (int r = 0; r < 4; ++r) {
       float dpr = dp[r];
       if constexpr (kDrop) {
+        // the same call for all four keys of the lane, and again for the other 16 keys of the 32
         const uint32_t k4 = (uint32_t)(j0 >> 2) + D.g;
         const u32x4 w = drop_bytes(2 * (drop.kb0 + (k4 >> 3)) + (k4 & 1), drop.q0 + (uint32_t)qi,
                                    (uint32_t)bh, dkey);

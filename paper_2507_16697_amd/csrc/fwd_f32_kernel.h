@@ -125,7 +125,9 @@ __global__ __launch_bounds__(kThreads, 2) void RINGX_KERNEL(fwd_f32)(
           for (int i = 0; i < 4; ++i) s[b][i] = expf(__builtin_fmaf(s[b][i], scale, -ref));
           l += (s[b][0] + s[b][1]) + (s[b][2] + s[b][3]);
           if constexpr (kDrop) {
-            // the row sum is the softmax's; a dropped score is taken from the product with V alone
+            // the row sum is the softmax's; a dropped score is taken from the product with V alone.  Of
+            // a call's four words a lane takes one here; another lane of the query makes the same call for
+            // a second one, and both make it again for the other 16 keys of the 32.
             const uint32_t k4 = (uint32_t)((key + 16 * b) >> 2) + D.g;   // this lane's four keys / 4
             const u32x4 w = drop_bytes(2 * (drop.kb0 + (k4 >> 3)) + (k4 & 1),
                                        drop.q0 + (uint32_t)qi, (uint32_t)bh, dkey);

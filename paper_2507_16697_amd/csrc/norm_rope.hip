@@ -15,7 +15,9 @@
 // may lie in any lane of the row and comes through LDS.
 //
 // Angles are formed in 64 bits, as a fraction of a turn: in 32 bits a position of 5e5 would leave
-// 0.03 of a radian.
+// 0.03 of a radian.  The fraction, at most half a turn, is rounded to 32 bits (2^-26 of a turn, 9.4e-8 of a
+// radian) and its cosine and sine are the hardware's, two instructions (1.25e-7 off): fp32 rows are off by
+// 7.9e-8 rms of their size against 64 bits, by 6.9e-8 with cosines and sines in 64 bits throughout.
 
 #include "ringx_device.h"
 #include "ringx_kernels.h"

@@ -413,8 +413,9 @@ inline int rope_lanes(int64_t d, bool bf16) {
 }
 // Workgroups of 4 waves along tokens and along heads.  A token's heads are split only to fill the chip,
 // since every workgroup forms its tokens' angles: up to 1024 workgroups forward and, where each also
-// leaves a part of the weights' gradients, about 512 backward.  Measured (us; 256, 512, 1024, 2048; 16 heads
-// of 128, the last 16/4 of 64):
+// leaves a part of the weights' gradients, about 512 backward.  Measured in bf16 (us; 256, 512, 1024, 2048; 16
+// heads of 128, the last 16/4 of 64); fp32, whose kernels take fewer registers (56 to 70 forward against 100),
+// follows the same numbers unmeasured:
 //              512 tokens             2048                   8192                   2 x 4097
 //   forward    7.2 6.6 7.2 9.2        18.9 12.8 11.4 15.2    35.5 35.0 33.0 33.0    18.1 13.5 14.5 17.5
 //   backward   12.3 11.6 13.6 16.8    30.6 22.1 22.9 27.0    78.4 78.4 79.6 82.6    30.8 23.1 29.0 30.8
