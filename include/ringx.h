@@ -70,10 +70,20 @@ typedef enum ringx_status RINGX_ENUM_BASE {
   RINGX_E_ALIAS = 8,       /* an output overlaps an input                                    */
   RINGX_E_SCRATCH = 9,     /* B*H*Nq above RINGX_NOALLOC_MAX_ROWS (ringx_attn_bwd_noalloc)   */
   RINGX_E_DROPOUT = 10,    /* dropout rate or mask position out of range (the _drop entries) */
-  RINGX_E_ROPE = 11        /* rotated sections, strides, position or eps (ringx_qkv_norm_rope) */
+  RINGX_E_ROPE = 11,       /* rotated sections, strides, position or eps (ringx_qkv_norm_rope) */
+  RINGX_E_NORM = 12,       /* row length, row stride or eps out of range (ringx_layer_norm)  */
+  RINGX_E_LINEAR = 13      /* widths, row stride, heads or activation (ringx_linear)         */
 } ringx_status;
 
 typedef enum ringx_dtype RINGX_ENUM_BASE { RINGX_FP32 = 0, RINGX_BF16 = 1 } ringx_dtype;
+
+/* Activations of ringx_linear. */
+typedef enum ringx_act RINGX_ENUM_BASE {
+  RINGX_ACT_NONE = 0,
+  RINGX_ACT_GELU = 1,       /* z Phi(z), Phi the normal distribution                       */
+  RINGX_ACT_GELU_TANH = 2,  /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2           */
+  RINGX_ACT_SILU = 3        /* z / (1 + exp(-z))                                           */
+} ringx_act;
 
 /*
  * Ring-chunked forward with the Eq. (5) merge fused (Sec. III-A, Eqs. (1)-(5)).
@@ -430,6 +440,85 @@ ringx_status ringx_qkv_norm_rope_bwd(const void* qkv, int64_t batch_stride, int6
 /* Bytes of its workspace (0 if the arguments are invalid).  Host only. */
 size_t ringx_qkv_norm_rope_bwd_workspace_bytes(int64_t B, int64_t N, int64_t H, int64_t Hkv, int64_t d,
                                                ringx_dtype dtype);
+
+/*
+ * Layer norm over rows of C values, as in front of a block's projections:
+ *   mean = sum_c x_c / C;  r = (sum_c (x_c - mean)^2 / C + eps)^(-1/2);  y_c = (x_c - mean) r weight_c + bias_c.
+ *   x [rows, C] (dtype), row n at element n row_stride (not looked at for one row); a row is contiguous.
+ *   y [rows, C] (dtype), contiguous.  weight, bias [C] fp32, either or both NULL for 1 and 0.
+ *   stats [2, rows] fp32 or NULL: mean and r of every row, the backward's input.
+ * fp32 arithmetic, one rounding at the end; the squares' sum has to stay in fp32's range.
+ * RINGX_E_NORM unless 1 <= C <= 16384, row_stride >= C, eps >= 0 and finite.
+ */
+ringx_status ringx_layer_norm(const void* x, int64_t row_stride, const float* weight,
+                              const float* bias, void* y, float* stats, int64_t rows, int64_t C,
+                              float eps, ringx_dtype dtype, hipStream_t stream);
+
+/*
+ * Backward of ringx_layer_norm, with n = (x - mean) r from its stats and g = dy weight:
+ *   dx = r (g - mean_c(g) - n mean_c(g n)) + dres;  dweight = sum over rows of dy n;  dbias = that of dy.
+ *   dy [rows, C] (dtype), contiguous; dres the same or NULL: the gradient that reaches x by another
+ *   way (the residual of a pre-norm block), added before dx is rounded.
+ *   dx [rows, C] (dtype), contiguous; dweight, dbias [C] fp32, either or both NULL.  All overwritten,
+ *   bitwise reproducible.
+ *   workspace: ringx_layer_norm_bwd_workspace_bytes(...) bytes, 16-byte aligned, contents ignored; not
+ *   needed without dweight and dbias.
+ */
+ringx_status ringx_layer_norm_bwd(const void* x, int64_t row_stride, const void* dy, const void* dres,
+                                  const float* weight, const float* stats, void* dx, float* dweight,
+                                  float* dbias, int64_t rows, int64_t C, ringx_dtype dtype,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of its workspace (0 if the arguments are invalid).  Host only. */
+size_t ringx_layer_norm_bwd_workspace_bytes(int64_t rows, int64_t C, ringx_dtype dtype);
+
+/*
+ * Linear layer with its epilogue, the products around the attention (Table II: projections; and the
+ * MLP's):  z = x w^T + bias;  y = act(z) + residual.
+ *   x    M rows of K (dtype).  heads = 0: row m at element m x_stride (not looked at for one row), a row is
+ *        contiguous.  heads > 0: an attention's output [M / tokens, heads, tokens, K / heads], contiguous,
+ *        whose row (b, t) is the heads' values of token t side by side (x_stride is not looked at).
+ *   w    [O, K] (dtype), contiguous.  bias [O] fp32 or NULL.
+ *   residual [M, O] (dtype), contiguous, or NULL.
+ *   y    [M, O] (dtype), contiguous.
+ *   pre  [M, O] (dtype), contiguous, or NULL: z, rounded, what the backward needs with an activation.
+ * Products and sums in fp32 (bf16 on bf16 MFMA), one rounding at the end (the activation is that of the
+ * unrounded z).  Any M, K and O, odd ones too.  A launch's split follows its sizes alone: repeated calls are
+ * bitwise identical.
+ *   workspace: ringx_linear_workspace_bytes(...) bytes (0 for many shapes), 16-byte aligned, contents ignored:
+ *   parts of products whose rows and features are few, operands whose rows do not come in 16-byte pieces.
+ * RINGX_E_LINEAR unless 1 <= K, O <= 2^20, M < 2^31, x_stride >= K (heads = 0), heads divides K and tokens
+ * M (heads > 0), and act is one of ringx_act.
+ */
+ringx_status ringx_linear(const void* x, int64_t x_stride, int64_t heads, int64_t tokens,
+                          const void* w, const float* bias, const void* residual, void* y, void* pre,
+                          int64_t M, int64_t K, int64_t O, ringx_act act, ringx_dtype dtype,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of its workspace (0 if none is needed, and if the arguments are invalid).  Host only. */
+size_t ringx_linear_workspace_bytes(int64_t x_stride, int64_t heads, int64_t tokens, int64_t M,
+                                    int64_t K, int64_t O, ringx_dtype dtype);
+
+/*
+ * Backward of ringx_linear:  dz = dy act'(pre);  dx = dz w;  dw = dz^T x;  dbias = sum over rows of dz.
+ * (The residual's gradient is dy.)
+ *   dy [M, O] (dtype), contiguous; pre [M, O] as the forward left it, NULL iff act is RINGX_ACT_NONE.
+ *   dx (dtype) or NULL: [M, K] contiguous, or the attention's layout where x has it (heads > 0).
+ *   dw [O, K] or NULL: in dw_dtype (fp32, or dtype); dbias [O] fp32 or NULL.
+ *   accumulate_dw != 0: dw and dbias are added to (dw_dtype fp32 alone, RINGX_E_UNSUPPORTED otherwise).
+ * dz is rounded to dtype for the products (the bias's gradient is that of the unrounded dz); products and
+ * sums in fp32.  Bitwise reproducible.  RINGX_E_NULLPTR unless one of dx, dw, dbias is given.
+ *   workspace: ringx_linear_bwd_workspace_bytes(...) bytes, 16-byte aligned, contents ignored.
+ */
+ringx_status ringx_linear_bwd(const void* x, int64_t x_stride, int64_t heads, int64_t tokens,
+                              const void* w, const void* dy, const void* pre, void* dx, void* dw,
+                              float* dbias, int64_t M, int64_t K, int64_t O, ringx_act act,
+                              ringx_dtype dtype, ringx_dtype dw_dtype, int accumulate_dw,
+                              void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of its workspace (0 if the arguments are invalid).  Host only. */
+size_t ringx_linear_bwd_workspace_bytes(int64_t x_stride, int64_t heads, int64_t tokens, int64_t M,
+                                        int64_t K, int64_t O, ringx_act act, ringx_dtype dtype);
 
 /*
  * One fidelity mode of the Turbulence Transformer's multi-fidelity input (Sec. III-B: the

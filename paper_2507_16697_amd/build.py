@@ -21,7 +21,8 @@ SOURCES = ["ringx_api.cpp", "fwd_bf16.hip", "fwd_f32.hip", "merge.hip", "bwd_pre
            "bwd_bf16.hip", "bwd_bf16_d64.hip", "bwd_dq_bf16.hip",
            "bwd_dq_bf16_d64.hip", "bwd_dq_ds.hip", "bwd_f32.hip", "tt_tokenize.hip",
            "fwd_drop_bf16.hip", "fwd_drop_f32.hip", "bwd_drop_bf16.hip",
-           "bwd_drop_f32.hip", "norm_rope.hip"]
+           "bwd_drop_f32.hip", "norm_rope.hip", "layer_norm.hip", "linear.hip", "gemm_bf16.hip",
+           "gemm_f32.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

@@ -1,0 +1,320 @@
+// Matrix products of the linear layer in bf16 with fp32 accumulation (gfx950):
+//   out[i][j] = sum over r of P(i, r) Q(j, r), then the epilogue of linear.h.
+// Forward: P = x, Q = w.  dx: P = dz, Q = w read along its rows.  dw: P = dz, Q = x, both read along
+// their rows.
+//
+// A workgroup makes a TI x TJ tile of out.  Operands go through LDS in steps of 64 along r, two buffers
+// filled by direct global->LDS loads: while one step is multiplied, the next one is in flight.  An operand
+// that is stored with r along its rows (contiguous) is a tile of W rows x 64; one stored the other way
+// (slow: r is the row) a tile of 64 rows x W, whose fragments come from transposed LDS reads.  16-byte
+// pieces of a row are XOR-swizzled by the row so that neither kind of read meets itself in a bank:
+// contiguous tiles, 128 bytes a row, by (row / 2) mod 8 (16 lanes read one piece of 16 rows); slow tiles by
+// 4 (row mod 4) + (row / 4) mod 4 (16 lanes read 32 bytes of 4 rows).
+//
+// All loads are buffer loads from the tile's place on: what lies past the tensor's end reads as zero, and
+// so do the pieces past R in the last step, whose offsets are moved outside.  Rows of i or j past the
+// end repeat the last one (contiguous) or are what follows (slow): they reach only values that are not
+// stored.
+//
+// v_mfma_f32_32x32x16_bf16 with Q as its first operand: a lane holds one row i and four neighbouring j at a
+// time.  The waves pass their values through LDS, 32 rows of i at a time, so that the epilogue has 8
+// neighbouring j of one row in a lane: 16-byte loads and stores, 128 bytes of a row in a piece.
+
+#include "linear.h"
+
+namespace ringx {
+namespace {
+
+typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+
+constexpr uint32_t kOutside = 0x80000000u;   // a byte offset past any buffer here
+constexpr uint32_t kMostBytes = 0x7ffffff0u;
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// One 16-byte direct buffer->LDS load per lane; LDS destination lds_base + 16 lane.  Volatile asm for the
+// same reasons as the global form in ringx_device.h.
+__device__ __forceinline__ void buffer_lds16(const u32x4& rsrc, uint32_t off, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :
+               : "s"(lds_base), "v"(off), "s"(rsrc)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+  return reinterpret_cast<int64_t>(uniform_ptr(reinterpret_cast<const void*>(x)));
+}
+
+// One operand's way into LDS, 64 of r at a time.
+template <bool SLOW, int W, int THREADS>
+struct Feed {
+  static constexpr int kLoads = W * 128 / (THREADS * 16);
+  static constexpr int kRowChunks = SLOW ? W / 8 : 8;
+  static_assert(kLoads * THREADS * 16 == W * 128 && (!SLOW || W >= 128), "whole rounds of loads");
+  uint32_t off[kLoads];
+  int64_t base, left;    // address of the step's first row or column; bytes from it to the tensor's end
+  int64_t step, turn;    // bytes to the next step; what is added where a head (or batch) ends
+  int in, per;           // steps left in this head (or batch), steps of one (0: there are none)
+  int chunk;             // contiguous: the lane's first r of a step / 8
+
+  static __device__ __forceinline__ int swz(int row) {
+    return SLOW ? ((row & 3) << 2) | ((row >> 2) & 3) : (row >> 1) & 7;
+  }
+
+  // width index w0 and r0 (a multiple of 64) on
+  __device__ __forceinline__ void start(const GemmIn& x, int64_t w0, int64_t r0, int tid) {
+    const int64_t total = x.heads ? x.rows * x.cols : (x.rows - 1) * x.ld + x.cols;
+    int64_t at;   // elements from the tensor's start
+    turn = 0, per = 0, in = 0;
+    if constexpr (!SLOW) {
+      if (x.heads) {
+        const int64_t b = w0 / x.tokens;
+        const int hd = (int)(x.d / 64), s = (int)(r0 / 64);
+        at = b * x.tokens * x.cols + s / hd * x.tokens * x.d + s % hd * 64;
+        step = 128, per = hd, in = hd - s % hd;
+        turn = (x.tokens * x.d - x.d) * 2;
+      } else {
+        at = w0 * x.ld + r0;
+        step = 128;
+      }
+    } else if (x.heads) {
+      const int64_t b = r0 / x.tokens, t = r0 % x.tokens;
+      at = b * x.tokens * x.cols + t * x.d;
+      step = 128 * x.d, per = (int)(x.tokens / 64), in = (int)((x.tokens - t) / 64);
+      turn = (x.cols - x.d) * x.tokens * 2;
+    } else {
+      at = r0 * x.ld + w0;
+      step = 128 * x.ld;
+    }
+    base = uniform64(reinterpret_cast<int64_t>(x.p) + 2 * at);
+    left = uniform64(2 * (total - at));
+    chunk = 0;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int slot = u * THREADS + tid;
+      const int row = slot / kRowChunks;
+      const int c = (slot % kRowChunks) ^ swz(row);
+      if constexpr (!SLOW) {
+        chunk = c;   // the same for every u: rounds are whole multiples of 16 rows
+        const int64_t i = min(w0 + row, x.rows - 1);
+        int64_t o = (i - w0) * x.ld;
+        if (x.heads) {
+          const uint32_t b0 = (uint32_t)w0 / (uint32_t)x.tokens, b = (uint32_t)i / (uint32_t)x.tokens;
+          o = (int64_t)(b - b0) * x.tokens * x.cols + (i - (int64_t)b * x.tokens) * x.d;
+        }
+        off[u] = (uint32_t)(2 * o) + c * 16;
+      } else {
+        int64_t o = row * x.ld + c * 8;
+        if (x.heads) {
+          const uint32_t col = (uint32_t)min(w0 + c * 8, x.cols - 8);
+          const uint32_t h = col / (uint32_t)x.d;
+          o = h * x.tokens * x.d + (col - h * (uint32_t)x.d) + row * x.d;
+        }
+        off[u] = (uint32_t)(2 * o);
+      }
+    }
+  }
+  __device__ __forceinline__ u32x4 rsrc() const {
+    const uint32_t n = left <= 0 ? 0u : left > (int64_t)kMostBytes ? kMostBytes : (uint32_t)left;
+    return u32x4{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, n, 0x00020000u};
+  }
+  __device__ __forceinline__ void next() {
+    int64_t s = step;
+    if (per && --in == 0) s += turn, in = per;
+    base += s, left -= s;
+  }
+  // the step whose first r has `rest` of them left, then on to the next; dst: the wave's place
+  __device__ __forceinline__ void issue(uint32_t dst, int64_t rest) {
+    const u32x4 d = rsrc();
+    if (SLOW || rest >= 64) {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) buffer_lds16(d, off[u], dst + u * THREADS * 16);
+    } else {
+      cold_path();
+      const bool inside = chunk * 8 < (int)rest;
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u)
+        buffer_lds16(d, inside ? off[u] : kOutside, dst + u * THREADS * 16);
+    }
+    next();
+  }
+};
+
+// Fragments of 32 of the width x 16 of r: lane l has width index l % 32 and r = 8 (l / 32) .. + 7.
+template <bool SLOW, int W, int BLOCKS>
+struct Frags {
+  int off[SLOW ? 2 : 4][SLOW ? BLOCKS : 1];
+  __device__ __forceinline__ void start(int w0, int lane) {   // w0: the wave's first of the tile
+    const int n = lane & 31, g = lane >> 5;
+    if constexpr (!SLOW) {
+      const int row = w0 + n;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) off[s][0] = row * 128 + (((2 * s + g) ^ ((row >> 1) & 7)) << 4);
+    } else {
+      const int rr = (lane & 15) >> 2;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) {
+          const int row = 8 * g + 4 * h + rr;
+          const int col = w0 + 32 * b + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+          off[h][b] = row * (2 * W) + (((col >> 3) ^ Feed<true, W, W * 8>::swz(row)) << 4) + (col & 7) * 2;
+        }
+    }
+  }
+  __device__ __forceinline__ bf16x8 get(const char* tile, int s, int b) const {
+    if constexpr (!SLOW) {
+      return *reinterpret_cast<const bf16x8*>(tile + off[s][0] + b * 32 * 128);
+    } else {
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+          (lds_bf16x4*)(tile + off[0][b] + s * 16 * 2 * W));
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+          (lds_bf16x4*)(tile + off[1][b] + s * 16 * 2 * W));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+};
+
+template <int TI, int TJ, int WI, int WJ>
+struct Tile {
+  static constexpr int kThreads = 64 * WI * WJ;
+  static constexpr int kBI = TI / WI / 32, kBJ = TJ / WJ / 32;
+  static constexpr int kP = TI * 128, kStage = (TI + TJ) * 128;   // bytes
+  static constexpr int kPitch = 32 * kBJ + 4;                     // floats of a staged row
+  static_assert(WI * WJ * 32 * kPitch * 4 <= 2 * kStage, "staging fits");
+};
+
+template <bool PS, bool QS, int TI, int TJ, int WI, int WJ>
+__global__ __launch_bounds__(64 * WI * WJ, 512 / (64 * WI * WJ) < 2 ? 2 : 2) void gemm_bf16_kernel(
+    GemmArgs a) {
+  using C = Tile<TI, TJ, WI, WJ>;
+  __shared__ __attribute__((aligned(1024))) char lds[2 * C::kStage];
+  const uint32_t lbase = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  // the workgroup's tile: tiles in groups of 4 along i, so that those at work on one XCD share operands
+  constexpr uint32_t kGroup = 4;
+  const uint32_t ti = (uint32_t)((a.I + TI - 1) / TI), tj = (uint32_t)((a.J + TJ - 1) / TJ);
+  uint32_t id = xcd_remap(blockIdx.x, gridDim.x);
+  const uint32_t split = id / (ti * tj);
+  id -= split * ti * tj;
+  const uint32_t g0 = id / (kGroup * tj) * kGroup, gn = min(kGroup, ti - g0);
+  id -= g0 * tj;
+  const int64_t i0 = (int64_t)(g0 + id % gn) * TI, j0 = (int64_t)(id / gn) * TJ;
+
+  const int64_t steps = (a.R + 63) / 64;
+  const int64_t s0 = steps * split / a.splits, s1 = steps * (split + 1) / a.splits;
+  Feed<PS, TI, C::kThreads> fp;
+  Feed<QS, TJ, C::kThreads> fq;
+  fp.start(a.P, i0, 64 * s0, tid);
+  fq.start(a.Q, j0, 64 * s0, tid);
+  const int wi = wave / WJ, wj = wave % WJ;
+  Frags<PS, TI, C::kBI> rp;
+  Frags<QS, TJ, C::kBJ> rq;
+  rp.start(wi * 32 * C::kBI, lane);
+  rq.start(wj * 32 * C::kBJ, lane);
+  const uint32_t wdst = (uint32_t)__builtin_amdgcn_readfirstlane(lbase + wave * 1024);
+
+  f32x16 acc[C::kBI][C::kBJ];
+#pragma unroll
+  for (int i = 0; i < C::kBI; ++i)
+#pragma unroll
+    for (int j = 0; j < C::kBJ; ++j) acc[i][j] = f32x16{};
+
+  int64_t rest = a.R - 64 * s0;   // of r, from the step to load on
+  if (s0 < s1) {
+    fp.issue(wdst, rest);
+    fq.issue(wdst + C::kP, rest);
+  }
+  wait_vmem_all();
+  __syncthreads();
+  int buf = 0;
+  for (int64_t s = s0; s < s1; ++s) {
+    rest -= 64;
+    if (s + 1 < s1) {
+      const uint32_t dst = wdst + (buf ^ 1) * C::kStage;
+      fp.issue(dst, rest);
+      fq.issue(dst + C::kP, rest);
+    }
+    const char* const tp = lds + buf * C::kStage;
+    const char* const tq = tp + C::kP;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      bf16x8 p[C::kBI], q[C::kBJ];
+#pragma unroll
+      for (int j = 0; j < C::kBJ; ++j) q[j] = rq.get(tq, k, j);
+#pragma unroll
+      for (int i = 0; i < C::kBI; ++i) p[i] = rp.get(tp, k, i);
+#pragma unroll
+      for (int i = 0; i < C::kBI; ++i)
+#pragma unroll
+        for (int j = 0; j < C::kBJ; ++j) acc[i][j] = mfma32(q[j], p[i], acc[i][j]);
+    }
+    wait_vmem_all();
+    __syncthreads();
+    buf ^= 1;
+  }
+
+  // epilogue, 32 rows of i at a time, in the wave's own part of LDS
+  GemmOut o = a.o;
+  float* const stage = reinterpret_cast<float*>(lds) + wave * 32 * C::kPitch;
+  constexpr int kPer = 4 * C::kBJ, kRows = 64 / kPer;   // lanes of a row, rows at a time
+  const int jc = lane % kPer * 8;
+  const int64_t j = j0 + wj * 32 * C::kBJ + jc;
+  const int inside = (int)max((int64_t)0, min((int64_t)8, a.J - j));
+  const bool vec = a.J % 8 == 0 && o.d % 8 == 0;
+  if (a.splits > 1) {
+    o = GemmOut{};
+    o.out = a.part + split * a.I * a.J, o.J = a.J, o.f32 = true;
+  }
+  float bias[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) bias[e] = o.bias && e < inside ? o.bias[j + e] : 0.f;
+#pragma unroll
+  for (int bi = 0; bi < C::kBI; ++bi) {
+#pragma unroll
+    for (int bj = 0; bj < C::kBJ; ++bj)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<f32x4*>(stage + (lane & 31) * C::kPitch + 32 * bj + 8 * r + 4 * (lane >> 5)) =
+            f32x4{acc[bi][bj][4 * r], acc[bi][bj][4 * r + 1], acc[bi][bj][4 * r + 2], acc[bi][bj][4 * r + 3]};
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int it = 0; it < 32 / kRows; ++it) {
+      const int row = it * kRows + lane / kPer;
+      const int64_t i = i0 + (wi * C::kBI + bi) * 32 + row;
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(stage + row * C::kPitch + jc);
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(stage + row * C::kPitch + jc + 4);
+      float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      if (i < a.I && inside > 0) {
+        if (vec) finish<8, true, __bf16>(o, i, j, 8, bias, x);
+        else finish<8, false, __bf16>(o, i, j, inside, bias, x);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+template <bool PS, bool QS, int TI, int TJ, int WI, int WJ>
+hipError_t launch(const GemmArgs& a) {
+  const int64_t tiles = ((a.I + TI - 1) / TI) * ((a.J + TJ - 1) / TJ) * a.splits;
+  hipLaunchKernelGGL((gemm_bf16_kernel<PS, QS, TI, TJ, WI, WJ>), dim3((uint32_t)tiles),
+                     dim3(64 * WI * WJ), 0, a.stream, a);
+  return hipGetLastError();
+}
+
+template <int TI, int TJ, int WI, int WJ>
+hipError_t by_layout(const GemmArgs& a) {
+  if (a.p_slow) return launch<true, true, TI, TJ, WI, WJ>(a);
+  return a.q_slow ? launch<false, true, TI, TJ, WI, WJ>(a) : launch<false, false, TI, TJ, WI, WJ>(a);
+}
+
+}  // namespace
+
+hipError_t launch_gemm_bf16(const GemmArgs& a) {
+  return gemm_bf16_large(a.I, a.J) ? by_layout<256, 256, 2, 4>(a) : by_layout<128, 128, 2, 2>(a);
+}
+
+}  // namespace ringx

@@ -1,0 +1,308 @@
+// Layer norm over the last dimension, forward and backward.
+//
+// Row x of C values: mean = sum x / C, r = (sum (x - mean)^2 / C + eps)^(-1/2), n = (x - mean) r,
+// y = n w + b.  Backward, g = dy w:
+//   dx = r (g - sum g / C - n sum(g n) / C) (+ dres),   dw = sum over rows of dy n,   db = sum of dy.
+//
+// Bound by HBM: x is read and y written once, backward x, dy and dres are read and dx written once.  A row
+// is held in registers by TPR threads, E values each, from its load to its store, so that the squares
+// are those of the differences from the mean (a second sum of the differences takes back the rounding of
+// the first mean).  Threads keep their columns for all rows that they take: weights are loaded once, and
+// the weights' gradients add up in registers until the workgroup writes one row of parts at its end.
+
+#include "ringx_device.h"
+#include "ringx_kernels.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace ringx {
+namespace {
+
+// The E values of a row that one thread holds: 16-byte pieces (VEC), piece v at columns (v TPR + t) V, or
+// one by one, value e at column e TPR + t.  Columns past C are zero.
+template <class T, bool VEC, int E, int TPR>
+struct Row {
+  static constexpr int V = VEC ? 16 / (int)sizeof(T) : 1;
+  static constexpr int NV = E / V;
+  static constexpr int kWords = VEC ? E * (int)sizeof(T) / 4 : E;
+  uint32_t w[kWords];
+
+  static __device__ __forceinline__ int col(int e, int t) { return (e / V * TPR + t) * V + e % V; }
+
+  __device__ __forceinline__ void load(const T* p, int t, int C) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = col(v * V, t);
+      if constexpr (VEC) {
+        u32x4 x = {};
+        if (c < C) x = *reinterpret_cast<const u32x4*>(p + c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[4 * v + j] = x[j];
+      } else if constexpr (std::is_same_v<T, float>) {
+        w[v] = c < C ? __float_as_uint(p[c]) : 0u;
+      } else {
+        w[v] = c < C ? (uint32_t)__builtin_bit_cast(uint16_t, p[c]) << 16 : 0u;
+      }
+    }
+  }
+  __device__ __forceinline__ float get(int e) const {
+    if constexpr (!VEC || std::is_same_v<T, float>) return __uint_as_float(w[e]);
+    else return e % 2 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
+  }
+  static __device__ __forceinline__ void store(T* p, int t, int C, const float (&x)[E]) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = col(v * V, t);
+      if (c >= C) continue;
+      if constexpr (VEC) {
+        u32x4 y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (std::is_same_v<T, float>) y[j] = __float_as_uint(x[v * V + j]);
+          else y[j] = pack_bf16x2(x[v * V + 2 * j], x[v * V + 2 * j + 1]);
+        }
+        *reinterpret_cast<u32x4*>(p + c) = y;
+      } else {
+        p[c] = (T)x[v];
+      }
+    }
+  }
+};
+
+// fp32 weights of the thread's columns, `otherwise` where there are none
+template <class T, bool VEC, int E, int TPR>
+__device__ __forceinline__ void load_vector(const float* p, float otherwise, int t, int C,
+                                            float (&x)[E]) {
+  using R = Row<T, VEC, E, TPR>;
+#pragma unroll
+  for (int e = 0; e < E; e += 4) {
+    if constexpr (VEC) {
+      f32x4 y = {otherwise, otherwise, otherwise, otherwise};
+      if (p && R::col(e, t) < C) y = *reinterpret_cast<const f32x4*>(p + R::col(e, t));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[e + j] = y[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int c = R::col(e + j, t);
+        x[e + j] = p && c < C ? p[c] : otherwise;
+      }
+    }
+  }
+}
+
+template <int CTRL>
+__device__ __forceinline__ float add_lane(float x) {
+  return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+template <int N>
+__device__ __forceinline__ float lane_sum(float x) {   // over N <= 64 neighbouring lanes, in each
+  if constexpr (N >= 2) x = add_lane<0xB1>(x);     // lanes 1 0 3 2 of every four
+  if constexpr (N >= 4) x = add_lane<0x4E>(x);     // lanes 2 3 0 1
+  if constexpr (N >= 8) x = add_lane<0x141>(x);    // mirrored in eight: the other four
+  if constexpr (N >= 16) x = add_lane<0x140>(x);   // mirrored in sixteen: the other eight
+  if constexpr (N >= 32) x += __shfl_xor(x, 16, 64);
+  if constexpr (N >= 64) x = sum_halves(x);
+  return x;
+}
+
+// Sums of two values over the TPR threads of a row.  Rows of several waves go through LDS, `slot`
+// alternating, so that one barrier serves: a slot is written again two sums later, behind the next one's
+// barrier.
+template <int TPR>
+struct RowSum {
+  f32x2 lds[2][TPR > 64 ? TPR / 64 : 1];
+  __device__ __forceinline__ f32x2 operator()(float a, float b, int& slot) {
+    a = lane_sum<(TPR < 64 ? TPR : 64)>(a);
+    b = lane_sum<(TPR < 64 ? TPR : 64)>(b);
+    if constexpr (TPR > 64) {
+      if ((threadIdx.x & 63) == 0) lds[slot][threadIdx.x >> 6] = f32x2{a, b};
+      __syncthreads();
+      a = b = 0.f;
+#pragma unroll
+      for (int i = 0; i < TPR / 64; ++i) {
+        const f32x2 x = lds[slot][i];
+        a += x[0], b += x[1];
+      }
+      slot ^= 1;
+    }
+    return f32x2{a, b};
+  }
+};
+
+// Workgroups of TPR > 256 threads hold one row; TPR <= 64: 256 / TPR rows, and 128 and 256: one row too, in a
+// workgroup of TPR threads.
+template <int TPR>
+constexpr int kGroup = TPR <= 64 ? 256 : TPR;   // threads of a workgroup
+template <int TPR>
+constexpr int kRowsAtOnce = kGroup<TPR> / TPR;
+
+template <class T, bool VEC, int E, int TPR>
+__global__ __launch_bounds__(kGroup<TPR>) void layer_norm_kernel(NormArgs a) {
+  using R = Row<T, VEC, E, TPR>;
+  __shared__ RowSum<TPR> sum;
+  const int t = threadIdx.x % TPR;
+  const int C = a.C;
+  const float inv = 1.f / (float)C;
+  const int64_t step = (int64_t)gridDim.x * kRowsAtOnce<TPR>;
+  int64_t row = (int64_t)blockIdx.x * kRowsAtOnce<TPR> + threadIdx.x / TPR;
+  const T* const x = (const T*)a.x;
+  T* const y = (T*)a.y;
+  R cur;
+  // rows past the end (of the last round) repeat the last one and are not stored
+  cur.load(x + min(row, a.rows - 1) * a.stride, t, C);
+  float w[E], b[E];
+  load_vector<T, VEC, E, TPR>(a.weight, 1.f, t, C, w);
+  load_vector<T, VEC, E, TPR>(a.bias, 0.f, t, C, b);
+  int slot = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * kRowsAtOnce<TPR>; r0 < a.rows; r0 += step, row += step) {
+    R next;
+    if (r0 + step < a.rows) next.load(x + min(row + step, a.rows - 1) * a.stride, t, C);
+    float s = 0.f, d[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) s += cur.get(e);
+    float m0 = sum(s, 0.f, slot)[0] * inv;
+    asm("" : "+v"(m0));   // rounded here once: the differences and the mean below are from the same m0
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      d[e] = R::col(e, t) < C ? cur.get(e) - m0 : 0.f;
+      s1 += d[e];
+      s2 = __builtin_fmaf(d[e], d[e], s2);
+    }
+    const f32x2 ss = sum(s1, s2, slot);
+    const float m1 = ss[0] * inv;   // what m0 is off by
+    const float var = fmaxf(__builtin_fmaf(-m1, m1, ss[1] * inv), 0.f);
+    const float r = 1.f / sqrtf(var + a.eps);
+#pragma unroll
+    for (int e = 0; e < E; ++e) d[e] = __builtin_fmaf((d[e] - m1) * r, w[e], b[e]);
+    if (row < a.rows) {
+      R::store(y + row * C, t, C, d);
+      if (a.stats && t == 0) a.stats[row] = m0 + m1, a.stats[a.rows + row] = r;
+    }
+    cur = next;
+  }
+}
+
+template <class T, bool VEC, int E, int TPR>
+__global__ __launch_bounds__(kGroup<TPR>) void layer_norm_bwd_kernel(NormArgs a) {
+  using R = Row<T, VEC, E, TPR>;
+  constexpr int kWidth = E * TPR;
+  __shared__ RowSum<TPR> sum;
+  __shared__ float lds[TPR <= 64 ? 2 * kWidth : 1];
+  const int t = threadIdx.x % TPR;
+  const int C = a.C;
+  const float inv = 1.f / (float)C;
+  const int64_t step = (int64_t)gridDim.x * kRowsAtOnce<TPR>;
+  const T *const x = (const T*)a.x, *const dy = (const T*)a.dy, *const dres = (const T*)a.dres;
+  T* const dx = (T*)a.dx;
+  float w[E], dw[E], db[E];
+  load_vector<T, VEC, E, TPR>(a.weight, 1.f, t, C, w);
+#pragma unroll
+  for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.f;
+  int slot = 0;
+  for (int64_t r0 = (int64_t)blockIdx.x * kRowsAtOnce<TPR>; r0 < a.rows; r0 += step) {
+    const int64_t at = r0 + threadIdx.x / TPR;
+    const bool live = at < a.rows;
+    const int64_t row = live ? at : a.rows - 1;   // rows past the end repeat the last one
+    R rx, rg, rr;
+    rx.load(x + row * a.stride, t, C);
+    rg.load(dy + row * C, t, C);
+    if (dres) rr.load(dres + row * C, t, C);
+    const float mean = a.stats_in[row], r = a.stats_in[a.rows + row];
+    float n[E], g[E], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      n[e] = R::col(e, t) < C ? (rx.get(e) - mean) * r : 0.f;
+      g[e] = rg.get(e) * w[e];
+      s1 += g[e];
+      s2 = __builtin_fmaf(g[e], n[e], s2);
+      if (live) {
+        dw[e] = __builtin_fmaf(rg.get(e), n[e], dw[e]);
+        db[e] += rg.get(e);
+      }
+    }
+    const f32x2 ss = sum(s1, s2, slot);
+    const float m1 = ss[0] * inv, m2 = ss[1] * inv;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      g[e] = r * (g[e] - m1 - n[e] * m2);
+      if (dres) g[e] += rr.get(e);
+    }
+    if (live) R::store(dx + row * C, t, C, g);
+  }
+  if (!a.part) return;
+  float* const part = a.part + (int64_t)blockIdx.x * 2 * C;
+  if constexpr (TPR > 64) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int c = R::col(e, t);
+      if (c < C) part[c] = dw[e], part[C + c] = db[e];
+    }
+  } else {
+    // over the rows of a wave, then wave after wave
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int off = TPR; off < 64; off <<= 1) {
+        dw[e] += __shfl_xor(dw[e], off, 64);
+        db[e] += __shfl_xor(db[e], off, 64);
+      }
+    for (int i = 0; i < kGroup<TPR> / 64; ++i) {
+      if ((int)threadIdx.x / 64 == i && threadIdx.x % 64 < TPR) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          lds[e * TPR + t] = dw[e] + (i ? lds[e * TPR + t] : 0.f);
+          lds[kWidth + e * TPR + t] = db[e] + (i ? lds[kWidth + e * TPR + t] : 0.f);
+        }
+      }
+      __syncthreads();
+    }
+    for (int j = threadIdx.x; j < kWidth; j += kGroup<TPR>) {
+      const int c = R::col(j / TPR, j % TPR);
+      if (c < C) part[c] = lds[j], part[C + c] = lds[kWidth + j];
+    }
+  }
+}
+
+template <class T, bool VEC, int E, int TPR>
+hipError_t launch(const NormArgs& a, bool bwd) {
+  const int64_t groups = (a.rows + kRowsAtOnce<TPR> - 1) / kRowsAtOnce<TPR>;
+  const int64_t grid = std::min<int64_t>(groups, norm_workgroups(a.C, bwd));
+  if (!bwd) {
+    hipLaunchKernelGGL((layer_norm_kernel<T, VEC, E, TPR>), dim3((uint32_t)grid), dim3(kGroup<TPR>), 0,
+                       a.stream, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((layer_norm_bwd_kernel<T, VEC, E, TPR>), dim3((uint32_t)grid), dim3(kGroup<TPR>), 0,
+                     a.stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.part) return e;
+  ColumnSums s;
+  s.part = a.part, s.parts = (int)grid, s.cols = 2 * a.C, s.split = a.C;
+  s.out[0] = a.dweight, s.out[1] = a.dbias, s.stream = a.stream;
+  return launch_column_sums(s);
+}
+
+template <class T, bool VEC>
+hipError_t by_width(const NormArgs& a, bool bwd) {
+  if (a.C <= 64) return launch<T, VEC, 8, 8>(a, bwd);
+  if (a.C <= 128) return launch<T, VEC, 8, 16>(a, bwd);
+  if (a.C <= 256) return launch<T, VEC, 8, 32>(a, bwd);
+  if (a.C <= 512) return launch<T, VEC, 8, 64>(a, bwd);
+  if (a.C <= 1024) return launch<T, VEC, 16, 64>(a, bwd);
+  if (a.C <= 2048) return launch<T, VEC, 32, 64>(a, bwd);
+  if (a.C <= 4096) return launch<T, VEC, 32, 128>(a, bwd);
+  if (a.C <= 8192) return launch<T, VEC, 32, 256>(a, bwd);
+  return launch<T, VEC, 32, 512>(a, bwd);
+}
+
+}  // namespace
+
+hipError_t launch_layer_norm(const NormArgs& a, bool bwd) {
+  if (a.bf16) return a.vec ? by_width<__bf16, true>(a, bwd) : by_width<__bf16, false>(a, bwd);
+  return a.vec ? by_width<float, true>(a, bwd) : by_width<float, false>(a, bwd);
+}
+
+}  // namespace ringx

@@ -1,0 +1,161 @@
+// What the kernels of the linear layer share: the activations with their derivatives, and what becomes of a
+// product's values on their way out (bias, activation, residual, the layout).
+#pragma once
+
+#include "ringx.h"
+#include "ringx_device.h"
+#include "ringx_kernels.h"
+
+#include <type_traits>
+
+namespace ringx {
+
+// The standard normal distribution at z and its density's exponential e = exp(-z^2 / 2).  The error
+// function by Abramowitz and Stegun 7.1.26 (1.5e-7 off at most), whose exponential is the density's: the
+// lower tail comes as a product, without a difference.
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float x = fabsf(z) * 0.70710678118654752f;
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.f));
+  e = fast_exp2(-kLog2e * x * x);
+  float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
+  p = __builtin_fmaf(p, t, 1.421413741f);
+  p = __builtin_fmaf(p, t, -0.284496736f);
+  p = __builtin_fmaf(p, t, 0.254829592f);
+  const float tail = 0.5f * p * t * e;
+  return z < 0.f ? tail : 1.f - tail;
+}
+__device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.f + fast_exp2(-kLog2e * z));
+}
+
+constexpr float kTanhA = 1.5957691216057308f;   // 2 sqrt(2 / pi): (1 + tanh u) / 2 = sigmoid(2 u)
+constexpr float kTanhB = 0.044715f;
+
+__device__ __forceinline__ float activate(float z, int act) {
+  float e;
+  switch (act) {
+    case RINGX_ACT_GELU: return z * normal_cdf(z, e);
+    case RINGX_ACT_GELU_TANH: return z * sigmoid(kTanhA * z * __builtin_fmaf(kTanhB * z, z, 1.f));
+    case RINGX_ACT_SILU: return z * sigmoid(z);
+  }
+  return z;
+}
+
+__device__ __forceinline__ float activate_grad(float z, int act) {
+  switch (act) {
+    case RINGX_ACT_GELU: {
+      float e;
+      const float p = normal_cdf(z, e);
+      return __builtin_fmaf(z * 0.39894228040143268f, e, p);
+    }
+    case RINGX_ACT_GELU_TANH: {
+      const float g = sigmoid(kTanhA * z * __builtin_fmaf(kTanhB * z, z, 1.f));
+      const float y = fminf(fmaxf(z, -32.f), 32.f);   // g (1 - g) is 0 long before: no 0 times infinity
+      return __builtin_fmaf(y * g * (1.f - g), kTanhA * __builtin_fmaf(3.f * kTanhB * y, y, 1.f), g);
+    }
+    case RINGX_ACT_SILU: {
+      const float g = sigmoid(z);
+      return g * __builtin_fmaf(z, 1.f - g, 1.f);
+    }
+  }
+  return 1.f;
+}
+
+// N neighbouring values from p on, as fp32: N values' 8- or 16-byte pieces (VEC), else the first `n`.
+template <int N, bool VEC, class T>
+__device__ __forceinline__ void load_values(const T* p, int n, float (&x)[N]) {
+  if constexpr (VEC) {
+    constexpr int kWords = N * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+    if constexpr (kWords % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < kWords / 4; ++i) {
+        const u32x4 y = reinterpret_cast<const u32x4*>(p)[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[4 * i + j] = y[j];
+      }
+    } else {
+      const u32x2 y = *reinterpret_cast<const u32x2*>(p);
+      w[0] = y[0], w[1] = y[1];
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if constexpr (std::is_same_v<T, float>) x[j] = __uint_as_float(w[j]);
+      else x[j] = j % 2 ? bf16_hi(w[j / 2]) : bf16_lo(w[j / 2]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = j < n ? (float)p[j] : 0.f;
+  }
+}
+template <int N, bool VEC, class T>
+__device__ __forceinline__ void store_values(T* p, int n, const float (&x)[N]) {
+  if constexpr (VEC) {
+    constexpr int kWords = N * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) {
+      if constexpr (std::is_same_v<T, float>) w[j] = __float_as_uint(x[j]);
+      else w[j] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
+    }
+    if constexpr (kWords % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < kWords / 4; ++i)
+        reinterpret_cast<u32x4*>(p)[i] = u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
+    } else {
+      *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[1]};
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j < n) p[j] = (T)x[j];
+  }
+}
+
+// Values (i, j0 .. j0 + N) of a product, n <= N of them inside, to where they go.  b: the bias of these
+// columns.  VEC: all N inside and every address a multiple of the piece.
+template <int N, bool VEC, class T>
+__device__ __forceinline__ void finish(const GemmOut& o, int64_t i, int64_t j0, int n, const float (&b)[N],
+                                       float (&x)[N]) {
+  const int64_t at = i * o.J + j0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) x[j] += b[j];
+  if (o.pre) store_values<N, VEC>((T*)o.pre + at, n, x);
+  if (o.act != RINGX_ACT_NONE) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = activate(x[j], o.act);
+  }
+  if (o.residual) {
+    float r[N];
+    load_values<N, VEC>((const T*)o.residual + at, n, r);
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] += r[j];
+  }
+  if (o.f32) {
+    float* const p = (float*)o.out + at;
+    if (o.accumulate) {
+      float r[N];
+      load_values<N, VEC>(p, n, r);
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] += r[j];
+    }
+    store_values<N, VEC>(p, n, x);
+  } else if (o.heads) {
+    // [.., heads, tokens, d]
+    const uint32_t b0 = (uint32_t)i / (uint32_t)o.tokens, t = (uint32_t)i - b0 * (uint32_t)o.tokens;
+    if constexpr (VEC) {
+      const uint32_t h = (uint32_t)j0 / (uint32_t)o.d, c = (uint32_t)j0 - h * (uint32_t)o.d;
+      store_values<N, VEC>((T*)o.out + (((int64_t)b0 * o.heads + h) * o.tokens + t) * o.d + c, n, x);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const uint32_t h = (uint32_t)(j0 + j) / (uint32_t)o.d, c = (uint32_t)(j0 + j) - h * (uint32_t)o.d;
+        if (j < n) ((T*)o.out)[(((int64_t)b0 * o.heads + h) * o.tokens + t) * o.d + c] = (T)x[j];
+      }
+    }
+  } else {
+    store_values<N, VEC>((T*)o.out + at, n, x);
+  }
+}
+
+}  // namespace ringx

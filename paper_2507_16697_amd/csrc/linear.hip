@@ -1,0 +1,403 @@
+// The linear layer y = act(x w^T + b) + residual and its backward, around the matrix products of
+// gemm_bf16.hip and gemm_f32.hip: the product for a few rows, what joins a split product, the pass over dy
+// that gives dz = dy act'(pre) and the bias's gradient, and operands copied to rows that the products take.
+
+#include "linear.h"
+
+#include <algorithm>
+
+namespace ringx {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+
+// -------------------------------------------------------------------------------------------------
+// A few rows (a token at a time, or some of them), bf16.  Bound by the weights' bytes: every weight is
+// loaded once, straight into the fragments of v_mfma_f32_16x16x32_bf16 (lane l: row l % 16, r = 8 (l / 16)
+// .. + 7), 16 features to a workgroup whose waves take turns at 64 of K.  The rows of x, MB blocks of 16 of
+// them (those past M repeat the last), come from the caches.
+
+template <int MB, bool VEC>
+__global__ __launch_bounds__(512) void few_rows_kernel(GemmArgs a) {
+  constexpr int kUnroll = MB == 1 ? 8 : 4;
+  __shared__ f32x4 lds[8][MB][64];
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int waves = blockDim.x / 64;
+  const int64_t j0 = (int64_t)blockIdx.x * 16;
+  const int K = (int)a.R;
+  const __bf16* const w = (const __bf16*)a.Q.p + min(j0 + n, a.J - 1) * a.Q.ld;
+  const __bf16* x[MB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m) {
+    const int64_t i = min((int64_t)(16 * m + n), a.I - 1);
+    int64_t at = i * a.P.ld;
+    if (a.P.heads) {
+      const uint32_t b = (uint32_t)i / (uint32_t)a.P.tokens;
+      at = (int64_t)b * a.P.tokens * a.P.cols + (i - (int64_t)b * a.P.tokens) * a.P.d;
+    }
+    x[m] = (const __bf16*)a.P.p + at;
+  }
+  auto get = [&](const __bf16* p, int k, bool heads) {
+    bf16x8 v = {};
+    if constexpr (VEC) {
+      if (k < K) {
+        int64_t at = k;
+        if (heads) {
+          const uint32_t h = (uint32_t)k / (uint32_t)a.P.d;
+          at = (int64_t)h * a.P.tokens * a.P.d + (k - (int)h * (int)a.P.d);
+        }
+        v = *reinterpret_cast<const bf16x8*>(p + at);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (k + e < K) {
+          int64_t at = k + e;
+          if (heads) {
+            const uint32_t h = (uint32_t)at / (uint32_t)a.P.d;
+            at = (int64_t)h * a.P.tokens * a.P.d + (at - (int64_t)h * a.P.d);
+          }
+          v[e] = p[at];
+        }
+      }
+    }
+    return v;
+  };
+  f32x4 acc[MB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m) acc[m] = f32x4{};
+  const bool heads = a.P.heads != 0;
+  for (int k0 = wave * 64; k0 < K; k0 += waves * 64 * kUnroll) {
+    bf16x8 wv[kUnroll][2], xv[kUnroll][2][MB];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) wv[u][h] = get(w, k0 + u * waves * 64 + 32 * h + 8 * g, false);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int m = 0; m < MB; ++m) xv[u][h][m] = get(x[m], k0 + u * waves * 64 + 32 * h + 8 * g, heads);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int m = 0; m < MB; ++m)
+          acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[u][h], xv[u][h][m], acc[m], 0, 0, 0);
+  }
+#pragma unroll
+  for (int m = 0; m < MB; ++m) lds[wave][m][lane] = acc[m];
+  __syncthreads();
+  // wave m ends block m: the waves' sums in their order
+  for (int m = wave; m < MB; m += waves) {
+    f32x4 s = lds[0][m][lane];
+    for (int i = 1; i < waves; ++i) s += lds[i][m][lane];
+    const int64_t i = 16 * m + n, j = j0 + 4 * g;
+    const int inside = (int)max((int64_t)0, min((int64_t)4, a.J - j));
+    if (i >= a.I || inside == 0) continue;
+    float b[4], y[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) b[e] = a.o.bias && e < inside ? a.o.bias[j + e] : 0.f;
+    if (a.J % 4 == 0) finish<4, true, __bf16>(a.o, i, j, 4, b, y);
+    else finish<4, false, __bf16>(a.o, i, j, inside, b, y);
+  }
+}
+
+template <bool VEC>
+hipError_t launch_few_rows(const GemmArgs& a) {
+  // 4 waves; 8 where there are few features and much of K
+  const int waves = a.J <= 4096 && a.R >= 1024 ? 8 : 4;
+  const dim3 grid((uint32_t)((a.J + 15) / 16)), threads(64 * waves);
+  if (a.I <= 16) hipLaunchKernelGGL((few_rows_kernel<1, VEC>), grid, threads, 0, a.stream, a);
+  else if (a.I <= 32) hipLaunchKernelGGL((few_rows_kernel<2, VEC>), grid, threads, 0, a.stream, a);
+  else hipLaunchKernelGGL((few_rows_kernel<4, VEC>), grid, threads, 0, a.stream, a);
+  return hipGetLastError();
+}
+
+// -------------------------------------------------------------------------------------------------
+// The parts of a split product, in their order, then its epilogue.
+
+template <class T, bool VEC>
+__global__ __launch_bounds__(256) void join_kernel(GemmArgs a) {
+  const int64_t per = (a.J + 3) / 4, total = a.I * per;
+  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
+    const int64_t i = t / per, j = (t - i * per) * 4;
+    const int inside = (int)min((int64_t)4, a.J - j);
+    float x[4] = {}, b[4];
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
+      float y[4];
+      load_values<4, VEC>(a.part + s * a.I * a.J + i * a.J + j, inside, y);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += y[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) b[e] = a.o.bias && e < inside ? a.o.bias[j + e] : 0.f;
+    finish<4, VEC, T>(a.o, i, j, inside, b, x);
+  }
+}
+
+template <class T>
+hipError_t launch_product(const GemmArgs& a) {
+  constexpr bool kBf16 = std::is_same_v<T, __bf16>;
+  hipError_t e = kBf16 ? launch_gemm_bf16(a) : launch_gemm_f32(a);
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t wgs = std::min<int64_t>((a.I * ((a.J + 3) / 4) + 255) / 256, 4096);
+  if (a.J % 4 == 0 && a.o.d % 4 == 0)
+    hipLaunchKernelGGL((join_kernel<T, true>), dim3((uint32_t)wgs), dim3(256), 0, a.stream, a);
+  else
+    hipLaunchKernelGGL((join_kernel<T, false>), dim3((uint32_t)wgs), dim3(256), 0, a.stream, a);
+  return hipGetLastError();
+}
+
+// -------------------------------------------------------------------------------------------------
+// An operand copied to rows of `ld` values, zeros behind its columns: bf16 whose rows do not come in 16-byte
+// pieces, and heads where a product does not walk them itself.
+
+template <class T, bool VEC>
+__global__ __launch_bounds__(256) void pack_kernel(GemmIn x, T* out, int64_t ld) {
+  constexpr int N = 16 / (int)sizeof(T);
+  const uint32_t per = (uint32_t)((ld + N - 1) / N);
+  const int64_t total = x.rows * per;
+  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
+    const int64_t i = t / per;
+    const int64_t c = (t - i * per) * N;
+    int64_t row = i * x.ld;
+    if (x.heads) row = i / x.tokens * x.tokens * x.cols + i % x.tokens * x.d;
+    const T* const p = (const T*)x.p + row;
+    T* const q = out + i * ld + c;
+    auto column = [&](int64_t k) {
+      if (!x.heads) return k;
+      const int64_t h = (uint32_t)k / (uint32_t)x.d;
+      return h * x.tokens * x.d + (k - h * x.d);
+    };
+    if constexpr (VEC) {
+      *reinterpret_cast<u32x4*>(q) = *reinterpret_cast<const u32x4*>(p + column(c));
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (c + e < ld) q[e] = c + e < x.cols ? p[column(c + e)] : (T)0.f;
+    }
+  }
+}
+
+template <class T>
+hipError_t launch_pack(const GemmIn& x, void* out, int64_t ld, hipStream_t stream) {
+  constexpr int N = 16 / (int)sizeof(T);
+  const int64_t wgs = std::min<int64_t>((x.rows * ((ld + N - 1) / N) + 255) / 256, 8192);
+  const bool vec = ld == x.cols && x.cols % N == 0 && (x.heads ? x.d % N == 0 : x.ld % N == 0);
+  if (vec)
+    hipLaunchKernelGGL((pack_kernel<T, true>), dim3((uint32_t)wgs), dim3(256), 0, stream, x, (T*)out, ld);
+  else
+    hipLaunchKernelGGL((pack_kernel<T, false>), dim3((uint32_t)wgs), dim3(256), 0, stream, x, (T*)out, ld);
+  return hipGetLastError();
+}
+
+// -------------------------------------------------------------------------------------------------
+// dz = dy act'(pre), with zeros up to `ld` columns, and parts [gridDim.y, O] of its column sums.  Bound by
+// HBM: dy and pre are read and dz written once; the sums are of dz before its rounding.
+
+struct GradPass {
+  const void *dy, *pre;   // [M, O]; pre null without an activation
+  void* dz;               // [M, ld] or null
+  float* part;            // or null
+  int64_t M, O, ld, rows; // rows of a workgroup
+  int act, across;        // threads across the columns, 8 of them each
+};
+
+template <class T, bool VEC>
+__global__ __launch_bounds__(256) void grad_pass_kernel(GradPass a) {
+  constexpr int U = 4;
+  __shared__ float lds[256 * 9];
+  const int c = threadIdx.x % a.across, down = 256 / a.across;
+  const int64_t col = ((int64_t)blockIdx.x * a.across + c) * 8;
+  const int n = (int)max((int64_t)0, min((int64_t)8, a.O - col));
+  const int64_t end = min(a.M, (blockIdx.y + 1) * a.rows);
+  float sum[8] = {};
+  if (n > 0) {
+    for (int64_t r = blockIdx.y * a.rows + threadIdx.x / a.across; r < end; r += U * down) {
+      float g[U][8], z[U][8];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t at = min(r + u * down, end - 1) * a.O + col;
+        load_values<8, VEC>((const T*)a.dy + at, n, g[u]);
+        if (a.pre) load_values<8, VEC>((const T*)a.pre + at, n, z[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (r + u * down >= end) continue;
+        if (a.pre) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) g[u][e] *= activate_grad(z[u][e], a.act);
+        }
+        if (a.dz) {
+          T* const p = (T*)a.dz + (r + u * down) * a.ld + col;
+          if constexpr (VEC || std::is_same_v<T, __bf16>) store_values<8, true>(p, 8, g[u]);
+          else store_values<8, false>(p, n, g[u]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += g[u][e];
+      }
+    }
+  }
+  if (!a.part) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) lds[threadIdx.x * 9 + e] = sum[e];
+  __syncthreads();
+  const int64_t first = (int64_t)blockIdx.x * a.across * 8;
+  for (int j = threadIdx.x; j < a.across * 8 && first + j < a.O; j += 256) {
+    float s = 0.f;
+    for (int d = 0; d < down; ++d) s += lds[(d * a.across + j / 8) * 9 + j % 8];
+    a.part[blockIdx.y * a.O + first + j] = s;
+  }
+}
+
+template <class T>
+hipError_t launch_grad_pass(GradPass a, hipStream_t stream) {
+  const GradGrid g = grad_grid(a.M, a.O);
+  a.across = g.across, a.rows = g.rows;
+  const dim3 grid((uint32_t)g.x, (uint32_t)g.y);
+  if (a.O % 8 == 0) hipLaunchKernelGGL((grad_pass_kernel<T, true>), grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((grad_pass_kernel<T, false>), grid, dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+// -------------------------------------------------------------------------------------------------
+// Column sums of parts: 16 columns x 64 groups of parts to a workgroup, 16 loads of a thread in flight,
+// since the loads' latency is all that it waits for.
+
+constexpr int kSumCols = 16, kSumGroups = 64;
+__global__ __launch_bounds__(1024) void column_sums_kernel(ColumnSums a) {
+  __shared__ float lds[kSumGroups][kSumCols + 1];
+  const int cl = threadIdx.x % kSumCols, grp = threadIdx.x / kSumCols;
+  const int64_t col = (int64_t)blockIdx.x * kSumCols + cl;
+  const int per = (a.parts + kSumGroups - 1) / kSumGroups;
+  float t = 0.f;
+  if (col < a.cols) {
+    const int hi = min(a.parts, (grp + 1) * per);
+    for (int p = grp * per; p < hi; p += 16) {
+      float x[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) x[u] = a.part[(int64_t)min(p + u, hi - 1) * a.cols + col];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) t += p + u < hi ? x[u] : 0.f;
+    }
+  }
+  lds[grp][cl] = t;
+  __syncthreads();
+  if (grp == 0 && col < a.cols) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSumGroups; ++i) s += lds[i][cl];
+    float* const p = col < a.split ? a.out[0] : a.out[1];
+    if (p) {
+      const int64_t j = col < a.split ? col : col - a.split;
+      p[j] = a.accumulate ? p[j] + s : s;
+    }
+  }
+}
+
+char* at(void* workspace, int64_t offset) { return static_cast<char*>(workspace) + offset; }
+
+// x or w as a product takes it, copied to the workspace where the plan says so
+template <class T>
+hipError_t operand(GemmIn& x, int64_t offset, int64_t ld, void* workspace, hipStream_t stream) {
+  if (offset < 0) return hipSuccess;
+  void* const out = at(workspace, offset);
+  const hipError_t e = launch_pack<T>(x, out, ld, stream);
+  x.p = out, x.heads = 0, x.ld = ld, x.cols = ld;
+  return e;
+}
+
+template <class T>
+hipError_t forward(const LinearArgs& a) {
+  const LinearPlan p = linear_plan(a.s);
+  GemmArgs g;
+  g.P = a.x(), g.Q = a.weights();
+  g.I = a.s.M, g.J = a.s.O, g.R = a.s.K, g.stream = a.stream;
+  g.o.out = a.y, g.o.pre = a.pre, g.o.residual = a.residual, g.o.bias = a.bias, g.o.J = a.s.O;
+  g.o.act = a.act;
+  if constexpr (std::is_same_v<T, __bf16>) {
+    if (p.few) {
+      const bool vec = a.s.K % 8 == 0 && (a.s.heads ? a.s.K / a.s.heads % 8 == 0 : a.s.ldx % 8 == 0);
+      return vec ? launch_few_rows<true>(g) : launch_few_rows<false>(g);
+    }
+  }
+  hipError_t e = operand<T>(g.P, p.x, p.ldx, a.workspace, a.stream);
+  if (e == hipSuccess) e = operand<T>(g.Q, p.w, p.ldw, a.workspace, a.stream);
+  if (e != hipSuccess) return e;
+  g.R = p.R;
+  g.splits = p.splits, g.part = (float*)at(a.workspace, p.part);
+  return launch_product<T>(g);
+}
+
+template <class T>
+hipError_t backward(const LinearArgs& a) {
+  const LinearPlan p = linear_bwd_plan(a.s, a.act);
+  hipError_t e = hipSuccess;
+  // dz, and the bias's gradient
+  GemmIn dz;
+  dz.p = a.dy, dz.rows = a.s.M, dz.cols = dz.ld = a.s.O;
+  const bool own = p.dz >= 0 && (a.dx || a.dw);
+  if (own || a.dbias) {
+    GradPass g{};
+    g.dy = a.dy, g.pre = a.act ? a.pre : nullptr, g.M = a.s.M, g.O = a.s.O, g.act = a.act;
+    g.dz = own ? at(a.workspace, p.dz) : nullptr, g.ld = p.ldz;
+    g.part = a.dbias ? (float*)at(a.workspace, p.sums) : nullptr;
+    e = launch_grad_pass<T>(g, a.stream);
+    if (e != hipSuccess) return e;
+    if (a.dbias) {
+      ColumnSums c;
+      c.part = g.part, c.parts = (int)grad_grid(a.s.M, a.s.O).y, c.cols = c.split = a.s.O;
+      c.out[0] = a.dbias, c.accumulate = a.accumulate, c.stream = a.stream;
+      e = launch_column_sums(c);
+      if (e != hipSuccess) return e;
+    }
+    if (own) dz.p = g.dz, dz.cols = dz.ld = p.ldz;
+  }
+  GemmArgs g;
+  g.stream = a.stream, g.P = dz, g.part = (float*)at(a.workspace, p.part);
+  if (a.dx) {
+    g.Q = a.weights();
+    e = operand<T>(g.Q, p.w, p.ldw, a.workspace, a.stream);
+    if (e != hipSuccess) return e;
+    g.q_slow = true;
+    g.I = a.s.M, g.J = a.s.K, g.R = dz.cols, g.splits = p.splits_dx;
+    g.o.out = a.dx, g.o.J = a.s.K;
+    if (a.s.heads) g.o.heads = a.s.heads, g.o.tokens = a.s.tokens, g.o.d = a.s.K / a.s.heads;
+    e = launch_product<T>(g);
+    if (e != hipSuccess) return e;
+  }
+  if (a.dw) {
+    g.Q = a.x();
+    e = operand<T>(g.Q, p.x, p.ldx, a.workspace, a.stream);
+    if (e != hipSuccess) return e;
+    g.p_slow = g.q_slow = true;
+    g.I = a.s.O, g.J = a.s.K, g.R = a.s.M, g.splits = p.splits_dw;
+    g.o = GemmOut{};
+    g.o.out = a.dw, g.o.J = a.s.K, g.o.f32 = a.dw_f32, g.o.accumulate = a.accumulate;
+    e = launch_product<T>(g);
+  }
+  return e;
+}
+
+}  // namespace
+
+hipError_t launch_column_sums(const ColumnSums& a) {
+  hipLaunchKernelGGL(column_sums_kernel, dim3((uint32_t)((a.cols + kSumCols - 1) / kSumCols)),
+                     dim3(kSumCols * kSumGroups), 0, a.stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_linear(const LinearArgs& a) {
+  return a.s.bf16 ? forward<__bf16>(a) : forward<float>(a);
+}
+
+hipError_t launch_linear_bwd(const LinearArgs& a) {
+  return a.s.bf16 ? backward<__bf16>(a) : backward<float>(a);
+}
+
+}  // namespace ringx

@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <cstring>
@@ -90,6 +91,8 @@ const char* ringx_status_str(int status) {
       return "dropout rate neither 0 nor between 1/512 and 511/512 (both excluded), or mask position out of "
              "range or not a multiple of 32 keys";
     case RINGX_E_ROPE: return "invalid rotated sections, strides, position or eps";
+    case RINGX_E_NORM: return "invalid row length (1 to 16384), row stride or eps";
+    case RINGX_E_LINEAR: return "invalid widths (1 to 2^20), rows, row stride, heads or activation";
   }
   return "unknown status";
 }
@@ -1127,6 +1130,221 @@ ringx_status ringx_qkv_norm_rope_bwd(const void* qkv, int64_t batch_stride, int6
   a.dq = dq, a.dk = dk, a.dv = dv, a.dx = dqkv, a.dqw = dq_weight, a.dkw = dk_weight;
   a.part = weights ? static_cast<float*>(workspace) : nullptr;
   return hip_status(ringx::launch_norm_rope(a, true));
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------------------------
+// layer norm
+
+namespace {
+
+// an input or output that may be missing (bytes 0 then)
+struct Part {
+  const void* p;
+  int64_t bytes;
+};
+Span span(const Part& x) { return span(x.p, x.p ? x.bytes : 0); }
+
+// outputs overlap neither inputs nor one another; missing parts overlap nothing
+bool apart(std::initializer_list<Part> outs, std::initializer_list<Part> ins) {
+  for (auto o = outs.begin(); o != outs.end(); ++o) {
+    const Span so = span(*o);
+    if (so.lo == so.hi) continue;
+    for (const Part& i : ins) {
+      const Span si = span(i);
+      if (si.lo != si.hi && overlap(so, si)) return false;
+    }
+    for (auto q = o + 1; q != outs.end(); ++q) {
+      const Span sq = span(*q);
+      if (sq.lo != sq.hi && overlap(so, sq)) return false;
+    }
+  }
+  return true;
+}
+bool all_aligned(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (!aligned16(p)) return false;
+  return true;
+}
+
+// checks what both directions take; *bytes: those of the rows of x from first to last
+ringx_status check_norm(int64_t rows, int64_t C, int64_t row_stride, float eps, ringx_dtype dtype,
+                        int64_t* bytes) {
+  if (rows < 1) return RINGX_E_SHAPE;
+  if (dtype != RINGX_BF16 && dtype != RINGX_FP32) return RINGX_E_UNSUPPORTED;
+  if (C < 1 || C > ringx::kNormMaxC || !(std::isfinite(eps) && eps >= 0.f)) return RINGX_E_NORM;
+  if (rows > 1 && row_stride < C) return RINGX_E_NORM;
+  int64_t x;
+  if (!mul_ok(rows, C, &x)) return RINGX_E_SHAPE;
+  *bytes = C;
+  if (rows > 1) {
+    if (!mul_ok(rows - 1, row_stride, &x) || x > kMaxElems - C) return RINGX_E_SHAPE;
+    *bytes = x + C;
+  }
+  *bytes *= esize(dtype);
+  return RINGX_OK;
+}
+ringx::NormArgs norm_args(const void* x, int64_t row_stride, int64_t rows, int64_t C,
+                          const float* weight, ringx_dtype dtype, hipStream_t stream) {
+  ringx::NormArgs a;
+  a.x = x, a.rows = rows, a.C = static_cast<int>(C), a.weight = weight;
+  a.stride = rows > 1 ? row_stride : C;
+  a.bf16 = dtype == RINGX_BF16;
+  const int64_t piece = 16 / esize(dtype);
+  a.vec = C % piece == 0 && a.stride % piece == 0;
+  a.stream = stream;
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+ringx_status ringx_layer_norm(const void* x, int64_t row_stride, const float* weight,
+                              const float* bias, void* y, float* stats, int64_t rows, int64_t C,
+                              float eps, ringx_dtype dtype, hipStream_t stream) {
+  if (!x || !y) return RINGX_E_NULLPTR;
+  int64_t bytes = 0;
+  const ringx_status st = check_norm(rows, C, row_stride, eps, dtype, &bytes);
+  if (st != RINGX_OK) return st;
+  if (!all_aligned({x, weight, bias, y, stats})) return RINGX_E_ALIGN;
+  if (!apart({{y, rows * C * esize(dtype)}, {stats, 8 * rows}}, {{x, bytes}, {weight, 4 * C}, {bias, 4 * C}}))
+    return RINGX_E_ALIAS;
+  ringx::NormArgs a = norm_args(x, row_stride, rows, C, weight, dtype, stream);
+  a.bias = bias, a.y = y, a.stats = stats, a.eps = eps;
+  return hip_status(ringx::launch_layer_norm(a, false));
+}
+
+size_t ringx_layer_norm_bwd_workspace_bytes(int64_t rows, int64_t C, ringx_dtype dtype) {
+  int64_t x;
+  if (check_norm(rows, C, C, 0.f, dtype, &x) != RINGX_OK) return 0;
+  return static_cast<size_t>(std::min(rows, ringx::norm_workgroups(C, true)) * 2 * C * 4 + 255) / 256 * 256;
+}
+
+ringx_status ringx_layer_norm_bwd(const void* x, int64_t row_stride, const void* dy, const void* dres,
+                                  const float* weight, const float* stats, void* dx, float* dweight,
+                                  float* dbias, int64_t rows, int64_t C, ringx_dtype dtype,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (!x || !dy || !stats || !dx) return RINGX_E_NULLPTR;
+  int64_t bytes = 0;
+  const ringx_status st = check_norm(rows, C, row_stride, 0.f, dtype, &bytes);
+  if (st != RINGX_OK) return st;
+  const bool sums = dweight || dbias;
+  const size_t need = sums ? ringx_layer_norm_bwd_workspace_bytes(rows, C, dtype) : 0;
+  if (sums && (!workspace || workspace_bytes < need)) return RINGX_E_WORKSPACE;
+  if (!sums) workspace = nullptr;
+  if (!all_aligned({x, dy, dres, weight, stats, dx, dweight, dbias, workspace})) return RINGX_E_ALIGN;
+  const int64_t n = rows * C * esize(dtype);
+  if (!apart({{dx, n}, {dweight, 4 * C}, {dbias, 4 * C}, {workspace, (int64_t)need}},
+             {{x, bytes}, {dy, n}, {dres, n}, {weight, 4 * C}, {stats, 8 * rows}}))
+    return RINGX_E_ALIAS;
+  ringx::NormArgs a = norm_args(x, row_stride, rows, C, weight, dtype, stream);
+  a.dy = dy, a.dres = dres, a.stats_in = stats, a.dx = dx, a.dweight = dweight, a.dbias = dbias;
+  a.part = static_cast<float*>(workspace);
+  return hip_status(ringx::launch_layer_norm(a, true));
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------------------------
+// linear layer
+
+namespace {
+
+// checks what both directions take; *bytes: those of x from first to last
+ringx_status make_linear(int64_t x_stride, int64_t heads, int64_t tokens, int64_t M, int64_t K,
+                         int64_t O, int act, ringx_dtype dtype, ringx::LinearShape* s,
+                         int64_t* bytes) {
+  if (M < 1) return RINGX_E_SHAPE;
+  if (dtype != RINGX_BF16 && dtype != RINGX_FP32) return RINGX_E_UNSUPPORTED;
+  if (K < 1 || O < 1 || K > ringx::kLinearMaxWidth || O > ringx::kLinearMaxWidth || M > INT32_MAX)
+    return RINGX_E_LINEAR;
+  if (act < RINGX_ACT_NONE || act > RINGX_ACT_SILU || heads < 0) return RINGX_E_LINEAR;
+  if (heads > 0 && (K % heads != 0 || tokens < 1 || M % tokens != 0)) return RINGX_E_LINEAR;
+  if (heads == 0 && M > 1 && x_stride < K) return RINGX_E_LINEAR;
+  int64_t x = 0;
+  if (!mul_ok(M, K, &x) || !mul_ok(M, O, &x) || !mul_ok(O, K, &x)) return RINGX_E_SHAPE;
+  s->M = M, s->K = K, s->O = O, s->heads = heads, s->tokens = heads ? tokens : 0;
+  s->ldx = heads == 0 && M > 1 ? x_stride : K;
+  s->bf16 = dtype == RINGX_BF16;
+  if (!mul_ok(M - 1, s->ldx, &x) || x > kMaxElems - K) return RINGX_E_SHAPE;
+  *bytes = (x + K) * esize(dtype);
+  // a launch has at most 2^32 threads: tiles of 128 x 128 in bf16 and 32 x 32 in fp32 in parts, 256 threads
+  const int64_t side = s->bf16 ? 128 : 32;
+  const auto tiles = [side](int64_t i, int64_t j) {
+    return ((i + side - 1) / side) * ((j + side - 1) / side);
+  };
+  if (std::max({tiles(M, O), tiles(M, K), tiles(O, K)}) >= (int64_t(1) << 24)) return RINGX_E_SHAPE;
+  return RINGX_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ringx_linear_workspace_bytes(int64_t x_stride, int64_t heads, int64_t tokens, int64_t M,
+                                    int64_t K, int64_t O, ringx_dtype dtype) {
+  ringx::LinearShape s;
+  int64_t x;
+  if (make_linear(x_stride, heads, tokens, M, K, O, 0, dtype, &s, &x) != RINGX_OK) return 0;
+  return static_cast<size_t>(ringx::linear_plan(s).bytes);
+}
+
+ringx_status ringx_linear(const void* x, int64_t x_stride, int64_t heads, int64_t tokens,
+                          const void* w, const float* bias, const void* residual, void* y, void* pre,
+                          int64_t M, int64_t K, int64_t O, ringx_act act, ringx_dtype dtype,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (!x || !w || !y) return RINGX_E_NULLPTR;
+  ringx::LinearArgs a;
+  int64_t bytes = 0;
+  const ringx_status st = make_linear(x_stride, heads, tokens, M, K, O, act, dtype, &a.s, &bytes);
+  if (st != RINGX_OK) return st;
+  const int64_t need = ringx::linear_plan(a.s).bytes;
+  if (need > 0 && (!workspace || workspace_bytes < static_cast<size_t>(need))) return RINGX_E_WORKSPACE;
+  if (need == 0) workspace = nullptr;
+  if (!all_aligned({x, w, bias, residual, y, pre, workspace})) return RINGX_E_ALIGN;
+  const int64_t es = esize(dtype), out = M * O * es;
+  if (!apart({{y, out}, {pre, out}, {workspace, need}},
+             {{x, bytes}, {w, O * K * es}, {bias, 4 * O}, {residual, out}}))
+    return RINGX_E_ALIAS;
+  a.xp = x, a.wp = w, a.bias = bias, a.residual = residual, a.y = y, a.pre = pre, a.act = act;
+  a.workspace = workspace, a.stream = stream;
+  return hip_status(ringx::launch_linear(a));
+}
+
+size_t ringx_linear_bwd_workspace_bytes(int64_t x_stride, int64_t heads, int64_t tokens, int64_t M,
+                                        int64_t K, int64_t O, ringx_act act, ringx_dtype dtype) {
+  ringx::LinearShape s;
+  int64_t x;
+  if (make_linear(x_stride, heads, tokens, M, K, O, act, dtype, &s, &x) != RINGX_OK) return 0;
+  return static_cast<size_t>(ringx::linear_bwd_plan(s, act).bytes);
+}
+
+ringx_status ringx_linear_bwd(const void* x, int64_t x_stride, int64_t heads, int64_t tokens,
+                              const void* w, const void* dy, const void* pre, void* dx, void* dw,
+                              float* dbias, int64_t M, int64_t K, int64_t O, ringx_act act,
+                              ringx_dtype dtype, ringx_dtype dw_dtype, int accumulate_dw,
+                              void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (!x || !w || !dy || !(dx || dw || dbias)) return RINGX_E_NULLPTR;
+  ringx::LinearArgs a;
+  int64_t bytes = 0;
+  const ringx_status st = make_linear(x_stride, heads, tokens, M, K, O, act, dtype, &a.s, &bytes);
+  if (st != RINGX_OK) return st;
+  if (!pre != (act == RINGX_ACT_NONE)) return RINGX_E_NULLPTR;
+  if (dw_dtype != RINGX_FP32 && dw_dtype != dtype) return RINGX_E_UNSUPPORTED;
+  if (accumulate_dw && dw && dw_dtype != RINGX_FP32) return RINGX_E_UNSUPPORTED;
+  const int64_t need = ringx::linear_bwd_plan(a.s, act).bytes;
+  if (!workspace || workspace_bytes < static_cast<size_t>(need)) return RINGX_E_WORKSPACE;
+  if (!all_aligned({x, w, dy, pre, dx, dw, dbias, workspace})) return RINGX_E_ALIGN;
+  const int64_t es = esize(dtype), out = M * O * es;
+  if (!apart({{dx, M * K * es}, {dw, O * K * esize(dw_dtype)}, {dbias, 4 * O}, {workspace, need}},
+             {{x, bytes}, {w, O * K * es}, {dy, out}, {pre, out}}))
+    return RINGX_E_ALIAS;
+  a.xp = x, a.wp = w, a.dy = dy, a.pre = const_cast<void*>(pre), a.dx = dx, a.dw = dw, a.dbias = dbias;
+  a.act = act, a.dw_f32 = dw_dtype == RINGX_FP32, a.accumulate = accumulate_dw != 0;
+  a.workspace = workspace, a.stream = stream;
+  return hip_status(ringx::launch_linear_bwd(a));
 }
 
 }  // extern "C"

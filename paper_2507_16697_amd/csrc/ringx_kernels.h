@@ -432,6 +432,196 @@ inline RopeGrid rope_grid(int64_t rows, int heads, int tokens_per_wave, bool bwd
   return g;
 }
 
+// Layer norm (layer_norm.hip).
+struct NormArgs {
+  const void* x = nullptr;                     // [rows, C], row stride `stride` (elements)
+  int64_t stride = 0, rows = 0;
+  const float *weight = nullptr, *bias = nullptr;              // [C] or null
+  void* y = nullptr;                           // forward: [rows, C]
+  float* stats = nullptr;                      // forward: [2, rows] or null
+  const void *dy = nullptr, *dres = nullptr;   // backward: [rows, C]; dres may be null
+  const float* stats_in = nullptr;             // backward
+  void* dx = nullptr;                          // backward: [rows, C]
+  float *dweight = nullptr, *dbias = nullptr;  // backward: [C] or null
+  float* part = nullptr;                       // backward: the workgroups' parts [.., 2, C], or null
+  int C = 0;
+  float eps = 0.f;
+  bool bf16 = false, vec = true;               // vec: rows in 16-byte pieces
+  hipStream_t stream = nullptr;
+};
+constexpr int64_t kNormMaxC = 16384;
+// Most workgroups of a launch.
+inline int64_t norm_workgroups(int64_t C, bool bwd) { return bwd ? 512 : 2048; }
+
+// Sums over parts [parts, cols] fp32, in their order; columns below `split` to out[0], the others to
+// out[1] (either may be null), which they overwrite or are added to.
+struct ColumnSums {
+  const float* part = nullptr;
+  int parts = 0;
+  int64_t cols = 0, split = 0;
+  float* out[2] = {nullptr, nullptr};
+  bool accumulate = false;
+  hipStream_t stream = nullptr;
+};
+
+// Linear layer (linear.hip, gemm_bf16.hip, gemm_f32.hip).
+//
+// An operand of a product, [rows, cols] with the columns next to each other and rows `ld` elements
+// apart; or, with heads > 0, rows and columns of an attention's tensor [rows / tokens, heads, tokens, d].
+struct GemmIn {
+  const void* p = nullptr;
+  int64_t rows = 0, cols = 0, ld = 0;
+  int64_t heads = 0, tokens = 0, d = 0;
+};
+// Where a product [I, J] goes.
+struct GemmOut {
+  void* out = nullptr;             // [I, J] in the operands' type, or fp32 (f32)
+  void* pre = nullptr;             // [I, J] or null: the activation's input
+  const void* residual = nullptr;  // [I, J] or null
+  const float* bias = nullptr;     // [J] or null
+  int64_t J = 0;
+  int64_t heads = 0, tokens = 0, d = 0;   // heads > 0: out is [I / tokens, heads, tokens, d]
+  int act = 0;
+  bool f32 = false, accumulate = false;   // accumulate: fp32 out alone
+};
+// out[i][j] = sum over r of P(i, r) Q(j, r); P is stored [I, R] or, with p_slow, [R, I]; Q likewise.
+struct GemmArgs {
+  GemmIn P, Q;
+  bool p_slow = false, q_slow = false;
+  int64_t I = 0, J = 0, R = 0;
+  GemmOut o;
+  int splits = 1;                  // parts of R, whose sums go to part [splits, I, J]
+  float* part = nullptr;
+  hipStream_t stream = nullptr;
+};
+// Whether a product takes large tiles (256 x 256 in bf16, 128 x 128 in fp32; else 128 x 128, 32 x 32).
+inline bool gemm_bf16_large(int64_t I, int64_t J) {
+  return ((I + 255) / 256) * ((J + 255) / 256) >= 192;
+}
+inline bool gemm_f32_large(int64_t I, int64_t J) {
+  return ((I + 127) / 128) * ((J + 127) / 128) >= 192;
+}
+// Parts that R is cut into where the tiles do not fill the chip.
+inline int gemm_splits(int64_t I, int64_t J, int64_t R, bool bf16) {
+  if (bf16 ? gemm_bf16_large(I, J) : gemm_f32_large(I, J)) return 1;
+  const int64_t side = bf16 ? 128 : 32;
+  const int64_t tiles = ((I + side - 1) / side) * ((J + side - 1) / side);
+  const int64_t steps = (R + 63) / 64;
+  const int64_t s = std::min<int64_t>({512 / tiles, steps / 4, 32});
+  return (int)std::max<int64_t>(s, 1);
+}
+
+// The pass over a gradient [M, O]: threads across 8 columns each, rows of a workgroup, workgroups.
+struct GradGrid {
+  int across;
+  int64_t rows, x, y;
+};
+inline GradGrid grad_grid(int64_t M, int64_t O) {
+  GradGrid g;
+  g.across = 1;
+  while (g.across < 64 && 8 * g.across < O) g.across *= 2;
+  g.x = (O + 8 * g.across - 1) / (8 * g.across);
+  const int64_t least = 4 * (256 / g.across);      // rows of one round
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(512, 2048 / g.x));
+  g.rows = std::max<int64_t>(least, ((M + most - 1) / most + least - 1) / least * least);
+  g.y = (M + g.rows - 1) / g.rows;
+  return g;
+}
+
+struct LinearShape {
+  int64_t M = 0, K = 0, O = 0;
+  int64_t ldx = 0;                 // row stride of x (heads = 0)
+  int64_t heads = 0, tokens = 0;   // heads > 0: x is [M / tokens, heads, tokens, K / heads]
+  bool bf16 = false;
+};
+struct LinearArgs {
+  LinearShape s;
+  const void *xp = nullptr, *wp = nullptr;
+  const float* bias = nullptr;
+  const void* residual = nullptr;
+  void *y = nullptr, *pre = nullptr;   // forward's outputs; the backward reads pre
+  const void* dy = nullptr;
+  void *dx = nullptr, *dw = nullptr;
+  float* dbias = nullptr;
+  int act = 0;
+  bool dw_f32 = true, accumulate = false;
+  void* workspace = nullptr;
+  hipStream_t stream = nullptr;
+  GemmIn x() const {
+    GemmIn g;
+    g.p = xp, g.rows = s.M, g.cols = s.K, g.ld = s.ldx;
+    if (s.heads) g.heads = s.heads, g.tokens = s.tokens, g.d = s.K / s.heads;
+    return g;
+  }
+  GemmIn weights() const {
+    GemmIn g;
+    g.p = wp, g.rows = s.O, g.cols = g.ld = s.K;
+    return g;
+  }
+};
+// What a call does, and where its workspace holds what (byte offsets; -1: not there).
+struct LinearPlan {
+  bool few = false;                        // forward: the kernel for a few rows
+  int64_t x = -1, w = -1, dz = -1;         // copies of the operands, dz
+  int64_t ldx = 0, ldw = 0, ldz = 0;       // their row lengths
+  int64_t sums = -1, part = 0;             // parts of the bias's gradient, of split products
+  int64_t R = 0;                           // forward: the product's r
+  int splits = 1, splits_dx = 1, splits_dw = 1;
+  int64_t bytes = 0;
+  int64_t take(int64_t n) {
+    const int64_t at = bytes;
+    bytes += (n + 255) / 256 * 256;
+    return at;
+  }
+};
+constexpr int64_t kLinearMaxWidth = int64_t(1) << 20;   // of K and O
+constexpr int64_t kFewRows = 64;
+// Offsets of an operand's tile are 31 bits: rows of at most 2^21 values, heads whose batch has at most 2^29.
+inline bool linear_near(const LinearShape& s) {
+  return s.heads ? s.tokens * s.K <= (int64_t(1) << 29) : s.ldx <= (int64_t(1) << 21);
+}
+inline LinearPlan linear_plan(const LinearShape& s) {
+  LinearPlan p;
+  const int64_t Kp = (s.K + 7) / 8 * 8;
+  p.R = s.K;
+  if (s.bf16) {
+    p.few = s.M <= kFewRows;
+    if (p.few) return p;
+    p.R = Kp;
+    const bool fits = s.K % 8 == 0 && linear_near(s) && (s.heads ? s.K / s.heads % 64 == 0 : s.ldx % 8 == 0);
+    if (!fits) p.x = p.take(2 * s.M * Kp), p.ldx = Kp;
+    if (Kp != s.K) p.w = p.take(2 * s.O * Kp), p.ldw = Kp;
+  } else if (s.heads || !linear_near(s)) {
+    p.x = p.take(4 * s.M * s.K), p.ldx = s.K;
+  }
+  p.splits = gemm_splits(s.M, s.O, p.R, s.bf16);
+  if (p.splits > 1) p.part = p.take(4 * p.splits * s.M * s.O);
+  return p;
+}
+inline LinearPlan linear_bwd_plan(const LinearShape& s, int act) {
+  LinearPlan p;
+  const int64_t Kp = (s.K + 7) / 8 * 8, Op = s.bf16 ? (s.O + 7) / 8 * 8 : s.O;
+  const int64_t es = s.bf16 ? 2 : 4;
+  p.ldz = Op;
+  if (act || Op != s.O) p.dz = p.take(es * s.M * Op);
+  if (s.bf16) {
+    // dw walks heads 64 tokens at a time
+    const bool fits = s.K % 8 == 0 && linear_near(s) &&
+                      (s.heads ? s.K / s.heads % 8 == 0 && s.tokens % 64 == 0 : s.ldx % 8 == 0);
+    if (!fits) p.x = p.take(2 * s.M * Kp), p.ldx = Kp;
+    if (Kp != s.K) p.w = p.take(2 * s.O * Kp), p.ldw = Kp;
+  } else if (s.heads || !linear_near(s)) {
+    p.x = p.take(4 * s.M * s.K), p.ldx = s.K;
+  }
+  p.splits_dx = gemm_splits(s.M, s.K, Op, s.bf16);
+  p.splits_dw = gemm_splits(s.O, s.K, s.M, s.bf16);
+  p.sums = p.take(4 * grad_grid(s.M, s.O).y * s.O);
+  const int64_t dx = p.splits_dx > 1 ? 4 * p.splits_dx * s.M * s.K : 0;
+  const int64_t dw = p.splits_dw > 1 ? 4 * p.splits_dw * s.O * s.K : 0;
+  if (dx || dw) p.part = p.take(std::max(dx, dw));
+  return p;
+}
+
 hipError_t launch_fwd_bf16(const FwdArgs& a, FwdMode mode);
 hipError_t launch_fwd_f32(const FwdArgs& a, FwdMode mode);
 hipError_t launch_lse_merge(const MergeArgs& a);
@@ -455,6 +645,13 @@ hipError_t launch_bwd_drop_bf16(const BwdArgs& a, const Drop& drop_kv, const Dro
 hipError_t launch_bwd_drop_f32(const BwdArgs& a, const Drop& drop);
 
 hipError_t launch_norm_rope(const RopeArgs& a, bool bwd);
+
+hipError_t launch_layer_norm(const NormArgs& a, bool bwd);
+hipError_t launch_column_sums(const ColumnSums& a);
+hipError_t launch_gemm_bf16(const GemmArgs& a);
+hipError_t launch_gemm_f32(const GemmArgs& a);
+hipError_t launch_linear(const LinearArgs& a);
+hipError_t launch_linear_bwd(const LinearArgs& a);
 
 hipError_t launch_tt_tokenize(const TokArgs& a);
 

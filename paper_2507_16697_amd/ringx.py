@@ -11,6 +11,9 @@ supplies device memory and the current HIP stream.  Function names follow the C 
     ringx_attn_bwd_step(q, k_r, v_r, dout, lse, delta, dq_acc, dk_r, dv_r, accumulate_dq=(r > 0))
     q, k, v = ringx_qkv_norm_rope(qkv, H, Hkv, freqs, rot)     # from a packed projection
     out, lse = ringx_attn_fwd_drop(q, k, v, p, rng)            # with dropout; rng: seed and offset
+    y, stats = ringx_layer_norm(x, weight, bias)               # x [..., C]
+    y, pre = ringx_linear(x, w, bias, act="gelu", need_pre=True)   # x [..., K] or [B,H,N,d], w [O, K]
+    dx, dw, dbias = ringx_linear_bwd(x, w, dy, pre=pre, act="gelu", bias=bias)
 
 stream= is a torch stream or a handle, by default the current stream; the caller orders it against the
 current one, as for any work on two streams.  Buffers that a call makes are that stream's memory.
@@ -37,7 +40,11 @@ STATUS_NAMES = {
     0: "RINGX_OK", 1: "RINGX_E_NULLPTR", 2: "RINGX_E_SHAPE", 3: "RINGX_E_CHUNKS",
     4: "RINGX_E_UNSUPPORTED", 5: "RINGX_E_ALIGN", 6: "RINGX_E_WORKSPACE", 7: "RINGX_E_HIP",
     8: "RINGX_E_ALIAS", 9: "RINGX_E_SCRATCH", 10: "RINGX_E_DROPOUT", 11: "RINGX_E_ROPE",
+    12: "RINGX_E_NORM", 13: "RINGX_E_LINEAR",
 }
+
+# activations of ringx_linear, by name
+ACTIVATIONS = {"none": 0, "gelu": 1, "gelu_tanh": 2, "silu": 3}
 
 # rows (B * H * Nq) of the fixed device array behind ringx_attn_bwd_noalloc (RINGX_NOALLOC_MAX_ROWS)
 NOALLOC_MAX_ROWS = 2097152
@@ -52,7 +59,9 @@ EXPORTED = ("ringx_attn_fwd", "ringx_attn_fwd_partials", "ringx_lse_merge", "rin
             "ringx_fwd_drop_workspace_bytes", "ringx_attn_bwd_drop", "ringx_bwd_drop_workspace_bytes",
             "ringx_attn_fwd_step_drop", "ringx_attn_bwd_step_drop", "ringx_bwd_preprocess_drop",
             "ringx_qkv_norm_rope", "ringx_qkv_norm_rope_bwd",
-            "ringx_qkv_norm_rope_bwd_workspace_bytes")
+            "ringx_qkv_norm_rope_bwd_workspace_bytes", "ringx_layer_norm", "ringx_layer_norm_bwd",
+            "ringx_layer_norm_bwd_workspace_bytes", "ringx_linear", "ringx_linear_workspace_bytes",
+            "ringx_linear_bwd", "ringx_linear_bwd_workspace_bytes")
 
 
 class RingxError(RuntimeError):
@@ -132,6 +141,17 @@ def lib() -> ctypes.CDLL:
                                               [_I] * 5 + [F, C, _P, ctypes.c_size_t, _P])
         L.ringx_qkv_norm_rope_bwd_workspace_bytes.argtypes = [_I] * 5 + [C]
         L.ringx_qkv_norm_rope_bwd_workspace_bytes.restype = ctypes.c_size_t
+        Z = ctypes.c_size_t
+        L.ringx_layer_norm.argtypes = [_P, _I, _P, _P, _P, _P, _I, _I, F, C, _P]
+        L.ringx_layer_norm_bwd.argtypes = [_P, _I] + [_P] * 7 + [_I, _I, C, _P, Z, _P]
+        L.ringx_layer_norm_bwd_workspace_bytes.argtypes = [_I, _I, C]
+        L.ringx_layer_norm_bwd_workspace_bytes.restype = Z
+        L.ringx_linear.argtypes = [_P, _I, _I, _I] + [_P] * 5 + [_I, _I, _I, C, C, _P, Z, _P]
+        L.ringx_linear_workspace_bytes.argtypes = [_I] * 6 + [C]
+        L.ringx_linear_workspace_bytes.restype = Z
+        L.ringx_linear_bwd.argtypes = ([_P, _I, _I, _I] + [_P] * 6 + [_I, _I, _I, C, C, C, C, _P, Z, _P])
+        L.ringx_linear_bwd_workspace_bytes.argtypes = [_I] * 6 + [C, C]
+        L.ringx_linear_bwd_workspace_bytes.restype = Z
         L.ringx_chunk_bounds.argtypes = [_I, _I, _I, ctypes.POINTER(_I), ctypes.POINTER(_I)]
         L.ringx_status_str.argtypes = [ctypes.c_int]
         L.ringx_status_str.restype = ctypes.c_char_p
@@ -143,7 +163,8 @@ def lib() -> ctypes.CDLL:
                      "ringx_attn_bwd_dq_ds", "ringx_attn_bwd_ds", "ringx_attn_fwd_drop",
                      "ringx_attn_bwd_drop", "ringx_attn_fwd_step_drop", "ringx_attn_bwd_step_drop",
                      "ringx_bwd_preprocess_drop", "ringx_qkv_norm_rope",
-                     "ringx_qkv_norm_rope_bwd"):
+                     "ringx_qkv_norm_rope_bwd", "ringx_layer_norm", "ringx_layer_norm_bwd",
+                     "ringx_linear", "ringx_linear_bwd"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -901,3 +922,199 @@ def ringx_qkv_norm_rope_bwd(qkv, dq, dk, dv, freqs, rot, pos=None, pos0: int = 0
             H, Hkv, d, float(eps), code, _ptr(workspace), 0 if workspace is None else
             _nbytes(workspace))
     return dqkv, dq_weight, dk_weight
+
+
+# ---------------------------------------------------------------------------------------------
+# layer norm and linear layers, around the attention
+
+
+def _rows_of(name, x):
+    """(rows, row stride) of x [..., C]: its last dimension contiguous, the others as rows of one stride."""
+    if not x.is_cuda:
+        raise ValueError("tensors must live on the GPU")
+    if x.dim() < 1:
+        raise ValueError(f"{name}: needs a last dimension")
+    shape, strides = x.shape, x.stride()
+    if shape[-1] > 1 and strides[-1] != 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    rows, step = 1, None
+    for n, s in zip(shape[-2::-1], strides[-2::-1]):
+        if n == 1:
+            continue
+        if step is None:
+            step = s
+        elif s != step * rows:
+            raise ValueError(f"{name}: its leading dimensions must lie as rows of one stride")
+        rows *= n
+    return rows, shape[-1] if step is None else step
+
+
+def _vector(name, t, n, device):
+    """Address of an fp32 vector [n], None where there is none."""
+    if t is None:
+        return None
+    _dev(t)
+    _expect(name, t, (n,), _T.float32, device)
+    return t.data_ptr()
+
+
+def _same(name, t, shape, like):
+    """Address of an input of `shape` in like's type, None where there is none."""
+    if t is None:
+        return None
+    _dev(t)
+    _expect(name, t, shape, like.dtype, like.device)
+    return t.data_ptr()
+
+
+def ringx_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, need_stats: bool = True, y=None,
+                     stats=None, stream=None):
+    """Layer norm over the last dimension of x [..., C] (rows contiguous, of any one stride); weight, bias
+    fp32 [C] or None.  Returns (y [..., C], stats fp32 [2, rows]: mean and 1 / deviation, what the
+    backward needs, or None with need_stats=False)."""
+    torch = _T or _torch()
+    rows, step = _rows_of("x", x)
+    C = x.shape[-1]
+    code = _dtype_code(x)
+    pw, pb = _vector("weight", weight, C, x.device), _vector("bias", bias, C, x.device)
+    y = _out("y", y, x.shape, x.dtype, x, stream)
+    if need_stats or stats is not None:
+        stats = _out("stats", stats, (2, rows), torch.float32, x, stream)
+    _launch("ringx_layer_norm", x, stream, x.data_ptr(), step, pw, pb, y.data_ptr(), _ptr(stats), rows, C,
+            float(eps), code)
+    return y, stats
+
+
+@functools.lru_cache(maxsize=256)   # a function of the sizes alone
+def ringx_layer_norm_bwd_workspace_bytes(rows, C, dtype) -> int:
+    return int(lib().ringx_layer_norm_bwd_workspace_bytes(rows, C, int(dtype)))
+
+
+def ringx_layer_norm_bwd(x, dy, stats, weight=None, bias=None, dres=None, dx=None, dweight=None,
+                         dbias=None, workspace=None, stream=None):
+    """Backward of ringx_layer_norm from dy [..., C] and the forward's stats; dres: the gradient that reaches x
+    by its residual, added to dx.  Returns (dx [..., C] in x's dtype, dweight, dbias fp32 [C], None where
+    there is no weight or bias)."""
+    torch = _T or _torch()
+    rows, step = _rows_of("x", x)
+    C = x.shape[-1]
+    code = _dtype_code(x)
+    _same("dy", dy, x.shape, x)
+    pr = _same("dres", dres, x.shape, x)
+    _dev(stats)
+    _expect("stats", stats, (2, rows), torch.float32, x.device)
+    pw = _vector("weight", weight, C, x.device)
+    _vector("bias", bias, C, x.device)
+    if (weight is None and dweight is not None) or (bias is None and dbias is not None):
+        raise ValueError("a weight's gradient without the weight")
+    dx = _out("dx", dx, x.shape, x.dtype, x, stream)
+    if weight is not None:
+        dweight = _out("dweight", dweight, (C,), torch.float32, x, stream)
+    if bias is not None:
+        dbias = _out("dbias", dbias, (C,), torch.float32, x, stream)
+    if weight is not None or bias is not None:
+        workspace = _workspace(workspace, ringx_layer_norm_bwd_workspace_bytes(rows, C, code), x, stream)
+    else:
+        workspace = None
+    _launch("ringx_layer_norm_bwd", x, stream, x.data_ptr(), step, dy.data_ptr(), pr, pw, stats.data_ptr(),
+            dx.data_ptr(), _ptr(dweight), _ptr(dbias), rows, C, code, _ptr(workspace),
+            0 if workspace is None else _nbytes(workspace))
+    return dx, dweight, dbias
+
+
+def _act_code(act) -> int:
+    try:
+        return ACTIVATIONS["none" if act is None else act]
+    except KeyError:
+        raise ValueError(f"act: {act!r}, expected one of {', '.join(ACTIVATIONS)}") from None
+
+
+def _linear_args(x, w):
+    """(row stride, heads, tokens, M, K, O, leading shape of the output) of x [..., K] or [B,H,N,d]."""
+    if w.dim() != 2:
+        raise ValueError("w must be 2-D [O, K]")
+    O, K = w.shape
+    if x.dim() == 4:
+        _dev(x)
+        B, H, N, d = x.shape
+        if H * d != K:
+            raise ValueError(f"x: {H} heads of {d}, w has {K} columns")
+        step, heads, tokens, M, lead = K, H, N, B * N, (B, N)
+    else:
+        M, step = _rows_of("x", x)
+        if x.shape[-1] != K:
+            raise ValueError(f"x: rows of {x.shape[-1]}, w has {K} columns")
+        heads, tokens, lead = 0, 0, x.shape[:-1]
+    _dev(w)
+    _expect("w", w, (O, K), x.dtype, x.device)
+    return step, heads, tokens, M, K, O, lead
+
+
+@functools.lru_cache(maxsize=256)   # a function of the sizes alone
+def ringx_linear_workspace_bytes(x_stride, heads, tokens, M, K, O, dtype) -> int:
+    return int(lib().ringx_linear_workspace_bytes(x_stride, heads, tokens, M, K, O, int(dtype)))
+
+
+@functools.lru_cache(maxsize=256)   # a function of the sizes alone
+def ringx_linear_bwd_workspace_bytes(x_stride, heads, tokens, M, K, O, act, dtype) -> int:
+    return int(lib().ringx_linear_bwd_workspace_bytes(x_stride, heads, tokens, M, K, O, int(act), int(dtype)))
+
+
+def ringx_linear(x, w, bias=None, act="none", residual=None, need_pre: bool = False, y=None, pre=None,
+                 workspace=None, stream=None):
+    """y = act(x w^T + bias) + residual.  x [..., K] (rows contiguous, of any one stride), or 4-D: an
+    attention's output [B,H,N,d] with H d = K, whose rows are tokens; w [O, K] in x's dtype; bias fp32 [O];
+    residual [..., O] ([B, N, O] for 4-D x); act: "none", "gelu", "gelu_tanh", "silu".  Returns (y [..., O],
+    pre: the activation's input, what the backward needs, or None with need_pre=False)."""
+    torch = _T or _torch()
+    step, heads, tokens, M, K, O, lead = _linear_args(x, w)
+    code, a = _dtype_code(x), _act_code(act)
+    shape = (*lead, O)
+    pb, pr = _vector("bias", bias, O, x.device), _same("residual", residual, shape, x)
+    y = _out("y", y, shape, x.dtype, x, stream)
+    if need_pre or pre is not None:
+        pre = _out("pre", pre, shape, x.dtype, x, stream)
+    need = ringx_linear_workspace_bytes(step, heads, tokens, M, K, O, code)
+    if workspace is not None or need:
+        workspace = _workspace(workspace, need, x, stream)
+    _launch("ringx_linear", x, stream, x.data_ptr(), step, heads, tokens, w.data_ptr(), pb, pr, y.data_ptr(),
+            _ptr(pre), M, K, O, a, code, _ptr(workspace), 0 if workspace is None else _nbytes(workspace))
+    return y, pre
+
+
+def ringx_linear_bwd(x, w, dy, pre=None, act="none", bias=None, need_dx: bool = True,
+                     need_dw: bool = True, dx=None, dw=None, dbias=None, dw_dtype=None,
+                     accumulate_dw=False, workspace=None, stream=None):
+    """Backward of ringx_linear from dy [..., O] and, with an activation, the forward's pre.  Returns (dx like x
+    and contiguous, dw [O, K] in dw_dtype (fp32 by default, or x's dtype), dbias fp32 [O], None where there is
+    no bias); dx or dw is None where it is not needed.  accumulate_dw: dw and dbias (fp32) are added to."""
+    torch = _T or _torch()
+    step, heads, tokens, M, K, O, lead = _linear_args(x, w)
+    code, a = _dtype_code(x), _act_code(act)
+    shape = (*lead, O)
+    _same("dy", dy, shape, x)
+    pp = _same("pre", pre, shape, x)
+    _vector("bias", bias, O, x.device)
+    if bias is None and dbias is not None:
+        raise ValueError("a bias's gradient without the bias")
+    if dw is not None:
+        dw_dtype = dw.dtype if dw_dtype is None else dw_dtype
+    dw_dtype = torch.float32 if dw_dtype is None else dw_dtype
+    if dw_dtype is not torch.float32 and dw_dtype is not x.dtype:
+        raise TypeError(f"dw_dtype: {dw_dtype}, expected float32 or {x.dtype}")
+    if need_dx or dx is not None:
+        dx = _out("dx", dx, x.shape, x.dtype, x, stream)
+    if need_dw or dw is not None:
+        if dw_dtype is torch.float32:
+            dw = _grad_out("dw", dw, (O, K), x, accumulate_dw, stream)
+        else:
+            dw = _out("dw", dw, (O, K), dw_dtype, x, stream)
+    if bias is not None:
+        dbias = _grad_out("dbias", dbias, (O,), x, accumulate_dw, stream)
+    workspace = _workspace(workspace, ringx_linear_bwd_workspace_bytes(step, heads, tokens, M, K, O, a, code),
+                           x, stream)
+    _launch("ringx_linear_bwd", x, stream, x.data_ptr(), step, heads, tokens, w.data_ptr(), dy.data_ptr(), pp,
+            _ptr(dx), _ptr(dw), _ptr(dbias), M, K, O, a, code,
+            RINGX_FP32 if dw_dtype is torch.float32 else RINGX_BF16, 1 if accumulate_dw else 0,
+            workspace.data_ptr(), _nbytes(workspace))
+    return dx, dw, dbias
