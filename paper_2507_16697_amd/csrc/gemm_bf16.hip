@@ -115,29 +115,20 @@ struct Feed {
       }
     }
   }
-  __device__ __forceinline__ u32x4 rsrc() const {
+  // The step whose first r has `rest` of them left (none: nothing is read, zeros arrive), then on to the
+  // next; dst: the wave's place.  No branch, so that a loop's body stays one.
+  __device__ __forceinline__ void issue(uint32_t dst, int rest) {
     const uint32_t n = left <= 0 ? 0u : left > (int64_t)kMostBytes ? kMostBytes : (uint32_t)left;
-    return u32x4{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, n, 0x00020000u};
-  }
-  __device__ __forceinline__ void next() {
+    const u32x4 d = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, rest > 0 ? n : 0u, 0x00020000u};
+    const bool inside = SLOW || chunk * 8 < rest;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u)
+      buffer_lds16(d, inside ? off[u] : kOutside, dst + u * THREADS * 16);
     int64_t s = step;
-    if (per && --in == 0) s += turn, in = per;
+    --in;
+    const bool end = per && in == 0;
+    s += end ? turn : 0, in = end ? per : in;
     base += s, left -= s;
-  }
-  // the step whose first r has `rest` of them left, then on to the next; dst: the wave's place
-  __device__ __forceinline__ void issue(uint32_t dst, int64_t rest) {
-    const u32x4 d = rsrc();
-    if (SLOW || rest >= 64) {
-#pragma unroll
-      for (int u = 0; u < kLoads; ++u) buffer_lds16(d, off[u], dst + u * THREADS * 16);
-    } else {
-      cold_path();
-      const bool inside = chunk * 8 < (int)rest;
-#pragma unroll
-      for (int u = 0; u < kLoads; ++u)
-        buffer_lds16(d, inside ? off[u] : kOutside, dst + u * THREADS * 16);
-    }
-    next();
   }
 };
 
@@ -186,7 +177,7 @@ struct Tile {
 };
 
 template <bool PS, bool QS, int TI, int TJ, int WI, int WJ>
-__global__ __launch_bounds__(64 * WI * WJ, 512 / (64 * WI * WJ) < 2 ? 2 : 2) void gemm_bf16_kernel(
+__global__ __launch_bounds__(64 * WI * WJ, 2) void gemm_bf16_kernel(
     GemmArgs a) {
   using C = Tile<TI, TJ, WI, WJ>;
   __shared__ __attribute__((aligned(1024))) char lds[2 * C::kStage];
@@ -223,39 +214,66 @@ __global__ __launch_bounds__(64 * WI * WJ, 512 / (64 * WI * WJ) < 2 ? 2 : 2) voi
 #pragma unroll
     for (int j = 0; j < C::kBJ; ++j) acc[i][j] = f32x16{};
 
-  int64_t rest = a.R - 64 * s0;   // of r, from the step to load on
-  if (s0 < s1) {
-    fp.issue(wdst, rest);
-    fq.issue(wdst + C::kP, rest);
+  // of r, from the step to load to the last one of this part
+  int rest = (int)min(a.R - 64 * s0, 64 * (s1 - s0));
+  auto issue = [&](uint32_t buf) {
+    fp.issue(wdst + buf, rest);
+    fq.issue(wdst + buf + C::kP, rest);
+    rest -= 64;
+  };
+  bf16x8 p[2][C::kBI], q[2][C::kBJ];
+  auto read = [&](int set, uint32_t buf, int k) {
+#pragma unroll
+    for (int j = 0; j < C::kBJ; ++j) q[set][j] = rq.get(lds + buf + C::kP, k, j);
+#pragma unroll
+    for (int i = 0; i < C::kBI; ++i) p[set][i] = rp.get(lds + buf, k, i);
+  };
+  auto multiply = [&](int set) {
+#pragma unroll
+    for (int i = 0; i < C::kBI; ++i)
+#pragma unroll
+      for (int j = 0; j < C::kBJ; ++j) acc[i][j] = mfma32(q[set][j], p[set][i], acc[i][j]);
+  };
+  // LDS reads beside the products, spread evenly.
+  constexpr int kProducts = C::kBI * C::kBJ, kReads = C::kBI * (PS ? 2 : 1) + C::kBJ * (QS ? 2 : 1);
+  constexpr int kPerProduct = (kReads + kProducts - 1) / kProducts;
+  auto mix = [&]() {
+#pragma unroll
+    for (int i = 0; i < kProducts; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, kPerProduct, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // Fragments are read one quarter of a step ahead, the first of the next step behind the barrier that
+  // ends the reads of this one, before its last products: those cover the barrier and the reads.
+  issue(0);
+  issue(C::kStage);
+  wait_vmem<Feed<PS, TI, C::kThreads>::kLoads + Feed<QS, TJ, C::kThreads>::kLoads>();
+  __syncthreads();
+  read(0, 0, 0);
+  uint32_t buf = 0;
+  for (int s = (int)(s1 - s0); s > 0; --s) {
+    __builtin_amdgcn_sched_barrier(0);
+    read(1, buf, 1);
+    multiply(0);
+    mix();
+    read(0, buf, 2);
+    multiply(1);
+    mix();
+    read(1, buf, 3);
+    multiply(0);
+    mix();
+    wait_vmem_all();
+    __syncthreads();
+    issue(buf);
+    buf = C::kStage - buf;
+    read(0, buf, 0);
+    multiply(1);
+    mix();
   }
   wait_vmem_all();
   __syncthreads();
-  int buf = 0;
-  for (int64_t s = s0; s < s1; ++s) {
-    rest -= 64;
-    if (s + 1 < s1) {
-      const uint32_t dst = wdst + (buf ^ 1) * C::kStage;
-      fp.issue(dst, rest);
-      fq.issue(dst + C::kP, rest);
-    }
-    const char* const tp = lds + buf * C::kStage;
-    const char* const tq = tp + C::kP;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      bf16x8 p[C::kBI], q[C::kBJ];
-#pragma unroll
-      for (int j = 0; j < C::kBJ; ++j) q[j] = rq.get(tq, k, j);
-#pragma unroll
-      for (int i = 0; i < C::kBI; ++i) p[i] = rp.get(tp, k, i);
-#pragma unroll
-      for (int i = 0; i < C::kBI; ++i)
-#pragma unroll
-        for (int j = 0; j < C::kBJ; ++j) acc[i][j] = mfma32(q[j], p[i], acc[i][j]);
-    }
-    wait_vmem_all();
-    __syncthreads();
-    buf ^= 1;
-  }
 
   // epilogue, 32 rows of i at a time, in the wave's own part of LDS
   GemmOut o = a.o;
@@ -281,16 +299,23 @@ __global__ __launch_bounds__(64 * WI * WJ, 512 / (64 * WI * WJ) < 2 ? 2 : 2) voi
         *reinterpret_cast<f32x4*>(stage + (lane & 31) * C::kPitch + 32 * bj + 8 * r + 4 * (lane >> 5)) =
             f32x4{acc[bi][bj][4 * r], acc[bi][bj][4 * r + 1], acc[bi][bj][4 * r + 2], acc[bi][bj][4 * r + 3]};
     __builtin_amdgcn_wave_barrier();
-#pragma unroll
+#pragma unroll 1
     for (int it = 0; it < 32 / kRows; ++it) {
       const int row = it * kRows + lane / kPer;
       const int64_t i = i0 + (wi * C::kBI + bi) * 32 + row;
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(stage + row * C::kPitch + jc);
-      const f32x4 hi = *reinterpret_cast<const f32x4*>(stage + row * C::kPitch + jc + 4);
-      float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      if (i < a.I && inside > 0) {
-        if (vec) finish<8, true, __bf16>(o, i, j, 8, bias, x);
-        else finish<8, false, __bf16>(o, i, j, inside, bias, x);
+      const float* const at = stage + row * C::kPitch + jc;
+      if (i >= a.I) continue;
+      if (vec) {
+        if (inside == 0) continue;
+        const f32x4 lo = *reinterpret_cast<const f32x4*>(at), hi = *reinterpret_cast<const f32x4*>(at + 4);
+        float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        finish<8, true, __bf16>(o, i, j, 8, bias, x);
+      } else {
+#pragma unroll 1
+        for (int e = 0; e < inside; ++e) {
+          float b1[1] = {o.bias ? o.bias[j + e] : 0.f}, x[1] = {at[e]};
+          finish<1, false, __bf16>(o, i, j + e, 1, b1, x);
+        }
       }
     }
     __builtin_amdgcn_wave_barrier();
