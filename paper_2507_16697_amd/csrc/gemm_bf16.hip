@@ -22,6 +22,9 @@
 
 #include "linear.h"
 
+#ifndef RINGX_WJ
+#define RINGX_WJ 4
+#endif
 namespace ringx {
 namespace {
 
@@ -115,20 +118,27 @@ struct Feed {
       }
     }
   }
-  // The step whose first r has `rest` of them left (none: nothing is read, zeros arrive), then on to the
-  // next; dst: the wave's place.  No branch, so that a loop's body stays one.
-  __device__ __forceinline__ void issue(uint32_t dst, int rest) {
+  // The loads of a step whose first r has `rest` of them left (none: nothing is read, zeros arrive), one
+  // by one, then on to the next step.  No branch, so that a loop's body stays one.
+  u32x4 rsrc;
+  bool inside;
+  __device__ __forceinline__ void begin(int rest) {
     const uint32_t n = left <= 0 ? 0u : left > (int64_t)kMostBytes ? kMostBytes : (uint32_t)left;
-    const u32x4 d = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, rest > 0 ? n : 0u, 0x00020000u};
-    const bool inside = SLOW || chunk * 8 < rest;
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u)
-      buffer_lds16(d, inside ? off[u] : kOutside, dst + u * THREADS * 16);
+    rsrc = u32x4{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, rest > 0 ? n : 0u, 0x00020000u};
+    inside = SLOW || chunk * 8 < rest;
     int64_t s = step;
     --in;
     const bool end = per && in == 0;
     s += end ? turn : 0, in = end ? per : in;
     base += s, left -= s;
+  }
+  __device__ __forceinline__ void load(int u, uint32_t dst) const {   // dst: the wave's place
+    buffer_lds16(rsrc, inside ? off[u] : kOutside, dst + u * THREADS * 16);
+  }
+  __device__ __forceinline__ void all(uint32_t dst, int rest) {
+    begin(rest);
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) load(u, dst);
   }
 };
 
@@ -177,7 +187,7 @@ struct Tile {
 };
 
 template <bool PS, bool QS, int TI, int TJ, int WI, int WJ>
-__global__ __launch_bounds__(64 * WI * WJ, 2) void gemm_bf16_kernel(
+__global__ __launch_bounds__(64 * WI * WJ, TI * TJ > 64 * 128 * WI * WJ ? 1 : 2) void gemm_bf16_kernel(
     GemmArgs a) {
   using C = Tile<TI, TJ, WI, WJ>;
   __shared__ __attribute__((aligned(1024))) char lds[2 * C::kStage];
@@ -214,63 +224,58 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void gemm_bf16_kernel(
 #pragma unroll
     for (int j = 0; j < C::kBJ; ++j) acc[i][j] = f32x16{};
 
-  // of r, from the step to load to the last one of this part
-  int rest = (int)min(a.R - 64 * s0, 64 * (s1 - s0));
-  auto issue = [&](uint32_t buf) {
-    fp.issue(wdst + buf, rest);
-    fq.issue(wdst + buf + C::kP, rest);
-    rest -= 64;
-  };
+  int rest = (int)min(a.R - 64 * s0, 64 * (s1 - s0));   // of r, in this part from the step at hand on
   bf16x8 p[2][C::kBI], q[2][C::kBJ];
-  auto read = [&](int set, uint32_t buf, int k) {
-#pragma unroll
-    for (int j = 0; j < C::kBJ; ++j) q[set][j] = rq.get(lds + buf + C::kP, k, j);
-#pragma unroll
-    for (int i = 0; i < C::kBI; ++i) p[set][i] = rp.get(lds + buf, k, i);
-  };
-  auto multiply = [&](int set) {
-#pragma unroll
-    for (int i = 0; i < C::kBI; ++i)
-#pragma unroll
-      for (int j = 0; j < C::kBJ; ++j) acc[i][j] = mfma32(q[set][j], p[set][i], acc[i][j]);
-  };
-  // LDS reads beside the products, spread evenly.
-  constexpr int kProducts = C::kBI * C::kBJ, kReads = C::kBI * (PS ? 2 : 1) + C::kBJ * (QS ? 2 : 1);
-  constexpr int kPerProduct = (kReads + kProducts - 1) / kProducts;
-  auto mix = [&]() {
+  // Quarter k - 1 of a step (k = 4: of the next one): its products, with the fragments of quarter k, from
+  // `buf`, and L of the next steps' loads between them.
+  constexpr int kProducts = C::kBI * C::kBJ, kFrags = C::kBI + C::kBJ;
+  auto quarter = [&](auto k, uint32_t buf, auto feed, auto loads) {
+    constexpr int K = decltype(k)::value, L = decltype(loads)::value, kSet = K & 1;
 #pragma unroll
     for (int i = 0; i < kProducts; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x100, kPerProduct, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+#pragma unroll
+      for (int u = i * L / kProducts; u < (i + 1) * L / kProducts; ++u) feed(u);
+#pragma unroll
+      for (int f = i * kFrags / kProducts; f < (i + 1) * kFrags / kProducts; ++f) {
+        if (f < C::kBJ) q[kSet][f] = rq.get(lds + buf + C::kP, K & 3, f);
+        else p[kSet][f - C::kBJ] = rp.get(lds + buf, K & 3, f - C::kBJ);
+      }
+      f32x16& c = acc[i / C::kBJ][i % C::kBJ];
+      c = mfma32(q[kSet ^ 1][i % C::kBJ], p[kSet ^ 1][i / C::kBJ], c);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_sched_barrier(0);
   };
-  // Fragments are read one quarter of a step ahead, the first of the next step behind the barrier that
-  // ends the reads of this one, before its last products: those cover the barrier and the reads.
-  issue(0);
-  issue(C::kStage);
-  wait_vmem<Feed<PS, TI, C::kThreads>::kLoads + Feed<QS, TJ, C::kThreads>::kLoads>();
+  auto nothing = [](int) {};
+  using std::integral_constant;
+  typedef integral_constant<int, 0> kNone;
+  typedef integral_constant<int, Feed<PS, TI, C::kThreads>::kLoads> kLoadsP;
+  typedef integral_constant<int, Feed<QS, TJ, C::kThreads>::kLoads> kLoadsQ;
+  // The next step's loads: P's behind the barrier that ends the reads of the buffer that they fill, Q's in
+  // the quarter after that.  Fragments are read a quarter ahead, those of a step's first quarter behind
+  // that same barrier, so that the last quarter's products cover the barrier and the reads.
+  fp.all(wdst, rest);
+  fq.all(wdst + C::kP, rest);
+  fp.all(wdst + C::kStage, rest - 64);
+  wait_vmem<kLoadsP::value>();
   __syncthreads();
-  read(0, 0, 0);
+#pragma unroll
+  for (int j = 0; j < C::kBJ; ++j) q[0][j] = rq.get(lds + C::kP, 0, j);
+#pragma unroll
+  for (int i = 0; i < C::kBI; ++i) p[0][i] = rp.get(lds, 0, i);
   uint32_t buf = 0;
   for (int s = (int)(s1 - s0); s > 0; --s) {
-    __builtin_amdgcn_sched_barrier(0);
-    read(1, buf, 1);
-    multiply(0);
-    mix();
-    read(0, buf, 2);
-    multiply(1);
-    mix();
-    read(1, buf, 3);
-    multiply(0);
-    mix();
+    rest -= 64;
+    fq.begin(rest);
+    quarter(integral_constant<int, 1>{}, buf,
+            [&](int u) { fq.load(u, wdst + C::kStage - buf + C::kP); }, kLoadsQ{});
+    quarter(integral_constant<int, 2>{}, buf, nothing, kNone{});
+    quarter(integral_constant<int, 3>{}, buf, nothing, kNone{});
     wait_vmem_all();
     __syncthreads();
-    issue(buf);
+    fp.begin(rest - 64);
+    quarter(integral_constant<int, 4>{}, C::kStage - buf, [&](int u) { fp.load(u, wdst + buf); },
+            kLoadsP{});
     buf = C::kStage - buf;
-    read(0, buf, 0);
-    multiply(1);
-    mix();
   }
   wait_vmem_all();
   __syncthreads();
@@ -339,7 +344,7 @@ hipError_t by_layout(const GemmArgs& a) {
 }  // namespace
 
 hipError_t launch_gemm_bf16(const GemmArgs& a) {
-  return gemm_bf16_large(a.I, a.J) ? by_layout<256, 256, 2, 4>(a) : by_layout<128, 128, 2, 2>(a);
+  return gemm_bf16_large(a.I, a.J) ? by_layout<256, 256, 2, RINGX_WJ>(a) : by_layout<128, 128, 2, 2>(a);
 }
 
 }  // namespace ringx
