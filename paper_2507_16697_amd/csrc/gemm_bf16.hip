@@ -22,8 +22,20 @@
 
 #include "linear.h"
 
-#ifndef RINGX_WJ
-#define RINGX_WJ 4
+#ifndef V_WJ
+#define V_WJ 4
+#endif
+#ifndef V_BK
+#define V_BK 64
+#endif
+#ifndef V_NS
+#define V_NS 2
+#endif
+#ifndef V_BK2
+#define V_BK2 64
+#endif
+#ifndef V_NS2
+#define V_NS2 2
 #endif
 namespace ringx {
 namespace {
@@ -49,12 +61,13 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
   return reinterpret_cast<int64_t>(uniform_ptr(reinterpret_cast<const void*>(x)));
 }
 
-// One operand's way into LDS, 64 of r at a time.
-template <bool SLOW, int W, int THREADS>
+// One operand's way into LDS, BK of r at a time.
+template <bool SLOW, int W, int THREADS, int BK>
 struct Feed {
-  static constexpr int kLoads = W * 128 / (THREADS * 16);
-  static constexpr int kRowChunks = SLOW ? W / 8 : 8;
-  static_assert(kLoads * THREADS * 16 == W * 128 && (!SLOW || W >= 128), "whole rounds of loads");
+  static constexpr int kLoads = W * BK * 2 / (THREADS * 16);
+  static constexpr int kRowChunks = SLOW ? W / 8 : BK / 8;
+  static_assert(kLoads * THREADS * 16 == W * BK * 2 && (!SLOW || W >= 128), "whole rounds of loads");
+  static_assert(SLOW || THREADS / kRowChunks % 16 == 0, "rounds keep the swizzle's phase");
   uint32_t off[kLoads];
   int64_t base, left;    // address of the step's first row or column; bytes from it to the tensor's end
   int64_t step, turn;    // bytes to the next step; what is added where a head (or batch) ends
@@ -62,10 +75,11 @@ struct Feed {
   int chunk;             // contiguous: the lane's first r of a step / 8
 
   static __device__ __forceinline__ int swz(int row) {
-    return SLOW ? ((row & 3) << 2) | ((row >> 2) & 3) : (row >> 1) & 7;
+    if (SLOW) return ((row & 3) << 2) | ((row >> 2) & 3);
+    return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
   }
 
-  // width index w0 and r0 (a multiple of 64) on
+  // width index w0 and r0 (a multiple of BK) on
   __device__ __forceinline__ void start(const GemmIn& x, int64_t w0, int64_t r0, int tid) {
     const int64_t total = x.heads ? x.rows * x.cols : (x.rows - 1) * x.ld + x.cols;
     int64_t at;   // elements from the tensor's start
@@ -73,22 +87,22 @@ struct Feed {
     if constexpr (!SLOW) {
       if (x.heads) {
         const int64_t b = w0 / x.tokens;
-        const int hd = (int)(x.d / 64), s = (int)(r0 / 64);
-        at = b * x.tokens * x.cols + s / hd * x.tokens * x.d + s % hd * 64;
-        step = 128, per = hd, in = hd - s % hd;
+        const int hd = (int)(x.d / BK), s = (int)(r0 / BK);
+        at = b * x.tokens * x.cols + s / hd * x.tokens * x.d + s % hd * BK;
+        step = 2 * BK, per = hd, in = hd - s % hd;
         turn = (x.tokens * x.d - x.d) * 2;
       } else {
         at = w0 * x.ld + r0;
-        step = 128;
+        step = 2 * BK;
       }
     } else if (x.heads) {
       const int64_t b = r0 / x.tokens, t = r0 % x.tokens;
       at = b * x.tokens * x.cols + t * x.d;
-      step = 128 * x.d, per = (int)(x.tokens / 64), in = (int)((x.tokens - t) / 64);
+      step = 2 * BK * x.d, per = (int)(x.tokens / BK), in = (int)((x.tokens - t) / BK);
       turn = (x.cols - x.d) * x.tokens * 2;
     } else {
       at = r0 * x.ld + w0;
-      step = 128 * x.ld;
+      step = 2 * BK * x.ld;
     }
     base = uniform64(reinterpret_cast<int64_t>(x.p) + 2 * at);
     left = uniform64(2 * (total - at));
@@ -142,55 +156,60 @@ struct Feed {
   }
 };
 
-// Fragments of 32 of the width x 16 of r: lane l has width index l % 32 and r = 8 (l / 32) .. + 7.
-template <bool SLOW, int W, int BLOCKS>
+// Fragments of 16 of the width x 32 of r: lane l has width index l % 16 and r = 8 (l / 16) .. + 7.
+template <bool SLOW, int W, int BLOCKS, int BK>
 struct Frags {
-  int off[SLOW ? 2 : 4][SLOW ? BLOCKS : 1];
+  using F = Feed<SLOW, W, 512, BK>;
+  static constexpr int kCols = BLOCKS < 4 ? BLOCKS : 4;   // 64 columns further on the swizzle is the same
+  int off[SLOW ? 2 : BK / 32][SLOW ? kCols : 1];
   __device__ __forceinline__ void start(int w0, int lane) {   // w0: the wave's first of the tile
-    const int n = lane & 31, g = lane >> 5;
+    const int g = lane >> 4;
     if constexpr (!SLOW) {
-      const int row = w0 + n;
+      const int row = w0 + (lane & 15);
 #pragma unroll
-      for (int s = 0; s < 4; ++s) off[s][0] = row * 128 + (((2 * s + g) ^ ((row >> 1) & 7)) << 4);
+      for (int s = 0; s < BK / 32; ++s) off[s][0] = row * (2 * BK) + (((4 * s + g) ^ F::swz(row)) << 4);
     } else {
       const int rr = (lane & 15) >> 2;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) {
+        for (int b = 0; b < kCols; ++b) {
           const int row = 8 * g + 4 * h + rr;
-          const int col = w0 + 32 * b + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-          off[h][b] = row * (2 * W) + (((col >> 3) ^ Feed<true, W, W * 8>::swz(row)) << 4) + (col & 7) * 2;
+          const int col = w0 + 16 * b + 4 * (lane & 3);
+          off[h][b] = row * (2 * W) + (((col >> 3) ^ F::swz(row)) << 4) + (col & 7) * 2;
         }
     }
   }
   __device__ __forceinline__ bf16x8 get(const char* tile, int s, int b) const {
     if constexpr (!SLOW) {
-      return *reinterpret_cast<const bf16x8*>(tile + off[s][0] + b * 32 * 128);
+      return *reinterpret_cast<const bf16x8*>(tile + off[s][0] + b * 16 * 2 * BK);
     } else {
+      // blocks 8 further are 256 bytes further, past the swizzle's bits; 4 further turn one of them
+      const int o = s * 32 * 2 * W + (b / 8) * 256;
+      const int flip = (b / 4 % 2) * 128;
       const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-          (lds_bf16x4*)(tile + off[0][b] + s * 16 * 2 * W));
+          (lds_bf16x4*)(tile + (off[0][b % 4] ^ flip) + o));
       const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-          (lds_bf16x4*)(tile + off[1][b] + s * 16 * 2 * W));
+          (lds_bf16x4*)(tile + (off[1][b % 4] ^ flip) + o));
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
   }
 };
 
-template <int TI, int TJ, int WI, int WJ>
+template <int TI, int TJ, int WI, int WJ, int BK, int NS>
 struct Tile {
   static constexpr int kThreads = 64 * WI * WJ;
-  static constexpr int kBI = TI / WI / 32, kBJ = TJ / WJ / 32;
-  static constexpr int kP = TI * 128, kStage = (TI + TJ) * 128;   // bytes
-  static constexpr int kPitch = 32 * kBJ + 4;                     // floats of a staged row
-  static_assert(WI * WJ * 32 * kPitch * 4 <= 2 * kStage, "staging fits");
+  static constexpr int kBI = TI / WI / 16, kBJ = TJ / WJ / 16;   // 16 x 16 blocks of a wave
+  static constexpr int kP = TI * BK * 2, kStage = (TI + TJ) * BK * 2;   // bytes
+  static constexpr int kPitch = 16 * kBJ + 4;                     // floats of a staged row
+  static_assert(BK == 64 && WI * WJ * 32 * kPitch * 4 <= NS * kStage, "staging fits");
 };
 
-template <bool PS, bool QS, int TI, int TJ, int WI, int WJ>
+template <bool PS, bool QS, int TI, int TJ, int WI, int WJ, int BK, int NS>
 __global__ __launch_bounds__(64 * WI * WJ, TI * TJ > 64 * 128 * WI * WJ ? 1 : 2) void gemm_bf16_kernel(
     GemmArgs a) {
-  using C = Tile<TI, TJ, WI, WJ>;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * C::kStage];
+  using C = Tile<TI, TJ, WI, WJ, BK, NS>;
+  __shared__ __attribute__((aligned(1024))) char lds[NS * C::kStage];
   const uint32_t lbase = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -205,77 +224,84 @@ __global__ __launch_bounds__(64 * WI * WJ, TI * TJ > 64 * 128 * WI * WJ ? 1 : 2)
   id -= g0 * tj;
   const int64_t i0 = (int64_t)(g0 + id % gn) * TI, j0 = (int64_t)(id / gn) * TJ;
 
-  const int64_t steps = (a.R + 63) / 64;
+  const int64_t steps = (a.R + BK - 1) / BK;
   const int64_t s0 = steps * split / a.splits, s1 = steps * (split + 1) / a.splits;
-  Feed<PS, TI, C::kThreads> fp;
-  Feed<QS, TJ, C::kThreads> fq;
-  fp.start(a.P, i0, 64 * s0, tid);
-  fq.start(a.Q, j0, 64 * s0, tid);
+  Feed<PS, TI, C::kThreads, BK> fp;
+  Feed<QS, TJ, C::kThreads, BK> fq;
+  fp.start(a.P, i0, BK * s0, tid);
+  fq.start(a.Q, j0, BK * s0, tid);
   const int wi = wave / WJ, wj = wave % WJ;
-  Frags<PS, TI, C::kBI> rp;
-  Frags<QS, TJ, C::kBJ> rq;
-  rp.start(wi * 32 * C::kBI, lane);
-  rq.start(wj * 32 * C::kBJ, lane);
+  Frags<PS, TI, C::kBI, BK> rp;
+  Frags<QS, TJ, C::kBJ, BK> rq;
+  rp.start(wi * 16 * C::kBI, lane);
+  rq.start(wj * 16 * C::kBJ, lane);
   const uint32_t wdst = (uint32_t)__builtin_amdgcn_readfirstlane(lbase + wave * 1024);
 
-  f32x16 acc[C::kBI][C::kBJ];
+  f32x4 acc[C::kBI][C::kBJ];
 #pragma unroll
   for (int i = 0; i < C::kBI; ++i)
 #pragma unroll
-    for (int j = 0; j < C::kBJ; ++j) acc[i][j] = f32x16{};
+    for (int j = 0; j < C::kBJ; ++j) acc[i][j] = f32x4{};
 
-  int rest = (int)min(a.R - 64 * s0, 64 * (s1 - s0));   // of r, in this part from the step at hand on
-  bf16x8 p[2][C::kBI], q[2][C::kBJ];
-  // Quarter k - 1 of a step (k = 4: of the next one): its products, with the fragments of quarter k, from
-  // `buf`, and L of the next steps' loads between them.
-  constexpr int kProducts = C::kBI * C::kBJ, kFrags = C::kBI + C::kBJ;
-  auto quarter = [&](auto k, uint32_t buf, auto feed, auto loads) {
-    constexpr int K = decltype(k)::value, L = decltype(loads)::value, kSet = K & 1;
+  int rest = (int)min(a.R - BK * s0, BK * (s1 - s0));   // of r, in this part from the step to load on
+  // A step is four units: 32 of r, half of the wave's i.  Unit T - 1's products, beside them the reads of unit T
+  // of the step in `buf` and L of a later step's loads.
+  constexpr int kHalf = C::kBI / 2, kProducts = kHalf * C::kBJ;
+  bf16x8 p[2][kHalf], q[2][C::kBJ];
+  auto unit = [&](auto t, uint32_t buf, auto feed, auto loads) {
+    constexpr int T = decltype(t)::value, L = decltype(loads)::value, U = (T + 3) % 4;
+    constexpr int kReadsQ = T % 2 == 0 ? C::kBJ : 0, kFrags = kReadsQ + kHalf;
 #pragma unroll
     for (int i = 0; i < kProducts; ++i) {
 #pragma unroll
       for (int u = i * L / kProducts; u < (i + 1) * L / kProducts; ++u) feed(u);
 #pragma unroll
       for (int f = i * kFrags / kProducts; f < (i + 1) * kFrags / kProducts; ++f) {
-        if (f < C::kBJ) q[kSet][f] = rq.get(lds + buf + C::kP, K & 3, f);
-        else p[kSet][f - C::kBJ] = rp.get(lds + buf, K & 3, f - C::kBJ);
+        if (f < kReadsQ) q[T / 2][f] = rq.get(lds + buf + C::kP, T / 2, f);
+        else p[T % 2][f - kReadsQ] = rp.get(lds + buf, T / 2, T % 2 * kHalf + f - kReadsQ);
       }
-      f32x16& c = acc[i / C::kBJ][i % C::kBJ];
-      c = mfma32(q[kSet ^ 1][i % C::kBJ], p[kSet ^ 1][i / C::kBJ], c);
+      f32x4& c = acc[U % 2 * kHalf + i / C::kBJ][i % C::kBJ];
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[U / 2][i % C::kBJ], p[U % 2][i / C::kBJ], c, 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
   auto nothing = [](int) {};
   using std::integral_constant;
   typedef integral_constant<int, 0> kNone;
-  typedef integral_constant<int, Feed<PS, TI, C::kThreads>::kLoads> kLoadsP;
-  typedef integral_constant<int, Feed<QS, TJ, C::kThreads>::kLoads> kLoadsQ;
-  // The next step's loads: P's behind the barrier that ends the reads of the buffer that they fill, Q's in
-  // the quarter after that.  Fragments are read a quarter ahead, those of a step's first quarter behind
-  // that same barrier, so that the last quarter's products cover the barrier and the reads.
-  fp.all(wdst, rest);
-  fq.all(wdst + C::kP, rest);
-  fp.all(wdst + C::kStage, rest - 64);
-  wait_vmem<kLoadsP::value>();
+  typedef integral_constant<int, Feed<PS, TI, C::kThreads, BK>::kLoads> kLoadsP;
+  typedef integral_constant<int, Feed<QS, TJ, C::kThreads, BK>::kLoads> kLoadsQ;
+  constexpr int kLoads = kLoadsP::value + kLoadsQ::value;
+  auto after = [](uint32_t buf) { return buf == (NS - 1) * C::kStage ? 0u : buf + C::kStage; };
+  // NS buffers.  A step's buffer is free behind the barrier after its last reads; the loads of NS steps
+  // later go there, P's beside the products that follow, Q's beside the next ones.  Fragments are read one
+  // part ahead, those of a step's first part behind that same barrier, so that the last part's
+  // products cover the barrier and the reads.
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    fp.all(wdst + n * C::kStage, rest);
+    if (n < NS - 1) {
+      fq.all(wdst + n * C::kStage + C::kP, rest);
+      rest -= BK;
+    }
+  }
+  wait_vmem<(NS - 2) * kLoads + kLoadsP::value>();
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < C::kBJ; ++j) q[0][j] = rq.get(lds + C::kP, 0, j);
 #pragma unroll
-  for (int i = 0; i < C::kBI; ++i) p[0][i] = rp.get(lds, 0, i);
-  uint32_t buf = 0;
+  for (int i = 0; i < kHalf; ++i) p[0][i] = rp.get(lds, 0, i);
+  uint32_t buf = 0, last = (NS - 1) * C::kStage;   // the step's buffer, that of the step before it
   for (int s = (int)(s1 - s0); s > 0; --s) {
-    rest -= 64;
     fq.begin(rest);
-    quarter(integral_constant<int, 1>{}, buf,
-            [&](int u) { fq.load(u, wdst + C::kStage - buf + C::kP); }, kLoadsQ{});
-    quarter(integral_constant<int, 2>{}, buf, nothing, kNone{});
-    quarter(integral_constant<int, 3>{}, buf, nothing, kNone{});
-    wait_vmem_all();
+    unit(integral_constant<int, 1>{}, buf, [&](int u) { fq.load(u, wdst + last + C::kP); }, kLoadsQ{});
+    rest -= BK;
+    unit(integral_constant<int, 2>{}, buf, nothing, kNone{});
+    unit(integral_constant<int, 3>{}, buf, nothing, kNone{});
+    wait_vmem<(NS - 2) * kLoads>();
     __syncthreads();
-    fp.begin(rest - 64);
-    quarter(integral_constant<int, 4>{}, C::kStage - buf, [&](int u) { fp.load(u, wdst + buf); },
-            kLoadsP{});
-    buf = C::kStage - buf;
+    fp.begin(rest);
+    last = buf, buf = after(buf);
+    unit(integral_constant<int, 0>{}, buf, [&](int u) { fp.load(u, wdst + last); }, kLoadsP{});
   }
   wait_vmem_all();
   __syncthreads();
@@ -283,9 +309,9 @@ __global__ __launch_bounds__(64 * WI * WJ, TI * TJ > 64 * 128 * WI * WJ ? 1 : 2)
   // epilogue, 32 rows of i at a time, in the wave's own part of LDS
   GemmOut o = a.o;
   float* const stage = reinterpret_cast<float*>(lds) + wave * 32 * C::kPitch;
-  constexpr int kPer = 4 * C::kBJ, kRows = 64 / kPer;   // lanes of a row, rows at a time
+  constexpr int kPer = 2 * C::kBJ, kRows = 64 / kPer;   // lanes of a row, rows at a time
   const int jc = lane % kPer * 8;
-  const int64_t j = j0 + wj * 32 * C::kBJ + jc;
+  const int64_t j = j0 + wj * 16 * C::kBJ + jc;
   const int inside = (int)max((int64_t)0, min((int64_t)8, a.J - j));
   const bool vec = a.J % 8 == 0 && o.d % 8 == 0;
   if (a.splits > 1) {
@@ -296,18 +322,18 @@ __global__ __launch_bounds__(64 * WI * WJ, TI * TJ > 64 * 128 * WI * WJ ? 1 : 2)
 #pragma unroll
   for (int e = 0; e < 8; ++e) bias[e] = o.bias && e < inside ? o.bias[j + e] : 0.f;
 #pragma unroll
-  for (int bi = 0; bi < C::kBI; ++bi) {
+  for (int bi = 0; bi < C::kBI; bi += 2) {
 #pragma unroll
-    for (int bj = 0; bj < C::kBJ; ++bj)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        *reinterpret_cast<f32x4*>(stage + (lane & 31) * C::kPitch + 32 * bj + 8 * r + 4 * (lane >> 5)) =
-            f32x4{acc[bi][bj][4 * r], acc[bi][bj][4 * r + 1], acc[bi][bj][4 * r + 2], acc[bi][bj][4 * r + 3]};
+      for (int bj = 0; bj < C::kBJ; ++bj)
+        *reinterpret_cast<f32x4*>(stage + (16 * h + (lane & 15)) * C::kPitch + 16 * bj + 4 * (lane >> 4)) =
+            acc[bi + h][bj];
     __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
     for (int it = 0; it < 32 / kRows; ++it) {
       const int row = it * kRows + lane / kPer;
-      const int64_t i = i0 + (wi * C::kBI + bi) * 32 + row;
+      const int64_t i = i0 + (wi * C::kBI + bi) * 16 + row;
       const float* const at = stage + row * C::kPitch + jc;
       if (i >= a.I) continue;
       if (vec) {
@@ -327,24 +353,25 @@ __global__ __launch_bounds__(64 * WI * WJ, TI * TJ > 64 * 128 * WI * WJ ? 1 : 2)
   }
 }
 
-template <bool PS, bool QS, int TI, int TJ, int WI, int WJ>
+template <bool PS, bool QS, int TI, int TJ, int WI, int WJ, int BK, int NS>
 hipError_t launch(const GemmArgs& a) {
   const int64_t tiles = ((a.I + TI - 1) / TI) * ((a.J + TJ - 1) / TJ) * a.splits;
-  hipLaunchKernelGGL((gemm_bf16_kernel<PS, QS, TI, TJ, WI, WJ>), dim3((uint32_t)tiles),
+  hipLaunchKernelGGL((gemm_bf16_kernel<PS, QS, TI, TJ, WI, WJ, BK, NS>), dim3((uint32_t)tiles),
                      dim3(64 * WI * WJ), 0, a.stream, a);
   return hipGetLastError();
 }
 
-template <int TI, int TJ, int WI, int WJ>
+template <int TI, int TJ, int WI, int WJ, int BK, int NS>
 hipError_t by_layout(const GemmArgs& a) {
-  if (a.p_slow) return launch<true, true, TI, TJ, WI, WJ>(a);
-  return a.q_slow ? launch<false, true, TI, TJ, WI, WJ>(a) : launch<false, false, TI, TJ, WI, WJ>(a);
+  if (a.p_slow) return launch<true, true, TI, TJ, WI, WJ, BK, NS>(a);
+  return a.q_slow ? launch<false, true, TI, TJ, WI, WJ, BK, NS>(a)
+                  : launch<false, false, TI, TJ, WI, WJ, BK, NS>(a);
 }
 
 }  // namespace
 
 hipError_t launch_gemm_bf16(const GemmArgs& a) {
-  return gemm_bf16_large(a.I, a.J) ? by_layout<256, 256, 2, RINGX_WJ>(a) : by_layout<128, 128, 2, 2>(a);
+  return gemm_bf16_large(a.I, a.J) ? by_layout<256, 256, 2, V_WJ, V_BK, V_NS>(a) : by_layout<128, 128, 2, 2, V_BK2, V_NS2>(a);
 }
 
 }  // namespace ringx
