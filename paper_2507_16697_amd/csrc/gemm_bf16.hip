@@ -22,21 +22,6 @@
 
 #include "linear.h"
 
-#ifndef V_WJ
-#define V_WJ 4
-#endif
-#ifndef V_BK
-#define V_BK 64
-#endif
-#ifndef V_NS
-#define V_NS 2
-#endif
-#ifndef V_BK2
-#define V_BK2 64
-#endif
-#ifndef V_NS2
-#define V_NS2 2
-#endif
 namespace ringx {
 namespace {
 
@@ -196,36 +181,178 @@ struct Frags {
   }
 };
 
-template <int TI, int TJ, int WI, int WJ, int BK, int NS>
+constexpr int BK = 64;   // r of a step
+
+template <int TI, int TJ, int WI, int WJ>
 struct Tile {
+  static constexpr int kTI = TI, kTJ = TJ, kWI = WI, kWJ = WJ;
   static constexpr int kThreads = 64 * WI * WJ;
-  static constexpr int kBI = TI / WI / 16, kBJ = TJ / WJ / 16;   // 16 x 16 blocks of a wave
+  static constexpr int kBI = TI / WI / 16, kBJ = 4;               // 16 x 16 blocks of a wave
   static constexpr int kP = TI * BK * 2, kStage = (TI + TJ) * BK * 2;   // bytes
-  static constexpr int kPitch = 16 * kBJ + 4;                     // floats of a staged row
-  static_assert(BK == 64 && WI * WJ * 32 * kPitch * 4 <= NS * kStage, "staging fits");
+  static_assert(TJ == WJ * 64 && kBI % 2 == 0, "waves of 64 columns");
 };
 
-template <bool PS, bool QS, int TI, int TJ, int WI, int WJ, int BK, int NS>
-__global__ __launch_bounds__(64 * WI * WJ, TI * TJ > 64 * 128 * WI * WJ ? 1 : 2) void gemm_bf16_kernel(
-    GemmArgs a) {
-  using C = Tile<TI, TJ, WI, WJ, BK, NS>;
+// The values of a wave's 16 rows x 64 columns on their way out: x[b][e] is row l % 16, column 16 b + 4 (l / 16)
+// + e.  Where rows come in 16-byte pieces, bf16 pairs change places among the four lanes of a row, so that
+// each has 16 neighbouring columns: two 16-byte stores, whole 128-byte lines of a row.  Otherwise, through
+// LDS, a lane takes one column of row after row.
+struct Out {
+  static constexpr int kPitch = 65;                 // floats of a staged row
+  static constexpr int kStage = 16 * kPitch;        // floats of a wave
+  int64_t j0;                                       // the wave's first column
+  int n, g;
+  bool vec;
+  f32x4 bias[4];
+  int64_t col[2];                                   // of the lane's two pieces, in an output of heads
+
+  __device__ __forceinline__ void start(const GemmOut& o, int64_t j0_, int lane) {
+    j0 = j0_, n = lane & 15, g = lane >> 4;
+    vec = o.f32 ? o.J % 4 == 0 : o.J % 8 == 0 && o.d % 8 == 0;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int64_t j = j0 + 16 * b + 4 * g;
+      bias[b] = f32x4{};
+      if (o.bias) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bias[b][e] = j + e < o.J ? o.bias[j + e] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t j = (uint32_t)(j0 + 16 * g + 8 * h);
+      col[h] = j;
+      if (o.heads) {
+        const uint32_t head = j / (uint32_t)o.d;
+        col[h] = (int64_t)head * o.tokens * o.d + (j - head * (uint32_t)o.d);
+      }
+    }
+  }
+  // register b of lane group g <-> register g of lane group b
+  static __device__ __forceinline__ void transpose(u32x2 (&v)[4]) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const auto r = __builtin_amdgcn_permlane32_swap(v[b][w], v[b + 2][w], false, false);
+        v[b][w] = r[0], v[b + 2][w] = r[1];
+      }
+#pragma unroll
+      for (int b = 0; b < 4; b += 2) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v[b][w], v[b + 1][w], false, false);
+        v[b][w] = r[0], v[b + 1][w] = r[1];
+      }
+    }
+  }
+  // rows' 64 columns in bf16 at p (the row's first value plus the lane's columns), where they exist
+  __device__ __forceinline__ void store(__bf16* p, const int64_t (&at)[2], bool live, int64_t J,
+                                        const f32x4 (&x)[4]) const {
+    u32x2 v[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+      v[b] = u32x2{pack_bf16x2(x[b][0], x[b][1]), pack_bf16x2(x[b][2], x[b][3])};
+    transpose(v);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (live && j0 + 16 * g + 8 * h < J)
+        *reinterpret_cast<u32x4*>(p + at[h]) = u32x4{v[2 * h][0], v[2 * h][1], v[2 * h + 1][0], v[2 * h + 1][1]};
+  }
+  __device__ __forceinline__ void rows(const GemmOut& o, int64_t I, int64_t i0, f32x4 (&x)[4],
+                                       float* stage) const {
+    const int64_t i = i0 + n;
+    const bool live = i < I;
+    if (!vec) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) stage[n * kPitch + 16 * b + 4 * g + e] = x[b][e];
+      __builtin_amdgcn_wave_barrier();
+      const int lane = 16 * g + n;
+      const int64_t j = j0 + lane;
+      float b1[1] = {o.bias && j < o.J ? o.bias[j] : 0.f};
+#pragma unroll 1
+      for (int r = 0; r < 16; ++r) {
+        float y[1] = {stage[r * kPitch + lane]};
+        if (i0 + r < I && j < o.J) finish<1, false, __bf16>(o, i0 + r, j, 1, b1, y);
+      }
+      __builtin_amdgcn_wave_barrier();
+      return;
+    }
+    const int64_t row = i * o.J;
+    if (o.f32) {
+      // products for the weights' gradient: no bias, activation or residual
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int64_t j = j0 + 16 * b + 4 * g;
+        f32x4* const p = reinterpret_cast<f32x4*>((float*)o.out + row + j);
+        if (live && j < o.J) *p = o.accumulate ? *p + x[b] : x[b];
+      }
+      return;
+    }
+    const int64_t flat[2] = {j0 + 16 * g, j0 + 16 * g + 8};
+#pragma unroll
+    for (int b = 0; b < 4; ++b) x[b] += bias[b];
+    if (o.pre) store((__bf16*)o.pre + row, flat, live, o.J, x);
+    if (o.act != RINGX_ACT_NONE) {
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[b][e] = activate(x[b][e], o.act);
+    }
+    if (o.residual) {
+      u32x2 v[4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4 y = {};
+        if (live && flat[h] < o.J) y = *reinterpret_cast<const u32x4*>((const __bf16*)o.residual + row + flat[h]);
+        v[2 * h] = u32x2{y[0], y[1]}, v[2 * h + 1] = u32x2{y[2], y[3]};
+      }
+      transpose(v);
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        x[b] += f32x4{bf16_lo(v[b][0]), bf16_hi(v[b][0]), bf16_lo(v[b][1]), bf16_hi(v[b][1])};
+    }
+    int64_t first = row;
+    if (o.heads) {
+      const uint32_t b = (uint32_t)i / (uint32_t)o.tokens, t = (uint32_t)i - b * (uint32_t)o.tokens;
+      first = (int64_t)b * o.tokens * o.J + t * o.d;
+    }
+    store((__bf16*)o.out + first, col, live, o.J, x);
+  }
+};
+
+// Tile t of a product: tiles in groups of 4 along i, so that those at work on one XCD share operands.
+__device__ __forceinline__ void place(uint32_t t, uint32_t ti, uint32_t tj, uint32_t& i, uint32_t& j) {
+  constexpr uint32_t kGroup = 4;
+  const uint32_t g0 = t / (kGroup * tj) * kGroup, gn = min(kGroup, ti - g0);
+  t -= g0 * tj;
+  i = g0 + t % gn, j = t / gn;
+}
+
+template <bool PS, bool QS, class C>
+__global__ __launch_bounds__(C::kThreads, 2) void gemm_bf16_kernel(GemmArgs a) {
+  constexpr int TI = C::kTI, TJ = C::kTJ, WJ = C::kWJ, NS = 2;
   __shared__ __attribute__((aligned(1024))) char lds[NS * C::kStage];
+  static_assert(C::kThreads / 64 * Out::kStage * 4 <= NS * C::kStage, "staging fits");
   const uint32_t lbase = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  // the workgroup's tile: tiles in groups of 4 along i, so that those at work on one XCD share operands
-  constexpr uint32_t kGroup = 4;
+  // whole tiles first, then the last ones in parts along r
   const uint32_t ti = (uint32_t)((a.I + TI - 1) / TI), tj = (uint32_t)((a.J + TJ - 1) / TJ);
-  uint32_t id = xcd_remap(blockIdx.x, gridDim.x);
-  const uint32_t split = id / (ti * tj);
-  id -= split * ti * tj;
-  const uint32_t g0 = id / (kGroup * tj) * kGroup, gn = min(kGroup, ti - g0);
-  id -= g0 * tj;
-  const int64_t i0 = (int64_t)(g0 + id % gn) * TI, j0 = (int64_t)(id / gn) * TJ;
+  const uint32_t whole = a.cut.whole, parts = a.cut.parts;
+  uint32_t tile, of = 0, i_tile, j_tile;
+  const bool split = blockIdx.x >= whole && parts > 1;
+  if (blockIdx.x < whole) {
+    tile = xcd_remap(blockIdx.x, whole);
+  } else {
+    tile = whole + (blockIdx.x - whole) / parts;
+    of = (blockIdx.x - whole) % parts;
+  }
+  place(tile, ti, tj, i_tile, j_tile);
+  const int64_t i0 = (int64_t)i_tile * TI, j0 = (int64_t)j_tile * TJ;
 
   const int64_t steps = (a.R + BK - 1) / BK;
-  const int64_t s0 = steps * split / a.splits, s1 = steps * (split + 1) / a.splits;
+  const int64_t s0 = split ? steps * of / parts : 0, s1 = split ? steps * (of + 1) / parts : steps;
   Feed<PS, TI, C::kThreads, BK> fp;
   Feed<QS, TJ, C::kThreads, BK> fq;
   fp.start(a.P, i0, BK * s0, tid);
@@ -306,72 +433,74 @@ __global__ __launch_bounds__(64 * WI * WJ, TI * TJ > 64 * 128 * WI * WJ ? 1 : 2)
   wait_vmem_all();
   __syncthreads();
 
-  // epilogue, 32 rows of i at a time, in the wave's own part of LDS
-  GemmOut o = a.o;
-  float* const stage = reinterpret_cast<float*>(lds) + wave * 32 * C::kPitch;
-  constexpr int kPer = 2 * C::kBJ, kRows = 64 / kPer;   // lanes of a row, rows at a time
-  const int jc = lane % kPer * 8;
-  const int64_t j = j0 + wj * 16 * C::kBJ + jc;
-  const int inside = (int)max((int64_t)0, min((int64_t)8, a.J - j));
-  const bool vec = a.J % 8 == 0 && o.d % 8 == 0;
-  if (a.splits > 1) {
-    o = GemmOut{};
-    o.out = a.part + split * a.I * a.J, o.J = a.J, o.f32 = true;
+  if (split) {
+    // as it lies in the registers
+    f32x4* const part = reinterpret_cast<f32x4*>(a.part) + (int64_t)(blockIdx.x - whole) * (TI * TJ / 4);
+#pragma unroll
+    for (int bi = 0; bi < C::kBI; ++bi)
+#pragma unroll
+      for (int bj = 0; bj < C::kBJ; ++bj) part[(bi * C::kBJ + bj) * C::kThreads + tid] = acc[bi][bj];
+    return;
   }
-  float bias[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) bias[e] = o.bias && e < inside ? o.bias[j + e] : 0.f;
-#pragma unroll
-  for (int bi = 0; bi < C::kBI; bi += 2) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int bj = 0; bj < C::kBJ; ++bj)
-        *reinterpret_cast<f32x4*>(stage + (16 * h + (lane & 15)) * C::kPitch + 16 * bj + 4 * (lane >> 4)) =
-            acc[bi + h][bj];
-    __builtin_amdgcn_wave_barrier();
+  Out out;
+  out.start(a.o, j0 + wj * 64, lane);
+  float* const stage = reinterpret_cast<float*>(lds) + wave * Out::kStage;
+  // a loop whose code is there once: unrolled it is 130 KB, which every tile would fetch
 #pragma unroll 1
-    for (int it = 0; it < 32 / kRows; ++it) {
-      const int row = it * kRows + lane / kPer;
-      const int64_t i = i0 + (wi * C::kBI + bi) * 16 + row;
-      const float* const at = stage + row * C::kPitch + jc;
-      if (i >= a.I) continue;
-      if (vec) {
-        if (inside == 0) continue;
-        const f32x4 lo = *reinterpret_cast<const f32x4*>(at), hi = *reinterpret_cast<const f32x4*>(at + 4);
-        float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        finish<8, true, __bf16>(o, i, j, 8, bias, x);
-      } else {
-#pragma unroll 1
-        for (int e = 0; e < inside; ++e) {
-          float b1[1] = {o.bias ? o.bias[j + e] : 0.f}, x[1] = {at[e]};
-          finish<1, false, __bf16>(o, i, j + e, 1, b1, x);
-        }
+  for (int bi = 0; bi < C::kBI; ++bi) {
+    f32x4 x[4] = {};
+#pragma unroll
+    for (int k = 0; k < C::kBI; ++k) {
+      if (bi == k) {
+        cold_path();
+#pragma unroll
+        for (int b = 0; b < C::kBJ; ++b) x[b] = acc[k][b];
       }
     }
-    __builtin_amdgcn_wave_barrier();
+    out.rows(a.o, a.I, i0 + (wi * C::kBI + bi) * 16, x, stage);
   }
 }
 
-template <bool PS, bool QS, int TI, int TJ, int WI, int WJ, int BK, int NS>
-hipError_t launch(const GemmArgs& a) {
-  const int64_t tiles = ((a.I + TI - 1) / TI) * ((a.J + TJ - 1) / TJ) * a.splits;
-  hipLaunchKernelGGL((gemm_bf16_kernel<PS, QS, TI, TJ, WI, WJ, BK, NS>), dim3((uint32_t)tiles),
-                     dim3(64 * WI * WJ), 0, a.stream, a);
-  return hipGetLastError();
+// The parts of the last tiles, in their order, then the epilogue; blockIdx.y: which block of 16 rows of
+// every wave.
+template <class C>
+__global__ __launch_bounds__(C::kThreads) void gemm_join_kernel(GemmArgs a) {
+  __shared__ float lds[C::kThreads / 64 * Out::kStage];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), bi = blockIdx.y;
+  const uint32_t ti = (uint32_t)((a.I + C::kTI - 1) / C::kTI), tj = (uint32_t)((a.J + C::kTJ - 1) / C::kTJ);
+  uint32_t i, j;
+  place(a.cut.whole + blockIdx.x, ti, tj, i, j);
+  constexpr int64_t kSize = C::kTI * C::kTJ / 4;
+  const f32x4* const part =
+      reinterpret_cast<const f32x4*>(a.part) + (int64_t)blockIdx.x * a.cut.parts * kSize + bi * C::kBJ * C::kThreads + tid;
+  f32x4 x[4] = {};
+#pragma unroll 4
+  for (uint32_t s = 0; s < a.cut.parts; ++s)
+#pragma unroll
+    for (int b = 0; b < C::kBJ; ++b) x[b] += part[s * kSize + b * C::kThreads];
+  Out out;
+  out.start(a.o, (int64_t)j * C::kTJ + wave % C::kWJ * 64, tid & 63);
+  out.rows(a.o, a.I, (int64_t)i * C::kTI + (wave / C::kWJ * C::kBI + bi) * 16, x, lds + wave * Out::kStage);
 }
 
-template <int TI, int TJ, int WI, int WJ, int BK, int NS>
-hipError_t by_layout(const GemmArgs& a) {
-  if (a.p_slow) return launch<true, true, TI, TJ, WI, WJ, BK, NS>(a);
-  return a.q_slow ? launch<false, true, TI, TJ, WI, WJ, BK, NS>(a)
-                  : launch<false, false, TI, TJ, WI, WJ, BK, NS>(a);
+template <class C>
+hipError_t launch(const GemmArgs& a) {
+  const uint32_t tiles = (uint32_t)(((a.I + C::kTI - 1) / C::kTI) * ((a.J + C::kTJ - 1) / C::kTJ));
+  const uint32_t rest = tiles - a.cut.whole;
+  const dim3 grid(a.cut.whole + rest * a.cut.parts), threads(C::kThreads);
+  if (a.p_slow) hipLaunchKernelGGL((gemm_bf16_kernel<true, true, C>), grid, threads, 0, a.stream, a);
+  else if (a.q_slow) hipLaunchKernelGGL((gemm_bf16_kernel<false, true, C>), grid, threads, 0, a.stream, a);
+  else hipLaunchKernelGGL((gemm_bf16_kernel<false, false, C>), grid, threads, 0, a.stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.cut.parts == 1 || rest == 0) return e;
+  hipLaunchKernelGGL((gemm_join_kernel<C>), dim3(rest, C::kBI), threads, 0, a.stream, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_gemm_bf16(const GemmArgs& a) {
-  return gemm_bf16_large(a.I, a.J) ? by_layout<256, 256, 2, V_WJ, V_BK, V_NS>(a) : by_layout<128, 128, 2, 2, V_BK2, V_NS2>(a);
+  return a.cut.large ? launch<Tile<256, 256, 2, 4>>(a) : launch<Tile<128, 128, 2, 2>>(a);
 }
 
 }  // namespace ringx

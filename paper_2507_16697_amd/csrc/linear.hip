@@ -118,7 +118,7 @@ hipError_t launch_few_rows(const GemmArgs& a) {
 }
 
 // -------------------------------------------------------------------------------------------------
-// The parts of a split product, in their order, then its epilogue.
+// The parts of a split fp32 product, in their order, then its epilogue.
 
 template <class T, bool VEC>
 __global__ __launch_bounds__(256) void join_kernel(GemmArgs a) {
@@ -142,15 +142,18 @@ __global__ __launch_bounds__(256) void join_kernel(GemmArgs a) {
 
 template <class T>
 hipError_t launch_product(const GemmArgs& a) {
-  constexpr bool kBf16 = std::is_same_v<T, __bf16>;
-  hipError_t e = kBf16 ? launch_gemm_bf16(a) : launch_gemm_f32(a);
-  if (e != hipSuccess || a.splits == 1) return e;
-  const int64_t wgs = std::min<int64_t>((a.I * ((a.J + 3) / 4) + 255) / 256, 4096);
-  if (a.J % 4 == 0 && a.o.d % 4 == 0)
-    hipLaunchKernelGGL((join_kernel<T, true>), dim3((uint32_t)wgs), dim3(256), 0, a.stream, a);
-  else
-    hipLaunchKernelGGL((join_kernel<T, false>), dim3((uint32_t)wgs), dim3(256), 0, a.stream, a);
-  return hipGetLastError();
+  if constexpr (std::is_same_v<T, __bf16>) {
+    return launch_gemm_bf16(a);
+  } else {
+    const hipError_t e = launch_gemm_f32(a);
+    if (e != hipSuccess || a.splits == 1) return e;
+    const int64_t wgs = std::min<int64_t>((a.I * ((a.J + 3) / 4) + 255) / 256, 4096);
+    if (a.J % 4 == 0 && a.o.d % 4 == 0)
+      hipLaunchKernelGGL((join_kernel<T, true>), dim3((uint32_t)wgs), dim3(256), 0, a.stream, a);
+    else
+      hipLaunchKernelGGL((join_kernel<T, false>), dim3((uint32_t)wgs), dim3(256), 0, a.stream, a);
+    return hipGetLastError();
+  }
 }
 
 // -------------------------------------------------------------------------------------------------
@@ -330,7 +333,7 @@ hipError_t forward(const LinearArgs& a) {
   if (e == hipSuccess) e = operand<T>(g.Q, p.w, p.ldw, a.workspace, a.stream);
   if (e != hipSuccess) return e;
   g.R = p.R;
-  g.splits = p.splits, g.part = (float*)at(a.workspace, p.part);
+  g.splits = p.splits, g.cut = p.cut, g.part = (float*)at(a.workspace, p.part);
   return launch_product<T>(g);
 }
 
@@ -365,7 +368,7 @@ hipError_t backward(const LinearArgs& a) {
     e = operand<T>(g.Q, p.w, p.ldw, a.workspace, a.stream);
     if (e != hipSuccess) return e;
     g.q_slow = true;
-    g.I = a.s.M, g.J = a.s.K, g.R = dz.cols, g.splits = p.splits_dx;
+    g.I = a.s.M, g.J = a.s.K, g.R = dz.cols, g.splits = p.splits_dx, g.cut = p.cut_dx;
     g.o.out = a.dx, g.o.J = a.s.K;
     if (a.s.heads) g.o.heads = a.s.heads, g.o.tokens = a.s.tokens, g.o.d = a.s.K / a.s.heads;
     e = launch_product<T>(g);
@@ -376,7 +379,7 @@ hipError_t backward(const LinearArgs& a) {
     e = operand<T>(g.Q, p.x, p.ldx, a.workspace, a.stream);
     if (e != hipSuccess) return e;
     g.p_slow = g.q_slow = true;
-    g.I = a.s.O, g.J = a.s.K, g.R = a.s.M, g.splits = p.splits_dw;
+    g.I = a.s.O, g.J = a.s.K, g.R = a.s.M, g.splits = p.splits_dw, g.cut = p.cut_dw;
     g.o = GemmOut{};
     g.o.out = a.dw, g.o.J = a.s.K, g.o.f32 = a.dw_f32, g.o.accumulate = a.accumulate;
     e = launch_product<T>(g);

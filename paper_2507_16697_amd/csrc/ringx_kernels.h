@@ -484,30 +484,57 @@ struct GemmOut {
   int act = 0;
   bool f32 = false, accumulate = false;   // accumulate: fp32 out alone
 };
+// How a bf16 product is cut: tiles of 256 x 256 (large) or 128 x 128, the first `whole` of them to a workgroup
+// each, the others in `parts` along R, which a second launch joins.
+struct GemmCut {
+  bool large = false;
+  uint32_t whole = 0, parts = 1;
+  int64_t part_bytes = 0;
+};
 // out[i][j] = sum over r of P(i, r) Q(j, r); P is stored [I, R] or, with p_slow, [R, I]; Q likewise.
 struct GemmArgs {
   GemmIn P, Q;
   bool p_slow = false, q_slow = false;
   int64_t I = 0, J = 0, R = 0;
   GemmOut o;
-  int splits = 1;                  // parts of R, whose sums go to part [splits, I, J]
+  int splits = 1;                  // fp32: parts of R, whose sums go to part [splits, I, J]
+  GemmCut cut;                     // bf16
   float* part = nullptr;
   hipStream_t stream = nullptr;
 };
-// Whether a product takes large tiles (256 x 256 in bf16, 128 x 128 in fp32; else 128 x 128, 32 x 32).
-inline bool gemm_bf16_large(int64_t I, int64_t J) {
-  return ((I + 255) / 256) * ((J + 255) / 256) >= 192;
+// 256 workgroups of large tiles or 512 of small ones are at work at a time.  A last round that would not be full
+// has its tiles cut into parts along R.  Taken is what a model of the time finds shorter: a step of 64 of R
+// takes a full chip 1.3 us in either, a tile's start and end 6 and 4 us, the join 5 us.
+inline GemmCut gemm_cut(int64_t I, int64_t J, int64_t R) {
+  GemmCut best;
+  double least = 0.;
+  const int64_t steps = (R + 63) / 64;
+  for (int large = 1; large >= 0; --large) {
+    const int64_t side = large ? 256 : 128, slots = large ? 256 : 512;
+    const int64_t tiles = ((I + side - 1) / side) * ((J + side - 1) / side), rest = tiles % slots;
+    const double step = 1.3, ends = large ? 6. : 4.;
+    GemmCut c;
+    c.large = large;
+    int64_t parts = rest ? std::min<int64_t>({slots / rest, steps / 4, 32}) : 1;
+    if (parts < 2) parts = 1;
+    double t = (double)(tiles / slots) * (steps * step + ends);
+    if (rest) t += (double)((steps + parts - 1) / parts) * step + ends + (parts > 1 ? 5. : 0.);
+    c.parts = (uint32_t)parts;
+    c.whole = (uint32_t)(parts > 1 ? tiles - rest : tiles);
+    c.part_bytes = parts > 1 ? rest * parts * side * side * 4 : 0;
+    if (large || t < least) best = c, least = t;
+  }
+  return best;
 }
+// fp32: whether a product takes tiles of 128 x 128 (else 32 x 32), and parts that R is cut into where the
+// tiles do not fill the chip.
 inline bool gemm_f32_large(int64_t I, int64_t J) {
   return ((I + 127) / 128) * ((J + 127) / 128) >= 192;
 }
-// Parts that R is cut into where the tiles do not fill the chip.
-inline int gemm_splits(int64_t I, int64_t J, int64_t R, bool bf16) {
-  if (bf16 ? gemm_bf16_large(I, J) : gemm_f32_large(I, J)) return 1;
-  const int64_t side = bf16 ? 128 : 32;
-  const int64_t tiles = ((I + side - 1) / side) * ((J + side - 1) / side);
-  const int64_t steps = (R + 63) / 64;
-  const int64_t s = std::min<int64_t>({512 / tiles, steps / 4, 32});
+inline int gemm_f32_splits(int64_t I, int64_t J, int64_t R) {
+  if (gemm_f32_large(I, J)) return 1;
+  const int64_t tiles = ((I + 31) / 32) * ((J + 31) / 32);
+  const int64_t s = std::min<int64_t>({512 / tiles, (R + 63) / 64 / 4, 32});
   return (int)std::max<int64_t>(s, 1);
 }
 
@@ -566,7 +593,8 @@ struct LinearPlan {
   int64_t ldx = 0, ldw = 0, ldz = 0;       // their row lengths
   int64_t sums = -1, part = 0;             // parts of the bias's gradient, of split products
   int64_t R = 0;                           // forward: the product's r
-  int splits = 1, splits_dx = 1, splits_dw = 1;
+  int splits = 1, splits_dx = 1, splits_dw = 1;   // fp32
+  GemmCut cut, cut_dx, cut_dw;             // bf16
   int64_t bytes = 0;
   int64_t take(int64_t n) {
     const int64_t at = bytes;
@@ -594,8 +622,10 @@ inline LinearPlan linear_plan(const LinearShape& s) {
   } else if (s.heads || !linear_near(s)) {
     p.x = p.take(4 * s.M * s.K), p.ldx = s.K;
   }
-  p.splits = gemm_splits(s.M, s.O, p.R, s.bf16);
-  if (p.splits > 1) p.part = p.take(4 * p.splits * s.M * s.O);
+  if (s.bf16) p.cut = gemm_cut(s.M, s.O, p.R);
+  else p.splits = gemm_f32_splits(s.M, s.O, p.R);
+  const int64_t part = p.splits > 1 ? 4 * p.splits * s.M * s.O : p.cut.part_bytes;
+  if (part) p.part = p.take(part);
   return p;
 }
 inline LinearPlan linear_bwd_plan(const LinearShape& s, int act) {
@@ -613,11 +643,16 @@ inline LinearPlan linear_bwd_plan(const LinearShape& s, int act) {
   } else if (s.heads || !linear_near(s)) {
     p.x = p.take(4 * s.M * s.K), p.ldx = s.K;
   }
-  p.splits_dx = gemm_splits(s.M, s.K, Op, s.bf16);
-  p.splits_dw = gemm_splits(s.O, s.K, s.M, s.bf16);
   p.sums = p.take(4 * grad_grid(s.M, s.O).y * s.O);
-  const int64_t dx = p.splits_dx > 1 ? 4 * p.splits_dx * s.M * s.K : 0;
-  const int64_t dw = p.splits_dw > 1 ? 4 * p.splits_dw * s.O * s.K : 0;
+  int64_t dx = 0, dw = 0;
+  if (s.bf16) {
+    p.cut_dx = gemm_cut(s.M, s.K, Op), p.cut_dw = gemm_cut(s.O, s.K, s.M);
+    dx = p.cut_dx.part_bytes, dw = p.cut_dw.part_bytes;
+  } else {
+    p.splits_dx = gemm_f32_splits(s.M, s.K, Op), p.splits_dw = gemm_f32_splits(s.O, s.K, s.M);
+    if (p.splits_dx > 1) dx = 4 * p.splits_dx * s.M * s.K;
+    if (p.splits_dw > 1) dw = 4 * p.splits_dw * s.O * s.K;
+  }
   if (dx || dw) p.part = p.take(std::max(dx, dw));
   return p;
 }
