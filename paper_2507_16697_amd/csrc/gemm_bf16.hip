@@ -64,56 +64,69 @@ struct Feed {
     return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
   }
 
-  // width index w0 and r0 (a multiple of BK) on
-  __device__ __forceinline__ void start(const GemmIn& x, int64_t w0, int64_t r0, int tid) {
-    const int64_t total = x.heads ? x.rows * x.cols : (x.rows - 1) * x.ld + x.cols;
-    int64_t at;   // elements from the tensor's start
+  // Width index w0 and r0 (a multiple of BK) on.  Sizes fit 32 bits, which divisions are made in: with those
+  // of 64 bits a workgroup's start took 1400 instructions, 5 us.
+  __device__ __forceinline__ void start(const GemmIn& x, uint32_t w0, uint32_t r0, int tid) {
+    const uint32_t rows = (uint32_t)x.rows, cols = (uint32_t)x.cols, ld = (uint32_t)x.ld;
+    int64_t total = (int64_t)(rows - 1) * ld + cols, at;   // elements; from the tensor's start
     turn = 0, per = 0, in = 0;
     if constexpr (!SLOW) {
-      if (x.heads) {
-        const int64_t b = w0 / x.tokens;
-        const int hd = (int)(x.d / BK), s = (int)(r0 / BK);
-        at = b * x.tokens * x.cols + s / hd * x.tokens * x.d + s % hd * BK;
-        step = 2 * BK, per = hd, in = hd - s % hd;
-        turn = (x.tokens * x.d - x.d) * 2;
-      } else {
-        at = w0 * x.ld + r0;
-        step = 2 * BK;
-      }
-    } else if (x.heads) {
-      const int64_t b = r0 / x.tokens, t = r0 % x.tokens;
-      at = b * x.tokens * x.cols + t * x.d;
-      step = 2 * BK * x.d, per = (int)(x.tokens / BK), in = (int)((x.tokens - t) / BK);
-      turn = (x.cols - x.d) * x.tokens * 2;
+      at = (int64_t)w0 * ld + r0;
+      step = 2 * BK;
     } else {
-      at = r0 * x.ld + w0;
-      step = 2 * BK * x.ld;
+      at = (int64_t)r0 * ld + w0;
+      step = 2 * BK * (int64_t)ld;
+    }
+    const uint32_t d = (uint32_t)x.d, tokens = (uint32_t)x.tokens;
+    uint32_t b0 = 0;
+    if (x.heads) {
+      cold_path();
+      total = (int64_t)rows * cols;
+      if constexpr (!SLOW) {
+        b0 = w0 / tokens;
+        const uint32_t hd = d / BK, s = r0 / BK;
+        at = (int64_t)b0 * tokens * cols + (int64_t)(s / hd) * tokens * d + s % hd * BK;
+        per = (int)hd, in = (int)(hd - s % hd);
+        turn = 2 * ((int64_t)tokens * d - d);
+      } else {
+        b0 = r0 / tokens;
+        const uint32_t t = r0 - b0 * tokens;
+        at = (int64_t)b0 * tokens * cols + (int64_t)t * d;
+        step = 2 * BK * (int64_t)d;
+        per = (int)(tokens / BK), in = (int)((tokens - t) / BK);
+        turn = 2 * (int64_t)(cols - d) * tokens;
+      }
     }
     base = uniform64(reinterpret_cast<int64_t>(x.p) + 2 * at);
     left = uniform64(2 * (total - at));
     chunk = 0;
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
-      const int slot = u * THREADS + tid;
-      const int row = slot / kRowChunks;
-      const int c = (slot % kRowChunks) ^ swz(row);
+      const uint32_t slot = u * THREADS + tid;
+      const uint32_t row = slot / kRowChunks;
+      const uint32_t c = (slot % kRowChunks) ^ swz(row);
       if constexpr (!SLOW) {
-        chunk = c;   // the same for every u: rounds are whole multiples of 16 rows
-        const int64_t i = min(w0 + row, x.rows - 1);
-        int64_t o = (i - w0) * x.ld;
-        if (x.heads) {
-          const uint32_t b0 = (uint32_t)w0 / (uint32_t)x.tokens, b = (uint32_t)i / (uint32_t)x.tokens;
-          o = (int64_t)(b - b0) * x.tokens * x.cols + (i - (int64_t)b * x.tokens) * x.d;
-        }
-        off[u] = (uint32_t)(2 * o) + c * 16;
+        chunk = (int)c;   // the same for every u: rounds are whole multiples of 16 rows
+        off[u] = 2 * (min(w0 + row, rows - 1) - w0) * ld + c * 16;
       } else {
-        int64_t o = row * x.ld + c * 8;
-        if (x.heads) {
-          const uint32_t col = (uint32_t)min(w0 + c * 8, x.cols - 8);
-          const uint32_t h = col / (uint32_t)x.d;
-          o = h * x.tokens * x.d + (col - h * (uint32_t)x.d) + row * x.d;
+        off[u] = 2 * row * ld + c * 16;
+      }
+    }
+    if (x.heads) {
+      cold_path();
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        const uint32_t slot = u * THREADS + tid;
+        const uint32_t row = slot / kRowChunks;
+        const uint32_t c = (slot % kRowChunks) ^ swz(row);
+        if constexpr (!SLOW) {
+          const uint32_t i = min(w0 + row, rows - 1), b = i / tokens;
+          off[u] = 2 * ((b - b0) * tokens * cols + (i - b * tokens) * d) + c * 16;
+        } else {
+          const uint32_t col = min(w0 + c * 8, cols - 8);
+          const uint32_t h = col / d;
+          off[u] = 2 * (h * tokens * d + (col - h * d) + row * d);
         }
-        off[u] = (uint32_t)(2 * o);
       }
     }
   }
@@ -183,9 +196,9 @@ struct Frags {
 
 constexpr int BK = 64;   // r of a step
 
-template <int TI, int TJ, int WI, int WJ>
+template <int TI, int TJ, int WI, int WJ, int NS>
 struct Tile {
-  static constexpr int kTI = TI, kTJ = TJ, kWI = WI, kWJ = WJ;
+  static constexpr int kTI = TI, kTJ = TJ, kWI = WI, kWJ = WJ, kNS = NS;
   static constexpr int kThreads = 64 * WI * WJ;
   static constexpr int kBI = TI / WI / 16, kBJ = 4;               // 16 x 16 blocks of a wave
   static constexpr int kP = TI * BK * 2, kStage = (TI + TJ) * BK * 2;   // bytes
@@ -212,10 +225,7 @@ struct Out {
     for (int b = 0; b < 4; ++b) {
       const int64_t j = j0 + 16 * b + 4 * g;
       bias[b] = f32x4{};
-      if (o.bias) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) bias[b][e] = j + e < o.J ? o.bias[j + e] : 0.f;
-      }
+      if (o.bias && vec && j < o.J) bias[b] = *reinterpret_cast<const f32x4*>(o.bias + j);
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -293,10 +303,7 @@ struct Out {
     for (int b = 0; b < 4; ++b) x[b] += bias[b];
     if (o.pre) store((__bf16*)o.pre + row, flat, live, o.J, x);
     if (o.act != RINGX_ACT_NONE) {
-#pragma unroll
-      for (int b = 0; b < 4; ++b)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[b][e] = activate(x[b][e], o.act);
+      activate_all(x, o.act);
     }
     if (o.residual) {
       u32x2 v[4];
@@ -330,7 +337,7 @@ __device__ __forceinline__ void place(uint32_t t, uint32_t ti, uint32_t tj, uint
 
 template <bool PS, bool QS, class C>
 __global__ __launch_bounds__(C::kThreads, 2) void gemm_bf16_kernel(GemmArgs a) {
-  constexpr int TI = C::kTI, TJ = C::kTJ, WJ = C::kWJ, NS = 2;
+  constexpr int TI = C::kTI, TJ = C::kTJ, WJ = C::kWJ, NS = C::kNS;
   __shared__ __attribute__((aligned(1024))) char lds[NS * C::kStage];
   static_assert(C::kThreads / 64 * Out::kStage * 4 <= NS * C::kStage, "staging fits");
   const uint32_t lbase = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
@@ -338,7 +345,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void gemm_bf16_kernel(GemmArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   // whole tiles first, then the last ones in parts along r
-  const uint32_t ti = (uint32_t)((a.I + TI - 1) / TI), tj = (uint32_t)((a.J + TJ - 1) / TJ);
+  const uint32_t ti = ((uint32_t)a.I + TI - 1) / TI, tj = ((uint32_t)a.J + TJ - 1) / TJ;
   const uint32_t whole = a.cut.whole, parts = a.cut.parts;
   uint32_t tile, of = 0, i_tile, j_tile;
   const bool split = blockIdx.x >= whole && parts > 1;
@@ -349,10 +356,11 @@ __global__ __launch_bounds__(C::kThreads, 2) void gemm_bf16_kernel(GemmArgs a) {
     of = (blockIdx.x - whole) % parts;
   }
   place(tile, ti, tj, i_tile, j_tile);
-  const int64_t i0 = (int64_t)i_tile * TI, j0 = (int64_t)j_tile * TJ;
+  const uint32_t i0 = i_tile * TI, j0 = j_tile * TJ;
 
-  const int64_t steps = (a.R + BK - 1) / BK;
-  const int64_t s0 = split ? steps * of / parts : 0, s1 = split ? steps * (of + 1) / parts : steps;
+  const uint32_t steps = ((uint32_t)a.R + BK - 1) / BK;
+  uint32_t s0 = 0, s1 = steps;
+  if (split) s0 = steps * of / parts, s1 = steps * (of + 1) / parts;
   Feed<PS, TI, C::kThreads, BK> fp;
   Feed<QS, TJ, C::kThreads, BK> fq;
   fp.start(a.P, i0, BK * s0, tid);
@@ -370,7 +378,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void gemm_bf16_kernel(GemmArgs a) {
 #pragma unroll
     for (int j = 0; j < C::kBJ; ++j) acc[i][j] = f32x4{};
 
-  int rest = (int)min(a.R - BK * s0, BK * (s1 - s0));   // of r, in this part from the step to load on
+  int rest = (int)min((uint32_t)a.R - BK * s0, BK * (s1 - s0));   // of r, in this part from the step to load on
   // A step is four units: 32 of r, half of the wave's i.  Unit T - 1's products, beside them the reads of unit T
   // of the step in `buf` and L of a later step's loads.
   constexpr int kHalf = C::kBI / 2, kProducts = kHalf * C::kBJ;
@@ -443,7 +451,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void gemm_bf16_kernel(GemmArgs a) {
     return;
   }
   Out out;
-  out.start(a.o, j0 + wj * 64, lane);
+  out.start(a.o, (int64_t)j0 + wj * 64, lane);
   float* const stage = reinterpret_cast<float*>(lds) + wave * Out::kStage;
   // a loop whose code is there once: unrolled it is 130 KB, which every tile would fetch
 #pragma unroll 1
@@ -457,7 +465,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void gemm_bf16_kernel(GemmArgs a) {
         for (int b = 0; b < C::kBJ; ++b) x[b] = acc[k][b];
       }
     }
-    out.rows(a.o, a.I, i0 + (wi * C::kBI + bi) * 16, x, stage);
+    out.rows(a.o, a.I, (int64_t)i0 + (wi * C::kBI + bi) * 16, x, stage);
   }
 }
 
@@ -467,7 +475,7 @@ template <class C>
 __global__ __launch_bounds__(C::kThreads) void gemm_join_kernel(GemmArgs a) {
   __shared__ float lds[C::kThreads / 64 * Out::kStage];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), bi = blockIdx.y;
-  const uint32_t ti = (uint32_t)((a.I + C::kTI - 1) / C::kTI), tj = (uint32_t)((a.J + C::kTJ - 1) / C::kTJ);
+  const uint32_t ti = ((uint32_t)a.I + C::kTI - 1) / C::kTI, tj = ((uint32_t)a.J + C::kTJ - 1) / C::kTJ;
   uint32_t i, j;
   place(a.cut.whole + blockIdx.x, ti, tj, i, j);
   constexpr int64_t kSize = C::kTI * C::kTJ / 4;
@@ -484,9 +492,7 @@ __global__ __launch_bounds__(C::kThreads) void gemm_join_kernel(GemmArgs a) {
 }
 
 template <class C>
-hipError_t launch(const GemmArgs& a) {
-  const uint32_t tiles = (uint32_t)(((a.I + C::kTI - 1) / C::kTI) * ((a.J + C::kTJ - 1) / C::kTJ));
-  const uint32_t rest = tiles - a.cut.whole;
+hipError_t launch(const GemmArgs& a, uint32_t rest) {
   const dim3 grid(a.cut.whole + rest * a.cut.parts), threads(C::kThreads);
   if (a.p_slow) hipLaunchKernelGGL((gemm_bf16_kernel<true, true, C>), grid, threads, 0, a.stream, a);
   else if (a.q_slow) hipLaunchKernelGGL((gemm_bf16_kernel<false, true, C>), grid, threads, 0, a.stream, a);
@@ -500,7 +506,11 @@ hipError_t launch(const GemmArgs& a) {
 }  // namespace
 
 hipError_t launch_gemm_bf16(const GemmArgs& a) {
-  return a.cut.large ? launch<Tile<256, 256, 2, 4>>(a) : launch<Tile<128, 128, 2, 2>>(a);
+  const int64_t side = a.cut.large ? 256 : 128;
+  const uint32_t rest = (uint32_t)(((a.I + side - 1) / side) * ((a.J + side - 1) / side) - a.cut.whole);
+  if (a.cut.large) return launch<Tile<256, 256, 2, 4, 2>>(a, rest);
+  if (a.cut.whole + rest * a.cut.parts <= 256) return launch<Tile<128, 128, 2, 2, 4>>(a, rest);
+  return launch<Tile<128, 128, 2, 2, 2>>(a, rest);
 }
 
 }  // namespace ringx

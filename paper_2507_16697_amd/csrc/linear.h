@@ -41,6 +41,19 @@ __device__ __forceinline__ float activate(float z, int act) {
   return z;
 }
 
+// 16 values of a lane: the choice is made once
+__device__ __forceinline__ void activate_all(f32x4 (&x)[4], int act) {
+  const auto each = [&](auto f) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[b][e] = f(x[b][e]);
+  };
+  if (act == RINGX_ACT_GELU) each([](float z) { return activate(z, RINGX_ACT_GELU); });
+  else if (act == RINGX_ACT_GELU_TANH) each([](float z) { return activate(z, RINGX_ACT_GELU_TANH); });
+  else each([](float z) { return activate(z, RINGX_ACT_SILU); });
+}
+
 __device__ __forceinline__ float activate_grad(float z, int act) {
   switch (act) {
     case RINGX_ACT_GELU: {
