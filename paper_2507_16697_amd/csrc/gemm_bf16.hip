@@ -196,13 +196,14 @@ struct Frags {
 
 constexpr int BK = 64;   // r of a step
 
-template <int TI, int TJ, int WI, int WJ, int NS>
+// GROUPS = 2: two groups of waves take half of the steps each, for launches that leave a compute unit one tile.
+template <int TI, int TJ, int WI, int WJ, int GROUPS>
 struct Tile {
-  static constexpr int kTI = TI, kTJ = TJ, kWI = WI, kWJ = WJ, kNS = NS;
-  static constexpr int kThreads = 64 * WI * WJ;
-  static constexpr int kBI = TI / WI / 16, kBJ = 4;               // 16 x 16 blocks of a wave
+  static constexpr int kTI = TI, kTJ = TJ, kWI = WI, kWJ = WJ, kGroups = GROUPS;
+  static constexpr int kWaves = WI * WJ, kThreads = 64 * kWaves;   // of a group
+  static constexpr int kBI = TI / WI / 16, kBJ = 4;                // 16 x 16 blocks of a wave
   static constexpr int kP = TI * BK * 2, kStage = (TI + TJ) * BK * 2;   // bytes
-  static_assert(TJ == WJ * 64 && kBI % 2 == 0, "waves of 64 columns");
+  static_assert(TJ == WJ * 64 && kBI % (2 * GROUPS) == 0, "waves of 64 columns");
 };
 
 // The values of a wave's 16 rows x 64 columns on their way out: x[b][e] is row l % 16, column 16 b + 4 (l / 16)
@@ -336,13 +337,15 @@ __device__ __forceinline__ void place(uint32_t t, uint32_t ti, uint32_t tj, uint
 }
 
 template <bool PS, bool QS, class C>
-__global__ __launch_bounds__(C::kThreads, 2) void gemm_bf16_kernel(GemmArgs a) {
-  constexpr int TI = C::kTI, TJ = C::kTJ, WJ = C::kWJ, NS = C::kNS;
-  __shared__ __attribute__((aligned(1024))) char lds[NS * C::kStage];
-  static_assert(C::kThreads / 64 * Out::kStage * 4 <= NS * C::kStage, "staging fits");
+__global__ __launch_bounds__(C::kThreads * C::kGroups, 2) void gemm_bf16_kernel(GemmArgs a) {
+  constexpr int TI = C::kTI, TJ = C::kTJ, WJ = C::kWJ, kGroups = C::kGroups;
+  __shared__ __attribute__((aligned(1024))) char lds_all[kGroups * 2 * C::kStage];
+  static_assert(C::kWaves * Out::kStage * 4 <= 2 * C::kStage, "staging fits");
+  const int tid = threadIdx.x % C::kThreads, lane = tid & 63;
+  const int wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = kGroups == 1 ? 0 : wave8 / C::kWaves, wave = kGroups == 1 ? wave8 : wave8 % C::kWaves;
+  char* const lds = lds_all + group * 2 * C::kStage;
   const uint32_t lbase = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   // whole tiles first, then the last ones in parts along r
   const uint32_t ti = ((uint32_t)a.I + TI - 1) / TI, tj = ((uint32_t)a.J + TJ - 1) / TJ;
@@ -361,6 +364,10 @@ __global__ __launch_bounds__(C::kThreads, 2) void gemm_bf16_kernel(GemmArgs a) {
   const uint32_t steps = ((uint32_t)a.R + BK - 1) / BK;
   uint32_t s0 = 0, s1 = steps;
   if (split) s0 = steps * of / parts, s1 = steps * (of + 1) / parts;
+  // the group's steps; with an odd number of them the second one's last holds zeros
+  const int count = (int)(s1 - s0 + kGroups - 1) / kGroups;
+  if (kGroups > 1 && group == 0) s1 = s0 + count;
+  if (kGroups > 1 && group == 1) s0 = s0 + count;
   Feed<PS, TI, C::kThreads, BK> fp;
   Feed<QS, TJ, C::kThreads, BK> fq;
   fp.start(a.P, i0, BK * s0, tid);
@@ -378,7 +385,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void gemm_bf16_kernel(GemmArgs a) {
 #pragma unroll
     for (int j = 0; j < C::kBJ; ++j) acc[i][j] = f32x4{};
 
-  int rest = (int)min((uint32_t)a.R - BK * s0, BK * (s1 - s0));   // of r, in this part from the step to load on
+  int rest = min((int)a.R - (int)(BK * s0), (int)(BK * s1) - (int)(BK * s0));   // of r, in this part from the step to load on
   // A step is four units: 32 of r, half of the wave's i.  Unit T - 1's products, beside them the reads of unit T
   // of the step in `buf` and L of a later step's loads.
   constexpr int kHalf = C::kBI / 2, kProducts = kHalf * C::kBJ;
@@ -405,49 +412,70 @@ __global__ __launch_bounds__(C::kThreads, 2) void gemm_bf16_kernel(GemmArgs a) {
   typedef integral_constant<int, 0> kNone;
   typedef integral_constant<int, Feed<PS, TI, C::kThreads, BK>::kLoads> kLoadsP;
   typedef integral_constant<int, Feed<QS, TJ, C::kThreads, BK>::kLoads> kLoadsQ;
-  constexpr int kLoads = kLoadsP::value + kLoadsQ::value;
-  auto after = [](uint32_t buf) { return buf == (NS - 1) * C::kStage ? 0u : buf + C::kStage; };
-  // NS buffers.  A step's buffer is free behind the barrier after its last reads; the loads of NS steps
+  // Two buffers.  A step's buffer is free behind the barrier after its last reads; the loads of two steps
   // later go there, P's beside the products that follow, Q's beside the next ones.  Fragments are read one
-  // part ahead, those of a step's first part behind that same barrier, so that the last part's
+  // unit ahead, those of a step's first unit behind that same barrier, so that the last unit's
   // products cover the barrier and the reads.
-#pragma unroll
-  for (int n = 0; n < NS; ++n) {
-    fp.all(wdst + n * C::kStage, rest);
-    if (n < NS - 1) {
-      fq.all(wdst + n * C::kStage + C::kP, rest);
-      rest -= BK;
-    }
-  }
-  wait_vmem<(NS - 2) * kLoads + kLoadsP::value>();
+  fp.all(wdst, rest);
+  fq.all(wdst + C::kP, rest);
+  rest -= BK;
+  fp.all(wdst + C::kStage, rest);
+  wait_vmem<kLoadsP::value>();
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < C::kBJ; ++j) q[0][j] = rq.get(lds + C::kP, 0, j);
 #pragma unroll
   for (int i = 0; i < kHalf; ++i) p[0][i] = rp.get(lds, 0, i);
-  uint32_t buf = 0, last = (NS - 1) * C::kStage;   // the step's buffer, that of the step before it
-  for (int s = (int)(s1 - s0); s > 0; --s) {
+  uint32_t buf = 0;   // the step's buffer
+  for (int s = count; s > 0; --s) {
     fq.begin(rest);
-    unit(integral_constant<int, 1>{}, buf, [&](int u) { fq.load(u, wdst + last + C::kP); }, kLoadsQ{});
+    unit(integral_constant<int, 1>{}, buf,
+         [&](int u) { fq.load(u, wdst + C::kStage - buf + C::kP); }, kLoadsQ{});
     rest -= BK;
     unit(integral_constant<int, 2>{}, buf, nothing, kNone{});
     unit(integral_constant<int, 3>{}, buf, nothing, kNone{});
-    wait_vmem<(NS - 2) * kLoads>();
+    wait_vmem_all();
     __syncthreads();
     fp.begin(rest);
-    last = buf, buf = after(buf);
-    unit(integral_constant<int, 0>{}, buf, [&](int u) { fp.load(u, wdst + last); }, kLoadsP{});
+    buf = C::kStage - buf;
+    unit(integral_constant<int, 0>{}, buf, [&](int u) { fp.load(u, wdst + C::kStage - buf); },
+         kLoadsP{});
   }
   wait_vmem_all();
   __syncthreads();
+
+  // of the groups' blocks each ends a half, with the other's sums of it through LDS
+  constexpr int kOwn = C::kBI / kGroups;
+  if constexpr (kGroups == 2) {
+    f32x4* const other = reinterpret_cast<f32x4*>(lds_all + (1 - group) * 2 * C::kStage) + tid;
+    f32x4* const mine = reinterpret_cast<f32x4*>(lds) + tid;
+    static_assert(kOwn * C::kBJ * C::kThreads * 16 <= 2 * C::kStage, "half of the sums fits");
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k)
+#pragma unroll
+      for (int b = 0; b < C::kBJ; ++b)
+        other[(k * C::kBJ + b) * C::kThreads] = group == 0 ? acc[kOwn + k][b] : acc[k][b];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k)
+#pragma unroll
+      for (int b = 0; b < C::kBJ; ++b) {
+        const f32x4 x = mine[(k * C::kBJ + b) * C::kThreads];
+        if (group == 0) acc[k][b] += x;
+        else acc[k][b] = x + acc[kOwn + k][b];
+      }
+    __syncthreads();
+  }
+  const int first = group * kOwn;   // acc[0 .. kOwn) are the wave's blocks from here on
 
   if (split) {
     // as it lies in the registers
     f32x4* const part = reinterpret_cast<f32x4*>(a.part) + (int64_t)(blockIdx.x - whole) * (TI * TJ / 4);
 #pragma unroll
-    for (int bi = 0; bi < C::kBI; ++bi)
+    for (int bi = 0; bi < kOwn; ++bi)
 #pragma unroll
-      for (int bj = 0; bj < C::kBJ; ++bj) part[(bi * C::kBJ + bj) * C::kThreads + tid] = acc[bi][bj];
+      for (int bj = 0; bj < C::kBJ; ++bj)
+        part[((first + bi) * C::kBJ + bj) * C::kThreads + tid] = acc[bi][bj];
     return;
   }
   Out out;
@@ -455,17 +483,17 @@ __global__ __launch_bounds__(C::kThreads, 2) void gemm_bf16_kernel(GemmArgs a) {
   float* const stage = reinterpret_cast<float*>(lds) + wave * Out::kStage;
   // a loop whose code is there once: unrolled it is 130 KB, which every tile would fetch
 #pragma unroll 1
-  for (int bi = 0; bi < C::kBI; ++bi) {
+  for (int bi = 0; bi < kOwn; ++bi) {
     f32x4 x[4] = {};
 #pragma unroll
-    for (int k = 0; k < C::kBI; ++k) {
+    for (int k = 0; k < kOwn; ++k) {
       if (bi == k) {
         cold_path();
 #pragma unroll
         for (int b = 0; b < C::kBJ; ++b) x[b] = acc[k][b];
       }
     }
-    out.rows(a.o, a.I, (int64_t)i0 + (wi * C::kBI + bi) * 16, x, stage);
+    out.rows(a.o, a.I, (int64_t)i0 + (wi * C::kBI + first + bi) * 16, x, stage);
   }
 }
 
@@ -493,13 +521,13 @@ __global__ __launch_bounds__(C::kThreads) void gemm_join_kernel(GemmArgs a) {
 
 template <class C>
 hipError_t launch(const GemmArgs& a, uint32_t rest) {
-  const dim3 grid(a.cut.whole + rest * a.cut.parts), threads(C::kThreads);
+  const dim3 grid(a.cut.whole + rest * a.cut.parts), threads(C::kThreads * C::kGroups);
   if (a.p_slow) hipLaunchKernelGGL((gemm_bf16_kernel<true, true, C>), grid, threads, 0, a.stream, a);
   else if (a.q_slow) hipLaunchKernelGGL((gemm_bf16_kernel<false, true, C>), grid, threads, 0, a.stream, a);
   else hipLaunchKernelGGL((gemm_bf16_kernel<false, false, C>), grid, threads, 0, a.stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.cut.parts == 1 || rest == 0) return e;
-  hipLaunchKernelGGL((gemm_join_kernel<C>), dim3(rest, C::kBI), threads, 0, a.stream, a);
+  hipLaunchKernelGGL((gemm_join_kernel<C>), dim3(rest, C::kBI), dim3(C::kThreads), 0, a.stream, a);
   return hipGetLastError();
 }
 
@@ -508,9 +536,9 @@ hipError_t launch(const GemmArgs& a, uint32_t rest) {
 hipError_t launch_gemm_bf16(const GemmArgs& a) {
   const int64_t side = a.cut.large ? 256 : 128;
   const uint32_t rest = (uint32_t)(((a.I + side - 1) / side) * ((a.J + side - 1) / side) - a.cut.whole);
-  if (a.cut.large) return launch<Tile<256, 256, 2, 4, 2>>(a, rest);
-  if (a.cut.whole + rest * a.cut.parts <= 256) return launch<Tile<128, 128, 2, 2, 4>>(a, rest);
-  return launch<Tile<128, 128, 2, 2, 2>>(a, rest);
+  if (a.cut.large) return launch<Tile<256, 256, 2, 4, 1>>(a, rest);
+  if (a.cut.groups == 2) return launch<Tile<128, 128, 2, 2, 2>>(a, rest);
+  return launch<Tile<128, 128, 2, 2, 1>>(a, rest);
 }
 
 }  // namespace ringx

@@ -488,6 +488,7 @@ struct GemmOut {
 // each, the others in `parts` along R, which a second launch joins.
 struct GemmCut {
   bool large = false;
+  int groups = 1;                  // of waves in a workgroup, which share the steps along R
   uint32_t whole = 0, parts = 1;
   int64_t part_bytes = 0;
 };
@@ -502,27 +503,40 @@ struct GemmArgs {
   float* part = nullptr;
   hipStream_t stream = nullptr;
 };
-// 256 workgroups of large tiles or 512 of small ones are at work at a time.  A last round that would not be full
-// has its tiles cut into parts along R.  Taken is what a model of the time finds shorter: a step of 64 of R
-// takes a full chip 1.3 us in either, a tile's start and end 6 and 4 us, the join 5 us.
+// 256 workgroups of large tiles or 512 of small ones are at work at a time; at most 256 of small ones have two
+// groups of waves each.  A last round that would not be full may have its tiles cut into parts along R.  Taken is
+// the cut that a model of the time finds shortest, in us (measured, 2.1 GHz): a step of 64 of R 1.07
+// (large, at most half of the chip at work) to 1.35 (large), 0.65 and 0.92 (small, one and two to a compute
+// unit), 0.9 for two steps in two groups; a tile's start and end 7, 5 and 5.5; the join 4 and its traffic.
 inline GemmCut gemm_cut(int64_t I, int64_t J, int64_t R) {
   GemmCut best;
   double least = 0.;
   const int64_t steps = (R + 63) / 64;
+  bool first = true;
   for (int large = 1; large >= 0; --large) {
     const int64_t side = large ? 256 : 128, slots = large ? 256 : 512;
     const int64_t tiles = ((I + side - 1) / side) * ((J + side - 1) / side), rest = tiles % slots;
-    const double step = 1.3, ends = large ? 6. : 4.;
-    GemmCut c;
-    c.large = large;
-    int64_t parts = rest ? std::min<int64_t>({slots / rest, steps / 4, 32}) : 1;
-    if (parts < 2) parts = 1;
-    double t = (double)(tiles / slots) * (steps * step + ends);
-    if (rest) t += (double)((steps + parts - 1) / parts) * step + ends + (parts > 1 ? 5. : 0.);
-    c.parts = (uint32_t)parts;
-    c.whole = (uint32_t)(parts > 1 ? tiles - rest : tiles);
-    c.part_bytes = parts > 1 ? rest * parts * side * side * 4 : 0;
-    if (large || t < least) best = c, least = t;
+    const int64_t most = rest ? std::min<int64_t>({slots / rest, steps / 2, 32}) : 1;
+    for (int64_t parts = 1; parts == 1 || parts <= most; parts *= 2) {
+      GemmCut c;
+      c.large = large, c.parts = (uint32_t)parts;
+      c.whole = (uint32_t)(parts > 1 ? tiles - rest : tiles);
+      c.part_bytes = parts > 1 ? rest * parts * side * side * 4 : 0;
+      double t = (double)(tiles / slots) * (large ? steps * 1.35 + 7. : steps * 0.92 + 5.);
+      const double s = (double)((steps + parts - 1) / parts);
+      const int64_t last = rest * parts;
+      if (last && large) {
+        t += s * (last <= 128 ? 1.07 : 1.35) + 7.;
+      } else if (last && tiles < slots && last <= 256 && s >= 2.) {
+        c.groups = 2;
+        t += s * 0.45 + 5.5;
+      } else if (last) {
+        t += s * (last <= 256 ? 0.65 : 0.92) + 5.;
+      }
+      if (parts > 1) t += 4. + (double)c.part_bytes * 2. / 6.5e6;
+      if (first || t < least) best = c, least = t;
+      first = false;
+    }
   }
   return best;
 }
