@@ -336,10 +336,10 @@ __device__ __forceinline__ void place(uint32_t t, uint32_t ti, uint32_t tj, uint
   i = g0 + t % gn, j = t / gn;
 }
 
+// Workgroup `id` of a product.
 template <bool PS, bool QS, class C>
-__global__ __launch_bounds__(C::kThreads * C::kGroups, 2) void gemm_bf16_kernel(GemmArgs a) {
+__device__ __forceinline__ void product(const GemmArgs& a, const uint32_t id, char* const lds_all) {
   constexpr int TI = C::kTI, TJ = C::kTJ, WJ = C::kWJ, kGroups = C::kGroups;
-  __shared__ __attribute__((aligned(1024))) char lds_all[kGroups * 2 * C::kStage];
   static_assert(C::kWaves * Out::kStage * 4 <= 2 * C::kStage, "staging fits");
   const int tid = threadIdx.x % C::kThreads, lane = tid & 63;
   const int wave8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -351,12 +351,12 @@ __global__ __launch_bounds__(C::kThreads * C::kGroups, 2) void gemm_bf16_kernel(
   const uint32_t ti = ((uint32_t)a.I + TI - 1) / TI, tj = ((uint32_t)a.J + TJ - 1) / TJ;
   const uint32_t whole = a.cut.whole, parts = a.cut.parts;
   uint32_t tile, of = 0, i_tile, j_tile;
-  const bool split = blockIdx.x >= whole && parts > 1;
-  if (blockIdx.x < whole) {
-    tile = xcd_remap(blockIdx.x, whole);
+  const bool split = id >= whole && parts > 1;
+  if (id < whole) {
+    tile = xcd_remap(id, whole);
   } else {
-    tile = whole + (blockIdx.x - whole) / parts;
-    of = (blockIdx.x - whole) % parts;
+    tile = whole + (id - whole) / parts;
+    of = (id - whole) % parts;
   }
   place(tile, ti, tj, i_tile, j_tile);
   const uint32_t i0 = i_tile * TI, j0 = j_tile * TJ;
@@ -470,7 +470,7 @@ __global__ __launch_bounds__(C::kThreads * C::kGroups, 2) void gemm_bf16_kernel(
 
   if (split) {
     // as it lies in the registers
-    f32x4* const part = reinterpret_cast<f32x4*>(a.part) + (int64_t)(blockIdx.x - whole) * (TI * TJ / 4);
+    f32x4* const part = reinterpret_cast<f32x4*>(a.part) + (int64_t)(id - whole) * (TI * TJ / 4);
 #pragma unroll
     for (int bi = 0; bi < kOwn; ++bi)
 #pragma unroll
@@ -497,18 +497,23 @@ __global__ __launch_bounds__(C::kThreads * C::kGroups, 2) void gemm_bf16_kernel(
   }
 }
 
-// The parts of the last tiles, in their order, then the epilogue; blockIdx.y: which block of 16 rows of
-// every wave.
+template <bool PS, bool QS, class C>
+__global__ __launch_bounds__(C::kThreads * C::kGroups, 2) void gemm_bf16_kernel(GemmArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[C::kGroups * 2 * C::kStage];
+  product<PS, QS, C>(a, blockIdx.x, lds);
+}
+
+// The parts of the last tile `rest`, in their order, then the epilogue; bi: which block of 16 rows of every
+// wave.
 template <class C>
-__global__ __launch_bounds__(C::kThreads) void gemm_join_kernel(GemmArgs a) {
-  __shared__ float lds[C::kThreads / 64 * Out::kStage];
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), bi = blockIdx.y;
+__device__ __forceinline__ void join(const GemmArgs& a, uint32_t rest, int bi, float* lds) {
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t ti = ((uint32_t)a.I + C::kTI - 1) / C::kTI, tj = ((uint32_t)a.J + C::kTJ - 1) / C::kTJ;
   uint32_t i, j;
-  place(a.cut.whole + blockIdx.x, ti, tj, i, j);
+  place(a.cut.whole + rest, ti, tj, i, j);
   constexpr int64_t kSize = C::kTI * C::kTJ / 4;
   const f32x4* const part =
-      reinterpret_cast<const f32x4*>(a.part) + (int64_t)blockIdx.x * a.cut.parts * kSize + bi * C::kBJ * C::kThreads + tid;
+      reinterpret_cast<const f32x4*>(a.part) + (int64_t)rest * a.cut.parts * kSize + bi * C::kBJ * C::kThreads + tid;
   f32x4 x[4] = {};
 #pragma unroll 4
   for (uint32_t s = 0; s < a.cut.parts; ++s)
@@ -520,7 +525,60 @@ __global__ __launch_bounds__(C::kThreads) void gemm_join_kernel(GemmArgs a) {
 }
 
 template <class C>
-hipError_t launch(const GemmArgs& a, uint32_t rest) {
+__global__ __launch_bounds__(C::kThreads) void gemm_join_kernel(GemmArgs a) {
+  __shared__ float lds[C::kWaves * Out::kStage];
+  join<C>(a, blockIdx.x, blockIdx.y, lds);
+}
+
+// Both products of a backward that do not fill the chip one by one, and the sums of the bias's gradient from
+// its parts, in one launch.
+template <class C>
+__global__ __launch_bounds__(C::kThreads * C::kGroups, 2) void gemm_pair_kernel(GemmPair p) {
+  __shared__ __attribute__((aligned(1024))) char lds[C::kGroups * 2 * C::kStage];
+  const uint32_t id = blockIdx.x;
+  if (id < p.wgs_dx) {
+    product<false, true, C>(p.dx, id, lds);
+  } else if (id < p.wgs_dx + p.wgs_dw) {
+    product<true, true, C>(p.dw, id - p.wgs_dx, lds);
+  } else {
+    // 64 columns, a wave for every so many parts, then the waves in their order
+    constexpr int kWaves = C::kWaves * C::kGroups;
+    float(*const sums)[64] = reinterpret_cast<float(*)[64]>(lds);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t col = (int64_t)(id - p.wgs_dx - p.wgs_dw) * 64 + lane;
+    float t = 0.f;
+    if (col < p.sums.cols) {
+#pragma unroll 8
+      for (int i = wave; i < p.sums.parts; i += kWaves) t += p.sums.part[i * p.sums.cols + col];
+    }
+    sums[wave][lane] = t;
+    __syncthreads();
+    if (wave == 0 && col < p.sums.cols) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) s += sums[i][lane];
+      float* const out = p.sums.out[0] + col;
+      *out = p.sums.accumulate ? *out + s : s;
+    }
+  }
+}
+
+template <class C>
+__global__ __launch_bounds__(C::kThreads) void gemm_join_pair_kernel(GemmPair p) {
+  __shared__ float lds[C::kWaves * Out::kStage];
+  if (blockIdx.x < p.rest_dx) join<C>(p.dx, blockIdx.x, blockIdx.y, lds);
+  else join<C>(p.dw, blockIdx.x - p.rest_dx, blockIdx.y, lds);
+}
+
+// last tiles, those that are cut
+uint32_t rest_of(const GemmArgs& a) {
+  const int64_t side = a.cut.large ? 256 : 128;
+  return (uint32_t)(((a.I + side - 1) / side) * ((a.J + side - 1) / side) - a.cut.whole);
+}
+
+template <class C>
+hipError_t launch(const GemmArgs& a) {
+  const uint32_t rest = rest_of(a);
   const dim3 grid(a.cut.whole + rest * a.cut.parts), threads(C::kThreads * C::kGroups);
   if (a.p_slow) hipLaunchKernelGGL((gemm_bf16_kernel<true, true, C>), grid, threads, 0, a.stream, a);
   else if (a.q_slow) hipLaunchKernelGGL((gemm_bf16_kernel<false, true, C>), grid, threads, 0, a.stream, a);
@@ -531,14 +589,34 @@ hipError_t launch(const GemmArgs& a, uint32_t rest) {
   return hipGetLastError();
 }
 
+template <class C>
+hipError_t launch_pair(GemmPair p) {
+  p.rest_dx = rest_of(p.dx), p.rest_dw = rest_of(p.dw);
+  p.wgs_dx = p.dx.cut.whole + p.rest_dx * p.dx.cut.parts;
+  p.wgs_dw = p.dw.cut.whole + p.rest_dw * p.dw.cut.parts;
+  const uint32_t sums = p.sums.part ? (uint32_t)((p.sums.cols + 63) / 64) : 0;
+  hipLaunchKernelGGL((gemm_pair_kernel<C>), dim3(p.wgs_dx + p.wgs_dw + sums),
+                     dim3(C::kThreads * C::kGroups), 0, p.dx.stream, p);
+  const hipError_t e = hipGetLastError();
+  if (p.dx.cut.parts == 1) p.rest_dx = 0;
+  if (p.dw.cut.parts == 1) p.rest_dw = 0;
+  if (e != hipSuccess || p.rest_dx + p.rest_dw == 0) return e;
+  hipLaunchKernelGGL((gemm_join_pair_kernel<C>), dim3(p.rest_dx + p.rest_dw, C::kBI), dim3(C::kThreads), 0,
+                     p.dx.stream, p);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_gemm_bf16(const GemmArgs& a) {
-  const int64_t side = a.cut.large ? 256 : 128;
-  const uint32_t rest = (uint32_t)(((a.I + side - 1) / side) * ((a.J + side - 1) / side) - a.cut.whole);
-  if (a.cut.large) return launch<Tile<256, 256, 2, 4, 1>>(a, rest);
-  if (a.cut.groups == 2) return launch<Tile<128, 128, 2, 2, 2>>(a, rest);
-  return launch<Tile<128, 128, 2, 2, 1>>(a, rest);
+  if (a.cut.large) return launch<Tile<256, 256, 2, 4, 1>>(a);
+  if (a.cut.groups == 2) return launch<Tile<128, 128, 2, 2, 2>>(a);
+  return launch<Tile<128, 128, 2, 2, 1>>(a);
+}
+
+hipError_t launch_gemm_pair_bf16(const GemmPair& p) {
+  return p.dx.cut.groups == 2 ? launch_pair<Tile<128, 128, 2, 2, 2>>(p)
+                              : launch_pair<Tile<128, 128, 2, 2, 1>>(p);
 }
 
 }  // namespace ringx

@@ -259,8 +259,8 @@ __global__ __launch_bounds__(256) void grad_pass_kernel(GradPass a) {
 }
 
 template <class T>
-hipError_t launch_grad_pass(GradPass a, hipStream_t stream) {
-  const GradGrid g = grad_grid(a.M, a.O);
+hipError_t launch_grad_pass(GradPass a, bool few, hipStream_t stream) {
+  const GradGrid g = grad_grid(a.M, a.O, few);
   a.across = g.across, a.rows = g.rows;
   const dim3 grid((uint32_t)g.x, (uint32_t)g.y);
   if (a.O % 8 == 0) hipLaunchKernelGGL((grad_pass_kernel<T, true>), grid, dim3(256), 0, stream, a);
@@ -350,40 +350,48 @@ hipError_t backward(const LinearArgs& a) {
     g.dy = a.dy, g.pre = a.act ? a.pre : nullptr, g.M = a.s.M, g.O = a.s.O, g.act = a.act;
     g.dz = own ? at(a.workspace, p.dz) : nullptr, g.ld = p.ldz;
     g.part = a.dbias ? (float*)at(a.workspace, p.sums) : nullptr;
-    e = launch_grad_pass<T>(g, a.stream);
+    e = launch_grad_pass<T>(g, p.pair, a.stream);
     if (e != hipSuccess) return e;
-    if (a.dbias) {
-      ColumnSums c;
-      c.part = g.part, c.parts = (int)grad_grid(a.s.M, a.s.O).y, c.cols = c.split = a.s.O;
-      c.out[0] = a.dbias, c.accumulate = a.accumulate, c.stream = a.stream;
-      e = launch_column_sums(c);
-      if (e != hipSuccess) return e;
-    }
     if (own) dz.p = g.dz, dz.cols = dz.ld = p.ldz;
   }
-  GemmArgs g;
-  g.stream = a.stream, g.P = dz, g.part = (float*)at(a.workspace, p.part);
+  ColumnSums c;
+  if (a.dbias) {
+    c.part = (float*)at(a.workspace, p.sums), c.parts = (int)grad_grid(a.s.M, a.s.O, p.pair).y;
+    c.cols = c.split = a.s.O, c.out[0] = a.dbias, c.accumulate = a.accumulate, c.stream = a.stream;
+    const bool later = p.pair && a.dx && a.dw;   // with the products
+    if (!later) e = launch_column_sums(c);
+    if (e != hipSuccess) return e;
+  }
+  GemmArgs x, w;
+  x.stream = w.stream = a.stream, x.P = w.P = dz;
   if (a.dx) {
-    g.Q = a.weights();
-    e = operand<T>(g.Q, p.w, p.ldw, a.workspace, a.stream);
+    x.Q = a.weights();
+    e = operand<T>(x.Q, p.w, p.ldw, a.workspace, a.stream);
     if (e != hipSuccess) return e;
-    g.q_slow = true;
-    g.I = a.s.M, g.J = a.s.K, g.R = dz.cols, g.splits = p.splits_dx, g.cut = p.cut_dx;
-    g.o.out = a.dx, g.o.J = a.s.K;
-    if (a.s.heads) g.o.heads = a.s.heads, g.o.tokens = a.s.tokens, g.o.d = a.s.K / a.s.heads;
-    e = launch_product<T>(g);
-    if (e != hipSuccess) return e;
+    x.q_slow = true;
+    x.I = a.s.M, x.J = a.s.K, x.R = dz.cols, x.splits = p.splits_dx, x.cut = p.cut_dx;
+    x.part = (float*)at(a.workspace, p.part);
+    x.o.out = a.dx, x.o.J = a.s.K;
+    if (a.s.heads) x.o.heads = a.s.heads, x.o.tokens = a.s.tokens, x.o.d = a.s.K / a.s.heads;
   }
   if (a.dw) {
-    g.Q = a.x();
-    e = operand<T>(g.Q, p.x, p.ldx, a.workspace, a.stream);
+    w.Q = a.x();
+    e = operand<T>(w.Q, p.x, p.ldx, a.workspace, a.stream);
     if (e != hipSuccess) return e;
-    g.p_slow = g.q_slow = true;
-    g.I = a.s.O, g.J = a.s.K, g.R = a.s.M, g.splits = p.splits_dw, g.cut = p.cut_dw;
-    g.o = GemmOut{};
-    g.o.out = a.dw, g.o.J = a.s.K, g.o.f32 = a.dw_f32, g.o.accumulate = a.accumulate;
-    e = launch_product<T>(g);
+    w.p_slow = w.q_slow = true;
+    w.I = a.s.O, w.J = a.s.K, w.R = a.s.M, w.splits = p.splits_dw, w.cut = p.cut_dw;
+    w.part = (float*)at(a.workspace, p.part_dw);
+    w.o.out = a.dw, w.o.J = a.s.K, w.o.f32 = a.dw_f32, w.o.accumulate = a.accumulate;
   }
+  if constexpr (std::is_same_v<T, __bf16>) {
+    if (p.pair && a.dx && a.dw) {
+      GemmPair both;
+      both.dx = x, both.dw = w, both.sums = c;
+      return launch_gemm_pair_bf16(both);
+    }
+  }
+  if (a.dx) e = launch_product<T>(x);
+  if (a.dw && e == hipSuccess) e = launch_product<T>(w);
   return e;
 }
 

@@ -491,6 +491,7 @@ struct GemmCut {
   int groups = 1;                  // of waves in a workgroup, which share the steps along R
   uint32_t whole = 0, parts = 1;
   int64_t part_bytes = 0;
+  double us = 0.;                  // what the model gives it
 };
 // out[i][j] = sum over r of P(i, r) Q(j, r); P is stored [I, R] or, with p_slow, [R, I]; Q likewise.
 struct GemmArgs {
@@ -503,6 +504,13 @@ struct GemmArgs {
   float* part = nullptr;
   hipStream_t stream = nullptr;
 };
+// Both products of a backward in one launch, with the sums of the bias's gradient (sums.part null: none).
+struct GemmPair {
+  GemmArgs dx, dw;
+  ColumnSums sums;
+  uint32_t wgs_dx = 0, wgs_dw = 0, rest_dx = 0, rest_dw = 0;   // set by the launch
+};
+
 // 256 workgroups of large tiles or 512 of small ones are at work at a time; at most 256 of small ones have two
 // groups of waves each.  A last round that would not be full may have its tiles cut into parts along R.  Taken is
 // the cut that a model of the time finds shortest, in us (measured, 2.1 GHz): a step of 64 of R 1.07
@@ -534,11 +542,40 @@ inline GemmCut gemm_cut(int64_t I, int64_t J, int64_t R) {
         t += s * (last <= 256 ? 0.65 : 0.92) + 5.;
       }
       if (parts > 1) t += 4. + (double)c.part_bytes * 2. / 6.5e6;
+      c.us = t;
       if (first || t < least) best = c, least = t;
       first = false;
     }
   }
   return best;
+}
+// The cuts of dx [M, K] (R = O) and dw [O, K] (R = M) for one launch of both, where that is shorter than one
+// after the other (false: it is not).
+inline bool gemm_cut_pair(int64_t M, int64_t K, int64_t O, GemmCut* dx, GemmCut* dw) {
+  const auto tiles = [](int64_t i, int64_t j) { return ((i + 127) / 128) * ((j + 127) / 128); };
+  const int64_t n1 = tiles(M, K), n2 = tiles(O, K), s1 = (O + 63) / 64, s2 = (M + 63) / 64;
+  if (n1 + n2 > 512) return false;
+  // 3 us for a launch less, 4 for the sums of the bias's gradient
+  double least = dx->us + dw->us + 7.;
+  bool found = false;
+  for (int64_t p1 = 1; p1 == 1 || (p1 <= 32 && p1 <= s1 / 2); p1 *= 2)
+    for (int64_t p2 = 1; p2 == 1 || (p2 <= 32 && p2 <= s2 / 2); p2 *= 2) {
+      const int64_t wgs = n1 * p1 + n2 * p2;
+      if (wgs > 512) break;
+      const double s = (double)std::max((s1 + p1 - 1) / p1, (s2 + p2 - 1) / p2);
+      const int64_t bytes = (p1 > 1 ? n1 * p1 : 0) * 65536 + (p2 > 1 ? n2 * p2 : 0) * 65536;
+      const bool two = wgs <= 256 && s >= 2.;
+      double t = two ? s * 0.45 + 5.5 : s * (wgs <= 256 ? 0.65 : 0.92) + 5.;
+      if (bytes) t += 4. + (double)bytes * 2. / 6.5e6;
+      if (t >= least) continue;
+      least = t, found = true;
+      *dx = GemmCut{}, *dw = GemmCut{};
+      dx->groups = dw->groups = two ? 2 : 1;
+      dx->parts = (uint32_t)p1, dw->parts = (uint32_t)p2;
+      dx->whole = p1 > 1 ? 0 : (uint32_t)n1, dw->whole = p2 > 1 ? 0 : (uint32_t)n2;
+      dx->part_bytes = p1 > 1 ? n1 * p1 * 65536 : 0, dw->part_bytes = p2 > 1 ? n2 * p2 * 65536 : 0;
+    }
+  return found;
 }
 // fp32: whether a product takes tiles of 128 x 128 (else 32 x 32), and parts that R is cut into where the
 // tiles do not fill the chip.
@@ -557,13 +594,13 @@ struct GradGrid {
   int across;
   int64_t rows, x, y;
 };
-inline GradGrid grad_grid(int64_t M, int64_t O) {
+inline GradGrid grad_grid(int64_t M, int64_t O, bool few) {   // few: at most 64 along the rows
   GradGrid g;
   g.across = 1;
   while (g.across < 64 && 8 * g.across < O) g.across *= 2;
   g.x = (O + 8 * g.across - 1) / (8 * g.across);
   const int64_t least = 4 * (256 / g.across);      // rows of one round
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(512, 2048 / g.x));
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(few ? 64 : 512, 2048 / g.x));
   g.rows = std::max<int64_t>(least, ((M + most - 1) / most + least - 1) / least * least);
   g.y = (M + g.rows - 1) / g.rows;
   return g;
@@ -605,10 +642,12 @@ struct LinearPlan {
   bool few = false;                        // forward: the kernel for a few rows
   int64_t x = -1, w = -1, dz = -1;         // copies of the operands, dz
   int64_t ldx = 0, ldw = 0, ldz = 0;       // their row lengths
-  int64_t sums = -1, part = 0;             // parts of the bias's gradient, of split products
+  int64_t sums = -1;                       // parts of the bias's gradient
+  int64_t part = 0, part_dw = 0;           // parts of split products
   int64_t R = 0;                           // forward: the product's r
   int splits = 1, splits_dx = 1, splits_dw = 1;   // fp32
   GemmCut cut, cut_dx, cut_dw;             // bf16
+  bool pair = false;                       // backward, bf16: both products in one launch
   int64_t bytes = 0;
   int64_t take(int64_t n) {
     const int64_t at = bytes;
@@ -657,17 +696,19 @@ inline LinearPlan linear_bwd_plan(const LinearShape& s, int act) {
   } else if (s.heads || !linear_near(s)) {
     p.x = p.take(4 * s.M * s.K), p.ldx = s.K;
   }
-  p.sums = p.take(4 * grad_grid(s.M, s.O).y * s.O);
   int64_t dx = 0, dw = 0;
   if (s.bf16) {
     p.cut_dx = gemm_cut(s.M, s.K, Op), p.cut_dw = gemm_cut(s.O, s.K, s.M);
+    p.pair = gemm_cut_pair(s.M, s.K, s.O, &p.cut_dx, &p.cut_dw);
     dx = p.cut_dx.part_bytes, dw = p.cut_dw.part_bytes;
   } else {
     p.splits_dx = gemm_f32_splits(s.M, s.K, Op), p.splits_dw = gemm_f32_splits(s.O, s.K, s.M);
     if (p.splits_dx > 1) dx = 4 * p.splits_dx * s.M * s.K;
     if (p.splits_dw > 1) dw = 4 * p.splits_dw * s.O * s.K;
   }
-  if (dx || dw) p.part = p.take(std::max(dx, dw));
+  p.sums = p.take(4 * grad_grid(s.M, s.O, p.pair).y * s.O);
+  if (dx || dw) p.part = p.part_dw = p.take(p.pair ? dx + dw : std::max(dx, dw));
+  if (p.pair) p.part_dw += dx;
   return p;
 }
 
@@ -698,6 +739,7 @@ hipError_t launch_norm_rope(const RopeArgs& a, bool bwd);
 hipError_t launch_layer_norm(const NormArgs& a, bool bwd);
 hipError_t launch_column_sums(const ColumnSums& a);
 hipError_t launch_gemm_bf16(const GemmArgs& a);
+hipError_t launch_gemm_pair_bf16(const GemmPair& p);
 hipError_t launch_gemm_f32(const GemmArgs& a);
 hipError_t launch_linear(const LinearArgs& a);
 hipError_t launch_linear_bwd(const LinearArgs& a);

@@ -678,13 +678,16 @@ def ringx_tt_tokenize(field, k: int, ratio: int, centre, p: int, sigma=None, out
 
 def _launch(name, like, stream, *args):
     """Call an entry point whose last argument is the stream, with `like`'s device current."""
-    fn = getattr(lib(), name)
-    cuda = _T.cuda
-    if like.device.index == cuda.current_device():
-        st = fn(*args, _stream(stream))
-    else:
-        with cuda.device(like.device):
+    fn = getattr(_lib or lib(), name)
+    cuda, device = _T.cuda, like.device
+    here = cuda.current_device()
+    if device.index != here:
+        with cuda.device(device):
             st = fn(*args, _stream(stream))
+    elif stream is None and _raw_stream is not None:
+        st = fn(*args, _raw_stream(here))
+    else:
+        st = fn(*args, _stream(stream))
     if st != 0:
         _check(name, st)
 
@@ -937,6 +940,8 @@ def _rows_of(name, x):
     shape, strides = x.shape, x.stride()
     if shape[-1] > 1 and strides[-1] != 1:
         raise ValueError(f"{name}: rows must be contiguous")
+    if len(shape) == 2:
+        return shape[0], strides[0] if shape[0] > 1 else shape[1]
     rows, step = 1, None
     for n, s in zip(shape[-2::-1], strides[-2::-1]):
         if n == 1:
@@ -953,8 +958,9 @@ def _vector(name, t, n, device):
     """Address of an fp32 vector [n], None where there is none."""
     if t is None:
         return None
-    _dev(t)
-    _expect(name, t, (n,), _T.float32, device)
+    if t.shape != (n,) or t.dtype is not _T.float32 or t.device != device or not t.is_contiguous():
+        _dev(t)
+        _expect(name, t, (n,), _T.float32, device)
     return t.data_ptr()
 
 
@@ -962,9 +968,17 @@ def _same(name, t, shape, like):
     """Address of an input of `shape` in like's type, None where there is none."""
     if t is None:
         return None
-    _dev(t)
-    _expect(name, t, shape, like.dtype, like.device)
+    if t.shape != shape or t.dtype is not like.dtype or t.device != like.device or not t.is_contiguous():
+        _dev(t)
+        _expect(name, t, shape, like.dtype, like.device)
     return t.data_ptr()
+
+
+def _out_as(name, t, like, stream):
+    """_out of like's shape and type, contiguous whether `like` is or not."""
+    if t is None and stream is None and type(like) is _T.Tensor and like.is_contiguous():
+        return _T.empty_like(like)
+    return _out(name, t, like.shape, like.dtype, like, stream)
 
 
 def ringx_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, need_stats: bool = True, y=None,
@@ -977,7 +991,7 @@ def ringx_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, need_stats: b
     C = x.shape[-1]
     code = _dtype_code(x)
     pw, pb = _vector("weight", weight, C, x.device), _vector("bias", bias, C, x.device)
-    y = _out("y", y, x.shape, x.dtype, x, stream)
+    y = _out_as("y", y, x, stream)
     if need_stats or stats is not None:
         stats = _out("stats", stats, (2, rows), torch.float32, x, stream)
     _launch("ringx_layer_norm", x, stream, x.data_ptr(), step, pw, pb, y.data_ptr(), _ptr(stats), rows, C,
@@ -1007,7 +1021,7 @@ def ringx_layer_norm_bwd(x, dy, stats, weight=None, bias=None, dres=None, dx=Non
     _vector("bias", bias, C, x.device)
     if (weight is None and dweight is not None) or (bias is None and dbias is not None):
         raise ValueError("a weight's gradient without the weight")
-    dx = _out("dx", dx, x.shape, x.dtype, x, stream)
+    dx = _out_as("dx", dx, x, stream)
     if weight is not None:
         dweight = _out("dweight", dweight, (C,), torch.float32, x, stream)
     if bias is not None:
@@ -1103,7 +1117,7 @@ def ringx_linear_bwd(x, w, dy, pre=None, act="none", bias=None, need_dx: bool = 
     if dw_dtype is not torch.float32 and dw_dtype is not x.dtype:
         raise TypeError(f"dw_dtype: {dw_dtype}, expected float32 or {x.dtype}")
     if need_dx or dx is not None:
-        dx = _out("dx", dx, x.shape, x.dtype, x, stream)
+        dx = _out_as("dx", dx, x, stream)
     if need_dw or dw is not None:
         if dw_dtype is torch.float32:
             dw = _grad_out("dw", dw, (O, K), x, accumulate_dw, stream)
