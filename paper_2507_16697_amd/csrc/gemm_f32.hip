@@ -23,22 +23,23 @@ constexpr uint32_t kMostBytes = 0x7ffffff0u;
 // One operand of a wave: B blocks of 32 of the width, 8 U of r at a time.
 template <bool SLOW, int B, int U>
 struct Feed {
-  uint32_t off[B];
-  int64_t base, left, step, row;   // bytes
+  uint32_t off[B], row;        // bytes
+  int64_t base, left, step;
   int g;
 
-  __device__ __forceinline__ void start(const GemmIn& x, int64_t w0, int64_t r0, int lane) {
+  // sizes fit 32 bits
+  __device__ __forceinline__ void start(const GemmIn& x, uint32_t w0, uint32_t r0, int lane) {
     g = lane >> 5;
-    const int n = lane & 31;
-    const int64_t at = SLOW ? r0 * x.ld + w0 : w0 * x.ld + r0;
+    const uint32_t n = lane & 31, rows = (uint32_t)x.rows, ld = (uint32_t)x.ld;
+    const int64_t at = SLOW ? (int64_t)r0 * ld + w0 : (int64_t)w0 * ld + r0;
     base = reinterpret_cast<int64_t>(uniform_ptr((const float*)x.p + at));
-    left = 4 * ((x.rows - 1) * x.ld + x.cols - at);
-    step = SLOW ? 32 * U * x.ld : 32 * U;
-    row = 4 * x.ld;
+    left = 4 * ((int64_t)(rows - 1) * ld + (uint32_t)x.cols - at);
+    step = SLOW ? 32 * U * (int64_t)ld : 32 * U;
+    row = 4 * ld;
 #pragma unroll
     for (int b = 0; b < B; ++b) {
-      if constexpr (SLOW) off[b] = (uint32_t)(16 * g * x.ld + 4 * (32 * b + n));
-      else off[b] = (uint32_t)(4 * (min(w0 + 32 * b + n, x.rows - 1) - w0) * x.ld + 16 * g);
+      if constexpr (SLOW) off[b] = 16 * g * ld + 4 * (32 * b + n);
+      else off[b] = 4 * (min(w0 + 32 * b + n, rows - 1) - w0) * ld + 16 * g;
     }
   }
   __device__ __forceinline__ void load(f32x4 (&x)[U][B]) {
@@ -54,7 +55,7 @@ struct Feed {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             x[u][b][e] = __builtin_bit_cast(
-                float, __builtin_amdgcn_raw_buffer_load_b32(rsrc, off[b] + (8 * u + e) * (uint32_t)row, 0, 0));
+                float, __builtin_amdgcn_raw_buffer_load_b32(rsrc, off[b] + (8 * u + e) * row, 0, 0));
         } else {
           x[u][b] = __builtin_bit_cast(
               f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off[b] + 32 * u, 0, 0));
@@ -75,33 +76,39 @@ struct Feed {
   }
 };
 
-// A workgroup of four waves: 2 x 2 wave tiles (KS = 1), or one, whose r the waves split (KS = 4).
+// A workgroup of four waves: 2 x 2 wave tiles (KS = 1), or one of 32 x 32, whose r the waves split (KS = 4).
 template <bool PS, bool QS, int B, int U, int KS>
 __global__ __launch_bounds__(256, B == 2 ? 2 : 4) void gemm_f32_kernel(GemmArgs a) {
-  constexpr int kTile = 32 * B * (KS == 1 ? 2 : 1), kStep = 8 * U;
-  __shared__ float lds[KS == 1 ? 1 : (KS - 1) * 64 * 16 * B * B];
+  constexpr uint32_t kTile = 32 * B * (KS == 1 ? 2 : 1), kStep = 8 * U;
+  static_assert(KS == 1 || B == 1, "one block of four waves");
+  // a wave's block of 32 x 32, by lane and register, or by row and column
+  constexpr int kBlock = 64 * 17;
+  __shared__ float lds[4 * kBlock];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t ti = (uint32_t)((a.I + kTile - 1) / kTile), tj = (uint32_t)((a.J + kTile - 1) / kTile);
+  const uint32_t I = (uint32_t)a.I, J = (uint32_t)a.J, R = (uint32_t)a.R;
+  const uint32_t ti = (I + kTile - 1) / kTile, tj = (J + kTile - 1) / kTile;
   constexpr uint32_t kGroup = 8;
-  uint32_t id = xcd_remap(blockIdx.x, gridDim.x);
-  const uint32_t split = id / (ti * tj);
-  id -= split * ti * tj;
+  uint32_t id = xcd_remap(blockIdx.x, gridDim.x), split = 0;
+  if (a.splits > 1) {
+    split = id / (ti * tj);
+    id -= split * ti * tj;
+  }
   const uint32_t g0 = id / (kGroup * tj) * kGroup, gn = min(kGroup, ti - g0);
   id -= g0 * tj;
-  int64_t i0 = (int64_t)(g0 + id % gn) * kTile, j0 = (int64_t)(id / gn) * kTile;
+  uint32_t i0 = (g0 + id % gn) * kTile, j0 = (id / gn) * kTile;
   if (KS == 1) i0 += 32 * B * (wave >> 1), j0 += 32 * B * (wave & 1);
-  const int ks = KS == 1 ? 0 : wave;
 
-  const int64_t steps = (a.R + kStep - 1) / kStep, parts = (int64_t)a.splits * KS;
-  const int64_t part = (int64_t)split * KS + ks;
-  const int64_t s0 = steps * part / parts, s1 = steps * (part + 1) / parts;
+  const uint32_t steps = (R + kStep - 1) / kStep, parts = (uint32_t)a.splits * KS;
+  const uint32_t part = split * KS + (KS == 1 ? 0 : wave);
+  uint32_t s0 = 0, s1 = steps;
+  if (parts > 1) s0 = (uint32_t)((uint64_t)steps * part / parts), s1 = (uint32_t)((uint64_t)steps * (part + 1) / parts);
   f32x16 acc[B][B];
 #pragma unroll
   for (int i = 0; i < B; ++i)
 #pragma unroll
     for (int j = 0; j < B; ++j) acc[i][j] = f32x16{};
-  if (s0 < s1 && i0 < a.I && j0 < a.J) {
+  if (s0 < s1 && i0 < I && j0 < J) {
     Feed<PS, B, U> fp;
     Feed<QS, B, U> fq;
     fp.start(a.P, i0, s0 * kStep, lane);
@@ -109,13 +116,13 @@ __global__ __launch_bounds__(256, B == 2 ? 2 : 4) void gemm_f32_kernel(GemmArgs 
     f32x4 p[U][B], q[U][B];
     fp.load(p);
     fq.load(q);
-    for (int64_t s = s0; s < s1; ++s) {
+    for (uint32_t s = s0; s < s1; ++s) {
       f32x4 pn[U][B], qn[U][B];
       if (s + 1 < s1) {
         fp.load(pn);
         fq.load(qn);
       }
-      const int64_t rest = a.R - s * kStep;
+      const uint32_t rest = R - s * kStep;
       if (rest < kStep) {
         cold_path();
         fp.mask(p, (int)rest);
@@ -135,53 +142,73 @@ __global__ __launch_bounds__(256, B == 2 ? 2 : 4) void gemm_f32_kernel(GemmArgs 
         for (int b = 0; b < B; ++b) p[u][b] = pn[u][b], q[u][b] = qn[u][b];
     }
   }
-  if constexpr (KS > 1) {
-    // the waves' sums, in their order
-    if (wave > 0) {
-#pragma unroll
-      for (int i = 0; i < B; ++i)
-#pragma unroll
-        for (int j = 0; j < B; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            lds[(((wave - 1) * B * B + i * B + j) * 16 + r) * 64 + lane] = acc[i][j][r];
-    }
-    __syncthreads();
-    if (wave > 0) return;
-#pragma unroll
-    for (int w = 0; w < KS - 1; ++w)
-#pragma unroll
-      for (int i = 0; i < B; ++i)
-#pragma unroll
-        for (int j = 0; j < B; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            acc[i][j][r] += lds[((w * B * B + i * B + j) * 16 + r) * 64 + lane];
-  }
   GemmOut o = a.o;
-  const bool vec = a.J % 4 == 0 && o.d % 4 == 0;
+  const bool vec = J % 4 == 0 && o.d % 4 == 0;
   if (a.splits > 1) {
     o = GemmOut{};
     o.out = a.part + split * a.I * a.J, o.J = a.J, o.f32 = true;
   }
+  const auto bias = [&](uint32_t j) { return o.bias && j < J ? o.bias[j] : 0.f; };
+  if constexpr (KS > 1) {
+    // the waves' sums in their order; then all of them end the block, neighbouring columns in neighbouring
+    // lanes
 #pragma unroll
-  for (int bi = 0; bi < B; ++bi) {
-    const int64_t i = i0 + 32 * bi + (lane & 31);
+    for (int r = 0; r < 16; ++r) lds[wave * kBlock + lane * 17 + r] = acc[0][0][r];
+    __syncthreads();
+    const auto sum = [&](uint32_t i, uint32_t j) {
+      const uint32_t at = (i + 32 * (j >> 2 & 1)) * 17 + 4 * (j >> 3) + (j & 3);
+      float t = lds[at];
 #pragma unroll
-    for (int bj = 0; bj < B; ++bj)
+      for (int w = 1; w < KS; ++w) t += lds[w * kBlock + at];
+      return t;
+    };
+    if (vec) {
+      const uint32_t i = threadIdx.x / 8, j = threadIdx.x % 8 * 4;
+      float x[4], b[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int64_t j = j0 + 32 * bj + 8 * r + 4 * (lane >> 5);
-        const int inside = (int)max((int64_t)0, min((int64_t)4, a.J - j));
-        if (i >= a.I || inside == 0) continue;
-        float b[4], x[4] = {acc[bi][bj][4 * r], acc[bi][bj][4 * r + 1], acc[bi][bj][4 * r + 2],
-                            acc[bi][bj][4 * r + 3]};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) b[e] = o.bias && e < inside ? o.bias[j + e] : 0.f;
-        if (vec) finish<4, true, float>(o, i, j, 4, b, x);
-        else finish<4, false, float>(o, i, j, inside, b, x);
+      for (int e = 0; e < 4; ++e) x[e] = sum(i, j + e), b[e] = bias(j0 + j + e);
+      if (i0 + i < I && j0 + j < J) finish<4, true, float>(o, i0 + i, j0 + j, 4, b, x);
+    } else {
+      const uint32_t j = threadIdx.x % 32;
+      float b[1] = {bias(j0 + j)};
+#pragma unroll 1
+      for (uint32_t i = threadIdx.x / 32; i < 32; i += 8) {
+        float x[1] = {sum(i, j)};
+        if (i0 + i < I && j0 + j < J) finish<1, false, float>(o, i0 + i, j0 + j, 1, b, x);
       }
+    }
+    return;
   }
+#pragma unroll
+  for (int bi = 0; bi < B; ++bi)
+#pragma unroll
+    for (int bj = 0; bj < B; ++bj) {
+      const uint32_t ib = i0 + 32 * bi, jb = j0 + 32 * bj;
+      if (vec) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const uint32_t i = ib + (lane & 31), j = jb + 8 * r + 4 * (lane >> 5);
+          float b[4], x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = acc[bi][bj][4 * r + e], b[e] = bias(j + e);
+          if (i < I && j < J) finish<4, true, float>(o, i, j, 4, b, x);
+        }
+      } else {
+        float* const stage = lds + wave * kBlock;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          stage[(lane & 31) * 33 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4] = acc[bi][bj][r];
+        __builtin_amdgcn_wave_barrier();
+        const uint32_t j = lane & 31;
+        float b[1] = {bias(jb + j)};
+#pragma unroll 1
+        for (uint32_t i = lane >> 5; i < 32; i += 2) {
+          float x[1] = {stage[i * 33 + j]};
+          if (ib + i < I && jb + j < J) finish<1, false, float>(o, ib + i, jb + j, 1, b, x);
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
 }
 
 template <bool PS, bool QS, int B, int U, int KS>
@@ -201,7 +228,7 @@ hipError_t by_layout(const GemmArgs& a) {
 }  // namespace
 
 hipError_t launch_gemm_f32(const GemmArgs& a) {
-  return gemm_f32_large(a.I, a.J) ? by_layout<2, 2, 1>(a) : by_layout<1, 4, 4>(a);
+  return gemm_f32_large(a.I, a.J) ? by_layout<2, 4, 1>(a) : by_layout<1, 4, 4>(a);
 }
 
 }  // namespace ringx

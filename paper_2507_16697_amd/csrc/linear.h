@@ -74,6 +74,20 @@ __device__ __forceinline__ float activate_grad(float z, int act) {
   return 1.f;
 }
 
+// g *= act'(z), the choice made once
+template <int U, int N>
+__device__ __forceinline__ void grad_all(float (&g)[U][N], const float (&z)[U][N], int act) {
+  const auto each = [&](auto f) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < N; ++e) g[u][e] *= f(z[u][e]);
+  };
+  if (act == RINGX_ACT_GELU) each([](float v) { return activate_grad(v, RINGX_ACT_GELU); });
+  else if (act == RINGX_ACT_GELU_TANH) each([](float v) { return activate_grad(v, RINGX_ACT_GELU_TANH); });
+  else each([](float v) { return activate_grad(v, RINGX_ACT_SILU); });
+}
+
 // N neighbouring values from p on, as fp32: N values' 8- or 16-byte pieces (VEC), else the first `n`.
 template <int N, bool VEC, class T>
 __device__ __forceinline__ void load_values(const T* p, int n, float (&x)[N]) {

@@ -160,42 +160,73 @@ hipError_t launch_product(const GemmArgs& a) {
 // An operand copied to rows of `ld` values, zeros behind its columns: bf16 whose rows do not come in 16-byte
 // pieces, and heads where a product does not walk them itself.
 
-template <class T, bool VEC>
-__global__ __launch_bounds__(256) void pack_kernel(GemmIn x, T* out, int64_t ld) {
+template <class T>
+struct Pack {
+  GemmIn x[2];
+  T* out[2];
+  int64_t ld[2];
+  uint32_t wgs[2];   // workgroups; 0: nothing to copy
+  bool vec[2];       // in 16-byte pieces
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void pack_kernel(Pack<T> a) {
   constexpr int N = 16 / (int)sizeof(T);
-  const uint32_t per = (uint32_t)((ld + N - 1) / N);
+  const int k = blockIdx.x >= a.wgs[0];
+  const GemmIn& x = a.x[k];
+  const uint32_t per = (uint32_t)((a.ld[k] + N - 1) / N), wg = k ? blockIdx.x - a.wgs[0] : blockIdx.x;
   const int64_t total = x.rows * per;
-  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
-    const int64_t i = t / per;
-    const int64_t c = (t - i * per) * N;
-    int64_t row = i * x.ld;
-    if (x.heads) row = i / x.tokens * x.tokens * x.cols + i % x.tokens * x.d;
+  for (int64_t t = (int64_t)wg * 256 + threadIdx.x; t < total; t += (int64_t)a.wgs[k] * 256) {
+    // rows of a tensor fit 32 bits, its pieces need not
+    const uint32_t i = total >> 32 ? (uint32_t)(t / per) : (uint32_t)t / per;
+    const uint32_t c = (uint32_t)(t - (int64_t)i * per) * N;
+    int64_t row = (int64_t)i * x.ld;
+    if (x.heads) {
+      const uint32_t b = i / (uint32_t)x.tokens;
+      row = (int64_t)b * x.tokens * x.cols + (int64_t)(i - b * (uint32_t)x.tokens) * x.d;
+    }
     const T* const p = (const T*)x.p + row;
-    T* const q = out + i * ld + c;
-    auto column = [&](int64_t k) {
-      if (!x.heads) return k;
-      const int64_t h = (uint32_t)k / (uint32_t)x.d;
-      return h * x.tokens * x.d + (k - h * x.d);
+    T* const q = a.out[k] + (int64_t)i * a.ld[k] + c;
+    auto column = [&](uint32_t j) {
+      if (!x.heads) return (int64_t)j;
+      const uint32_t h = j / (uint32_t)x.d;
+      return (int64_t)h * x.tokens * x.d + (j - h * (uint32_t)x.d);
     };
-    if constexpr (VEC) {
+    if (a.vec[k]) {
       *reinterpret_cast<u32x4*>(q) = *reinterpret_cast<const u32x4*>(p + column(c));
     } else {
+      T v[N];
 #pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (c + e < ld) q[e] = c + e < x.cols ? p[column(c + e)] : (T)0.f;
+      for (int e = 0; e < N; ++e) v[e] = c + e < x.cols ? p[column(c + e)] : (T)0.f;
+      if (a.ld[k] % N == 0) {
+        *reinterpret_cast<u32x4*>(q) = __builtin_bit_cast(u32x4, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (c + e < a.ld[k]) q[e] = v[e];
+      }
     }
   }
 }
 
+// Operands x and y as the products take them, copied to the workspace where the plan says so (offset >= 0).
 template <class T>
-hipError_t launch_pack(const GemmIn& x, void* out, int64_t ld, hipStream_t stream) {
+hipError_t pack(GemmIn* x, int64_t at_x, int64_t ld_x, GemmIn* y, int64_t at_y, int64_t ld_y, void* workspace,
+                hipStream_t stream) {
   constexpr int N = 16 / (int)sizeof(T);
-  const int64_t wgs = std::min<int64_t>((x.rows * ((ld + N - 1) / N) + 255) / 256, 8192);
-  const bool vec = ld == x.cols && x.cols % N == 0 && (x.heads ? x.d % N == 0 : x.ld % N == 0);
-  if (vec)
-    hipLaunchKernelGGL((pack_kernel<T, true>), dim3((uint32_t)wgs), dim3(256), 0, stream, x, (T*)out, ld);
-  else
-    hipLaunchKernelGGL((pack_kernel<T, false>), dim3((uint32_t)wgs), dim3(256), 0, stream, x, (T*)out, ld);
+  Pack<T> a{};
+  const int64_t at[2] = {x ? at_x : -1, y ? at_y : -1}, ld[2] = {ld_x, ld_y};
+  GemmIn* const in[2] = {x, y};
+  for (int k = 0; k < 2; ++k) {
+    if (at[k] < 0) continue;
+    GemmIn& s = *in[k];
+    a.x[k] = s, a.ld[k] = ld[k], a.out[k] = (T*)(static_cast<char*>(workspace) + at[k]);
+    a.wgs[k] = (uint32_t)std::min<int64_t>((s.rows * ((ld[k] + N - 1) / N) + 255) / 256, 8192);
+    a.vec[k] = ld[k] == s.cols && s.cols % N == 0 && (s.heads ? s.d % N == 0 : s.ld % N == 0);
+    s.p = a.out[k], s.heads = 0, s.ld = s.cols = ld[k];
+  }
+  if (a.wgs[0] + a.wgs[1] == 0) return hipSuccess;
+  hipLaunchKernelGGL((pack_kernel<T>), dim3(a.wgs[0] + a.wgs[1]), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -211,35 +242,46 @@ struct GradPass {
   int act, across;        // threads across the columns, 8 of them each
 };
 
+// A thread's 8 columns lie side by side (VEC), or `across` apart, neighbours in neighbouring lanes.
 template <class T, bool VEC>
 __global__ __launch_bounds__(256) void grad_pass_kernel(GradPass a) {
   constexpr int U = 4;
   __shared__ float lds[256 * 9];
   const int c = threadIdx.x % a.across, down = 256 / a.across;
-  const int64_t col = ((int64_t)blockIdx.x * a.across + c) * 8;
-  const int n = (int)max((int64_t)0, min((int64_t)8, a.O - col));
+  const int64_t first = (int64_t)blockIdx.x * a.across * 8;
   const int64_t end = min(a.M, (blockIdx.y + 1) * a.rows);
+  const auto column = [&](int e) { return VEC ? first + c * 8 + e : first + e * a.across + c; };
   float sum[8] = {};
-  if (n > 0) {
+  if (column(0) < a.ld) {
     for (int64_t r = blockIdx.y * a.rows + threadIdx.x / a.across; r < end; r += U * down) {
       float g[U][8], z[U][8];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int64_t at = min(r + u * down, end - 1) * a.O + col;
-        load_values<8, VEC>((const T*)a.dy + at, n, g[u]);
-        if (a.pre) load_values<8, VEC>((const T*)a.pre + at, n, z[u]);
+        const int64_t at = min(r + u * down, end - 1) * a.O;
+        if constexpr (VEC) {
+          load_values<8, true>((const T*)a.dy + at + column(0), 8, g[u]);
+          if (a.pre) load_values<8, true>((const T*)a.pre + at + column(0), 8, z[u]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            g[u][e] = column(e) < a.O ? (float)((const T*)a.dy)[at + column(e)] : 0.f;
+            z[u][e] = a.pre && column(e) < a.O ? (float)((const T*)a.pre)[at + column(e)] : 0.f;
+          }
+        }
       }
+      if (a.pre) grad_all(g, z, a.act);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (r + u * down >= end) continue;
-        if (a.pre) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) g[u][e] *= activate_grad(z[u][e], a.act);
-        }
         if (a.dz) {
-          T* const p = (T*)a.dz + (r + u * down) * a.ld + col;
-          if constexpr (VEC || std::is_same_v<T, __bf16>) store_values<8, true>(p, 8, g[u]);
-          else store_values<8, false>(p, n, g[u]);
+          T* const p = (T*)a.dz + (r + u * down) * a.ld;
+          if constexpr (VEC) {
+            store_values<8, true>(p + column(0), 8, g[u]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (column(e) < a.ld) p[column(e)] = (T)g[u][e];
+          }
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum[e] += g[u][e];
@@ -250,10 +292,10 @@ __global__ __launch_bounds__(256) void grad_pass_kernel(GradPass a) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) lds[threadIdx.x * 9 + e] = sum[e];
   __syncthreads();
-  const int64_t first = (int64_t)blockIdx.x * a.across * 8;
   for (int j = threadIdx.x; j < a.across * 8 && first + j < a.O; j += 256) {
     float s = 0.f;
-    for (int d = 0; d < down; ++d) s += lds[(d * a.across + j / 8) * 9 + j % 8];
+    const int of = VEC ? j / 8 : j % a.across, e = VEC ? j % 8 : j / a.across;
+    for (int d = 0; d < down; ++d) s += lds[(d * a.across + of) * 9 + e];
     a.part[blockIdx.y * a.O + first + j] = s;
   }
 }
@@ -305,16 +347,6 @@ __global__ __launch_bounds__(1024) void column_sums_kernel(ColumnSums a) {
 
 char* at(void* workspace, int64_t offset) { return static_cast<char*>(workspace) + offset; }
 
-// x or w as a product takes it, copied to the workspace where the plan says so
-template <class T>
-hipError_t operand(GemmIn& x, int64_t offset, int64_t ld, void* workspace, hipStream_t stream) {
-  if (offset < 0) return hipSuccess;
-  void* const out = at(workspace, offset);
-  const hipError_t e = launch_pack<T>(x, out, ld, stream);
-  x.p = out, x.heads = 0, x.ld = ld, x.cols = ld;
-  return e;
-}
-
 template <class T>
 hipError_t forward(const LinearArgs& a) {
   const LinearPlan p = linear_plan(a.s);
@@ -329,8 +361,7 @@ hipError_t forward(const LinearArgs& a) {
       return vec ? launch_few_rows<true>(g) : launch_few_rows<false>(g);
     }
   }
-  hipError_t e = operand<T>(g.P, p.x, p.ldx, a.workspace, a.stream);
-  if (e == hipSuccess) e = operand<T>(g.Q, p.w, p.ldw, a.workspace, a.stream);
+  const hipError_t e = pack<T>(&g.P, p.x, p.ldx, &g.Q, p.w, p.ldw, a.workspace, a.stream);
   if (e != hipSuccess) return e;
   g.R = p.R;
   g.splits = p.splits, g.cut = p.cut, g.part = (float*)at(a.workspace, p.part);
@@ -364,10 +395,10 @@ hipError_t backward(const LinearArgs& a) {
   }
   GemmArgs x, w;
   x.stream = w.stream = a.stream, x.P = w.P = dz;
+  x.Q = a.weights(), w.Q = a.x();
+  e = pack<T>(a.dx ? &x.Q : nullptr, p.w, p.ldw, a.dw ? &w.Q : nullptr, p.x, p.ldx, a.workspace, a.stream);
+  if (e != hipSuccess) return e;
   if (a.dx) {
-    x.Q = a.weights();
-    e = operand<T>(x.Q, p.w, p.ldw, a.workspace, a.stream);
-    if (e != hipSuccess) return e;
     x.q_slow = true;
     x.I = a.s.M, x.J = a.s.K, x.R = dz.cols, x.splits = p.splits_dx, x.cut = p.cut_dx;
     x.part = (float*)at(a.workspace, p.part);
@@ -375,9 +406,6 @@ hipError_t backward(const LinearArgs& a) {
     if (a.s.heads) x.o.heads = a.s.heads, x.o.tokens = a.s.tokens, x.o.d = a.s.K / a.s.heads;
   }
   if (a.dw) {
-    w.Q = a.x();
-    e = operand<T>(w.Q, p.x, p.ldx, a.workspace, a.stream);
-    if (e != hipSuccess) return e;
     w.p_slow = w.q_slow = true;
     w.I = a.s.O, w.J = a.s.K, w.R = a.s.M, w.splits = p.splits_dw, w.cut = p.cut_dw;
     w.part = (float*)at(a.workspace, p.part_dw);

@@ -247,7 +247,7 @@ def _new(shape, dtype, like):
     """A new plain tensor on `like`'s device (new_empty is the faster call, but gives a subclass's
     own type)."""
     if type(like) is _T.Tensor:
-        return like.new_empty(shape, dtype=dtype)
+        return like.new_empty(shape) if dtype is like.dtype else like.new_empty(shape, dtype=dtype)
     return _T.empty(shape, dtype=dtype, device=like.device)
 
 
