@@ -487,8 +487,9 @@ size_t ringx_layer_norm_bwd_workspace_bytes(int64_t rows, int64_t C, ringx_dtype
  * bitwise identical.
  *   workspace: ringx_linear_workspace_bytes(...) bytes (0 for many shapes), 16-byte aligned, contents ignored:
  *   parts of products whose rows and features are few, operands whose rows do not come in 16-byte pieces.
- * RINGX_E_LINEAR unless 1 <= K, O <= 2^20, M < 2^31, x_stride >= K (heads = 0), heads divides K and tokens
- * M (heads > 0), and act is one of ringx_act.
+ * RINGX_E_LINEAR unless 1 <= K, O <= 2^20, M <= 2^31 - 1024, x_stride >= K (heads = 0), heads divides K and
+ * tokens M (heads > 0), and act is one of ringx_act; RINGX_E_SHAPE for products of more than 2^24 tiles of
+ * 128 x 128 (bf16) or 32 x 32 (fp32).
  */
 ringx_status ringx_linear(const void* x, int64_t x_stride, int64_t heads, int64_t tokens,
                           const void* w, const float* bias, const void* residual, void* y, void* pre,

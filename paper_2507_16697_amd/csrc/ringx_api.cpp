@@ -1258,7 +1258,7 @@ ringx_status make_linear(int64_t x_stride, int64_t heads, int64_t tokens, int64_
                          int64_t* bytes) {
   if (M < 1) return RINGX_E_SHAPE;
   if (dtype != RINGX_BF16 && dtype != RINGX_FP32) return RINGX_E_UNSUPPORTED;
-  if (K < 1 || O < 1 || K > ringx::kLinearMaxWidth || O > ringx::kLinearMaxWidth || M > INT32_MAX)
+  if (K < 1 || O < 1 || K > ringx::kLinearMaxWidth || O > ringx::kLinearMaxWidth || M > ringx::kLinearMaxRows)
     return RINGX_E_LINEAR;
   if (act < RINGX_ACT_NONE || act > RINGX_ACT_SILU || heads < 0) return RINGX_E_LINEAR;
   if (heads > 0 && (K % heads != 0 || tokens < 1 || M % tokens != 0)) return RINGX_E_LINEAR;
@@ -1270,7 +1270,7 @@ ringx_status make_linear(int64_t x_stride, int64_t heads, int64_t tokens, int64_
   s->bf16 = dtype == RINGX_BF16;
   if (!mul_ok(M - 1, s->ldx, &x) || x > kMaxElems - K) return RINGX_E_SHAPE;
   *bytes = (x + K) * esize(dtype);
-  // a launch has at most 2^32 threads: tiles of 128 x 128 in bf16 and 32 x 32 in fp32 in parts, 256 threads
+  // a launch has at most 2^32 threads: 256 to a tile of 128 x 128 in bf16 and 32 x 32 in fp32
   const int64_t side = s->bf16 ? 128 : 32;
   const auto tiles = [side](int64_t i, int64_t j) {
     return ((i + side - 1) / side) * ((j + side - 1) / side);

@@ -656,6 +656,7 @@ struct LinearPlan {
   }
 };
 constexpr int64_t kLinearMaxWidth = int64_t(1) << 20;   // of K and O
+constexpr int64_t kLinearMaxRows = (int64_t(1) << 31) - 1024;   // 32-bit positions, a step of headroom
 constexpr int64_t kFewRows = 64;
 // Offsets of an operand's tile are 31 bits: rows of at most 2^21 values, heads whose batch has at most 2^29.
 inline bool linear_near(const LinearShape& s) {

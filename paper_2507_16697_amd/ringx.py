@@ -247,7 +247,7 @@ def _new(shape, dtype, like):
     """A new plain tensor on `like`'s device (new_empty is the faster call, but gives a subclass's
     own type)."""
     if type(like) is _T.Tensor:
-        return like.new_empty(shape) if dtype is like.dtype else like.new_empty(shape, dtype=dtype)
+        return like.new_empty(shape, dtype=dtype)
     return _T.empty(shape, dtype=dtype, device=like.device)
 
 
@@ -678,7 +678,7 @@ def ringx_tt_tokenize(field, k: int, ratio: int, centre, p: int, sigma=None, out
 
 def _launch(name, like, stream, *args):
     """Call an entry point whose last argument is the stream, with `like`'s device current."""
-    fn = getattr(_lib or lib(), name)
+    fn = getattr(lib(), name)
     cuda, device = _T.cuda, like.device
     here = cuda.current_device()
     if device.index != here:
@@ -1023,9 +1023,9 @@ def ringx_layer_norm_bwd(x, dy, stats, weight=None, bias=None, dres=None, dx=Non
         raise ValueError("a weight's gradient without the weight")
     dx = _out_as("dx", dx, x, stream)
     if weight is not None:
-        dweight = _out("dweight", dweight, (C,), torch.float32, x, stream)
+        dweight = _out_like("dweight", dweight, weight, stream)
     if bias is not None:
-        dbias = _out("dbias", dbias, (C,), torch.float32, x, stream)
+        dbias = _out_like("dbias", dbias, bias, stream)
     if weight is not None or bias is not None:
         workspace = _workspace(workspace, ringx_layer_norm_bwd_workspace_bytes(rows, C, code), x, stream)
     else:
@@ -1122,9 +1122,10 @@ def ringx_linear_bwd(x, w, dy, pre=None, act="none", bias=None, need_dx: bool = 
         if dw_dtype is torch.float32:
             dw = _grad_out("dw", dw, (O, K), x, accumulate_dw, stream)
         else:
-            dw = _out("dw", dw, (O, K), dw_dtype, x, stream)
+            dw = _out_like("dw", dw, w, stream)
     if bias is not None:
-        dbias = _grad_out("dbias", dbias, (O,), x, accumulate_dw, stream)
+        dbias = (_grad_out("dbias", dbias, (O,), x, True, stream) if accumulate_dw else
+                 _out_like("dbias", dbias, bias, stream))
     workspace = _workspace(workspace, ringx_linear_bwd_workspace_bytes(step, heads, tokens, M, K, O, a, code),
                            x, stream)
     _launch("ringx_linear_bwd", x, stream, x.data_ptr(), step, heads, tokens, w.data_ptr(), dy.data_ptr(), pp,

@@ -140,14 +140,16 @@ def test_activations_at_their_ends(act):
 @pytest.mark.parametrize("store", ["bf16", "fp32"])
 @pytest.mark.parametrize("M,K,O,heads", [
     (4100, 384, 1152, 0),      # parts of r along the weights' gradient
-    (2049, 1024, 4104, 0),     # large tiles, ragged
+    (4097, 328, 3848, 0),      # large tiles, ragged
+    (8194, 1032, 520, 0),      # last tiles in parts
     (5000, 250, 60, 0),        # rows copied
     (4608, 512, 768, 8),       # heads of 64, batches of whole steps
+    (1000, 520, 264, 0),       # both gradients in one launch, two groups of waves
+    (3000, 712, 392, 0),       # and one group
     (70, 4096, 96, 0),         # parts of r forward
+    (300, 2072, 200, 0),
 ])
 def test_large(M, K, O, heads, store):
-    if store == "fp32" and O > 4000:
-        O = 1032
     lead = (2, M // 2) if heads else (M,)
     x, w, b, res, dy = make(M, lead, K, O, store, heads)
     y, pre = ringx.ringx_linear(x, w, b, act="gelu", residual=res, need_pre=True)
