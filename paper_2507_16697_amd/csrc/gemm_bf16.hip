@@ -3,23 +3,15 @@
 // Forward: P = x, Q = w.  dx: P = dz, Q = w read along its rows.  dw: P = dz, Q = x, both read along
 // their rows.
 //
-// A workgroup makes a TI x TJ tile of out.  Operands go through LDS in steps of 64 along r, two buffers
-// filled by direct global->LDS loads: while one step is multiplied, the next one is in flight.  An operand
-// that is stored with r along its rows (contiguous) is a tile of W rows x 64; one stored the other way
-// (slow: r is the row) a tile of 64 rows x W, whose fragments come from transposed LDS reads.  16-byte
-// pieces of a row are XOR-swizzled by the row so that neither kind of read meets itself in a bank:
-// contiguous tiles, 128 bytes a row, by (row / 2) mod 8 (16 lanes read one piece of 16 rows); slow tiles by
-// 4 (row mod 4) + (row / 4) mod 4 (16 lanes read 32 bytes of 4 rows).
+// v_mfma_f32_16x16x32_bf16 with Q as its first operand: a lane holds one row i and four neighbouring j at a
+// time (32 x 32 x 16, whose accumulators are read and written twice as often, took 4 to 7% more time).  Steps are of
+// 64 of r (gemm_feed.h).
 //
-// All loads are buffer loads from the tile's place on: what lies past the tensor's end reads as zero, and
-// so do the pieces past R in the last step, whose offsets are moved outside.  Rows of i or j past the
-// end repeat the last one (contiguous) or are what follows (slow): they reach only values that are not
-// stored.
-//
-// v_mfma_f32_32x32x16_bf16 with Q as its first operand: a lane holds one row i and four neighbouring j at a
-// time.  The waves pass their values through LDS, 32 rows of i at a time, so that the epilogue has 8
-// neighbouring j of one row in a lane: 16-byte loads and stores, 128 bytes of a row in a piece.
+// Bound by the matrix cores' power: 8192^3 of normally distributed values runs at 1.5 GHz, with the cores busy for
+// 75% of the cycles (1390 TFLOP/s, rocprofv3 counters); zeros take 20% less time, launches without the barriers
+// 4%.  Deeper buffers (four of 32 of r) took 6% more, wave tiles of 128 x 128 from four waves as much.
 
+#include "gemm_feed.h"
 #include "linear.h"
 
 namespace ringx {
@@ -27,137 +19,10 @@ namespace {
 
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
-constexpr uint32_t kOutside = 0x80000000u;   // a byte offset past any buffer here
-constexpr uint32_t kMostBytes = 0x7ffffff0u;
-
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-// One 16-byte direct buffer->LDS load per lane; LDS destination lds_base + 16 lane.  Volatile asm for the
-// same reasons as the global form in ringx_device.h.
-__device__ __forceinline__ void buffer_lds16(const u32x4& rsrc, uint32_t off, uint32_t lds_base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :
-               : "s"(lds_base), "v"(off), "s"(rsrc)
-               : "memory", "m0");
-}
-#pragma clang diagnostic pop
-
-__device__ __forceinline__ int64_t uniform64(int64_t x) {
-  return reinterpret_cast<int64_t>(uniform_ptr(reinterpret_cast<const void*>(x)));
-}
-
-// One operand's way into LDS, BK of r at a time.
-template <bool SLOW, int W, int THREADS, int BK>
-struct Feed {
-  static constexpr int kLoads = W * BK * 2 / (THREADS * 16);
-  static constexpr int kRowChunks = SLOW ? W / 8 : BK / 8;
-  static_assert(kLoads * THREADS * 16 == W * BK * 2 && (!SLOW || W >= 128), "whole rounds of loads");
-  static_assert(SLOW || THREADS / kRowChunks % 16 == 0, "rounds keep the swizzle's phase");
-  uint32_t off[kLoads];
-  int64_t base, left;    // address of the step's first row or column; bytes from it to the tensor's end
-  int64_t step, turn;    // bytes to the next step; what is added where a head (or batch) ends
-  int in, per;           // steps left in this head (or batch), steps of one (0: there are none)
-  int chunk;             // contiguous: the lane's first r of a step / 8
-
-  static __device__ __forceinline__ int swz(int row) {
-    if (SLOW) return ((row & 3) << 2) | ((row >> 2) & 3);
-    return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
-  }
-
-  // Width index w0 and r0 (a multiple of BK) on.  Sizes fit 32 bits, which divisions are made in: with those
-  // of 64 bits a workgroup's start took 1400 instructions, 5 us.
-  __device__ __forceinline__ void start(const GemmIn& x, uint32_t w0, uint32_t r0, int tid) {
-    const uint32_t rows = (uint32_t)x.rows, cols = (uint32_t)x.cols, ld = (uint32_t)x.ld;
-    int64_t total = (int64_t)(rows - 1) * ld + cols, at;   // elements; from the tensor's start
-    turn = 0, per = 0, in = 0;
-    if constexpr (!SLOW) {
-      at = (int64_t)w0 * ld + r0;
-      step = 2 * BK;
-    } else {
-      at = (int64_t)r0 * ld + w0;
-      step = 2 * BK * (int64_t)ld;
-    }
-    const uint32_t d = (uint32_t)x.d, tokens = (uint32_t)x.tokens;
-    uint32_t b0 = 0;
-    if (x.heads) {
-      cold_path();
-      total = (int64_t)rows * cols;
-      if constexpr (!SLOW) {
-        b0 = w0 / tokens;
-        const uint32_t hd = d / BK, s = r0 / BK;
-        at = (int64_t)b0 * tokens * cols + (int64_t)(s / hd) * tokens * d + s % hd * BK;
-        per = (int)hd, in = (int)(hd - s % hd);
-        turn = 2 * ((int64_t)tokens * d - d);
-      } else {
-        b0 = r0 / tokens;
-        const uint32_t t = r0 - b0 * tokens;
-        at = (int64_t)b0 * tokens * cols + (int64_t)t * d;
-        step = 2 * BK * (int64_t)d;
-        per = (int)(tokens / BK), in = (int)((tokens - t) / BK);
-        turn = 2 * (int64_t)(cols - d) * tokens;
-      }
-    }
-    base = uniform64(reinterpret_cast<int64_t>(x.p) + 2 * at);
-    left = uniform64(2 * (total - at));
-    chunk = 0;
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) {
-      const uint32_t slot = u * THREADS + tid;
-      const uint32_t row = slot / kRowChunks;
-      const uint32_t c = (slot % kRowChunks) ^ swz(row);
-      if constexpr (!SLOW) {
-        chunk = (int)c;   // the same for every u: rounds are whole multiples of 16 rows
-        off[u] = 2 * (min(w0 + row, rows - 1) - w0) * ld + c * 16;
-      } else {
-        off[u] = 2 * row * ld + c * 16;
-      }
-    }
-    if (x.heads) {
-      cold_path();
-#pragma unroll
-      for (int u = 0; u < kLoads; ++u) {
-        const uint32_t slot = u * THREADS + tid;
-        const uint32_t row = slot / kRowChunks;
-        const uint32_t c = (slot % kRowChunks) ^ swz(row);
-        if constexpr (!SLOW) {
-          const uint32_t i = min(w0 + row, rows - 1), b = i / tokens;
-          off[u] = 2 * ((b - b0) * tokens * cols + (i - b * tokens) * d) + c * 16;
-        } else {
-          const uint32_t col = min(w0 + c * 8, cols - 8);
-          const uint32_t h = col / d;
-          off[u] = 2 * (h * tokens * d + (col - h * d) + row * d);
-        }
-      }
-    }
-  }
-  // The loads of a step whose first r has `rest` of them left (none: nothing is read, zeros arrive), one
-  // by one, then on to the next step.  No branch, so that a loop's body stays one.
-  u32x4 rsrc;
-  bool inside;
-  __device__ __forceinline__ void begin(int rest) {
-    const uint32_t n = left <= 0 ? 0u : left > (int64_t)kMostBytes ? kMostBytes : (uint32_t)left;
-    rsrc = u32x4{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, rest > 0 ? n : 0u, 0x00020000u};
-    inside = SLOW || chunk * 8 < rest;
-    int64_t s = step;
-    --in;
-    const bool end = per && in == 0;
-    s += end ? turn : 0, in = end ? per : in;
-    base += s, left -= s;
-  }
-  __device__ __forceinline__ void load(int u, uint32_t dst) const {   // dst: the wave's place
-    buffer_lds16(rsrc, inside ? off[u] : kOutside, dst + u * THREADS * 16);
-  }
-  __device__ __forceinline__ void all(uint32_t dst, int rest) {
-    begin(rest);
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) load(u, dst);
-  }
-};
-
 // Fragments of 16 of the width x 32 of r: lane l has width index l % 16 and r = 8 (l / 16) .. + 7.
 template <bool SLOW, int W, int BLOCKS, int BK>
 struct Frags {
-  using F = Feed<SLOW, W, 512, BK>;
+  using F = Feed<__bf16, SLOW, W, 512>;
   static constexpr int kCols = BLOCKS < 4 ? BLOCKS : 4;   // 64 columns further on the swizzle is the same
   int off[SLOW ? 2 : BK / 32][SLOW ? kCols : 1];
   __device__ __forceinline__ void start(int w0, int lane) {   // w0: the wave's first of the tile
@@ -328,14 +193,6 @@ struct Out {
   }
 };
 
-// Tile t of a product: tiles in groups of 4 along i, so that those at work on one XCD share operands.
-__device__ __forceinline__ void place(uint32_t t, uint32_t ti, uint32_t tj, uint32_t& i, uint32_t& j) {
-  constexpr uint32_t kGroup = 4;
-  const uint32_t g0 = t / (kGroup * tj) * kGroup, gn = min(kGroup, ti - g0);
-  t -= g0 * tj;
-  i = g0 + t % gn, j = t / gn;
-}
-
 // Workgroup `id` of a product.
 template <bool PS, bool QS, class C>
 __device__ __forceinline__ void product(const GemmArgs& a, const uint32_t id, char* const lds_all) {
@@ -368,8 +225,8 @@ __device__ __forceinline__ void product(const GemmArgs& a, const uint32_t id, ch
   const int count = (int)(s1 - s0 + kGroups - 1) / kGroups;
   if (kGroups > 1 && group == 0) s1 = s0 + count;
   if (kGroups > 1 && group == 1) s0 = s0 + count;
-  Feed<PS, TI, C::kThreads, BK> fp;
-  Feed<QS, TJ, C::kThreads, BK> fq;
+  Feed<__bf16, PS, TI, C::kThreads> fp;
+  Feed<__bf16, QS, TJ, C::kThreads> fq;
   fp.start(a.P, i0, BK * s0, tid);
   fq.start(a.Q, j0, BK * s0, tid);
   const int wi = wave / WJ, wj = wave % WJ;
@@ -410,8 +267,8 @@ __device__ __forceinline__ void product(const GemmArgs& a, const uint32_t id, ch
   auto nothing = [](int) {};
   using std::integral_constant;
   typedef integral_constant<int, 0> kNone;
-  typedef integral_constant<int, Feed<PS, TI, C::kThreads, BK>::kLoads> kLoadsP;
-  typedef integral_constant<int, Feed<QS, TJ, C::kThreads, BK>::kLoads> kLoadsQ;
+  typedef integral_constant<int, Feed<__bf16, PS, TI, C::kThreads>::kLoads> kLoadsP;
+  typedef integral_constant<int, Feed<__bf16, QS, TJ, C::kThreads>::kLoads> kLoadsQ;
   // Two buffers.  A step's buffer is free behind the barrier after its last reads; the loads of two steps
   // later go there, P's beside the products that follow, Q's beside the next ones.  Fragments are read one
   // unit ahead, those of a step's first unit behind that same barrier, so that the last unit's
@@ -541,25 +398,7 @@ __global__ __launch_bounds__(C::kThreads * C::kGroups, 2) void gemm_pair_kernel(
   } else if (id < p.wgs_dx + p.wgs_dw) {
     product<true, true, C>(p.dw, id - p.wgs_dx, lds);
   } else {
-    // 64 columns, a wave for every so many parts, then the waves in their order
-    constexpr int kWaves = C::kWaves * C::kGroups;
-    float(*const sums)[64] = reinterpret_cast<float(*)[64]>(lds);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t col = (int64_t)(id - p.wgs_dx - p.wgs_dw) * 64 + lane;
-    float t = 0.f;
-    if (col < p.sums.cols) {
-#pragma unroll 8
-      for (int i = wave; i < p.sums.parts; i += kWaves) t += p.sums.part[i * p.sums.cols + col];
-    }
-    sums[wave][lane] = t;
-    __syncthreads();
-    if (wave == 0 && col < p.sums.cols) {
-      float s = 0.f;
-#pragma unroll
-      for (int i = 0; i < kWaves; ++i) s += sums[i][lane];
-      float* const out = p.sums.out[0] + col;
-      *out = p.sums.accumulate ? *out + s : s;
-    }
+    sum_columns<C::kWaves * C::kGroups>(p.sums, id - p.wgs_dx - p.wgs_dw, reinterpret_cast<float(*)[64]>(lds));
   }
 }
 

@@ -39,10 +39,10 @@ struct Row {
         if (c < C) x = *reinterpret_cast<const u32x4*>(p + c);
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[4 * v + j] = x[j];
-      } else if constexpr (std::is_same_v<T, float>) {
-        w[v] = c < C ? __float_as_uint(p[c]) : 0u;
       } else {
-        w[v] = c < C ? (uint32_t)__builtin_bit_cast(uint16_t, p[c]) << 16 : 0u;
+        // without a branch, which would wait for each load alone
+        const float x = (float)p[min(c, C - 1)];
+        w[v] = c < C ? __float_as_uint(x) : 0u;
       }
     }
   }
@@ -86,7 +86,8 @@ __device__ __forceinline__ void load_vector(const float* p, float otherwise, int
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int c = R::col(e + j, t);
-        x[e + j] = p && c < C ? p[c] : otherwise;
+        x[e + j] = otherwise;
+        if (p) x[e + j] = p[min(c, C - 1)];
       }
     }
   }
@@ -131,8 +132,7 @@ struct RowSum {
   }
 };
 
-// Workgroups of TPR > 256 threads hold one row; TPR <= 64: 256 / TPR rows, and 128 and 256: one row too, in a
-// workgroup of TPR threads.
+// Rows of up to 64 threads share a workgroup of 256, wider ones have one of their own.
 template <int TPR>
 constexpr int kGroup = TPR <= 64 ? 256 : TPR;   // threads of a workgroup
 template <int TPR>
@@ -186,7 +186,7 @@ __global__ __launch_bounds__(kGroup<TPR>) void layer_norm_kernel(NormArgs a) {
 }
 
 template <class T, bool VEC, int E, int TPR>
-__global__ __launch_bounds__(kGroup<TPR>) void layer_norm_bwd_kernel(NormArgs a) {
+__global__ __launch_bounds__(kGroup<TPR>, TPR <= 256 ? 2 : 1) void layer_norm_bwd_kernel(NormArgs a) {
   using R = Row<T, VEC, E, TPR>;
   constexpr int kWidth = E * TPR;
   __shared__ RowSum<TPR> sum;
@@ -292,10 +292,13 @@ hipError_t by_width(const NormArgs& a, bool bwd) {
   if (a.C <= 256) return launch<T, VEC, 8, 32>(a, bwd);
   if (a.C <= 512) return launch<T, VEC, 8, 64>(a, bwd);
   if (a.C <= 1024) return launch<T, VEC, 16, 64>(a, bwd);
-  if (a.C <= 2048) return launch<T, VEC, 32, 64>(a, bwd);
-  if (a.C <= 4096) return launch<T, VEC, 32, 128>(a, bwd);
-  if (a.C <= 8192) return launch<T, VEC, 32, 256>(a, bwd);
-  return launch<T, VEC, 32, 512>(a, bwd);
+  // 32 values to a thread only in bf16 pieces: the others' backward would not keep them in registers (with 16,
+  // only the widest rows' does not, of 1024 threads)
+  constexpr int E = VEC && std::is_same_v<T, __bf16> ? 32 : 16;
+  if (a.C <= 2048) return launch<T, VEC, E, 2048 / E>(a, bwd);
+  if (a.C <= 4096) return launch<T, VEC, E, 4096 / E>(a, bwd);
+  if (a.C <= 8192) return launch<T, VEC, E, 8192 / E>(a, bwd);
+  return launch<T, VEC, E, 16384 / E>(a, bwd);
 }
 
 }  // namespace

@@ -185,4 +185,26 @@ __device__ __forceinline__ void finish(const GemmOut& o, int64_t i, int64_t j0, 
   }
 }
 
+// Sums of 64 columns of parts, by WAVES waves of a workgroup: a wave every so many parts, then the waves in their
+// order.
+template <int WAVES>
+__device__ __forceinline__ void sum_columns(const ColumnSums& a, uint32_t id, float (*lds)[64]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t col = (int64_t)id * 64 + lane;
+  float t = 0.f;
+  if (col < a.cols) {
+#pragma unroll 8
+    for (int i = wave; i < a.parts; i += WAVES) t += a.part[i * a.cols + col];
+  }
+  lds[wave][lane] = t;
+  __syncthreads();
+  if (wave == 0 && col < a.cols) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) s += lds[i][lane];
+    float* const out = a.out[0] + col;
+    *out = a.accumulate ? *out + s : s;
+  }
+}
+
 }  // namespace ringx

@@ -19,7 +19,7 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 
 template <int MB, bool VEC>
 __global__ __launch_bounds__(512) void few_rows_kernel(GemmArgs a) {
-  constexpr int kUnroll = MB == 1 ? 8 : 4;
+  constexpr int kUnroll = VEC ? (MB == 1 ? 8 : 4) : (MB == 4 ? 1 : 2);   // what the registers hold
   __shared__ f32x4 lds[8][MB][64];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -52,14 +52,13 @@ __global__ __launch_bounds__(512) void few_rows_kernel(GemmArgs a) {
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if (k + e < K) {
-          int64_t at = k + e;
-          if (heads) {
-            const uint32_t h = (uint32_t)at / (uint32_t)a.P.d;
-            at = (int64_t)h * a.P.tokens * a.P.d + (at - (int64_t)h * a.P.d);
-          }
-          v[e] = p[at];
+        int64_t at = min(k + e, K - 1);
+        if (heads) {
+          const uint32_t h = (uint32_t)at / (uint32_t)a.P.d;
+          at = (int64_t)h * a.P.tokens * a.P.d + (at - (int64_t)h * a.P.d);
         }
+        const __bf16 y = p[at];
+        v[e] = k + e < K ? y : (__bf16)0.f;
       }
     }
     return v;
@@ -197,7 +196,10 @@ __global__ __launch_bounds__(256) void pack_kernel(Pack<T> a) {
     } else {
       T v[N];
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = c + e < x.cols ? p[column(c + e)] : (T)0.f;
+      for (int e = 0; e < N; ++e) {
+        const T y = p[column(min(c + e, (uint32_t)x.cols - 1))];
+        v[e] = c + e < x.cols ? y : (T)0.f;
+      }
       if (a.ld[k] % N == 0) {
         *reinterpret_cast<u32x4*>(q) = __builtin_bit_cast(u32x4, v);
       } else {
@@ -264,8 +266,16 @@ __global__ __launch_bounds__(256) void grad_pass_kernel(GradPass a) {
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            g[u][e] = column(e) < a.O ? (float)((const T*)a.dy)[at + column(e)] : 0.f;
-            z[u][e] = a.pre && column(e) < a.O ? (float)((const T*)a.pre)[at + column(e)] : 0.f;
+            // without a branch, which would wait for each load alone
+            const float y = (float)((const T*)a.dy)[at + min(column(e), a.O - 1)];
+            g[u][e] = column(e) < a.O ? y : 0.f;
+          }
+          if (a.pre) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float y = (float)((const T*)a.pre)[at + min(column(e), a.O - 1)];
+              z[u][e] = column(e) < a.O ? y : 0.f;
+            }
           }
         }
       }
@@ -411,12 +421,10 @@ hipError_t backward(const LinearArgs& a) {
     w.part = (float*)at(a.workspace, p.part_dw);
     w.o.out = a.dw, w.o.J = a.s.K, w.o.f32 = a.dw_f32, w.o.accumulate = a.accumulate;
   }
-  if constexpr (std::is_same_v<T, __bf16>) {
-    if (p.pair && a.dx && a.dw) {
-      GemmPair both;
-      both.dx = x, both.dw = w, both.sums = c;
-      return launch_gemm_pair_bf16(both);
-    }
+  if (p.pair && a.dx && a.dw) {
+    GemmPair both;
+    both.dx = x, both.dw = w, both.sums = c;
+    return std::is_same_v<T, __bf16> ? launch_gemm_pair_bf16(both) : launch_gemm_pair_f32(both);
   }
   if (a.dx) e = launch_product<T>(x);
   if (a.dw && e == hipSuccess) e = launch_product<T>(w);

@@ -588,19 +588,23 @@ inline int gemm_f32_splits(int64_t I, int64_t J, int64_t R) {
   const int64_t s = std::min<int64_t>({512 / tiles, (R + 63) / 64 / 4, 32});
   return (int)std::max<int64_t>(s, 1);
 }
+// Both products of a backward in one launch: small tiles, without parts, whose r is short.
+inline bool gemm_f32_pair(int64_t M, int64_t K, int64_t O) {
+  return !gemm_f32_large(M, K) && !gemm_f32_large(O, K) && std::max(M, O) <= 2048;
+}
 
 // The pass over a gradient [M, O]: threads across 8 columns each, rows of a workgroup, workgroups.
 struct GradGrid {
   int across;
   int64_t rows, x, y;
 };
-inline GradGrid grad_grid(int64_t M, int64_t O, bool few) {   // few: at most 64 along the rows
+inline GradGrid grad_grid(int64_t M, int64_t O, bool few) {   // few: at most 160 along the rows
   GradGrid g;
   g.across = 1;
   while (g.across < 64 && 8 * g.across < O) g.across *= 2;
   g.x = (O + 8 * g.across - 1) / (8 * g.across);
   const int64_t least = 4 * (256 / g.across);      // rows of one round
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(few ? 64 : 512, 2048 / g.x));
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(few ? 160 : 512, 2048 / g.x));
   g.rows = std::max<int64_t>(least, ((M + most - 1) / most + least - 1) / least * least);
   g.y = (M + g.rows - 1) / g.rows;
   return g;
@@ -647,7 +651,7 @@ struct LinearPlan {
   int64_t R = 0;                           // forward: the product's r
   int splits = 1, splits_dx = 1, splits_dw = 1;   // fp32
   GemmCut cut, cut_dx, cut_dw;             // bf16
-  bool pair = false;                       // backward, bf16: both products in one launch
+  bool pair = false;                       // backward: both products in one launch
   int64_t bytes = 0;
   int64_t take(int64_t n) {
     const int64_t at = bytes;
@@ -673,8 +677,13 @@ inline LinearPlan linear_plan(const LinearShape& s) {
     const bool fits = s.K % 8 == 0 && linear_near(s) && (s.heads ? s.K / s.heads % 64 == 0 : s.ldx % 8 == 0);
     if (!fits) p.x = p.take(2 * s.M * Kp), p.ldx = Kp;
     if (Kp != s.K) p.w = p.take(2 * s.O * Kp), p.ldw = Kp;
-  } else if (s.heads || !linear_near(s)) {
-    p.x = p.take(4 * s.M * s.K), p.ldx = s.K;
+  } else {
+    const int64_t Kt = (s.K + 3) / 4 * 4;
+    const bool large = gemm_f32_large(s.M, s.O);   // in 16-byte pieces
+    if (large) p.R = Kt;
+    if (s.heads || !linear_near(s) || (large && (Kt != s.K || s.ldx % 4 != 0))) p.ldx = large ? Kt : s.K;
+    if (p.ldx) p.x = p.take(4 * s.M * p.ldx);
+    if (large && Kt != s.K) p.w = p.take(4 * s.O * Kt), p.ldw = Kt;
   }
   if (s.bf16) p.cut = gemm_cut(s.M, s.O, p.R);
   else p.splits = gemm_f32_splits(s.M, s.O, p.R);
@@ -684,26 +693,25 @@ inline LinearPlan linear_plan(const LinearShape& s) {
 }
 inline LinearPlan linear_bwd_plan(const LinearShape& s, int act) {
   LinearPlan p;
-  const int64_t Kp = (s.K + 7) / 8 * 8, Op = s.bf16 ? (s.O + 7) / 8 * 8 : s.O;
-  const int64_t es = s.bf16 ? 2 : 4;
+  // rows in 16-byte pieces: bf16, and fp32 where one of the products is large
+  const bool pieces = s.bf16 || gemm_f32_large(s.M, s.K) || gemm_f32_large(s.O, s.K);
+  const int64_t es = s.bf16 ? 2 : 4, piece = pieces ? 16 / es : 1;
+  const int64_t Kp = (s.K + piece - 1) / piece * piece, Op = (s.O + piece - 1) / piece * piece;
   p.ldz = Op;
   if (act || Op != s.O) p.dz = p.take(es * s.M * Op);
-  if (s.bf16) {
-    // dw walks heads 64 tokens at a time
-    const bool fits = s.K % 8 == 0 && linear_near(s) &&
-                      (s.heads ? s.K / s.heads % 8 == 0 && s.tokens % 64 == 0 : s.ldx % 8 == 0);
-    if (!fits) p.x = p.take(2 * s.M * Kp), p.ldx = Kp;
-    if (Kp != s.K) p.w = p.take(2 * s.O * Kp), p.ldw = Kp;
-  } else if (s.heads || !linear_near(s)) {
-    p.x = p.take(4 * s.M * s.K), p.ldx = s.K;
-  }
+  // dw walks bf16 heads 64 tokens at a time
+  const bool fits = Kp == s.K && linear_near(s) &&
+                    (s.heads ? s.bf16 && s.K / s.heads % 8 == 0 && s.tokens % 64 == 0 : s.ldx % piece == 0);
+  if (!fits) p.x = p.take(es * s.M * Kp), p.ldx = Kp;
+  if (Kp != s.K) p.w = p.take(es * s.O * Kp), p.ldw = Kp;
   int64_t dx = 0, dw = 0;
   if (s.bf16) {
     p.cut_dx = gemm_cut(s.M, s.K, Op), p.cut_dw = gemm_cut(s.O, s.K, s.M);
     p.pair = gemm_cut_pair(s.M, s.K, s.O, &p.cut_dx, &p.cut_dw);
     dx = p.cut_dx.part_bytes, dw = p.cut_dw.part_bytes;
   } else {
-    p.splits_dx = gemm_f32_splits(s.M, s.K, Op), p.splits_dw = gemm_f32_splits(s.O, s.K, s.M);
+    p.pair = gemm_f32_pair(s.M, s.K, s.O);
+    if (!p.pair) p.splits_dx = gemm_f32_splits(s.M, s.K, Op), p.splits_dw = gemm_f32_splits(s.O, s.K, s.M);
     if (p.splits_dx > 1) dx = 4 * p.splits_dx * s.M * s.K;
     if (p.splits_dw > 1) dw = 4 * p.splits_dw * s.O * s.K;
   }
@@ -742,6 +750,7 @@ hipError_t launch_column_sums(const ColumnSums& a);
 hipError_t launch_gemm_bf16(const GemmArgs& a);
 hipError_t launch_gemm_pair_bf16(const GemmPair& p);
 hipError_t launch_gemm_f32(const GemmArgs& a);
+hipError_t launch_gemm_pair_f32(GemmPair p);
 hipError_t launch_linear(const LinearArgs& a);
 hipError_t launch_linear_bwd(const LinearArgs& a);
 
