@@ -40,15 +40,23 @@ struct Row {
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[4 * v + j] = x[j];
       } else {
-        // without a branch, which would wait for each load alone
-        const float x = (float)p[min(c, C - 1)];
-        w[v] = c < C ? __float_as_uint(x) : 0u;
+        w[v] = 0u;
+        if (c < C) w[v] = raw_bits(p + c);
       }
     }
   }
   __device__ __forceinline__ float get(int e) const {
-    if constexpr (!VEC || std::is_same_v<T, float>) return __uint_as_float(w[e]);
+    if constexpr (!VEC || std::is_same_v<T, float>) return from_raw<T>(w[e]);
     else return e % 2 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
+  }
+  // Values loaded one by one, each under its condition, have arrived: nothing that uses them joins their
+  // conditional blocks, where it would wait for every load alone (bf16, 4000 rows of 2047, backward: 121 -> 31 us;
+  // fp32's use joins none).
+  __device__ __forceinline__ void arrived() {
+    if constexpr (!VEC && std::is_same_v<T, __bf16>) {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) asm volatile("" : "+v"(w[i]));
+    }
   }
   static __device__ __forceinline__ void store(T* p, int t, int C, const float (&x)[E]) {
 #pragma unroll
@@ -87,7 +95,7 @@ __device__ __forceinline__ void load_vector(const float* p, float otherwise, int
       for (int j = 0; j < 4; ++j) {
         const int c = R::col(e + j, t);
         x[e + j] = otherwise;
-        if (p) x[e + j] = p[min(c, C - 1)];
+        if (p && c < C) x[e + j] = p[c];
       }
     }
   }
@@ -211,6 +219,8 @@ __global__ __launch_bounds__(kGroup<TPR>, TPR <= 256 ? 2 : 1) void layer_norm_bw
     rg.load(dy + row * C, t, C);
     if (dres) rr.load(dres + row * C, t, C);
     const float mean = a.stats_in[row], r = a.stats_in[a.rows + row];
+    rx.arrived();
+    rg.arrived();
     float n[E], g[E], s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -225,6 +235,7 @@ __global__ __launch_bounds__(kGroup<TPR>, TPR <= 256 ? 2 : 1) void layer_norm_bw
     }
     const f32x2 ss = sum(s1, s2, slot);
     const float m1 = ss[0] * inv, m2 = ss[1] * inv;
+    if (dres) rr.arrived();
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       g[e] = r * (g[e] - m1 - n[e] * m2);

@@ -257,6 +257,7 @@ __global__ __launch_bounds__(256) void grad_pass_kernel(GradPass a) {
   if (column(0) < a.ld) {
     for (int64_t r = blockIdx.y * a.rows + threadIdx.x / a.across; r < end; r += U * down) {
       float g[U][8], z[U][8];
+      uint32_t gw[U][8], zw[U][8];   // not VEC: as they are stored
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int64_t at = min(r + u * down, end - 1) * a.O;
@@ -266,18 +267,20 @@ __global__ __launch_bounds__(256) void grad_pass_kernel(GradPass a) {
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            // without a branch, which would wait for each load alone
-            const float y = (float)((const T*)a.dy)[at + min(column(e), a.O - 1)];
-            g[u][e] = column(e) < a.O ? y : 0.f;
-          }
-          if (a.pre) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float y = (float)((const T*)a.pre)[at + min(column(e), a.O - 1)];
-              z[u][e] = column(e) < a.O ? y : 0.f;
+            uint32_t y = 0u, w = 0u;
+            if (column(e) < a.O) {
+              y = raw_bits((const T*)a.dy + at + column(e));
+              if (a.pre) w = raw_bits((const T*)a.pre + at + column(e));
             }
+            gw[u][e] = y, zw[u][e] = w;
           }
         }
+      }
+      if constexpr (!VEC) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) g[u][e] = from_raw<T>(gw[u][e]), z[u][e] = from_raw<T>(zw[u][e]);
       }
       if (a.pre) grad_all(g, z, a.act);
 #pragma unroll

@@ -39,6 +39,15 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
+// A value as it is stored, and from that.  Where a load is under a condition of its own its conversion is kept
+// out of it: inside, it would wait for the load before the next one is issued.
+__device__ __forceinline__ uint32_t raw_bits(const float* p) { return __float_as_uint(*p); }
+__device__ __forceinline__ uint32_t raw_bits(const __bf16* p) { return __builtin_bit_cast(uint16_t, *p); }
+template <class T>
+__device__ __forceinline__ float from_raw(uint32_t w) {
+  return __uint_as_float(sizeof(T) == 4 ? w : w << 16);
+}
+
 // x[l] + x[l ^ 32] and max(x[l], x[l ^ 32]) for every lane l, through v_permlane32_swap.  The
 // swap of two copies of x returns, for lanes below 32, (x[l], x[l + 32]) and for the others
 // (x[l - 32], x[l]): each result alone holds the lane's own value on one half of the wave, so the
