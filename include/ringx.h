@@ -457,8 +457,9 @@ ringx_status ringx_layer_norm(const void* x, int64_t row_stride, const float* we
 /*
  * Backward of ringx_layer_norm, with n = (x - mean) r from its stats and g = dy weight:
  *   dx = r (g - mean_c(g) - n mean_c(g n)) + dres;  dweight = sum over rows of dy n;  dbias = that of dy.
- *   dy [rows, C] (dtype), contiguous; dres the same or NULL: the gradient that reaches x by another
- *   way (the residual of a pre-norm block), added before dx is rounded.
+ *   dy [rows, C], contiguous, in dy_dtype: dtype, or fp32 (as a product's backward gives it without rounding).
+ *   dres [rows, C] (dtype), contiguous, or NULL: the gradient that reaches x by another way (the residual of a
+ *   pre-norm block), added before dx is rounded.
  *   dx [rows, C] (dtype), contiguous; dweight, dbias [C] fp32, either or both NULL.  All overwritten,
  *   bitwise reproducible.
  *   workspace: ringx_layer_norm_bwd_workspace_bytes(...) bytes, 16-byte aligned, contents ignored; not
@@ -467,7 +468,8 @@ ringx_status ringx_layer_norm(const void* x, int64_t row_stride, const float* we
 ringx_status ringx_layer_norm_bwd(const void* x, int64_t row_stride, const void* dy, const void* dres,
                                   const float* weight, const float* stats, void* dx, float* dweight,
                                   float* dbias, int64_t rows, int64_t C, ringx_dtype dtype,
-                                  void* workspace, size_t workspace_bytes, hipStream_t stream);
+                                  ringx_dtype dy_dtype, void* workspace, size_t workspace_bytes,
+                                  hipStream_t stream);
 
 /* Bytes of its workspace (0 if the arguments are invalid).  Host only. */
 size_t ringx_layer_norm_bwd_workspace_bytes(int64_t rows, int64_t C, ringx_dtype dtype);
@@ -504,7 +506,8 @@ size_t ringx_linear_workspace_bytes(int64_t x_stride, int64_t heads, int64_t tok
  * Backward of ringx_linear:  dz = dy act'(pre);  dx = dz w;  dw = dz^T x;  dbias = sum over rows of dz.
  * (The residual's gradient is dy.)
  *   dy [M, O] (dtype), contiguous; pre [M, O] as the forward left it, NULL iff act is RINGX_ACT_NONE.
- *   dx (dtype) or NULL: [M, K] contiguous, or the attention's layout where x has it (heads > 0).
+ *   dx or NULL: [M, K] contiguous, in dx_dtype (dtype, or fp32), or the attention's layout where x has it
+ *   (heads > 0; dtype alone, RINGX_E_UNSUPPORTED otherwise).
  *   dw [O, K] or NULL: in dw_dtype (fp32, or dtype); dbias [O] fp32 or NULL.
  *   accumulate_dw != 0: dw and dbias are added to (dw_dtype fp32 alone, RINGX_E_UNSUPPORTED otherwise).
  * dz is rounded to dtype for the products (the bias's gradient is that of the unrounded dz); products and
@@ -514,7 +517,8 @@ size_t ringx_linear_workspace_bytes(int64_t x_stride, int64_t heads, int64_t tok
 ringx_status ringx_linear_bwd(const void* x, int64_t x_stride, int64_t heads, int64_t tokens,
                               const void* w, const void* dy, const void* pre, void* dx, void* dw,
                               float* dbias, int64_t M, int64_t K, int64_t O, ringx_act act,
-                              ringx_dtype dtype, ringx_dtype dw_dtype, int accumulate_dw,
+                              ringx_dtype dtype, ringx_dtype dx_dtype, ringx_dtype dw_dtype,
+                              int accumulate_dw,
                               void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* Bytes of its workspace (0 if the arguments are invalid).  Host only. */

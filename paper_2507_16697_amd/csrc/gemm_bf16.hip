@@ -155,7 +155,7 @@ struct Out {
     }
     const int64_t row = i * o.J;
     if (o.f32) {
-      // products for the weights' gradient: no bias, activation or residual
+      // gradients: no bias, activation or residual
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const int64_t j = j0 + 16 * b + 4 * g;

@@ -78,6 +78,37 @@ struct Row {
   }
 };
 
+// The same columns of a row of G, fp32 beside a bf16 x.
+template <class T, class G, bool VEC, int E, int TPR>
+struct GradRow : Row<T, VEC, E, TPR> {};
+template <bool VEC, int E, int TPR>
+struct GradRow<__bf16, float, VEC, E, TPR> {
+  using R = Row<__bf16, VEC, E, TPR>;
+  float w[E];
+  __device__ __forceinline__ void load(const float* p, int t, int C) {
+#pragma unroll
+    for (int e = 0; e < E; e += VEC ? 4 : 1) {
+      const int c = R::col(e, t);
+      if constexpr (VEC) {
+        f32x4 x = {};
+        if (c < C) x = *reinterpret_cast<const f32x4*>(p + c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[e + j] = x[j];
+      } else {
+        w[e] = 0.f;
+        if (c < C) w[e] = p[c];
+      }
+    }
+  }
+  __device__ __forceinline__ float get(int e) const { return w[e]; }
+  __device__ __forceinline__ void arrived() {
+    if constexpr (!VEC) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) asm volatile("" : "+v"(w[e]));
+    }
+  }
+};
+
 // fp32 weights of the thread's columns, `otherwise` where there are none
 template <class T, bool VEC, int E, int TPR>
 __device__ __forceinline__ void load_vector(const float* p, float otherwise, int t, int C,
@@ -193,7 +224,7 @@ __global__ __launch_bounds__(kGroup<TPR>) void layer_norm_kernel(NormArgs a) {
   }
 }
 
-template <class T, bool VEC, int E, int TPR>
+template <class T, class G, bool VEC, int E, int TPR>
 __global__ __launch_bounds__(kGroup<TPR>, TPR <= 256 ? 2 : 1) void layer_norm_bwd_kernel(NormArgs a) {
   using R = Row<T, VEC, E, TPR>;
   constexpr int kWidth = E * TPR;
@@ -203,7 +234,8 @@ __global__ __launch_bounds__(kGroup<TPR>, TPR <= 256 ? 2 : 1) void layer_norm_bw
   const int C = a.C;
   const float inv = 1.f / (float)C;
   const int64_t step = (int64_t)gridDim.x * kRowsAtOnce<TPR>;
-  const T *const x = (const T*)a.x, *const dy = (const T*)a.dy, *const dres = (const T*)a.dres;
+  const T *const x = (const T*)a.x, *const dres = (const T*)a.dres;
+  const G* const dy = (const G*)a.dy;
   T* const dx = (T*)a.dx;
   float w[E], dw[E], db[E];
   load_vector<T, VEC, E, TPR>(a.weight, 1.f, t, C, w);
@@ -214,7 +246,8 @@ __global__ __launch_bounds__(kGroup<TPR>, TPR <= 256 ? 2 : 1) void layer_norm_bw
     const int64_t at = r0 + threadIdx.x / TPR;
     const bool live = at < a.rows;
     const int64_t row = live ? at : a.rows - 1;   // rows past the end repeat the last one
-    R rx, rg, rr;
+    R rx, rr;
+    GradRow<T, G, VEC, E, TPR> rg;
     rx.load(x + row * a.stride, t, C);
     rg.load(dy + row * C, t, C);
     if (dres) rr.load(dres + row * C, t, C);
@@ -277,8 +310,8 @@ __global__ __launch_bounds__(kGroup<TPR>, TPR <= 256 ? 2 : 1) void layer_norm_bw
   }
 }
 
-template <class T, bool VEC, int E, int TPR>
-hipError_t launch(const NormArgs& a, bool bwd) {
+template <class T, class G, bool VEC, int E, int TPR>
+hipError_t launch_as(const NormArgs& a, bool bwd) {
   const int64_t groups = (a.rows + kRowsAtOnce<TPR> - 1) / kRowsAtOnce<TPR>;
   const int64_t grid = std::min<int64_t>(groups, norm_workgroups(a.C, bwd));
   if (!bwd) {
@@ -286,7 +319,7 @@ hipError_t launch(const NormArgs& a, bool bwd) {
                        a.stream, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((layer_norm_bwd_kernel<T, VEC, E, TPR>), dim3((uint32_t)grid), dim3(kGroup<TPR>), 0,
+  hipLaunchKernelGGL((layer_norm_bwd_kernel<T, G, VEC, E, TPR>), dim3((uint32_t)grid), dim3(kGroup<TPR>), 0,
                      a.stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.part) return e;
@@ -294,6 +327,11 @@ hipError_t launch(const NormArgs& a, bool bwd) {
   s.part = a.part, s.parts = (int)grid, s.cols = 2 * a.C, s.split = a.C;
   s.out[0] = a.dweight, s.out[1] = a.dbias, s.stream = a.stream;
   return launch_column_sums(s);
+}
+
+template <class T, bool VEC, int E, int TPR>
+hipError_t launch(const NormArgs& a, bool bwd) {
+  return bwd && a.dy_f32 ? launch_as<T, float, VEC, E, TPR>(a, bwd) : launch_as<T, T, VEC, E, TPR>(a, bwd);
 }
 
 template <class T, bool VEC>

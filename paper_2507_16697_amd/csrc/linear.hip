@@ -415,7 +415,7 @@ hipError_t backward(const LinearArgs& a) {
     x.q_slow = true;
     x.I = a.s.M, x.J = a.s.K, x.R = dz.cols, x.splits = p.splits_dx, x.cut = p.cut_dx;
     x.part = (float*)at(a.workspace, p.part);
-    x.o.out = a.dx, x.o.J = a.s.K;
+    x.o.out = a.dx, x.o.J = a.s.K, x.o.f32 = a.dx_f32 && !a.s.heads;
     if (a.s.heads) x.o.heads = a.s.heads, x.o.tokens = a.s.tokens, x.o.d = a.s.K / a.s.heads;
   }
   if (a.dw) {

@@ -1225,11 +1225,13 @@ size_t ringx_layer_norm_bwd_workspace_bytes(int64_t rows, int64_t C, ringx_dtype
 ringx_status ringx_layer_norm_bwd(const void* x, int64_t row_stride, const void* dy, const void* dres,
                                   const float* weight, const float* stats, void* dx, float* dweight,
                                   float* dbias, int64_t rows, int64_t C, ringx_dtype dtype,
-                                  void* workspace, size_t workspace_bytes, hipStream_t stream) {
+                                  ringx_dtype dy_dtype, void* workspace, size_t workspace_bytes,
+                                  hipStream_t stream) {
   if (!x || !dy || !stats || !dx) return RINGX_E_NULLPTR;
   int64_t bytes = 0;
   const ringx_status st = check_norm(rows, C, row_stride, 0.f, dtype, &bytes);
   if (st != RINGX_OK) return st;
+  if (dy_dtype != dtype && dy_dtype != RINGX_FP32) return RINGX_E_UNSUPPORTED;
   const bool sums = dweight || dbias;
   const size_t need = sums ? ringx_layer_norm_bwd_workspace_bytes(rows, C, dtype) : 0;
   if (sums && (!workspace || workspace_bytes < need)) return RINGX_E_WORKSPACE;
@@ -1237,11 +1239,11 @@ ringx_status ringx_layer_norm_bwd(const void* x, int64_t row_stride, const void*
   if (!all_aligned({x, dy, dres, weight, stats, dx, dweight, dbias, workspace})) return RINGX_E_ALIGN;
   const int64_t n = rows * C * esize(dtype);
   if (!apart({{dx, n}, {dweight, 4 * C}, {dbias, 4 * C}, {workspace, (int64_t)need}},
-             {{x, bytes}, {dy, n}, {dres, n}, {weight, 4 * C}, {stats, 8 * rows}}))
+             {{x, bytes}, {dy, rows * C * esize(dy_dtype)}, {dres, n}, {weight, 4 * C}, {stats, 8 * rows}}))
     return RINGX_E_ALIAS;
   ringx::NormArgs a = norm_args(x, row_stride, rows, C, weight, dtype, stream);
   a.dy = dy, a.dres = dres, a.stats_in = stats, a.dx = dx, a.dweight = dweight, a.dbias = dbias;
-  a.part = static_cast<float*>(workspace);
+  a.part = static_cast<float*>(workspace), a.dy_f32 = dy_dtype == RINGX_FP32;
   return hip_status(ringx::launch_layer_norm(a, true));
 }
 
@@ -1324,8 +1326,9 @@ size_t ringx_linear_bwd_workspace_bytes(int64_t x_stride, int64_t heads, int64_t
 ringx_status ringx_linear_bwd(const void* x, int64_t x_stride, int64_t heads, int64_t tokens,
                               const void* w, const void* dy, const void* pre, void* dx, void* dw,
                               float* dbias, int64_t M, int64_t K, int64_t O, ringx_act act,
-                              ringx_dtype dtype, ringx_dtype dw_dtype, int accumulate_dw,
-                              void* workspace, size_t workspace_bytes, hipStream_t stream) {
+                              ringx_dtype dtype, ringx_dtype dx_dtype, ringx_dtype dw_dtype,
+                              int accumulate_dw, void* workspace, size_t workspace_bytes,
+                              hipStream_t stream) {
   if (!x || !w || !dy || !(dx || dw || dbias)) return RINGX_E_NULLPTR;
   ringx::LinearArgs a;
   int64_t bytes = 0;
@@ -1333,16 +1336,18 @@ ringx_status ringx_linear_bwd(const void* x, int64_t x_stride, int64_t heads, in
   if (st != RINGX_OK) return st;
   if (!pre != (act == RINGX_ACT_NONE)) return RINGX_E_NULLPTR;
   if (dw_dtype != RINGX_FP32 && dw_dtype != dtype) return RINGX_E_UNSUPPORTED;
+  if (dx_dtype != dtype && (dx_dtype != RINGX_FP32 || heads > 0)) return RINGX_E_UNSUPPORTED;
   if (accumulate_dw && dw && dw_dtype != RINGX_FP32) return RINGX_E_UNSUPPORTED;
   const int64_t need = ringx::linear_bwd_plan(a.s, act).bytes;
   if (!workspace || workspace_bytes < static_cast<size_t>(need)) return RINGX_E_WORKSPACE;
   if (!all_aligned({x, w, dy, pre, dx, dw, dbias, workspace})) return RINGX_E_ALIGN;
   const int64_t es = esize(dtype), out = M * O * es;
-  if (!apart({{dx, M * K * es}, {dw, O * K * esize(dw_dtype)}, {dbias, 4 * O}, {workspace, need}},
+  if (!apart({{dx, M * K * esize(dx_dtype)}, {dw, O * K * esize(dw_dtype)}, {dbias, 4 * O}, {workspace, need}},
              {{x, bytes}, {w, O * K * es}, {dy, out}, {pre, out}}))
     return RINGX_E_ALIAS;
   a.xp = x, a.wp = w, a.dy = dy, a.pre = const_cast<void*>(pre), a.dx = dx, a.dw = dw, a.dbias = dbias;
-  a.act = act, a.dw_f32 = dw_dtype == RINGX_FP32, a.accumulate = accumulate_dw != 0;
+  a.act = act, a.dx_f32 = dx_dtype == RINGX_FP32, a.dw_f32 = dw_dtype == RINGX_FP32;
+  a.accumulate = accumulate_dw != 0;
   a.workspace = workspace, a.stream = stream;
   return hip_status(ringx::launch_linear_bwd(a));
 }

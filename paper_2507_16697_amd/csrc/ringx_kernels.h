@@ -447,6 +447,7 @@ struct NormArgs {
   int C = 0;
   float eps = 0.f;
   bool bf16 = false, vec = true;               // vec: rows in 16-byte pieces
+  bool dy_f32 = false;                         // dy in fp32 whatever x is
   hipStream_t stream = nullptr;
 };
 constexpr int64_t kNormMaxC = 16384;
@@ -626,7 +627,7 @@ struct LinearArgs {
   void *dx = nullptr, *dw = nullptr;
   float* dbias = nullptr;
   int act = 0;
-  bool dw_f32 = true, accumulate = false;
+  bool dx_f32 = false, dw_f32 = true, accumulate = false;
   void* workspace = nullptr;
   hipStream_t stream = nullptr;
   GemmIn x() const {

@@ -143,13 +143,13 @@ def lib() -> ctypes.CDLL:
         L.ringx_qkv_norm_rope_bwd_workspace_bytes.restype = ctypes.c_size_t
         Z = ctypes.c_size_t
         L.ringx_layer_norm.argtypes = [_P, _I, _P, _P, _P, _P, _I, _I, F, C, _P]
-        L.ringx_layer_norm_bwd.argtypes = [_P, _I] + [_P] * 7 + [_I, _I, C, _P, Z, _P]
+        L.ringx_layer_norm_bwd.argtypes = [_P, _I] + [_P] * 7 + [_I, _I, C, C, _P, Z, _P]
         L.ringx_layer_norm_bwd_workspace_bytes.argtypes = [_I, _I, C]
         L.ringx_layer_norm_bwd_workspace_bytes.restype = Z
         L.ringx_linear.argtypes = [_P, _I, _I, _I] + [_P] * 5 + [_I, _I, _I, C, C, _P, Z, _P]
         L.ringx_linear_workspace_bytes.argtypes = [_I] * 6 + [C]
         L.ringx_linear_workspace_bytes.restype = Z
-        L.ringx_linear_bwd.argtypes = ([_P, _I, _I, _I] + [_P] * 6 + [_I, _I, _I, C, C, C, C, _P, Z, _P])
+        L.ringx_linear_bwd.argtypes = ([_P, _I, _I, _I] + [_P] * 6 + [_I, _I, _I, C, C, C, C, C, _P, Z, _P])
         L.ringx_linear_bwd_workspace_bytes.argtypes = [_I] * 6 + [C, C]
         L.ringx_linear_bwd_workspace_bytes.restype = Z
         L.ringx_chunk_bounds.argtypes = [_I, _I, _I, ctypes.POINTER(_I), ctypes.POINTER(_I)]
@@ -1006,14 +1006,20 @@ def ringx_layer_norm_bwd_workspace_bytes(rows, C, dtype) -> int:
 
 def ringx_layer_norm_bwd(x, dy, stats, weight=None, bias=None, dres=None, dx=None, dweight=None,
                          dbias=None, workspace=None, stream=None):
-    """Backward of ringx_layer_norm from dy [..., C] and the forward's stats; dres: the gradient that reaches x
-    by its residual, added to dx.  Returns (dx [..., C] in x's dtype, dweight, dbias fp32 [C], None where
+    """Backward of ringx_layer_norm from dy [..., C] (in x's dtype or fp32) and the forward's stats; dres: the
+    gradient that reaches x by its residual, added to dx.  Returns (dx [..., C] in x's dtype, dweight, dbias fp32 [C], None where
     there is no weight or bias)."""
     torch = _T or _torch()
     rows, step = _rows_of("x", x)
     C = x.shape[-1]
     code = _dtype_code(x)
-    _same("dy", dy, x.shape, x)
+    if dy.dtype is torch.float32 and code != RINGX_FP32:
+        _dev(dy)
+        _expect("dy", dy, x.shape, torch.float32, x.device)
+        dy_code = RINGX_FP32
+    else:
+        _same("dy", dy, x.shape, x)
+        dy_code = code
     pr = _same("dres", dres, x.shape, x)
     _dev(stats)
     _expect("stats", stats, (2, rows), torch.float32, x.device)
@@ -1031,7 +1037,7 @@ def ringx_layer_norm_bwd(x, dy, stats, weight=None, bias=None, dres=None, dx=Non
     else:
         workspace = None
     _launch("ringx_layer_norm_bwd", x, stream, x.data_ptr(), step, dy.data_ptr(), pr, pw, stats.data_ptr(),
-            dx.data_ptr(), _ptr(dweight), _ptr(dbias), rows, C, code, _ptr(workspace),
+            dx.data_ptr(), _ptr(dweight), _ptr(dbias), rows, C, code, dy_code, _ptr(workspace),
             0 if workspace is None else _nbytes(workspace))
     return dx, dweight, dbias
 
@@ -1097,10 +1103,10 @@ def ringx_linear(x, w, bias=None, act="none", residual=None, need_pre: bool = Fa
 
 
 def ringx_linear_bwd(x, w, dy, pre=None, act="none", bias=None, need_dx: bool = True,
-                     need_dw: bool = True, dx=None, dw=None, dbias=None, dw_dtype=None,
+                     need_dw: bool = True, dx=None, dw=None, dbias=None, dx_dtype=None, dw_dtype=None,
                      accumulate_dw=False, workspace=None, stream=None):
     """Backward of ringx_linear from dy [..., O] and, with an activation, the forward's pre.  Returns (dx like x
-    and contiguous, dw [O, K] in dw_dtype (fp32 by default, or x's dtype), dbias fp32 [O], None where there is
+    and contiguous, in x's dtype or dx_dtype=torch.float32, dw [O, K] in dw_dtype (fp32 by default, or x's dtype), dbias fp32 [O], None where there is
     no bias); dx or dw is None where it is not needed.  accumulate_dw: dw and dbias (fp32) are added to."""
     torch = _T or _torch()
     step, heads, tokens, M, K, O, lead = _linear_args(x, w)
@@ -1116,8 +1122,16 @@ def ringx_linear_bwd(x, w, dy, pre=None, act="none", bias=None, need_dx: bool = 
     dw_dtype = torch.float32 if dw_dtype is None else dw_dtype
     if dw_dtype is not torch.float32 and dw_dtype is not x.dtype:
         raise TypeError(f"dw_dtype: {dw_dtype}, expected float32 or {x.dtype}")
+    if dx is not None and dx_dtype is None:
+        dx_dtype = dx.dtype
+    dx_code = code
+    if dx_dtype is not None and dx_dtype is not x.dtype:
+        if dx_dtype is not torch.float32:
+            raise TypeError(f"dx_dtype: {dx_dtype}, expected float32 or {x.dtype}")
+        dx_code = RINGX_FP32
     if need_dx or dx is not None:
-        dx = _out_as("dx", dx, x, stream)
+        dx = (_out_as("dx", dx, x, stream) if dx_code == code else
+              _out("dx", dx, x.shape, torch.float32, x, stream))
     if need_dw or dw is not None:
         if dw_dtype is torch.float32:
             dw = _grad_out("dw", dw, (O, K), x, accumulate_dw, stream)
@@ -1129,7 +1143,7 @@ def ringx_linear_bwd(x, w, dy, pre=None, act="none", bias=None, need_dx: bool = 
     workspace = _workspace(workspace, ringx_linear_bwd_workspace_bytes(step, heads, tokens, M, K, O, a, code),
                            x, stream)
     _launch("ringx_linear_bwd", x, stream, x.data_ptr(), step, heads, tokens, w.data_ptr(), dy.data_ptr(), pp,
-            _ptr(dx), _ptr(dw), _ptr(dbias), M, K, O, a, code,
+            _ptr(dx), _ptr(dw), _ptr(dbias), M, K, O, a, code, dx_code,
             RINGX_FP32 if dw_dtype is torch.float32 else RINGX_BF16, 1 if accumulate_dw else 0,
             workspace.data_ptr(), _nbytes(workspace))
     return dx, dw, dbias

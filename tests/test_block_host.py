@@ -71,8 +71,9 @@ def norm(x=P[0], stride=512, w=P[1], b=P[2], y=P[3], stats=P[4], rows=100, C=512
 
 
 def norm_bwd(x=P[0], stride=512, dy=P[1], dres=P[2], w=P[3], stats=P[4], dx=P[5], dw=P[6], db=P[7], rows=100,
-             C=512, dt=BF16, ws=P[8], wsb=GB):
-    return ringx.lib().ringx_layer_norm_bwd(x, stride, dy, dres, w, stats, dx, dw, db, rows, C, dt, ws, wsb, None)
+             C=512, dt=BF16, dyt=None, ws=P[8], wsb=GB):
+    return ringx.lib().ringx_layer_norm_bwd(x, stride, dy, dres, w, stats, dx, dw, db, rows, C, dt,
+                                            dt if dyt is None else dyt, ws, wsb, None)
 
 
 @needs_lib
@@ -100,6 +101,9 @@ def test_norm_refusals_of_each_way():
     need = ringx.ringx_layer_norm_bwd_workspace_bytes(100, 512, BF16)
     assert need > 0 and norm_bwd(ws=0) == WORKSPACE and norm_bwd(wsb=need - 1) == WORKSPACE
     assert norm_bwd(dx=P[1]) == ALIAS and norm_bwd(dx=P[2]) == ALIAS and norm_bwd(dw=P[7]) == ALIAS
+    assert norm_bwd(dyt=5) == UNSUP and norm_bwd(dt=FP32, dyt=BF16) == UNSUP
+    # an fp32 gradient is twice as long
+    assert norm_bwd(dx=P[1] + 102400, dyt=FP32) == ALIAS
     assert norm_bwd(ws=P[5]) == ALIAS and norm_bwd(db=P[4]) == ALIAS and norm_bwd(ws=P[8] + 8) == ALIGN
     ask = ringx.ringx_layer_norm_bwd_workspace_bytes
     assert ask(0, 8, BF16) == 0 and ask(8, 16385, BF16) == 0 and ask(8, 8, 5) == 0
@@ -112,9 +116,9 @@ def lin(x=P[0], stride=512, heads=0, tokens=0, w=P[1], b=P[2], res=P[3], y=P[4],
 
 
 def lin_bwd(x=P[0], stride=512, heads=0, tokens=0, w=P[1], dy=P[2], pre=P[3], dx=P[4], dw=P[5], db=P[6], M=300,
-            K=512, O=256, act=1, dt=BF16, dwt=FP32, acc=0, ws=P[7], wsb=GB):
-    return ringx.lib().ringx_linear_bwd(x, stride, heads, tokens, w, dy, pre, dx, dw, db, M, K, O, act, dt, dwt,
-                                        acc, ws, wsb, None)
+            K=512, O=256, act=1, dt=BF16, dxt=None, dwt=FP32, acc=0, ws=P[7], wsb=GB):
+    return ringx.lib().ringx_linear_bwd(x, stride, heads, tokens, w, dy, pre, dx, dw, db, M, K, O, act, dt,
+                                        dt if dxt is None else dxt, dwt, acc, ws, wsb, None)
 
 
 @needs_lib
@@ -129,7 +133,7 @@ def test_linear_refusals(fn):
     assert fn(stride=1 << 38) == SHAPE and fn(M=(1 << 31) - 1024, K=8192, stride=8192) == SHAPE
     assert fn(x=P[0] + 8) == ALIGN and fn(w=P[1] + 2) == ALIGN
     # more tiles than a launch takes, each product's
-    assert fn(M=(1 << 31) - 1024, K=8, stride=8, O=128) == SHAPE
+    assert fn(M=(1 << 31) - 1024, K=8, stride=8, O=136) == SHAPE
     assert fn(M=128, K=1 << 20, stride=1 << 20, O=1 << 20) == SHAPE
 
 
@@ -145,6 +149,8 @@ def test_linear_refusals_of_each_way():
     # what the activation's derivative needs, and nothing where there is none
     assert lin_bwd(pre=0) == NULLPTR and lin_bwd(act=0) == NULLPTR
     assert lin_bwd(dwt=5) == UNSUP and lin_bwd(dt=FP32, dwt=BF16) == UNSUP and lin_bwd(dwt=BF16, acc=1) == UNSUP
+    assert lin_bwd(dxt=5) == UNSUP and lin_bwd(dt=FP32, dxt=BF16) == UNSUP
+    assert lin_bwd(dxt=FP32, heads=2, tokens=100) == UNSUP
     need = ringx.ringx_linear_bwd_workspace_bytes(512, 0, 0, 300, 512, 256, 1, BF16)
     assert need > 0 and lin_bwd(ws=0) == WORKSPACE and lin_bwd(wsb=need - 1) == WORKSPACE
     assert lin_bwd(dx=P[2]) == ALIAS and lin_bwd(dw=P[4]) == ALIAS and lin_bwd(db=P[3]) == ALIAS

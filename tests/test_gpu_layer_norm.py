@@ -110,6 +110,21 @@ def test_without_some(store, weight, bias, res):
     check_backward(x, dy, stats, w, dres, store, dx, dw, db)
 
 
+@pytest.mark.parametrize("shape,pad", [((1, 8), 0), ((33, 65), 0), ((65, 136), 0), ((41, 375), 3), ((2, 19, 520), 0),
+                                       ((18, 1032), 8), ((9, 2056), 0), ((6, 4099), 0), ((4, 8200), 0),
+                                       ((3, 16383), 0)])
+def test_gradient_in_32_bits(shape, pad):
+    x, w, b, dy, dres = make(sum(shape) + 1, shape, "bf16", pad)
+    dy = torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    _, stats = ringx.ringx_layer_norm(x, w, b)
+    dx, dw, db = ringx.ringx_layer_norm_bwd(x, dy, stats, w, b, dres=dres)
+    assert dx.dtype is torch.bfloat16
+    check_backward(x, dy, stats, w, dres, "bf16", dx, dw, db)
+    same = ringx.ringx_layer_norm_bwd(x, dy.bfloat16(), stats, w, b, dres=dres)
+    wide = ringx.ringx_layer_norm_bwd(x, dy.bfloat16().float(), stats, w, b, dres=dres)
+    assert all(torch.equal(p, q) for p, q in zip(same, wide))
+
+
 @pytest.mark.parametrize("store,rows,C", [("bf16", 5003, 192), ("fp32", 4501, 384), ("bf16", 3001, 2048),
                                           ("fp32", 1201, 4096), ("bf16", 20011, 40)])
 def test_many_rows(store, rows, C):
@@ -220,7 +235,8 @@ def test_refusals():
                 lambda: ln(x, w.cpu()), lambda: ln(x.half()), lambda: ln(x.cpu()),
                 lambda: ln(x.view(2, 4, 64).transpose(0, 1)), lambda: ln(x, y=x.float()),
                 lambda: ln(x, stats=torch.empty(2, 7, device="cuda")),
-                lambda: bwd(x, dy[:4], stats, w), lambda: bwd(x, dy.float(), stats, w),
+                lambda: bwd(x, dy[:4], stats, w), lambda: bwd(x, dy.double(), stats, w),
+                lambda: bwd(x, dy[:4].float(), stats, w), lambda: bwd(x.float(), dy, stats, w),
                 lambda: bwd(x, dy, stats[:, :4], w), lambda: bwd(x, dy, stats, w, dres=dres.float()),
                 lambda: bwd(x, dy, stats, None, b, dweight=torch.empty(64, device="cuda")),
                 lambda: ln(x, eps=-1.0), lambda: ln(x, eps=float("nan")), lambda: ln(x, y=x),

@@ -188,6 +188,11 @@ def test_gradients_in_parts_and_types(M, K, O):
     assert none is None and no_bias is None and torch.equal(dx, whole[0])
     none, dw, db = ringx.ringx_linear_bwd(x, w, dy, bias=b, need_dx=False, dw_dtype=torch.bfloat16)
     assert none is None and torch.equal(dw, whole[1].to(torch.bfloat16)) and torch.equal(db, whole[2])
+    wide, _, _ = ringx.ringx_linear_bwd(x, w, dy, need_dw=False, dx_dtype=torch.float32)
+    assert wide.dtype is torch.float32 and torch.equal(wide.to(torch.bfloat16), whole[0])
+    check_backward(x, w, dy, None, "none", "fp32", wide, None, None)
+    both = ringx.ringx_linear_bwd(x, w, dy, bias=b, dx=torch.empty_like(wide))
+    assert torch.equal(both[0], wide) and torch.equal(both[1], whole[1])
     none, none2, db = ringx.ringx_linear_bwd(x, w, dy, bias=b, need_dx=False, need_dw=False)
     assert none is None and none2 is None and torch.equal(db, whole[2])
     # added to
@@ -319,7 +324,8 @@ def test_refusals():
                 lambda: lin(x, w, y=res, residual=res), lambda: lin(x, w, y=x), lambda: lin(x4.transpose(1, 2), w),
                 lambda: lin(x4[..., :16], w), lambda: bwd(x, w, dy[:4]), lambda: bwd(x, w, dy.float()),
                 lambda: bwd(x, w, dy, act="gelu"), lambda: bwd(x, w, dy, pre=dy), lambda: bwd(x, w, dy, dx=x),
-                lambda: bwd(x, w, dy, dw_dtype=torch.float16), lambda: bwd(x, w, dy, dw=w),
+                lambda: bwd(x, w, dy, dx_dtype=torch.float16),
+                lambda: bwd(x4, w, dy.view(2, 4, 48)), lambda: bwd(x, w, dy, dw_dtype=torch.float16), lambda: bwd(x, w, dy, dw=w),
                 lambda: bwd(x, w, dy, need_dx=False, need_dw=False),
                 lambda: bwd(x, w, dy, dw_dtype=torch.bfloat16, accumulate_dw=True),
                 lambda: bwd(x, w, dy, dbias=torch.zeros(48, device="cuda")),
