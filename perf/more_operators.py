@@ -348,7 +348,7 @@ def _run_own(c, s):
     y, _ = ringx.ringx_linear(h, s["w2"], s["b2"], residual=s["x"])
     dh, dw2, db2 = ringx.ringx_linear_bwd(h, s["w2"], s["dy"], bias=s["b2"], dw_dtype=dtype)
     da, dw1, db1 = ringx.ringx_linear_bwd(a, s["w1"], dh, pre=z, act=c["act"], bias=s["b1"],
-                                          dw_dtype=dtype)
+                                          dx_dtype=torch.float32, dw_dtype=dtype)
     dx, dw, db = ringx.ringx_layer_norm_bwd(s["x"], da, stats, s["w"], s["b"], dres=s["dy"])
     return _mlp_out(dtype, y, dx, dw, db, dw1, db1, dw2, db2)
 
