@@ -433,7 +433,7 @@ hipError_t launch_pair(GemmPair p) {
   p.rest_dx = rest_of(p.dx), p.rest_dw = rest_of(p.dw);
   p.wgs_dx = p.dx.cut.whole + p.rest_dx * p.dx.cut.parts;
   p.wgs_dw = p.dw.cut.whole + p.rest_dw * p.dw.cut.parts;
-  const uint32_t sums = p.sums.part ? (uint32_t)((p.sums.cols + 63) / 64) : 0;
+  const uint32_t sums = p.sums.parts ? (uint32_t)((p.sums.cols + 63) / 64) : 0;
   hipLaunchKernelGGL((gemm_pair_kernel<C>), dim3(p.wgs_dx + p.wgs_dw + sums),
                      dim3(C::kThreads * C::kGroups), 0, p.dx.stream, p);
   const hipError_t e = hipGetLastError();

@@ -338,7 +338,7 @@ hipError_t launch_gemm_f32(const GemmArgs& a) {
 
 hipError_t launch_gemm_pair_f32(GemmPair p) {
   p.wgs_dx = workgroups(p.dx, kSide), p.wgs_dw = workgroups(p.dw, kSide);
-  const uint32_t sums = p.sums.part ? (uint32_t)((p.sums.cols + 63) / 64) : 0;
+  const uint32_t sums = p.sums.parts ? (uint32_t)((p.sums.cols + 63) / 64) : 0;
   hipLaunchKernelGGL(gemm_f32_pair_kernel, dim3(p.wgs_dx + p.wgs_dw + sums), dim3(256), 0, p.dx.stream, p);
   return hipGetLastError();
 }

@@ -277,12 +277,19 @@ __global__ __launch_bounds__(kGroup<TPR>, TPR <= 256 ? 2 : 1) void layer_norm_bw
     if (live) R::store(dx + row * C, t, C, g);
   }
   if (!a.part) return;
+  // the workgroup's parts; a launch of one has the sums
+  const bool alone = gridDim.x == 1;
   float* const part = a.part + (int64_t)blockIdx.x * 2 * C;
+  float* const pw = alone ? a.dweight : part;
+  float* const pb = alone ? a.dbias : part + C;
   if constexpr (TPR > 64) {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int c = R::col(e, t);
-      if (c < C) part[c] = dw[e], part[C + c] = db[e];
+      if (c < C) {
+        if (pw) pw[c] = dw[e];
+        if (pb) pb[c] = db[e];
+      }
     }
   } else {
     // over the rows of a wave, then wave after wave
@@ -305,7 +312,10 @@ __global__ __launch_bounds__(kGroup<TPR>, TPR <= 256 ? 2 : 1) void layer_norm_bw
     }
     for (int j = threadIdx.x; j < kWidth; j += kGroup<TPR>) {
       const int c = R::col(j / TPR, j % TPR);
-      if (c < C) part[c] = lds[j], part[C + c] = lds[kWidth + j];
+      if (c < C) {
+        if (pw) pw[c] = lds[j];
+        if (pb) pb[c] = lds[kWidth + j];
+      }
     }
   }
 }
@@ -313,7 +323,9 @@ __global__ __launch_bounds__(kGroup<TPR>, TPR <= 256 ? 2 : 1) void layer_norm_bw
 template <class T, class G, bool VEC, int E, int TPR>
 hipError_t launch_as(const NormArgs& a, bool bwd) {
   const int64_t groups = (a.rows + kRowsAtOnce<TPR> - 1) / kRowsAtOnce<TPR>;
-  const int64_t grid = std::min<int64_t>(groups, norm_workgroups(a.C, bwd));
+  int64_t grid = std::min<int64_t>(groups, norm_workgroups(a.C, bwd));
+  // Few rows: one workgroup, four rounds at most (5 us), and no second launch (4 us, and as much of the host).
+  if (bwd && a.part && groups <= 4) grid = 1;
   if (!bwd) {
     hipLaunchKernelGGL((layer_norm_kernel<T, VEC, E, TPR>), dim3((uint32_t)grid), dim3(kGroup<TPR>), 0,
                        a.stream, a);
@@ -322,7 +334,7 @@ hipError_t launch_as(const NormArgs& a, bool bwd) {
   hipLaunchKernelGGL((layer_norm_bwd_kernel<T, G, VEC, E, TPR>), dim3((uint32_t)grid), dim3(kGroup<TPR>), 0,
                      a.stream, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.part) return e;
+  if (e != hipSuccess || !a.part || grid == 1) return e;
   ColumnSums s;
   s.part = a.part, s.parts = (int)grid, s.cols = 2 * a.C, s.split = a.C;
   s.out[0] = a.dweight, s.out[1] = a.dbias, s.stream = a.stream;

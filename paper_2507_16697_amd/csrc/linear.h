@@ -193,8 +193,18 @@ __device__ __forceinline__ void sum_columns(const ColumnSums& a, uint32_t id, fl
   const int64_t col = (int64_t)id * 64 + lane;
   float t = 0.f;
   if (col < a.cols) {
+    if (a.rows) {
+      // the gradient's own rows
+      const auto add = [&](const auto* p) {
 #pragma unroll 8
-    for (int i = wave; i < a.parts; i += WAVES) t += a.part[i * a.cols + col];
+        for (int i = wave; i < a.parts; i += WAVES) t += (float)p[i * a.cols + col];
+      };
+      if (a.rows_bf16) add((const __bf16*)a.rows);
+      else add((const float*)a.rows);
+    } else {
+#pragma unroll 8
+      for (int i = wave; i < a.parts; i += WAVES) t += a.part[i * a.cols + col];
+    }
   }
   lds[wave][lane] = t;
   __syncthreads();

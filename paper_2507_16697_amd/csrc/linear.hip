@@ -389,7 +389,9 @@ hipError_t backward(const LinearArgs& a) {
   GemmIn dz;
   dz.p = a.dy, dz.rows = a.s.M, dz.cols = dz.ld = a.s.O;
   const bool own = p.dz >= 0 && (a.dx || a.dw);
-  if (own || a.dbias) {
+  const bool both = p.pair && a.dx && a.dw;
+  const bool rows = a.dbias && both && !own && !a.act && a.s.M <= kRowsSummed;   // summed beside the products
+  if (own || (a.dbias && !rows)) {
     GradPass g{};
     g.dy = a.dy, g.pre = a.act ? a.pre : nullptr, g.M = a.s.M, g.O = a.s.O, g.act = a.act;
     g.dz = own ? at(a.workspace, p.dz) : nullptr, g.ld = p.ldz;
@@ -401,9 +403,9 @@ hipError_t backward(const LinearArgs& a) {
   ColumnSums c;
   if (a.dbias) {
     c.part = (float*)at(a.workspace, p.sums), c.parts = (int)grad_grid(a.s.M, a.s.O, p.pair).y;
+    if (rows) c.rows = a.dy, c.rows_bf16 = a.s.bf16, c.parts = (int)a.s.M;
     c.cols = c.split = a.s.O, c.out[0] = a.dbias, c.accumulate = a.accumulate, c.stream = a.stream;
-    const bool later = p.pair && a.dx && a.dw;   // with the products
-    if (!later) e = launch_column_sums(c);
+    if (!both) e = launch_column_sums(c);
     if (e != hipSuccess) return e;
   }
   GemmArgs x, w;
@@ -424,10 +426,10 @@ hipError_t backward(const LinearArgs& a) {
     w.part = (float*)at(a.workspace, p.part_dw);
     w.o.out = a.dw, w.o.J = a.s.K, w.o.f32 = a.dw_f32, w.o.accumulate = a.accumulate;
   }
-  if (p.pair && a.dx && a.dw) {
-    GemmPair both;
-    both.dx = x, both.dw = w, both.sums = c;
-    return std::is_same_v<T, __bf16> ? launch_gemm_pair_bf16(both) : launch_gemm_pair_f32(both);
+  if (both) {
+    GemmPair pair;
+    pair.dx = x, pair.dw = w, pair.sums = c;
+    return std::is_same_v<T, __bf16> ? launch_gemm_pair_bf16(pair) : launch_gemm_pair_f32(pair);
   }
   if (a.dx) e = launch_product<T>(x);
   if (a.dw && e == hipSuccess) e = launch_product<T>(w);

@@ -458,6 +458,8 @@ inline int64_t norm_workgroups(int64_t C, bool bwd) { return bwd ? 512 : 2048; }
 // out[1] (either may be null), which they overwrite or are added to.
 struct ColumnSums {
   const float* part = nullptr;
+  const void* rows = nullptr;      // in its place (GemmPair alone): a few rows [parts, cols] in fp32 or bf16
+  bool rows_bf16 = false;
   int parts = 0;
   int64_t cols = 0, split = 0;
   float* out[2] = {nullptr, nullptr};
@@ -505,7 +507,7 @@ struct GemmArgs {
   float* part = nullptr;
   hipStream_t stream = nullptr;
 };
-// Both products of a backward in one launch, with the sums of the bias's gradient (sums.part null: none).
+// Both products of a backward in one launch, with the sums of the bias's gradient (sums.parts 0: none).
 struct GemmPair {
   GemmArgs dx, dw;
   ColumnSums sums;
@@ -610,6 +612,9 @@ inline GradGrid grad_grid(int64_t M, int64_t O, bool few) {   // few: at most 16
   g.y = (M + g.rows - 1) / g.rows;
   return g;
 }
+
+// Rows of a gradient that the launch of both products sums itself, without a pass before it.
+constexpr int64_t kRowsSummed = 256;
 
 struct LinearShape {
   int64_t M = 0, K = 0, O = 0;

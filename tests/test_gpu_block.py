@@ -34,7 +34,7 @@ def step(x, w, rng, H, Hkv, rot, freqs, pos, p, scale, dy, dtype):
     g = {}
     g["h"], g["w2"], g["b2"] = ringx.ringx_linear_bwd(t["h"], w["w2"], dy, bias=w["b2"])
     g["m"], g["w1"], g["b1"] = ringx.ringx_linear_bwd(t["m"], w["w1"], g["h"], pre=t["z"], act="gelu", bias=w["b1"],
-                                                      dw_dtype=dtype)
+                                                      dx_dtype=torch.float32, dw_dtype=dtype)
     g["x1"], g["n2"], g["c2"] = ringx.ringx_layer_norm_bwd(t["x1"], g["m"], t["sm"], w["n2"], w["c2"], dres=dy)
     g["o"], g["wo"], g["bo"] = ringx.ringx_linear_bwd(t["o"], w["wo"], g["x1"], bias=w["bo"])
     g["q"], g["k"], g["v"] = ringx.ringx_attn_bwd_drop(t["q"], t["k"], t["v"], t["o"], g["o"], t["lse"], p, rng,

@@ -69,7 +69,8 @@ def check_backward(x, w, dy, pre, act, store, dx, dw, db, dw_unit=0.0, had=(0.0,
     if dx is not None:
         b = (cut + S * (G.shape[1] + 8) * dz) @ np.abs(W) if act != "none" else \
             S * (G.shape[1] + 8) * (dz @ np.abs(W))
-        check(dx, rx, ob.unrows(b, f64(x)) + unit(store) * np.abs(rx))
+        u = 0.0 if dx.dtype is torch.float32 else unit(store)
+        check(dx, rx, ob.unrows(b, f64(x)) + (u + E) * np.abs(rx))
     if dw is not None:
         b = S * (G.shape[0] + 8) * (dz.T @ np.abs(X))
         if act != "none":
