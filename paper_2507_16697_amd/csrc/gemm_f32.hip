@@ -6,9 +6,9 @@
 // and, of 8 r, the four from 4 (l / 32) on; product e takes the e-th of them, so that an operand stored with r
 // along its rows is one 16-byte read, one stored the other way four reads of 128 bytes of a row.
 //
-// Large products: tiles of 128 x 128 through LDS (gemm_feed.h), a wave 64 x 64 of them.  Others: tiles of 32 x 32,
-// whose r the four waves of a workgroup split, from the caches without LDS; these take operands of any stride and
-// alignment.
+// Tiles of 128 x 128 or 64 x 64 through LDS (gemm_feed.h), a quarter to a wave.  Where those are few: blocks of
+// 32 x 32, whose r the four waves of a workgroup split, from the caches without LDS; these take operands of any
+// stride and alignment.
 
 #include "gemm_feed.h"
 #include "linear.h"
@@ -157,27 +157,12 @@ __device__ __forceinline__ void small_product(const GemmArgs& a, uint32_t id, ui
 }
 constexpr int kSmallLds = kWaves * 64 * 17;
 
-template <bool PS, bool QS>
-__global__ __launch_bounds__(256, 4) void gemm_f32_small_kernel(GemmArgs a) {
-  __shared__ float lds[kSmallLds];
-  small_product<PS, QS>(a, blockIdx.x, gridDim.x, lds);
-}
-
-// Both products of a backward that do not fill the chip one by one, and the sums of the bias's gradient from
-// its parts, in one launch.
-__global__ __launch_bounds__(256, 4) void gemm_f32_pair_kernel(GemmPair p) {
-  __shared__ float lds[kSmallLds];
-  const uint32_t id = blockIdx.x;
-  if (id < p.wgs_dx) small_product<false, true>(p.dx, id, p.wgs_dx, lds);
-  else if (id < p.wgs_dx + p.wgs_dw) small_product<true, true>(p.dw, id - p.wgs_dx, p.wgs_dw, lds);
-  else sum_columns<kWaves>(p.sums, id - p.wgs_dx - p.wgs_dw, reinterpret_cast<float(*)[64]>(lds));
-}
-
 // Fragments of a tile in LDS: 32 of the width x 8 of r.
-template <bool SLOW>
+template <bool SLOW, int W>
 struct Frags {
-  using F = Feed<float, SLOW, 128, 256>;
-  int off[SLOW ? 2 : 4];
+  using F = Feed<float, SLOW, W, 256>;
+  static constexpr int kBlocks = W / 64, kRow = 4 * W;   // of a wave; bytes of a slow row
+  int off[SLOW ? kBlocks : 4];
   __device__ __forceinline__ void start(int w0, int lane) {   // w0: the wave's first of the tile
     const int n = lane & 31, g = lane >> 5;
     if constexpr (!SLOW) {
@@ -185,9 +170,9 @@ struct Frags {
       for (int u = 0; u < 4; ++u) off[u] = (w0 + n) * 128 + (((2 * u + g) ^ F::swz(w0 + n)) << 4);
     } else {
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < kBlocks; ++b) {
         const int col = w0 + 32 * b + n;
-        off[b] = 4 * g * 512 + (((col >> 2) ^ F::swz(4 * g)) << 4) + (col & 3) * 4;
+        off[b] = 4 * g * kRow + (((col >> 2) ^ F::swz(4 * g)) << 4) + (col & 3) * 4;
       }
     }
   }
@@ -197,54 +182,56 @@ struct Frags {
     } else {
       f32x4 x;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const float*>(tile + off[b] + (8 * u + e) * 512);
+      for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const float*>(tile + off[b] + (8 * u + e) * kRow);
       return x;
     }
   }
 };
 
-// Tiles of 128 x 128, four waves of 64 x 64, two workgroups to a compute unit.  Bound by the matrix cores.
-template <bool PS, bool QS>
-__global__ __launch_bounds__(256, 2) void gemm_f32_kernel(GemmArgs a) {
-  constexpr int kP = 128 * 128, kStage = 2 * kP, BK = 32;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
+// Tiles of W x W, four waves of W / 2 x W / 2 in blocks of 32 x 32.  Bound by the matrix cores (W = 128, two
+// workgroups to a compute unit), or by the latency of a step (W = 64, four).
+constexpr int tile_lds(int W) { return 4 * W * 128; }   // two buffers of two operands
+
+template <bool PS, bool QS, int W>
+__device__ __forceinline__ void tile_product(const GemmArgs& a, uint32_t id, uint32_t wgs, char* lds) {
+  constexpr int kP = W * 128, kStage = 2 * kP, BK = 32, B = W / 64, kProducts = 4 * B * B;
   const uint32_t lbase = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wi = wave / 2, wj = wave % 2;
   const uint32_t I = (uint32_t)a.I, J = (uint32_t)a.J;
   uint32_t i_tile, j_tile;
-  place(xcd_remap(blockIdx.x, gridDim.x), (I + 127) / 128, (J + 127) / 128, i_tile, j_tile);
-  const uint32_t i0 = i_tile * 128, j0 = j_tile * 128;
-  Feed<float, PS, 128, 256> fp;
-  Feed<float, QS, 128, 256> fq;
+  place(xcd_remap(id, wgs), (I + W - 1) / W, (J + W - 1) / W, i_tile, j_tile);
+  const uint32_t i0 = i_tile * W, j0 = j_tile * W;
+  Feed<float, PS, W, 256> fp;
+  Feed<float, QS, W, 256> fq;
   fp.start(a.P, i0, 0, tid);
   fq.start(a.Q, j0, 0, tid);
-  Frags<PS> rp;
-  Frags<QS> rq;
-  rp.start(wi * 64, lane);
-  rq.start(wj * 64, lane);
+  Frags<PS, W> rp;
+  Frags<QS, W> rq;
+  rp.start(wi * (W / 2), lane);
+  rq.start(wj * (W / 2), lane);
   const uint32_t wdst = (uint32_t)__builtin_amdgcn_readfirstlane(lbase + wave * 1024);
-  f32x16 acc[2][2];
+  f32x16 acc[B][B];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < B; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) acc[i][j] = f32x16{};
+    for (int j = 0; j < B; ++j) acc[i][j] = f32x16{};
 
   // Unit T - 1's products (8 of r), beside them the reads of unit T of the step in `buf` and a later step's
   // loads.
-  f32x4 p[2][2], q[2][2];
+  f32x4 p[2][B], q[2][B];
   auto unit = [&](auto t, uint32_t buf, auto feed, auto loads) {
     constexpr int T = decltype(t)::value, L = decltype(loads)::value, S = T & 1;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < kProducts; ++i) {
 #pragma unroll
-      for (int u = i * L / 16; u < (i + 1) * L / 16; ++u) feed(u);
-      if (i % 4 == 0) {
-        const int b = i / 8;
-        if (i % 8 == 0) q[S][b] = rq.get(lds + buf + kP, T, b);
-        else p[S][b] = rp.get(lds + buf, T, b);
+      for (int u = i * L / kProducts; u < (i + 1) * L / kProducts; ++u) feed(u);
+#pragma unroll
+      for (int f = i * 2 * B / kProducts; f < (i + 1) * 2 * B / kProducts; ++f) {
+        if (f % 2 == 0) q[S][f / 2] = rq.get(lds + buf + kP, T, f / 2);
+        else p[S][f / 2] = rp.get(lds + buf, T, f / 2);
       }
-      const int e = i / 4, bi = i / 2 % 2, bj = i % 2;
+      const int e = i / (B * B), bi = i / B % B, bj = i % B;
       acc[bi][bj] = mfma32f(q[S ^ 1][bj][e], p[S ^ 1][bi][e], acc[bi][bj]);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -252,7 +239,7 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_kernel(GemmArgs a) {
   auto nothing = [](int) {};
   using std::integral_constant;
   typedef integral_constant<int, 0> kNone;
-  typedef integral_constant<int, Feed<float, PS, 128, 256>::kLoads> kLoads;
+  typedef integral_constant<int, Feed<float, PS, W, 256>::kLoads> kLoads;
   int rest = (int)a.R;
   const int steps = (rest + BK - 1) / BK;
   fp.all(wdst, rest);
@@ -262,7 +249,7 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_kernel(GemmArgs a) {
   wait_vmem<kLoads::value>();
   __syncthreads();
 #pragma unroll
-  for (int b = 0; b < 2; ++b) q[0][b] = rq.get(lds + kP, 0, b), p[0][b] = rp.get(lds, 0, b);
+  for (int b = 0; b < B; ++b) q[0][b] = rq.get(lds + kP, 0, b), p[0][b] = rp.get(lds, 0, b);
   uint32_t buf = 0;
   for (int s = steps; s > 0; --s) {
     fq.begin(rest);
@@ -284,10 +271,10 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_kernel(GemmArgs a) {
   const auto bias = [&](uint32_t j) { return o.bias && j < J ? o.bias[j] : 0.f; };
   float* const stage = reinterpret_cast<float*>(lds) + wave * 32 * 33;
 #pragma unroll
-  for (int bi = 0; bi < 2; ++bi)
+  for (int bi = 0; bi < B; ++bi)
 #pragma unroll
-    for (int bj = 0; bj < 2; ++bj) {
-      const uint32_t ib = i0 + wi * 64 + 32 * bi, jb = j0 + wj * 64 + 32 * bj;
+    for (int bj = 0; bj < B; ++bj) {
+      const uint32_t ib = i0 + wi * (W / 2) + 32 * bi, jb = j0 + wj * (W / 2) + 32 * bj;
       if (vec) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
@@ -315,32 +302,68 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_kernel(GemmArgs a) {
     }
 }
 
+// SIDE: of a tile, or 32 for small blocks
+template <bool PS, bool QS, int SIDE>
+__device__ __forceinline__ void product(const GemmArgs& a, uint32_t id, uint32_t wgs, char* lds) {
+  if constexpr (SIDE == 32) small_product<PS, QS>(a, id, wgs, reinterpret_cast<float*>(lds));
+  else tile_product<PS, QS, SIDE>(a, id, wgs, lds);
+}
+template <int SIDE>
+constexpr int kLds = SIDE == 32 ? kSmallLds * 4 : tile_lds(SIDE);
+template <int SIDE>
+constexpr int kPerUnit = SIDE == 128 ? 2 : 4;   // workgroups of a compute unit
+
+template <bool PS, bool QS, int SIDE>
+__global__ __launch_bounds__(256, kPerUnit<SIDE>) void gemm_f32_kernel(GemmArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[kLds<SIDE>];
+  product<PS, QS, SIDE>(a, blockIdx.x, gridDim.x, lds);
+}
+
+// Both products of a backward that do not fill the chip one by one, and the sums of the bias's gradient from
+// its parts, in one launch.
+template <int SIDE>
+__global__ __launch_bounds__(256, kPerUnit<SIDE>) void gemm_f32_pair_kernel(GemmPair p) {
+  __shared__ __attribute__((aligned(1024))) char lds[kLds<SIDE>];
+  const uint32_t id = blockIdx.x;
+  if (id < p.wgs_dx) product<false, true, SIDE>(p.dx, id, p.wgs_dx, lds);
+  else if (id < p.wgs_dx + p.wgs_dw) product<true, true, SIDE>(p.dw, id - p.wgs_dx, p.wgs_dw, lds);
+  else sum_columns<kWaves>(p.sums, id - p.wgs_dx - p.wgs_dw, reinterpret_cast<float(*)[64]>(lds));
+}
+
 uint32_t workgroups(const GemmArgs& a, int64_t side) {
   return (uint32_t)(((a.I + side - 1) / side) * ((a.J + side - 1) / side));
+}
+
+template <int SIDE>
+hipError_t launch(const GemmArgs& a) {
+  const dim3 grid(workgroups(a, SIDE) * (uint32_t)a.splits);
+  if (a.p_slow) hipLaunchKernelGGL((gemm_f32_kernel<true, true, SIDE>), grid, dim3(256), 0, a.stream, a);
+  else if (a.q_slow) hipLaunchKernelGGL((gemm_f32_kernel<false, true, SIDE>), grid, dim3(256), 0, a.stream, a);
+  else hipLaunchKernelGGL((gemm_f32_kernel<false, false, SIDE>), grid, dim3(256), 0, a.stream, a);
+  return hipGetLastError();
+}
+
+template <int SIDE>
+hipError_t launch_pair(GemmPair p) {
+  p.wgs_dx = workgroups(p.dx, SIDE), p.wgs_dw = workgroups(p.dw, SIDE);
+  const uint32_t sums = p.sums.parts ? (uint32_t)((p.sums.cols + 63) / 64) : 0;
+  hipLaunchKernelGGL((gemm_f32_pair_kernel<SIDE>), dim3(p.wgs_dx + p.wgs_dw + sums), dim3(256), 0,
+                     p.dx.stream, p);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_gemm_f32(const GemmArgs& a) {
-  if (gemm_f32_large(a.I, a.J)) {
-    const dim3 grid(workgroups(a, 128));
-    if (a.p_slow) hipLaunchKernelGGL((gemm_f32_kernel<true, true>), grid, dim3(256), 0, a.stream, a);
-    else if (a.q_slow) hipLaunchKernelGGL((gemm_f32_kernel<false, true>), grid, dim3(256), 0, a.stream, a);
-    else hipLaunchKernelGGL((gemm_f32_kernel<false, false>), grid, dim3(256), 0, a.stream, a);
-  } else {
-    const dim3 grid(workgroups(a, kSide) * (uint32_t)a.splits);
-    if (a.p_slow) hipLaunchKernelGGL((gemm_f32_small_kernel<true, true>), grid, dim3(256), 0, a.stream, a);
-    else if (a.q_slow) hipLaunchKernelGGL((gemm_f32_small_kernel<false, true>), grid, dim3(256), 0, a.stream, a);
-    else hipLaunchKernelGGL((gemm_f32_small_kernel<false, false>), grid, dim3(256), 0, a.stream, a);
+  switch (a.side) {
+    case 128: return launch<128>(a);
+    case 64: return launch<64>(a);
+    default: return launch<32>(a);
   }
-  return hipGetLastError();
 }
 
-hipError_t launch_gemm_pair_f32(GemmPair p) {
-  p.wgs_dx = workgroups(p.dx, kSide), p.wgs_dw = workgroups(p.dw, kSide);
-  const uint32_t sums = p.sums.parts ? (uint32_t)((p.sums.cols + 63) / 64) : 0;
-  hipLaunchKernelGGL(gemm_f32_pair_kernel, dim3(p.wgs_dx + p.wgs_dw + sums), dim3(256), 0, p.dx.stream, p);
-  return hipGetLastError();
+hipError_t launch_gemm_pair_f32(const GemmPair& p) {
+  return p.dx.side == 64 ? launch_pair<64>(p) : launch_pair<32>(p);
 }
 
 }  // namespace ringx

@@ -47,7 +47,8 @@ struct Feed {
   static constexpr int kSize = (int)sizeof(T), E = 16 / kSize, BK = 128 / kSize;   // values of a piece, of a step
   static constexpr int kLoads = W * 128 / (THREADS * 16);
   static constexpr int kRowChunks = SLOW ? W / E : 8;
-  static_assert(kLoads * THREADS * 16 == W * 128 && (!SLOW || W >= 128), "whole rounds of loads");
+  static_assert(kLoads * THREADS * 16 == W * 128 && kRowChunks % 8 == 0, "whole rounds of loads");
+  static_assert(!SLOW || kRowChunks >= 16, "the swizzle stays in a row");
   static_assert(SLOW || THREADS / kRowChunks % 16 == 0, "rounds keep the swizzle's phase");
   uint32_t off[kLoads];
   int64_t base, left;    // address of the step's first row or column; bytes from it to the tensor's end

@@ -377,7 +377,7 @@ hipError_t forward(const LinearArgs& a) {
   const hipError_t e = pack<T>(&g.P, p.x, p.ldx, &g.Q, p.w, p.ldw, a.workspace, a.stream);
   if (e != hipSuccess) return e;
   g.R = p.R;
-  g.splits = p.splits, g.cut = p.cut, g.part = (float*)at(a.workspace, p.part);
+  g.splits = p.splits, g.side = p.side, g.cut = p.cut, g.part = (float*)at(a.workspace, p.part);
   return launch_product<T>(g);
 }
 
@@ -415,14 +415,14 @@ hipError_t backward(const LinearArgs& a) {
   if (e != hipSuccess) return e;
   if (a.dx) {
     x.q_slow = true;
-    x.I = a.s.M, x.J = a.s.K, x.R = dz.cols, x.splits = p.splits_dx, x.cut = p.cut_dx;
+    x.I = a.s.M, x.J = a.s.K, x.R = dz.cols, x.splits = p.splits_dx, x.side = p.side_dx, x.cut = p.cut_dx;
     x.part = (float*)at(a.workspace, p.part);
     x.o.out = a.dx, x.o.J = a.s.K, x.o.f32 = a.dx_f32 && !a.s.heads;
     if (a.s.heads) x.o.heads = a.s.heads, x.o.tokens = a.s.tokens, x.o.d = a.s.K / a.s.heads;
   }
   if (a.dw) {
     w.p_slow = w.q_slow = true;
-    w.I = a.s.O, w.J = a.s.K, w.R = a.s.M, w.splits = p.splits_dw, w.cut = p.cut_dw;
+    w.I = a.s.O, w.J = a.s.K, w.R = a.s.M, w.splits = p.splits_dw, w.side = p.side_dw, w.cut = p.cut_dw;
     w.part = (float*)at(a.workspace, p.part_dw);
     w.o.out = a.dw, w.o.J = a.s.K, w.o.f32 = a.dw_f32, w.o.accumulate = a.accumulate;
   }

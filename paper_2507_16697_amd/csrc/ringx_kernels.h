@@ -503,6 +503,7 @@ struct GemmArgs {
   int64_t I = 0, J = 0, R = 0;
   GemmOut o;
   int splits = 1;                  // fp32: parts of R, whose sums go to part [splits, I, J]
+  int side = 32;                   // fp32: of a tile
   GemmCut cut;                     // bf16
   float* part = nullptr;
   hipStream_t stream = nullptr;
@@ -580,20 +581,28 @@ inline bool gemm_cut_pair(int64_t M, int64_t K, int64_t O, GemmCut* dx, GemmCut*
     }
   return found;
 }
-// fp32: whether a product takes tiles of 128 x 128 (else 32 x 32), and parts that R is cut into where the
-// tiles do not fill the chip.
-inline bool gemm_f32_large(int64_t I, int64_t J) {
-  return ((I + 127) / 128) * ((J + 127) / 128) >= 192;
+// fp32: side of the tiles that a product takes, and parts that R is cut into where the smallest do not fill the
+// chip.  `slow`: an operand has r across its rows.  us of sides 128 / 64 / 32 (I x J, R):
+//   r along the rows of both: 2048 x 4096, 2048: 257 / 273 / 451; 2048 x 2048, 1024: 79 / 75 / 118;
+//     1024 x 1024, 1024: 78 / 32 / 35; 1531 x 577, 192: 30 / 11.9 / 11.3; 700 x 900, 300: 30 / 12.9 / 10.2
+//   others: 4096 x 2048, 2048: 251 / 261 / 301; 2048 x 1024, 2048: 138 / 84 / 88; 1400 x 1000, 1400: 97 / 58 / 52
+inline int gemm_f32_side(int64_t I, int64_t J, bool slow) {
+  const auto tiles = [&](int64_t side) { return ((I + side - 1) / side) * ((J + side - 1) / side); };
+  return tiles(128) >= 512 ? 128 : tiles(64) >= (slow ? 512 : 256) ? 64 : 32;
 }
-inline int gemm_f32_splits(int64_t I, int64_t J, int64_t R) {
-  if (gemm_f32_large(I, J)) return 1;
+inline int gemm_f32_splits(int64_t I, int64_t J, int64_t R, int side) {
+  if (side != 32) return 1;
   const int64_t tiles = ((I + 31) / 32) * ((J + 31) / 32);
   const int64_t s = std::min<int64_t>({512 / tiles, (R + 63) / 64 / 4, 32});
   return (int)std::max<int64_t>(s, 1);
 }
-// Both products of a backward in one launch: small tiles, without parts, whose r is short.
-inline bool gemm_f32_pair(int64_t M, int64_t K, int64_t O) {
-  return !gemm_f32_large(M, K) && !gemm_f32_large(O, K) && std::max(M, O) <= 2048;
+// Side of the tiles of both products of a backward in one launch, without parts of r, which is short (0: each by
+// itself).  us of the backward, sides 64 / 32 (M x K to O): 1024 x 1024 to 1024: 55 / 60; 256 x 4096 to 256:
+// 20.5 / 23.8; 2048 x 512 to 1536: 86.0 / 86.5; 2048 x 512 to 1024: 75 / 71; 1531 x 192 to 577: 46 / 29
+inline int gemm_f32_pair(int64_t M, int64_t K, int64_t O) {
+  if (std::max(M, O) > 2048 || gemm_f32_side(M, K, true) == 128 || gemm_f32_side(O, K, true) == 128) return 0;
+  const auto tiles = [](int64_t i, int64_t j) { return ((i + 63) / 64) * ((j + 63) / 64); };
+  return tiles(M, K) + tiles(O, K) >= 448 ? 64 : 32;
 }
 
 // The pass over a gradient [M, O]: threads across 8 columns each, rows of a workgroup, workgroups.
@@ -656,6 +665,7 @@ struct LinearPlan {
   int64_t part = 0, part_dw = 0;           // parts of split products
   int64_t R = 0;                           // forward: the product's r
   int splits = 1, splits_dx = 1, splits_dw = 1;   // fp32
+  int side = 32, side_dx = 32, side_dw = 32;
   GemmCut cut, cut_dx, cut_dw;             // bf16
   bool pair = false;                       // backward: both products in one launch
   int64_t bytes = 0;
@@ -685,22 +695,25 @@ inline LinearPlan linear_plan(const LinearShape& s) {
     if (Kp != s.K) p.w = p.take(2 * s.O * Kp), p.ldw = Kp;
   } else {
     const int64_t Kt = (s.K + 3) / 4 * 4;
-    const bool large = gemm_f32_large(s.M, s.O);   // in 16-byte pieces
-    if (large) p.R = Kt;
-    if (s.heads || !linear_near(s) || (large && (Kt != s.K || s.ldx % 4 != 0))) p.ldx = large ? Kt : s.K;
+    p.side = gemm_f32_side(s.M, s.O, false);
+    const bool pieces = p.side != 32;   // rows in 16-byte pieces
+    if (pieces) p.R = Kt;
+    if (s.heads || !linear_near(s) || (pieces && (Kt != s.K || s.ldx % 4 != 0))) p.ldx = pieces ? Kt : s.K;
     if (p.ldx) p.x = p.take(4 * s.M * p.ldx);
-    if (large && Kt != s.K) p.w = p.take(4 * s.O * Kt), p.ldw = Kt;
+    if (pieces && Kt != s.K) p.w = p.take(4 * s.O * Kt), p.ldw = Kt;
   }
   if (s.bf16) p.cut = gemm_cut(s.M, s.O, p.R);
-  else p.splits = gemm_f32_splits(s.M, s.O, p.R);
+  else p.splits = gemm_f32_splits(s.M, s.O, p.R, p.side);
   const int64_t part = p.splits > 1 ? 4 * p.splits * s.M * s.O : p.cut.part_bytes;
   if (part) p.part = p.take(part);
   return p;
 }
 inline LinearPlan linear_bwd_plan(const LinearShape& s, int act) {
   LinearPlan p;
-  // rows in 16-byte pieces: bf16, and fp32 where one of the products is large
-  const bool pieces = s.bf16 || gemm_f32_large(s.M, s.K) || gemm_f32_large(s.O, s.K);
+  const int pair = s.bf16 ? 0 : gemm_f32_pair(s.M, s.K, s.O);
+  p.side_dx = pair ? pair : gemm_f32_side(s.M, s.K, true), p.side_dw = pair ? pair : gemm_f32_side(s.O, s.K, true);
+  // rows in 16-byte pieces
+  const bool pieces = s.bf16 || p.side_dx != 32 || p.side_dw != 32;
   const int64_t es = s.bf16 ? 2 : 4, piece = pieces ? 16 / es : 1;
   const int64_t Kp = (s.K + piece - 1) / piece * piece, Op = (s.O + piece - 1) / piece * piece;
   p.ldz = Op;
@@ -716,8 +729,9 @@ inline LinearPlan linear_bwd_plan(const LinearShape& s, int act) {
     p.pair = gemm_cut_pair(s.M, s.K, s.O, &p.cut_dx, &p.cut_dw);
     dx = p.cut_dx.part_bytes, dw = p.cut_dw.part_bytes;
   } else {
-    p.pair = gemm_f32_pair(s.M, s.K, s.O);
-    if (!p.pair) p.splits_dx = gemm_f32_splits(s.M, s.K, Op), p.splits_dw = gemm_f32_splits(s.O, s.K, s.M);
+    p.pair = pair != 0;
+    if (!p.pair)
+      p.splits_dx = gemm_f32_splits(s.M, s.K, Op, p.side_dx), p.splits_dw = gemm_f32_splits(s.O, s.K, s.M, p.side_dw);
     if (p.splits_dx > 1) dx = 4 * p.splits_dx * s.M * s.K;
     if (p.splits_dw > 1) dw = 4 * p.splits_dw * s.O * s.K;
   }
@@ -756,7 +770,7 @@ hipError_t launch_column_sums(const ColumnSums& a);
 hipError_t launch_gemm_bf16(const GemmArgs& a);
 hipError_t launch_gemm_pair_bf16(const GemmPair& p);
 hipError_t launch_gemm_f32(const GemmArgs& a);
-hipError_t launch_gemm_pair_f32(GemmPair p);
+hipError_t launch_gemm_pair_f32(const GemmPair& p);
 hipError_t launch_linear(const LinearArgs& a);
 hipError_t launch_linear_bwd(const LinearArgs& a);
 

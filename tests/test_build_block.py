@@ -23,7 +23,7 @@ KERNELS = {
                       (r"gemm_bf16_kernel.*TileILi128ELi128ELi2ELi2ELi2E", 1, 8),
                       (r"gemm_bf16_kernel.*TileILi256E", 1, 8), (r"gemm_pair_kernel", 1, 8),
                       (r"gemm_join", 2, 4)],
-    "gemm_f32.hip": [(r"gemm_f32_kernel", 2, 4), (r"gemm_f32_(small|pair)_kernel", 4, 4)],
+    "gemm_f32.hip": [(r"gemm_f32_kernel.*ELi128E", 2, 4), (r"gemm_f32_(kernel|pair_kernel).*Li(64|32)E", 4, 4)],
 }
 
 

@@ -149,6 +149,10 @@ def test_activations_at_their_ends(act):
     (3000, 712, 392, 0),       # and one group
     (70, 4096, 96, 0),         # parts of r forward
     (300, 2072, 200, 0),
+    (1500, 301, 1100, 0),      # fp32: tiles of 64 forward
+    (1500, 1501, 700, 0),      # and of both gradients in one launch
+    (2100, 1601, 1400, 0),     # and of each by itself
+    (8190, 1101, 8200, 0),     # tiles of 128, ragged
 ])
 def test_large(M, K, O, heads, store):
     lead = (2, M // 2) if heads else (M,)
