@@ -610,13 +610,13 @@ struct GradGrid {
   int across;
   int64_t rows, x, y;
 };
-inline GradGrid grad_grid(int64_t M, int64_t O, bool few) {   // few: at most 160 along the rows
+inline GradGrid grad_grid(int64_t M, int64_t O, bool few) {   // few: at most 256 along the rows
   GradGrid g;
   g.across = 1;
   while (g.across < 64 && 8 * g.across < O) g.across *= 2;
   g.x = (O + 8 * g.across - 1) / (8 * g.across);
-  const int64_t least = 4 * (256 / g.across);      // rows of one round
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(few ? 160 : 512, 2048 / g.x));
+  const int64_t least = 2 * (256 / g.across);      // rows of one round
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(few ? 256 : 512, 2048 / g.x));
   g.rows = std::max<int64_t>(least, ((M + most - 1) / most + least - 1) / least * least);
   g.y = (M + g.rows - 1) / g.rows;
   return g;
