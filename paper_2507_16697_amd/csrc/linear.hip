@@ -14,87 +14,119 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 // -------------------------------------------------------------------------------------------------
 // A few rows (a token at a time, or some of them), bf16.  Bound by the weights' bytes: every weight is
 // loaded once, straight into the fragments of v_mfma_f32_16x16x32_bf16 (lane l: row l % 16, r = 8 (l / 16)
-// .. + 7), 16 features to a workgroup whose waves take turns at 64 of K.  The rows of x, MB blocks of 16 of
-// them (those past M repeat the last), come from the caches.
+// .. + 7), NB blocks of 16 features to a workgroup whose waves take turns at 64 of K.  The rows of x, MB blocks
+// of 16 of them (those past M repeat the last), come from the caches, once for each workgroup.
+//
+// VEC: x goes through the wave's own LDS, since a fragment's load touches 16 lines at a time and takes four times
+// as long as one of whole 64-byte pieces: lane l loads row l / 4 of a block, piece l % 4, XORed with (row / 4) so
+// that 16 rows' same piece lies in 16 places.
 
-template <int MB, bool VEC>
-__global__ __launch_bounds__(512) void few_rows_kernel(GemmArgs a) {
-  constexpr int kUnroll = VEC ? (MB == 1 ? 8 : 4) : (MB == 4 ? 1 : 2);   // what the registers hold
-  __shared__ f32x4 lds[8][MB][64];
+template <int MB, int NB, int WAVES, bool VEC>
+__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(GemmArgs a) {
+  constexpr int kUnroll = VEC ? (MB == 1 ? 8 : MB == 2 ? 4 : 2) : (MB >= 3 ? 1 : 2);   // what registers and LDS hold
+  constexpr int kStage = VEC ? kUnroll * 2 * MB * 1024 : 0, kSums = MB * NB * 1024;   // bytes of a wave
+  __shared__ __attribute__((aligned(1024))) char lds[WAVES * (kStage > kSums ? kStage : kSums)];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int waves = blockDim.x / 64;
-  const int64_t j0 = (int64_t)blockIdx.x * 16;
+  const int64_t j0 = (int64_t)blockIdx.x * (16 * NB);
   const int K = (int)a.R;
-  const __bf16* const w = (const __bf16*)a.Q.p + min(j0 + n, a.J - 1) * a.Q.ld;
+  const bool heads = a.P.heads != 0;
+  const __bf16* w[NB];
+#pragma unroll
+  for (int f = 0; f < NB; ++f) w[f] = (const __bf16*)a.Q.p + min(j0 + 16 * f + n, a.J - 1) * a.Q.ld;
   const __bf16* x[MB];
+  const int row = VEC ? lane >> 2 : n;
 #pragma unroll
   for (int m = 0; m < MB; ++m) {
-    const int64_t i = min((int64_t)(16 * m + n), a.I - 1);
+    const int64_t i = min((int64_t)(16 * m + row), a.I - 1);
     int64_t at = i * a.P.ld;
-    if (a.P.heads) {
+    if (heads) {
       const uint32_t b = (uint32_t)i / (uint32_t)a.P.tokens;
       at = (int64_t)b * a.P.tokens * a.P.cols + (i - (int64_t)b * a.P.tokens) * a.P.d;
     }
     x[m] = (const __bf16*)a.P.p + at;
   }
-  auto get = [&](const __bf16* p, int k, bool heads) {
+  const auto place = [&](int k) {   // column k of a row of x
+    if (!heads) return (int64_t)k;
+    const uint32_t h = (uint32_t)k / (uint32_t)a.P.d;
+    return (int64_t)h * a.P.tokens * a.P.d + (k - (int)h * (int)a.P.d);
+  };
+  const auto values = [&](const __bf16* p, int k, auto at) {   // 8 from column k on, zeros past K
     bf16x8 v = {};
     if constexpr (VEC) {
-      if (k < K) {
-        int64_t at = k;
-        if (heads) {
-          const uint32_t h = (uint32_t)k / (uint32_t)a.P.d;
-          at = (int64_t)h * a.P.tokens * a.P.d + (k - (int)h * (int)a.P.d);
-        }
-        v = *reinterpret_cast<const bf16x8*>(p + at);
-      }
+      if (k < K) v = *reinterpret_cast<const bf16x8*>(p + at(k));
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        int64_t at = min(k + e, K - 1);
-        if (heads) {
-          const uint32_t h = (uint32_t)at / (uint32_t)a.P.d;
-          at = (int64_t)h * a.P.tokens * a.P.d + (at - (int64_t)h * a.P.d);
-        }
-        const __bf16 y = p[at];
+        const __bf16 y = p[at(min(k + e, K - 1))];
         v[e] = k + e < K ? y : (__bf16)0.f;
       }
     }
     return v;
   };
-  f32x4 acc[MB];
+  f32x4 acc[MB * NB];
 #pragma unroll
-  for (int m = 0; m < MB; ++m) acc[m] = f32x4{};
-  const bool heads = a.P.heads != 0;
-  for (int k0 = wave * 64; k0 < K; k0 += waves * 64 * kUnroll) {
-    bf16x8 wv[kUnroll][2], xv[kUnroll][2][MB];
+  for (int m = 0; m < MB * NB; ++m) acc[m] = f32x4{};
+  const uint32_t base = __builtin_amdgcn_readfirstlane(
+      (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * kStage);
+  const int piece = (lane & 3) ^ (lane >> 4), read = wave * kStage + n * 64 + ((g ^ (n >> 2)) << 4);
+  for (int k0 = wave * 64; k0 < K; k0 += WAVES * 64 * kUnroll) {
+    bf16x8 wv[kUnroll][2][NB], xv[kUnroll][2][MB];
+    if constexpr (VEC) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what lies there has been read
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
+      for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) wv[u][h] = get(w, k0 + u * waves * 64 + 32 * h + 8 * g, false);
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int m = 0; m < MB; ++m)
+            load_lds16(x[m] + place(min(k0 + u * WAVES * 64 + 32 * h + 8 * piece, K - 8)),
+                       base + ((u * 2 + h) * MB + m) * 1024);
+    }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int m = 0; m < MB; ++m) xv[u][h][m] = get(x[m], k0 + u * waves * 64 + 32 * h + 8 * g, heads);
+        for (int f = 0; f < NB; ++f)
+          wv[u][h][f] = values(w[f], k0 + u * WAVES * 64 + 32 * h + 8 * g, [](int k) { return (int64_t)k; });
+    if constexpr (VEC) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+          const int k = k0 + u * WAVES * 64 + 32 * h + 8 * g;
+          if constexpr (VEC) {
+            const bf16x8 v = *reinterpret_cast<const bf16x8*>(lds + read + ((u * 2 + h) * MB + m) * 1024);
+            xv[u][h][m] = k < K ? v : bf16x8{};
+          } else {
+            xv[u][h][m] = values(x[m], k, place);
+          }
+        }
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int m = 0; m < MB; ++m)
-          acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[u][h], xv[u][h][m], acc[m], 0, 0, 0);
-  }
 #pragma unroll
-  for (int m = 0; m < MB; ++m) lds[wave][m][lane] = acc[m];
+          for (int f = 0; f < NB; ++f)
+            acc[NB * m + f] =
+                __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[u][h][f], xv[u][h][m], acc[NB * m + f], 0, 0, 0);
+  }
+  f32x4* const sums = reinterpret_cast<f32x4*>(lds) + lane;   // [wave][block][lane]
   __syncthreads();
-  // wave m ends block m: the waves' sums in their order
-  for (int m = wave; m < MB; m += waves) {
-    f32x4 s = lds[0][m][lane];
-    for (int i = 1; i < waves; ++i) s += lds[i][m][lane];
-    const int64_t i = 16 * m + n, j = j0 + 4 * g;
+#pragma unroll
+  for (int m = 0; m < MB * NB; ++m) sums[(wave * MB * NB + m) * 64] = acc[m];
+  __syncthreads();
+  // a wave ends a block at a time: the waves' sums in their order
+  for (int m = wave; m < MB * NB; m += WAVES) {
+    f32x4 s = sums[m * 64];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) s += sums[(i * MB * NB + m) * 64];
+    const int64_t i = 16 * (m / NB) + n, j = j0 + 16 * (m % NB) + 4 * g;
     const int inside = (int)max((int64_t)0, min((int64_t)4, a.J - j));
     if (i >= a.I || inside == 0) continue;
     float b[4], y[4] = {s[0], s[1], s[2], s[3]};
@@ -105,15 +137,31 @@ __global__ __launch_bounds__(512) void few_rows_kernel(GemmArgs a) {
   }
 }
 
+template <int MB, int NB, bool VEC>
+hipError_t launch_few_rows_as(const GemmArgs& a) {
+  const dim3 grid((uint32_t)((a.J + 16 * NB - 1) / (16 * NB)));
+  // 4 waves; 8 where there are few workgroups and much of K
+  if (grid.x <= 256 && a.R >= 1024)
+    hipLaunchKernelGGL((few_rows_kernel<MB, NB, 8, VEC>), grid, dim3(512), 0, a.stream, a);
+  else
+    hipLaunchKernelGGL((few_rows_kernel<MB, NB, 4, VEC>), grid, dim3(256), 0, a.stream, a);
+  return hipGetLastError();
+}
+
 template <bool VEC>
 hipError_t launch_few_rows(const GemmArgs& a) {
-  // 4 waves; 8 where there are few features and much of K
-  const int waves = a.J <= 4096 && a.R >= 1024 ? 8 : 4;
-  const dim3 grid((uint32_t)((a.J + 15) / 16)), threads(64 * waves);
-  if (a.I <= 16) hipLaunchKernelGGL((few_rows_kernel<1, VEC>), grid, threads, 0, a.stream, a);
-  else if (a.I <= 32) hipLaunchKernelGGL((few_rows_kernel<2, VEC>), grid, threads, 0, a.stream, a);
-  else hipLaunchKernelGGL((few_rows_kernel<4, VEC>), grid, threads, 0, a.stream, a);
-  return hipGetLastError();
+  if (a.I <= 16) return launch_few_rows_as<1, 1, VEC>(a);
+  if constexpr (VEC) {
+    // two blocks of features where that leaves a workgroup to every compute unit
+    if (a.J >= 8192) {
+      if (a.I <= 32) return launch_few_rows_as<2, 2, VEC>(a);
+      if (a.I <= 48) return launch_few_rows_as<3, 2, VEC>(a);
+      return launch_few_rows_as<4, 2, VEC>(a);
+    }
+  }
+  if (a.I <= 32) return launch_few_rows_as<2, 1, VEC>(a);
+  if (a.I <= 48) return launch_few_rows_as<3, 1, VEC>(a);
+  return launch_few_rows_as<4, 1, VEC>(a);
 }
 
 // -------------------------------------------------------------------------------------------------
