@@ -132,6 +132,19 @@ __device__ __forceinline__ void load_vector(const float* p, float otherwise, int
   }
 }
 
+template <class T, bool VEC, int E, int TPR>
+__device__ __forceinline__ void store_vector(float* p, int t, int C, const float (&x)[E]) {
+  using R = Row<T, VEC, E, TPR>;
+  if (!p) return;
+#pragma unroll
+  for (int e = 0; e < E; e += VEC ? 4 : 1) {
+    const int c = R::col(e, t);
+    if (c >= C) continue;
+    if constexpr (VEC) *reinterpret_cast<f32x4*>(p + c) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+    else p[c] = x[e];
+  }
+}
+
 template <int CTRL>
 __device__ __forceinline__ float add_lane(float x) {
   return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
@@ -147,12 +160,20 @@ __device__ __forceinline__ float lane_sum(float x) {   // over N <= 64 neighbour
   return x;
 }
 
+// Threads of a workgroup.  Rows of up to 64 threads share 256.  Wider ones have one of their own forward (8192 x
+// 8192 bf16 44 us, sharing 512 56) and share 512 backward, where a workgroup has parts to write (99 -> 91 us with half
+// as many of them).
+template <int TPR, bool BWD>
+constexpr int kGroup = TPR <= 64 ? 256 : BWD && TPR <= 512 ? 512 : TPR;
+template <int TPR, bool BWD>
+constexpr int kRowsAtOnce = kGroup<TPR, BWD> / TPR;
+
 // Sums of two values over the TPR threads of a row.  Rows of several waves go through LDS, `slot`
 // alternating, so that one barrier serves: a slot is written again two sums later, behind the next one's
 // barrier.
-template <int TPR>
+template <int TPR, bool BWD>
 struct RowSum {
-  f32x2 lds[2][TPR > 64 ? TPR / 64 : 1];
+  f32x2 lds[2][kGroup<TPR, BWD> / 64];
   __device__ __forceinline__ f32x2 operator()(float a, float b, int& slot) {
     a = lane_sum<(TPR < 64 ? TPR : 64)>(a);
     b = lane_sum<(TPR < 64 ? TPR : 64)>(b);
@@ -162,7 +183,7 @@ struct RowSum {
       a = b = 0.f;
 #pragma unroll
       for (int i = 0; i < TPR / 64; ++i) {
-        const f32x2 x = lds[slot][i];
+        const f32x2 x = lds[slot][threadIdx.x / TPR * (TPR / 64) + i];
         a += x[0], b += x[1];
       }
       slot ^= 1;
@@ -171,21 +192,15 @@ struct RowSum {
   }
 };
 
-// Rows of up to 64 threads share a workgroup of 256, wider ones have one of their own.
-template <int TPR>
-constexpr int kGroup = TPR <= 64 ? 256 : TPR;   // threads of a workgroup
-template <int TPR>
-constexpr int kRowsAtOnce = kGroup<TPR> / TPR;
-
 template <class T, bool VEC, int E, int TPR>
-__global__ __launch_bounds__(kGroup<TPR>) void layer_norm_kernel(NormArgs a) {
+__global__ __launch_bounds__((kGroup<TPR, false>)) void layer_norm_kernel(NormArgs a) {
   using R = Row<T, VEC, E, TPR>;
-  __shared__ RowSum<TPR> sum;
+  __shared__ RowSum<TPR, false> sum;
   const int t = threadIdx.x % TPR;
   const int C = a.C;
   const float inv = 1.f / (float)C;
-  const int64_t step = (int64_t)gridDim.x * kRowsAtOnce<TPR>;
-  int64_t row = (int64_t)blockIdx.x * kRowsAtOnce<TPR> + threadIdx.x / TPR;
+  const int64_t step = (int64_t)gridDim.x * kRowsAtOnce<TPR, false>;
+  int64_t row = (int64_t)blockIdx.x * kRowsAtOnce<TPR, false> + threadIdx.x / TPR;
   const T* const x = (const T*)a.x;
   T* const y = (T*)a.y;
   R cur;
@@ -195,7 +210,7 @@ __global__ __launch_bounds__(kGroup<TPR>) void layer_norm_kernel(NormArgs a) {
   load_vector<T, VEC, E, TPR>(a.weight, 1.f, t, C, w);
   load_vector<T, VEC, E, TPR>(a.bias, 0.f, t, C, b);
   int slot = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * kRowsAtOnce<TPR>; r0 < a.rows; r0 += step, row += step) {
+  for (int64_t r0 = (int64_t)blockIdx.x * kRowsAtOnce<TPR, false>; r0 < a.rows; r0 += step, row += step) {
     R next;
     if (r0 + step < a.rows) next.load(x + min(row + step, a.rows - 1) * a.stride, t, C);
     float s = 0.f, d[E];
@@ -225,15 +240,15 @@ __global__ __launch_bounds__(kGroup<TPR>) void layer_norm_kernel(NormArgs a) {
 }
 
 template <class T, class G, bool VEC, int E, int TPR>
-__global__ __launch_bounds__(kGroup<TPR>, TPR <= 256 ? 2 : 1) void layer_norm_bwd_kernel(NormArgs a) {
+__global__ __launch_bounds__((kGroup<TPR, true>), TPR <= 256 ? 2 : 1) void layer_norm_bwd_kernel(NormArgs a) {
   using R = Row<T, VEC, E, TPR>;
-  constexpr int kWidth = E * TPR;
-  __shared__ RowSum<TPR> sum;
-  __shared__ float lds[TPR <= 64 ? 2 * kWidth : 1];
+  __shared__ RowSum<TPR, true> sum;
+  constexpr int kPitch = TPR + 1;   // of a thread's e-th values in LDS: neither way meets itself in a bank
+  __shared__ float lds[kRowsAtOnce<TPR, true> > 1 ? 2 * E * kPitch : 1];
   const int t = threadIdx.x % TPR;
   const int C = a.C;
   const float inv = 1.f / (float)C;
-  const int64_t step = (int64_t)gridDim.x * kRowsAtOnce<TPR>;
+  const int64_t step = (int64_t)gridDim.x * kRowsAtOnce<TPR, true>;
   const T *const x = (const T*)a.x, *const dres = (const T*)a.dres;
   const G* const dy = (const G*)a.dy;
   T* const dx = (T*)a.dx;
@@ -242,7 +257,7 @@ __global__ __launch_bounds__(kGroup<TPR>, TPR <= 256 ? 2 : 1) void layer_norm_bw
 #pragma unroll
   for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.f;
   int slot = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * kRowsAtOnce<TPR>; r0 < a.rows; r0 += step) {
+  for (int64_t r0 = (int64_t)blockIdx.x * kRowsAtOnce<TPR, true>; r0 < a.rows; r0 += step) {
     const int64_t at = r0 + threadIdx.x / TPR;
     const bool live = at < a.rows;
     const int64_t row = live ? at : a.rows - 1;   // rows past the end repeat the last one
@@ -282,17 +297,12 @@ __global__ __launch_bounds__(kGroup<TPR>, TPR <= 256 ? 2 : 1) void layer_norm_bw
   float* const part = a.part + (int64_t)blockIdx.x * 2 * C;
   float* const pw = alone ? a.dweight : part;
   float* const pb = alone ? a.dbias : part + C;
-  if constexpr (TPR > 64) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = R::col(e, t);
-      if (c < C) {
-        if (pw) pw[c] = dw[e];
-        if (pb) pb[c] = db[e];
-      }
-    }
+  if constexpr (kRowsAtOnce<TPR, true> == 1) {
+    store_vector<T, VEC, E, TPR>(pw, t, C, dw);
+    store_vector<T, VEC, E, TPR>(pb, t, C, db);
   } else {
-    // over the rows of a wave, then wave after wave
+    // over the rows of a wave, then row after row (of waves)
+    constexpr int kHeld = TPR < 64 ? 64 : TPR;
 #pragma unroll
     for (int e = 0; e < E; ++e)
 #pragma unroll
@@ -300,38 +310,39 @@ __global__ __launch_bounds__(kGroup<TPR>, TPR <= 256 ? 2 : 1) void layer_norm_bw
         dw[e] += __shfl_xor(dw[e], off, 64);
         db[e] += __shfl_xor(db[e], off, 64);
       }
-    for (int i = 0; i < kGroup<TPR> / 64; ++i) {
-      if ((int)threadIdx.x / 64 == i && threadIdx.x % 64 < TPR) {
+    float *const sw = lds + t, *const sb = sw + E * kPitch;
+    for (int i = 0; i < kGroup<TPR, true> / kHeld; ++i) {
+      if ((int)threadIdx.x / kHeld == i && threadIdx.x % kHeld < TPR) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          lds[e * TPR + t] = dw[e] + (i ? lds[e * TPR + t] : 0.f);
-          lds[kWidth + e * TPR + t] = db[e] + (i ? lds[kWidth + e * TPR + t] : 0.f);
+          sw[e * kPitch] = dw[e] + (i ? sw[e * kPitch] : 0.f);
+          sb[e * kPitch] = db[e] + (i ? sb[e * kPitch] : 0.f);
         }
       }
       __syncthreads();
     }
-    for (int j = threadIdx.x; j < kWidth; j += kGroup<TPR>) {
-      const int c = R::col(j / TPR, j % TPR);
-      if (c < C) {
-        if (pw) pw[c] = lds[j];
-        if (pb) pb[c] = lds[kWidth + j];
-      }
+    // neighbouring columns in neighbouring lanes: 4 bytes to a lane 32 apart took 20 us of 95 at 8192 x 8192 bf16
+    for (int c = threadIdx.x; c < C; c += kGroup<TPR, true>) {
+      const int at = (c / (R::V * TPR) * R::V + c % R::V) * kPitch + c / R::V % TPR;
+      if (pw) pw[c] = lds[at];
+      if (pb) pb[c] = lds[E * kPitch + at];
     }
   }
 }
 
 template <class T, class G, bool VEC, int E, int TPR>
 hipError_t launch_as(const NormArgs& a, bool bwd) {
-  const int64_t groups = (a.rows + kRowsAtOnce<TPR> - 1) / kRowsAtOnce<TPR>;
+  const int64_t at_once = bwd ? kRowsAtOnce<TPR, true> : kRowsAtOnce<TPR, false>;
+  const int64_t groups = (a.rows + at_once - 1) / at_once;
   int64_t grid = std::min<int64_t>(groups, norm_workgroups(a.C, bwd));
   // Few rows: one workgroup, four rounds at most (5 us), and no second launch (4 us, and as much of the host).
   if (bwd && a.part && groups <= 4) grid = 1;
   if (!bwd) {
-    hipLaunchKernelGGL((layer_norm_kernel<T, VEC, E, TPR>), dim3((uint32_t)grid), dim3(kGroup<TPR>), 0,
+    hipLaunchKernelGGL((layer_norm_kernel<T, VEC, E, TPR>), dim3((uint32_t)grid), dim3(kGroup<TPR, false>), 0,
                        a.stream, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((layer_norm_bwd_kernel<T, G, VEC, E, TPR>), dim3((uint32_t)grid), dim3(kGroup<TPR>), 0,
+  hipLaunchKernelGGL((layer_norm_bwd_kernel<T, G, VEC, E, TPR>), dim3((uint32_t)grid), dim3(kGroup<TPR, true>), 0,
                      a.stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.part || grid == 1) return e;

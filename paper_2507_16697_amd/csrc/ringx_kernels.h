@@ -451,8 +451,9 @@ struct NormArgs {
   hipStream_t stream = nullptr;
 };
 constexpr int64_t kNormMaxC = 16384;
-// Most workgroups of a launch.
-inline int64_t norm_workgroups(int64_t C, bool bwd) { return bwd ? 512 : 2048; }
+// Most workgroups of a launch.  Backward each writes one row of parts; past 2048 columns, where it has eight waves,
+// half as many take 4096 x 16384 bf16 112 -> 97 us.
+inline int64_t norm_workgroups(int64_t C, bool bwd) { return bwd ? (C > 2048 ? 256 : 512) : 2048; }
 
 // Sums over parts [parts, cols] fp32, in their order; columns below `split` to out[0], the others to
 // out[1] (either may be null), which they overwrite or are added to.

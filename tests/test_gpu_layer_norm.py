@@ -126,7 +126,9 @@ def test_gradient_in_32_bits(shape, pad):
 
 
 @pytest.mark.parametrize("store,rows,C", [("bf16", 5003, 192), ("fp32", 4501, 384), ("bf16", 3001, 2048),
-                                          ("fp32", 1201, 4096), ("bf16", 20011, 40)])
+                                          ("fp32", 1201, 4096), ("bf16", 20011, 40), ("bf16", 1301, 3000),
+                                          ("bf16", 1203, 2051), ("bf16", 1201, 4104), ("bf16", 603, 8200),
+                                          ("fp32", 601, 5001), ("fp32", 401, 9001)])
 def test_many_rows(store, rows, C):
     # more rows than workgroups take at once, the last ones short
     x, w, b, dy, dres = make(rows, (rows, C), store)
