@@ -65,7 +65,7 @@ typedef enum ringx_status RINGX_ENUM_BASE {
   RINGX_E_CHUNKS = 3,      /* R < 1 or R > Nk, or chunk index out of range                   */
   RINGX_E_UNSUPPORTED = 4, /* dtype or head dim not supported (bf16: d in {64,128}; fp32: 1..128) */
   RINGX_E_ALIGN = 5,       /* a tensor pointer is not 16-byte aligned                        */
-  RINGX_E_WORKSPACE = 6,   /* backward workspace missing or smaller than required            */
+  RINGX_E_WORKSPACE = 6,   /* workspace missing or smaller than required                     */
   RINGX_E_HIP = 7,         /* a HIP launch failed                                            */
   RINGX_E_ALIAS = 8,       /* an output overlaps an input                                    */
   RINGX_E_SCRATCH = 9,     /* B*H*Nq above RINGX_NOALLOC_MAX_ROWS (ringx_attn_bwd_noalloc)   */

@@ -242,7 +242,8 @@ __device__ __forceinline__ void product(const GemmArgs& a, const uint32_t id, ch
 #pragma unroll
     for (int j = 0; j < C::kBJ; ++j) acc[i][j] = f32x4{};
 
-  int rest = min((int)a.R - (int)(BK * s0), (int)(BK * s1) - (int)(BK * s0));   // of r, in this part from the step to load on
+  // of r, in this part from the step to load on
+  int rest = min((int)a.R - (int)(BK * s0), (int)(BK * s1) - (int)(BK * s0));
   // A step is four units: 32 of r, half of the wave's i.  Unit T - 1's products, beside them the reads of unit T
   // of the step in `buf` and L of a later step's loads.
   constexpr int kHalf = C::kBI / 2, kProducts = kHalf * C::kBJ;

@@ -81,7 +81,7 @@ const char* ringx_status_str(int status) {
     case RINGX_E_CHUNKS: return "chunk count or index out of range (need 1 <= R <= Nk)";
     case RINGX_E_UNSUPPORTED: return "unsupported dtype or head dim";
     case RINGX_E_ALIGN: return "tensor pointer not 16-byte aligned";
-    case RINGX_E_WORKSPACE: return "backward workspace missing or too small";
+    case RINGX_E_WORKSPACE: return "workspace missing or too small";
     case RINGX_E_HIP: return "HIP launch failed";
     case RINGX_E_ALIAS: return "an output overlaps an input";
     case RINGX_E_SCRATCH:

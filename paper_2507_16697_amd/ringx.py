@@ -1007,8 +1007,8 @@ def ringx_layer_norm_bwd_workspace_bytes(rows, C, dtype) -> int:
 def ringx_layer_norm_bwd(x, dy, stats, weight=None, bias=None, dres=None, dx=None, dweight=None,
                          dbias=None, workspace=None, stream=None):
     """Backward of ringx_layer_norm from dy [..., C] (in x's dtype or fp32) and the forward's stats; dres: the
-    gradient that reaches x by its residual, added to dx.  Returns (dx [..., C] in x's dtype, dweight, dbias fp32 [C], None where
-    there is no weight or bias)."""
+    gradient that reaches x by its residual, added to dx.  Returns (dx [..., C] in x's dtype, dweight, dbias
+    fp32 [C], None where there is no weight or bias)."""
     torch = _T or _torch()
     rows, step = _rows_of("x", x)
     C = x.shape[-1]
@@ -1106,8 +1106,9 @@ def ringx_linear_bwd(x, w, dy, pre=None, act="none", bias=None, need_dx: bool = 
                      need_dw: bool = True, dx=None, dw=None, dbias=None, dx_dtype=None, dw_dtype=None,
                      accumulate_dw=False, workspace=None, stream=None):
     """Backward of ringx_linear from dy [..., O] and, with an activation, the forward's pre.  Returns (dx like x
-    and contiguous, in x's dtype or dx_dtype=torch.float32, dw [O, K] in dw_dtype (fp32 by default, or x's dtype), dbias fp32 [O], None where there is
-    no bias); dx or dw is None where it is not needed.  accumulate_dw: dw and dbias (fp32) are added to."""
+    and contiguous, in x's dtype or dx_dtype=torch.float32, dw [O, K] in dw_dtype (fp32 by default, or x's
+    dtype), dbias fp32 [O], None where there is no bias); dx or dw is None where it is not needed.
+    accumulate_dw: dw and dbias (fp32) are added to."""
     torch = _T or _torch()
     step, heads, tokens, M, K, O, lead = _linear_args(x, w)
     code, a = _dtype_code(x), _act_code(act)

@@ -189,6 +189,46 @@ def test_another_stream():
     assert all(torch.equal(p, q) for p, q in zip(got, back))
 
 
+def test_two_streams_at_once_and_operands_that_are_one():
+    sets = [make(i, (900 + 77 * i, 200), "bf16") for i in range(2)]
+
+    def step(i, **kw):
+        x, w, b, dy, dres = sets[i]
+        y, stats = ringx.ringx_layer_norm(x, w, b, **kw)
+        return (y, stats, *ringx.ringx_layer_norm_bwd(x, dy, stats, w, b, dres=dres, **kw))
+
+    ref = [step(i) for i in range(2)]
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    for side in sides:
+        side.wait_stream(torch.cuda.current_stream())
+    got = [step(i, stream=sides[i]) for _ in range(4) for i in range(2)]
+    for side in sides:
+        torch.cuda.current_stream().wait_stream(side)
+    for k, out in enumerate(got):
+        assert all(torch.equal(p, q) for p, q in zip(ref[k % 2], out))
+    # inputs may be the same tensor
+    x, w, b, _, _ = sets[0]
+    stats = ref[0][1]
+    one = ringx.ringx_layer_norm_bwd(x, x, stats, w, w, dres=x)
+    two = ringx.ringx_layer_norm_bwd(x, x.clone(), stats, w.clone(), b, dres=x.clone())
+    assert all(torch.equal(p, q) for p, q in zip(one, two))
+
+
+def test_offsets_past_32_bits():
+    rows, C = 2 ** 20 + 300, 2056      # 2.16e9 values
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, dres = (torch.randn(rows, C, generator=g, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    w, b = (torch.randn(C, generator=g, device="cuda") for _ in range(2))
+    at = torch.cat([torch.arange(64), torch.arange(rows - 200, rows)]).cuda()
+    y, stats = ringx.ringx_layer_norm(x, w, b)
+    check_forward(x[at], w, b, "bf16", y[at], stats[:, at])
+    # the other rows' gradients are zero, which adds nothing to the weights'
+    dy = torch.zeros_like(x)
+    dy[at] = torch.randn(len(at), C, generator=g, dtype=torch.bfloat16, device="cuda")
+    dx, dw, db = ringx.ringx_layer_norm_bwd(x, dy, stats, w, b, dres=dres)
+    check_backward(x[at], dy[at], stats[:, at], w, dres[at], "bf16", dx[at], dw, db)
+
+
 def test_captured_and_replayed():
     x, w, b, dy, dres = make(7, (700, 192), "bf16")
 

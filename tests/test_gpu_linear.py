@@ -87,6 +87,11 @@ SHAPES = [
     ((1,), 8, 8, 0, 0), ((1,), 64, 16, 0, 0), ((3,), 200, 40, 0, 8), ((16,), 512, 130, 0, 0),
     ((17,), 72, 33, 0, 0), ((2, 16), 1000, 64, 0, 0), ((64,), 136, 200, 0, 16), ((65,), 64, 64, 0, 0),
     ((2, 45), 8, 24, 0, 0), ((129,), 192, 128, 0, 0), ((130,), 200, 136, 0, 24), ((257,), 264, 120, 0, 0),
+    # a few rows: blocks of 16 of them, two blocks of features at a time, ends of both and of K
+    ((20,), 72, 8200, 0, 0), ((40,), 1032, 8210, 0, 0), ((60,), 200, 8192, 0, 8), ((45,), 200, 4100, 0, 0),
+    ((48,), 1096, 40, 0, 0), ((2, 20), 192, 72, 3, 0),
+    # the bias's gradient beside the products, and before them
+    ((700,), 64, 40, 0, 0), ((1024,), 64, 64, 0, 0), ((1025,), 64, 64, 0, 0),
     # widths and rows that fit no 16-byte piece
     ((1,), 1, 1, 0, 0), ((5,), 7, 3, 0, 0), ((77,), 375, 96, 0, 0), ((70,), 33, 129, 0, 5),
     ((131,), 64, 131, 0, 3), ((200,), 129, 65, 0, 0),
@@ -274,6 +279,74 @@ def test_another_stream_and_its_workspace():
     assert all(torch.equal(p, q) for p, q in zip(ref, got))
 
 
+def test_two_streams_at_once_and_operands_that_are_one():
+    sets = [make(i, (500 + 77 * i,), 136, 200, "bf16") for i in range(2)]
+
+    def step(i, **kw):
+        x, w, b, res, dy = sets[i]
+        y, pre = ringx.ringx_linear(x, w, b, act="silu", residual=res, need_pre=True, **kw)
+        return (y, pre, *ringx.ringx_linear_bwd(x, w, dy, pre=pre, act="silu", bias=b, **kw))
+
+    ref = [step(i) for i in range(2)]
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    for side in sides:
+        side.wait_stream(torch.cuda.current_stream())
+    got = [step(i, stream=sides[i]) for _ in range(4) for i in range(2)]
+    for side in sides:
+        torch.cuda.current_stream().wait_stream(side)
+    for k, out in enumerate(got):
+        assert all(torch.equal(p, q) for p, q in zip(ref[k % 2], out))
+    # inputs may be the same tensor
+    t = sets[0][0][:136].contiguous()
+    a, b, c = t.clone(), t.clone(), t.clone()
+    assert torch.equal(ringx.ringx_linear(t, t, residual=t)[0], ringx.ringx_linear(a, b, residual=c)[0])
+    one = ringx.ringx_linear_bwd(t, t, t, pre=t, act="gelu")
+    two = ringx.ringx_linear_bwd(a, b, c, pre=t, act="gelu")
+    assert all(torch.equal(p, q) for p, q in zip(one[:2], two[:2]))
+
+
+def ends(M):
+    return torch.cat([torch.arange(64), torch.arange(M - 200, M)]).cuda()
+
+
+@pytest.mark.parametrize("K,O", [(16, 4104), (4104, 16)])
+def test_offsets_past_32_bits(K, O):
+    M = 2 ** 19 + 300     # times 4104: 2.15e9 values
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rnd = lambda *n: torch.randn(*n, generator=g, dtype=torch.bfloat16, device="cuda")   # noqa: E731
+    x, w, b, res = rnd(M, K), rnd(O, K), rnd(O).float(), rnd(M, O)
+    at = ends(M)
+    y, pre = ringx.ringx_linear(x, w, b, act="gelu", residual=res, need_pre=True)
+    check_forward(x[at], w, b, "gelu", res[at], "bf16", y[at], pre[at])
+    # the other rows' gradients are zero, which adds nothing to any sum
+    dy = torch.zeros_like(y)
+    dy[at] = rnd(len(at), O)
+    dx, dw, db = ringx.ringx_linear_bwd(x, w, dy, pre=pre, act="gelu", bias=b)
+    check_backward(x[at], w, dy[at], pre[at], "gelu", "bf16", dx[at], dw, db)
+
+
+@pytest.mark.parametrize("store,M,step", [("bf16", 1100, 2 ** 21 - 8), ("bf16", 1100, 2 ** 21 + 8),
+                                          ("bf16", 40, 2 ** 26), ("fp32", 1030, 2 ** 21)])
+def test_rows_far_apart(store, M, step):
+    K, O = 64, 72
+    x, w, b, res, dy = make(3, (M,), K, O, store)
+    far = torch.empty(M * step, dtype=x.dtype, device="cuda").as_strided((M, K), (step, 1))
+    far.copy_(x)
+    y, pre = ringx.ringx_linear(far, w, b, act="silu", residual=res, need_pre=True)
+    check_forward(x, w, b, "silu", res, store, y, pre)
+    dx, dw, db = ringx.ringx_linear_bwd(far, w, dy, pre=pre, act="silu", bias=b)
+    check_backward(x, w, dy, pre, "silu", store, dx, dw, db)
+
+
+@pytest.mark.parametrize("M", [2, 70])
+@pytest.mark.parametrize("K,O", [(2 ** 20, 5), (5, 2 ** 20)])
+def test_widest(K, O, M):
+    x, w, b, _, dy = make(4, (M,), K, O, "bf16")
+    y, _ = ringx.ringx_linear(x, w, b)
+    check_forward(x, w, b, "none", None, "bf16", y, None)
+    check_backward(x, w, dy, None, "none", "bf16", *ringx.ringx_linear_bwd(x, w, dy, bias=b))
+
+
 def test_captured_and_replayed():
     shapes = [((7,), 128, 64), ((150,), 250, 96), ((2000,), 64, 64)]
     sets = [make(i, *s, "bf16") for i, s in enumerate(shapes)]
@@ -330,7 +403,8 @@ def test_refusals():
                 lambda: lin(x4[..., :16], w), lambda: bwd(x, w, dy[:4]), lambda: bwd(x, w, dy.float()),
                 lambda: bwd(x, w, dy, act="gelu"), lambda: bwd(x, w, dy, pre=dy), lambda: bwd(x, w, dy, dx=x),
                 lambda: bwd(x, w, dy, dx_dtype=torch.float16),
-                lambda: bwd(x4, w, dy.view(2, 4, 48)), lambda: bwd(x, w, dy, dw_dtype=torch.float16), lambda: bwd(x, w, dy, dw=w),
+                lambda: bwd(x4, w, dy.view(2, 4, 48)), lambda: bwd(x, w, dy, dw_dtype=torch.float16),
+                lambda: bwd(x, w, dy, dw=w),
                 lambda: bwd(x, w, dy, need_dx=False, need_dw=False),
                 lambda: bwd(x, w, dy, dw_dtype=torch.bfloat16, accumulate_dw=True),
                 lambda: bwd(x, w, dy, dbias=torch.zeros(48, device="cuda")),
