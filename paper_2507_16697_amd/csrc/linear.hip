@@ -13,29 +13,29 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 
 // -------------------------------------------------------------------------------------------------
 // A few rows (a token at a time, or some of them), bf16.  Bound by the weights' bytes: every weight is
-// loaded once, straight into the fragments of v_mfma_f32_16x16x32_bf16 (lane l: row l % 16, r = 8 (l / 16)
-// .. + 7), NB blocks of 16 features to a workgroup whose waves take turns at 64 of K.  The rows of x, MB blocks
-// of 16 of them (those past M repeat the last), come from the caches, once for each workgroup.
+// loaded once, for v_mfma_f32_16x16x32_bf16 (lane l: row l % 16, r = 8 (l / 16) .. + 7), NB blocks of 16 features
+// to a workgroup whose waves take turns at 64 of K.  The rows of x, MB blocks of 16 of them (those past M repeat
+// the last), come from the caches, once for each workgroup.
 //
-// VEC: x goes through the wave's own LDS, since a fragment's load touches 16 lines at a time and takes four times
+// VEC: both go through the wave's own LDS, since a fragment's load touches 16 lines at a time and takes four times
 // as long as one of whole 64-byte pieces: lane l loads row l / 4 of a block, piece l % 4, XORed with (row / 4) so
 // that 16 rows' same piece lies in 16 places.
 
 template <int MB, int NB, int WAVES, bool VEC>
 __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(GemmArgs a) {
-  constexpr int kUnroll = VEC ? (MB == 1 ? 8 : MB == 2 ? 4 : 2) : (MB >= 3 ? 1 : 2);   // what registers and LDS hold
-  constexpr int kStage = VEC ? kUnroll * 2 * MB * 1024 : 0, kSums = MB * NB * 1024;   // bytes of a wave
+  constexpr int kBlocks = MB + NB;
+  constexpr int kUnroll = VEC ? (kBlocks == 2 ? 4 : kBlocks <= 4 ? 2 : 1) : (MB >= 3 ? 1 : 2);   // LDS, registers
+  constexpr int kStage = VEC ? kUnroll * 2 * kBlocks * 1024 : 0, kSums = MB * NB * 1024;   // bytes of a wave
   __shared__ __attribute__((aligned(1024))) char lds[WAVES * (kStage > kSums ? kStage : kSums)];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t j0 = (int64_t)blockIdx.x * (16 * NB);
   const int K = (int)a.R;
   const bool heads = a.P.heads != 0;
-  const __bf16* w[NB];
-#pragma unroll
-  for (int f = 0; f < NB; ++f) w[f] = (const __bf16*)a.Q.p + min(j0 + 16 * f + n, a.J - 1) * a.Q.ld;
-  const __bf16* x[MB];
   const int row = VEC ? lane >> 2 : n;
+  const __bf16 *w[NB], *x[MB];
+#pragma unroll
+  for (int f = 0; f < NB; ++f) w[f] = (const __bf16*)a.Q.p + min(j0 + 16 * f + row, a.J - 1) * a.Q.ld;
 #pragma unroll
   for (int m = 0; m < MB; ++m) {
     const int64_t i = min((int64_t)(16 * m + row), a.I - 1);
@@ -51,16 +51,13 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(GemmArgs a) {
     const uint32_t h = (uint32_t)k / (uint32_t)a.P.d;
     return (int64_t)h * a.P.tokens * a.P.d + (k - (int)h * (int)a.P.d);
   };
-  const auto values = [&](const __bf16* p, int k, auto at) {   // 8 from column k on, zeros past K
+  const auto straight = [](int k) { return (int64_t)k; };
+  const auto values = [&](const __bf16* p, int k, auto at) {   // one by one, zeros past K
     bf16x8 v = {};
-    if constexpr (VEC) {
-      if (k < K) v = *reinterpret_cast<const bf16x8*>(p + at(k));
-    } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const __bf16 y = p[at(min(k + e, K - 1))];
-        v[e] = k + e < K ? y : (__bf16)0.f;
-      }
+    for (int e = 0; e < 8; ++e) {
+      const __bf16 y = p[at(min(k + e, K - 1))];
+      v[e] = k + e < K ? y : (__bf16)0.f;
     }
     return v;
   };
@@ -71,50 +68,47 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(GemmArgs a) {
       (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * kStage);
   const int piece = (lane & 3) ^ (lane >> 4), read = wave * kStage + n * 64 + ((g ^ (n >> 2)) << 4);
   for (int k0 = wave * 64; k0 < K; k0 += WAVES * 64 * kUnroll) {
-    bf16x8 wv[kUnroll][2][NB], xv[kUnroll][2][MB];
     if constexpr (VEC) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what lies there has been read
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
+      for (int u = 0; u < 2 * kUnroll; ++u) {
+        const int k = min(k0 + u / 2 * WAVES * 64 + u % 2 * 32 + 8 * piece, K - 8);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int f = 0; f < NB; ++f) load_lds16(w[f] + k, base + (u * kBlocks + f) * 1024);
+      }
 #pragma unroll
-          for (int m = 0; m < MB; ++m)
-            load_lds16(x[m] + place(min(k0 + u * WAVES * 64 + 32 * h + 8 * piece, K - 8)),
-                       base + ((u * 2 + h) * MB + m) * 1024);
+      for (int u = 0; u < 2 * kUnroll; ++u) {
+        const int64_t k = place(min(k0 + u / 2 * WAVES * 64 + u % 2 * 32 + 8 * piece, K - 8));
+#pragma unroll
+        for (int m = 0; m < MB; ++m) load_lds16(x[m] + k, base + (u * kBlocks + NB + m) * 1024);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
+    for (int u = 0; u < 2 * kUnroll; ++u) {
+      const int k = k0 + u / 2 * WAVES * 64 + u % 2 * 32 + 8 * g;
+      bf16x8 wv[NB], xv[MB];
+      if constexpr (VEC) {
+        const auto get = [&](int i) {
+          const bf16x8 v = *reinterpret_cast<const bf16x8*>(lds + read + (u * kBlocks + i) * 1024);
+          return k < K ? v : bf16x8{};
+        };
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+        for (int f = 0; f < NB; ++f) wv[f] = get(f);
+#pragma unroll
+        for (int m = 0; m < MB; ++m) xv[m] = get(NB + m);
+      } else {
+#pragma unroll
+        for (int f = 0; f < NB; ++f) wv[f] = values(w[f], k, straight);
+#pragma unroll
+        for (int m = 0; m < MB; ++m) xv[m] = values(x[m], k, place);
+      }
+#pragma unroll
+      for (int m = 0; m < MB; ++m)
 #pragma unroll
         for (int f = 0; f < NB; ++f)
-          wv[u][h][f] = values(w[f], k0 + u * WAVES * 64 + 32 * h + 8 * g, [](int k) { return (int64_t)k; });
-    if constexpr (VEC) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int m = 0; m < MB; ++m) {
-          const int k = k0 + u * WAVES * 64 + 32 * h + 8 * g;
-          if constexpr (VEC) {
-            const bf16x8 v = *reinterpret_cast<const bf16x8*>(lds + read + ((u * 2 + h) * MB + m) * 1024);
-            xv[u][h][m] = k < K ? v : bf16x8{};
-          } else {
-            xv[u][h][m] = values(x[m], k, place);
-          }
-        }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int m = 0; m < MB; ++m)
-#pragma unroll
-          for (int f = 0; f < NB; ++f)
-            acc[NB * m + f] =
-                __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[u][h][f], xv[u][h][m], acc[NB * m + f], 0, 0, 0);
+          acc[NB * m + f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[f], xv[m], acc[NB * m + f], 0, 0, 0);
+    }
   }
   f32x4* const sums = reinterpret_cast<f32x4*>(lds) + lane;   // [wave][block][lane]
   __syncthreads();
