@@ -14,18 +14,20 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 // -------------------------------------------------------------------------------------------------
 // A few rows (a token at a time, or some of them), bf16.  Bound by the weights' bytes: every weight is
 // loaded once, for v_mfma_f32_16x16x32_bf16 (lane l: row l % 16, r = 8 (l / 16) .. + 7), NB blocks of 16 features
-// to a workgroup whose waves take turns at 64 of K.  The rows of x, MB blocks of 16 of them (those past M repeat
+// to a workgroup whose waves take turns along K.  The rows of x, MB blocks of 16 of them (those past M repeat
 // the last), come from the caches, once for each workgroup.
 //
 // VEC: both go through the wave's own LDS, since a fragment's load touches 16 lines at a time and takes four times
 // as long as one of whole 64-byte pieces: lane l loads row l / 4 of a block, piece l % 4, XORed with (row / 4) so
-// that 16 rows' same piece lies in 16 places.
+// that 16 rows' same piece lies in 16 places.  Two buffers: the next turn's loads are in flight while a turn is
+// multiplied.
 
 template <int MB, int NB, int WAVES, bool VEC>
 __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(GemmArgs a) {
   constexpr int kBlocks = MB + NB;
-  constexpr int kUnroll = VEC ? (kBlocks == 2 ? 4 : kBlocks <= 4 ? 2 : 1) : (MB >= 3 ? 1 : 2);   // LDS, registers
-  constexpr int kStage = VEC ? kUnroll * 2 * kBlocks * 1024 : 0, kSums = MB * NB * 1024;   // bytes of a wave
+  // steps of 32 of K in a turn: what LDS (VEC) or the registers hold
+  constexpr int kSteps = VEC ? (kBlocks == 2 ? 4 : kBlocks <= 4 ? 2 : 1) : (MB >= 3 ? 2 : 4);
+  constexpr int kTurn = kSteps * kBlocks * 1024, kStage = VEC ? 2 * kTurn : 0, kSums = MB * NB * 1024;   // of a wave
   __shared__ __attribute__((aligned(1024))) char lds[WAVES * (kStage > kSums ? kStage : kSums)];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -67,30 +69,36 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(GemmArgs a) {
   const uint32_t base = __builtin_amdgcn_readfirstlane(
       (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * kStage);
   const int piece = (lane & 3) ^ (lane >> 4), read = wave * kStage + n * 64 + ((g ^ (n >> 2)) << 4);
-  for (int k0 = wave * 64; k0 < K; k0 += WAVES * 64 * kUnroll) {
+  const auto load = [&](int k0, uint32_t to) {   // what lies past K repeats what does not
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+      const int k = min(k0 + 32 * u + 8 * piece, K - 8);
+#pragma unroll
+      for (int f = 0; f < NB; ++f) load_lds16(w[f] + k, to + (u * kBlocks + f) * 1024);
+#pragma unroll
+      for (int m = 0; m < MB; ++m) load_lds16(x[m] + place(k), to + (u * kBlocks + NB + m) * 1024);
+    }
+  };
+  constexpr int kTurns = WAVES * 32 * kSteps;   // of K, from a wave's turn to its next
+  int at = 0;                                   // the turn's buffer
+  if constexpr (VEC) load(wave * 32 * kSteps, base);
+  for (int k0 = wave * 32 * kSteps; k0 < K; k0 += kTurns) {
     if constexpr (VEC) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what lies there has been read
-#pragma unroll
-      for (int u = 0; u < 2 * kUnroll; ++u) {
-        const int k = min(k0 + u / 2 * WAVES * 64 + u % 2 * 32 + 8 * piece, K - 8);
-#pragma unroll
-        for (int f = 0; f < NB; ++f) load_lds16(w[f] + k, base + (u * kBlocks + f) * 1024);
+      if (k0 + kTurns < K) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what lies there has been read
+        load(k0 + kTurns, base + kTurn - at);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kSteps * kBlocks) : "memory");
+      } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       }
-#pragma unroll
-      for (int u = 0; u < 2 * kUnroll; ++u) {
-        const int64_t k = place(min(k0 + u / 2 * WAVES * 64 + u % 2 * 32 + 8 * piece, K - 8));
-#pragma unroll
-        for (int m = 0; m < MB; ++m) load_lds16(x[m] + k, base + (u * kBlocks + NB + m) * 1024);
-      }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
 #pragma unroll
-    for (int u = 0; u < 2 * kUnroll; ++u) {
-      const int k = k0 + u / 2 * WAVES * 64 + u % 2 * 32 + 8 * g;
+    for (int u = 0; u < kSteps; ++u) {
+      const int k = k0 + 32 * u + 8 * g;
       bf16x8 wv[NB], xv[MB];
       if constexpr (VEC) {
         const auto get = [&](int i) {
-          const bf16x8 v = *reinterpret_cast<const bf16x8*>(lds + read + (u * kBlocks + i) * 1024);
+          const bf16x8 v = *reinterpret_cast<const bf16x8*>(lds + at + read + (u * kBlocks + i) * 1024);
           return k < K ? v : bf16x8{};
         };
 #pragma unroll
@@ -109,6 +117,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(GemmArgs a) {
         for (int f = 0; f < NB; ++f)
           acc[NB * m + f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[f], xv[m], acc[NB * m + f], 0, 0, 0);
     }
+    at = kTurn - at;
   }
   f32x4* const sums = reinterpret_cast<f32x4*>(lds) + lane;   // [wave][block][lane]
   __syncthreads();

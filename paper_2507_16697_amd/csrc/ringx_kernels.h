@@ -680,8 +680,8 @@ struct LinearPlan {
 constexpr int64_t kLinearMaxWidth = int64_t(1) << 20;   // of K and O
 constexpr int64_t kLinearMaxRows = (int64_t(1) << 31) - 1024;   // 32-bit positions, a step of headroom
 // bf16 rows up to which the kernel for a few of them is taken.  us of it and of the tiles, K 2048 to O 2048: one row
-// 6.0 / 14.8, 64 7.7 / 14.9; 4096 to 4096: 8.4 / 18.8, 15.7 / 18.9; 4096 to 16384: 25.8 / 31.5, 37.4 / 32.7;
-// 8192 to 2048: 12.6 / 19.5, 23.5 / 19.7.
+// 4.7 / 14.8, 64 6.8 / 14.9; 4096 to 4096: 6.7 / 18.8, 13.7 / 18.9; 4096 to 16384: 23.3 / 31.5, 35.0 / 32.7;
+// 8192 to 2048: 8.7 / 19.5, 21.0 / 19.7.
 constexpr int64_t kFewRows = 64;
 // Offsets of an operand's tile are 31 bits: rows of at most 2^21 values, heads whose batch has at most 2^29.
 inline bool linear_near(const LinearShape& s) {
