@@ -143,7 +143,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(GemmArgs a) {
 template <int MB, int NB, bool VEC>
 hipError_t launch_few_rows_as(const GemmArgs& a) {
   const dim3 grid((uint32_t)((a.J + 16 * NB - 1) / (16 * NB)));
-  // 4 waves; 8 where there are few workgroups and much of K
+  // 4 waves; 8 where there are few workgroups and much of K (us of 8 / 4: one row of 8192 to 2048 8.7 / 10.6, of 2048
+  // to 8192 7.8 / 6.5; 64 rows of 2048 to 2048 6.8 / 9.2)
   if (grid.x <= 256 && a.R >= 1024)
     hipLaunchKernelGGL((few_rows_kernel<MB, NB, 8, VEC>), grid, dim3(512), 0, a.stream, a);
   else
@@ -155,8 +156,9 @@ template <bool VEC>
 hipError_t launch_few_rows(const GemmArgs& a) {
   if (a.I <= 16) return launch_few_rows_as<1, 1, VEC>(a);
   if constexpr (VEC) {
-    // two blocks of features where that leaves a workgroup to every compute unit
-    if (a.J >= 8192) {
+    // two blocks of features where one to each compute unit does not do (64 rows, us of two / one: 2048 to 6144
+    // 9.4 / 11.5, to 8192 10.2 / 12.8, to 4096 9.2 / 8.2)
+    if (a.J > 4096) {
       if (a.I <= 32) return launch_few_rows_as<2, 2, VEC>(a);
       if (a.I <= 48) return launch_few_rows_as<3, 2, VEC>(a);
       return launch_few_rows_as<4, 2, VEC>(a);

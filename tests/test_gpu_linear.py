@@ -88,7 +88,7 @@ SHAPES = [
     ((17,), 72, 33, 0, 0), ((2, 16), 1000, 64, 0, 0), ((64,), 136, 200, 0, 16), ((65,), 64, 64, 0, 0),
     ((2, 45), 8, 24, 0, 0), ((129,), 192, 128, 0, 0), ((130,), 200, 136, 0, 24), ((257,), 264, 120, 0, 0),
     # a few rows: blocks of 16 of them, two blocks of features at a time, ends of both and of K
-    ((20,), 72, 8200, 0, 0), ((40,), 1032, 8210, 0, 0), ((60,), 200, 8192, 0, 8), ((45,), 200, 4100, 0, 0),
+    ((20,), 72, 8200, 0, 0), ((40,), 1032, 8210, 0, 0), ((60,), 200, 8192, 0, 8), ((45,), 200, 4100, 0, 0), ((33,), 72, 4096, 0, 0),
     ((48,), 1096, 40, 0, 0), ((2, 20), 192, 72, 3, 0),
     # the bias's gradient beside the products, and before them
     ((700,), 64, 40, 0, 0), ((1024,), 64, 64, 0, 0), ((1025,), 64, 64, 0, 0),
