@@ -19,13 +19,15 @@
 namespace ringx {
 namespace {
 
-// The E values of a row that one thread holds: 16-byte pieces (VEC), piece v at columns (v TPR + t) V, or
-// one by one, value e at column e TPR + t.  Columns past C are zero.
-template <class T, bool VEC, int E, int TPR>
+// The E values of a row that one thread holds: pieces of V values (16 bytes; 4 of bf16; one), piece v at columns
+// (v TPR + t) V.  Columns past C are zero.  (bf16 in pieces of 4 bytes against one by one: 32768 x 2046 backward 85
+// us, 109; 8192 x 5002 forward 42, 67.)
+template <class T, int V_, int E, int TPR>
 struct Row {
-  static constexpr int V = VEC ? 16 / (int)sizeof(T) : 1;
+  static constexpr int V = V_;
+  static_assert(V == 1 || V * sizeof(T) == 16 || V * sizeof(T) == 4, "pieces");
   static constexpr int NV = E / V;
-  static constexpr int kWords = VEC ? E * (int)sizeof(T) / 4 : E;
+  static constexpr int kPiece = V * (int)sizeof(T) / 4, kWords = V > 1 ? NV * kPiece : E;   // words
   uint32_t w[kWords];
 
   static __device__ __forceinline__ int col(int e, int t) { return (e / V * TPR + t) * V + e % V; }
@@ -34,11 +36,14 @@ struct Row {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = col(v * V, t);
-      if constexpr (VEC) {
+      if constexpr (kPiece == 4) {
         u32x4 x = {};
         if (c < C) x = *reinterpret_cast<const u32x4*>(p + c);
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[4 * v + j] = x[j];
+      } else if constexpr (V > 1) {
+        w[v] = 0u;
+        if (c < C) w[v] = *reinterpret_cast<const uint32_t*>(p + c);
       } else {
         w[v] = 0u;
         if (c < C) w[v] = raw_bits(p + c);
@@ -46,14 +51,14 @@ struct Row {
     }
   }
   __device__ __forceinline__ float get(int e) const {
-    if constexpr (!VEC || std::is_same_v<T, float>) return from_raw<T>(w[e]);
+    if constexpr (V == 1 || std::is_same_v<T, float>) return from_raw<T>(w[e]);
     else return e % 2 ? bf16_hi(w[e / 2]) : bf16_lo(w[e / 2]);
   }
-  // Values loaded one by one, each under its condition, have arrived: nothing that uses them joins their
+  // Small pieces, each loaded under its condition, have arrived: nothing that uses them joins their
   // conditional blocks, where it would wait for every load alone (bf16, 4000 rows of 2047, backward: 121 -> 31 us;
   // fp32's use joins none).
   __device__ __forceinline__ void arrived() {
-    if constexpr (!VEC && std::is_same_v<T, __bf16>) {
+    if constexpr (kPiece < 4 && std::is_same_v<T, __bf16>) {
 #pragma unroll
       for (int i = 0; i < kWords; ++i) asm volatile("" : "+v"(w[i]));
     }
@@ -63,7 +68,7 @@ struct Row {
     for (int v = 0; v < NV; ++v) {
       const int c = col(v * V, t);
       if (c >= C) continue;
-      if constexpr (VEC) {
+      if constexpr (kPiece == 4) {
         u32x4 y;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -71,6 +76,8 @@ struct Row {
           else y[j] = pack_bf16x2(x[v * V + 2 * j], x[v * V + 2 * j + 1]);
         }
         *reinterpret_cast<u32x4*>(p + c) = y;
+      } else if constexpr (V > 1) {
+        *reinterpret_cast<uint32_t*>(p + c) = pack_bf16x2(x[v * V], x[v * V + 1]);
       } else {
         p[c] = (T)x[v];
       }
@@ -78,72 +85,55 @@ struct Row {
   }
 };
 
+// fp32 values of the thread's columns, min(V, 4) at a time
+template <class R>
+constexpr int kAtOnce = R::V < 4 ? R::V : 4;
+template <class R, int E>
+__device__ __forceinline__ void load_floats(const float* p, float otherwise, int t, int C, float (&x)[E]) {
+  constexpr int N = kAtOnce<R>;
+  typedef __attribute__((ext_vector_type(N))) float Piece;
+#pragma unroll
+  for (int e = 0; e < E; e += N) {
+    const int c = R::col(e, t);
+    Piece y = otherwise;
+    if (p && c < C) y = *reinterpret_cast<const Piece*>(p + c);
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[e + j] = y[j];
+  }
+}
+template <class R, int E>
+__device__ __forceinline__ void store_floats(float* p, int t, int C, const float (&x)[E]) {
+  constexpr int N = kAtOnce<R>;
+  typedef __attribute__((ext_vector_type(N))) float Piece;
+  if (!p) return;
+#pragma unroll
+  for (int e = 0; e < E; e += N) {
+    const int c = R::col(e, t);
+    if (c >= C) continue;
+    Piece y;
+#pragma unroll
+    for (int j = 0; j < N; ++j) y[j] = x[e + j];
+    *reinterpret_cast<Piece*>(p + c) = y;
+  }
+}
+
 // The same columns of a row of G, fp32 beside a bf16 x.
-template <class T, class G, bool VEC, int E, int TPR>
-struct GradRow : Row<T, VEC, E, TPR> {};
-template <bool VEC, int E, int TPR>
-struct GradRow<__bf16, float, VEC, E, TPR> {
-  using R = Row<__bf16, VEC, E, TPR>;
+template <class T, class G, int V, int E, int TPR>
+struct GradRow : Row<T, V, E, TPR> {};
+template <int V, int E, int TPR>
+struct GradRow<__bf16, float, V, E, TPR> {
   float w[E];
   __device__ __forceinline__ void load(const float* p, int t, int C) {
-#pragma unroll
-    for (int e = 0; e < E; e += VEC ? 4 : 1) {
-      const int c = R::col(e, t);
-      if constexpr (VEC) {
-        f32x4 x = {};
-        if (c < C) x = *reinterpret_cast<const f32x4*>(p + c);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[e + j] = x[j];
-      } else {
-        w[e] = 0.f;
-        if (c < C) w[e] = p[c];
-      }
-    }
+    load_floats<Row<__bf16, V, E, TPR>>(p, 0.f, t, C, w);
   }
   __device__ __forceinline__ float get(int e) const { return w[e]; }
   __device__ __forceinline__ void arrived() {
-    if constexpr (!VEC) {
+    if constexpr (V < 8) {
 #pragma unroll
       for (int e = 0; e < E; ++e) asm volatile("" : "+v"(w[e]));
     }
   }
 };
-
-// fp32 weights of the thread's columns, `otherwise` where there are none
-template <class T, bool VEC, int E, int TPR>
-__device__ __forceinline__ void load_vector(const float* p, float otherwise, int t, int C,
-                                            float (&x)[E]) {
-  using R = Row<T, VEC, E, TPR>;
-#pragma unroll
-  for (int e = 0; e < E; e += 4) {
-    if constexpr (VEC) {
-      f32x4 y = {otherwise, otherwise, otherwise, otherwise};
-      if (p && R::col(e, t) < C) y = *reinterpret_cast<const f32x4*>(p + R::col(e, t));
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[e + j] = y[j];
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int c = R::col(e + j, t);
-        x[e + j] = otherwise;
-        if (p && c < C) x[e + j] = p[c];
-      }
-    }
-  }
-}
-
-template <class T, bool VEC, int E, int TPR>
-__device__ __forceinline__ void store_vector(float* p, int t, int C, const float (&x)[E]) {
-  using R = Row<T, VEC, E, TPR>;
-  if (!p) return;
-#pragma unroll
-  for (int e = 0; e < E; e += VEC ? 4 : 1) {
-    const int c = R::col(e, t);
-    if (c >= C) continue;
-    if constexpr (VEC) *reinterpret_cast<f32x4*>(p + c) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
-    else p[c] = x[e];
-  }
-}
 
 template <int CTRL>
 __device__ __forceinline__ float add_lane(float x) {
@@ -192,9 +182,9 @@ struct RowSum {
   }
 };
 
-template <class T, bool VEC, int E, int TPR>
+template <class T, int V, int E, int TPR>
 __global__ __launch_bounds__((kGroup<TPR, false>)) void layer_norm_kernel(NormArgs a) {
-  using R = Row<T, VEC, E, TPR>;
+  using R = Row<T, V, E, TPR>;
   __shared__ RowSum<TPR, false> sum;
   const int t = threadIdx.x % TPR;
   const int C = a.C;
@@ -207,8 +197,8 @@ __global__ __launch_bounds__((kGroup<TPR, false>)) void layer_norm_kernel(NormAr
   // rows past the end (of the last round) repeat the last one and are not stored
   cur.load(x + min(row, a.rows - 1) * a.stride, t, C);
   float w[E], b[E];
-  load_vector<T, VEC, E, TPR>(a.weight, 1.f, t, C, w);
-  load_vector<T, VEC, E, TPR>(a.bias, 0.f, t, C, b);
+  load_floats<R>(a.weight, 1.f, t, C, w);
+  load_floats<R>(a.bias, 0.f, t, C, b);
   int slot = 0;
   for (int64_t r0 = (int64_t)blockIdx.x * kRowsAtOnce<TPR, false>; r0 < a.rows; r0 += step, row += step) {
     R next;
@@ -239,9 +229,9 @@ __global__ __launch_bounds__((kGroup<TPR, false>)) void layer_norm_kernel(NormAr
   }
 }
 
-template <class T, class G, bool VEC, int E, int TPR>
+template <class T, class G, int V, int E, int TPR>
 __global__ __launch_bounds__((kGroup<TPR, true>), TPR <= 256 ? 2 : 1) void layer_norm_bwd_kernel(NormArgs a) {
-  using R = Row<T, VEC, E, TPR>;
+  using R = Row<T, V, E, TPR>;
   __shared__ RowSum<TPR, true> sum;
   constexpr int kPitch = TPR + 1;   // of a thread's e-th values in LDS: neither way meets itself in a bank
   __shared__ float lds[kRowsAtOnce<TPR, true> > 1 ? 2 * E * kPitch : 1];
@@ -253,7 +243,7 @@ __global__ __launch_bounds__((kGroup<TPR, true>), TPR <= 256 ? 2 : 1) void layer
   const G* const dy = (const G*)a.dy;
   T* const dx = (T*)a.dx;
   float w[E], dw[E], db[E];
-  load_vector<T, VEC, E, TPR>(a.weight, 1.f, t, C, w);
+  load_floats<R>(a.weight, 1.f, t, C, w);
 #pragma unroll
   for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.f;
   int slot = 0;
@@ -262,7 +252,7 @@ __global__ __launch_bounds__((kGroup<TPR, true>), TPR <= 256 ? 2 : 1) void layer
     const bool live = at < a.rows;
     const int64_t row = live ? at : a.rows - 1;   // rows past the end repeat the last one
     R rx, rr;
-    GradRow<T, G, VEC, E, TPR> rg;
+    GradRow<T, G, V, E, TPR> rg;
     rx.load(x + row * a.stride, t, C);
     rg.load(dy + row * C, t, C);
     if (dres) rr.load(dres + row * C, t, C);
@@ -298,8 +288,8 @@ __global__ __launch_bounds__((kGroup<TPR, true>), TPR <= 256 ? 2 : 1) void layer
   float* const pw = alone ? a.dweight : part;
   float* const pb = alone ? a.dbias : part + C;
   if constexpr (kRowsAtOnce<TPR, true> == 1) {
-    store_vector<T, VEC, E, TPR>(pw, t, C, dw);
-    store_vector<T, VEC, E, TPR>(pb, t, C, db);
+    store_floats<R>(pw, t, C, dw);
+    store_floats<R>(pb, t, C, db);
   } else {
     // over the rows of a wave, then row after row (of waves)
     constexpr int kHeld = TPR < 64 ? 64 : TPR;
@@ -330,7 +320,7 @@ __global__ __launch_bounds__((kGroup<TPR, true>), TPR <= 256 ? 2 : 1) void layer
   }
 }
 
-template <class T, class G, bool VEC, int E, int TPR>
+template <class T, class G, int V, int E, int TPR>
 hipError_t launch_as(const NormArgs& a, bool bwd) {
   const int64_t at_once = bwd ? kRowsAtOnce<TPR, true> : kRowsAtOnce<TPR, false>;
   const int64_t groups = (a.rows + at_once - 1) / at_once;
@@ -338,11 +328,11 @@ hipError_t launch_as(const NormArgs& a, bool bwd) {
   // Few rows: one workgroup, four rounds at most (5 us), and no second launch (4 us, and as much of the host).
   if (bwd && a.part && groups <= 4) grid = 1;
   if (!bwd) {
-    hipLaunchKernelGGL((layer_norm_kernel<T, VEC, E, TPR>), dim3((uint32_t)grid), dim3(kGroup<TPR, false>), 0,
+    hipLaunchKernelGGL((layer_norm_kernel<T, V, E, TPR>), dim3((uint32_t)grid), dim3(kGroup<TPR, false>), 0,
                        a.stream, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((layer_norm_bwd_kernel<T, G, VEC, E, TPR>), dim3((uint32_t)grid), dim3(kGroup<TPR, true>), 0,
+  hipLaunchKernelGGL((layer_norm_bwd_kernel<T, G, V, E, TPR>), dim3((uint32_t)grid), dim3(kGroup<TPR, true>), 0,
                      a.stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.part || grid == 1) return e;
@@ -352,32 +342,33 @@ hipError_t launch_as(const NormArgs& a, bool bwd) {
   return launch_column_sums(s);
 }
 
-template <class T, bool VEC, int E, int TPR>
+template <class T, int V, int E, int TPR>
 hipError_t launch(const NormArgs& a, bool bwd) {
-  return bwd && a.dy_f32 ? launch_as<T, float, VEC, E, TPR>(a, bwd) : launch_as<T, T, VEC, E, TPR>(a, bwd);
+  return bwd && a.dy_f32 ? launch_as<T, float, V, E, TPR>(a, bwd) : launch_as<T, T, V, E, TPR>(a, bwd);
 }
 
-template <class T, bool VEC>
+template <class T, int V>
 hipError_t by_width(const NormArgs& a, bool bwd) {
-  if (a.C <= 64) return launch<T, VEC, 8, 8>(a, bwd);
-  if (a.C <= 128) return launch<T, VEC, 8, 16>(a, bwd);
-  if (a.C <= 256) return launch<T, VEC, 8, 32>(a, bwd);
-  if (a.C <= 512) return launch<T, VEC, 8, 64>(a, bwd);
-  if (a.C <= 1024) return launch<T, VEC, 16, 64>(a, bwd);
-  // 32 values to a thread only in bf16 pieces: the others' backward would not keep them in registers (with 16,
+  if (a.C <= 64) return launch<T, V, 8, 8>(a, bwd);
+  if (a.C <= 128) return launch<T, V, 8, 16>(a, bwd);
+  if (a.C <= 256) return launch<T, V, 8, 32>(a, bwd);
+  if (a.C <= 512) return launch<T, V, 8, 64>(a, bwd);
+  if (a.C <= 1024) return launch<T, V, 16, 64>(a, bwd);
+  // 32 values to a thread only in 16-byte pieces of bf16: the others' backward would not keep them in registers (with 16,
   // only the widest rows' does not, of 1024 threads)
-  constexpr int E = VEC && std::is_same_v<T, __bf16> ? 32 : 16;
-  if (a.C <= 2048) return launch<T, VEC, E, 2048 / E>(a, bwd);
-  if (a.C <= 4096) return launch<T, VEC, E, 4096 / E>(a, bwd);
-  if (a.C <= 8192) return launch<T, VEC, E, 8192 / E>(a, bwd);
-  return launch<T, VEC, E, 16384 / E>(a, bwd);
+  constexpr int E = V == 8 ? 32 : 16;
+  if (a.C <= 2048) return launch<T, V, E, 2048 / E>(a, bwd);
+  if (a.C <= 4096) return launch<T, V, E, 4096 / E>(a, bwd);
+  if (a.C <= 8192) return launch<T, V, E, 8192 / E>(a, bwd);
+  return launch<T, V, E, 16384 / E>(a, bwd);
 }
 
 }  // namespace
 
 hipError_t launch_layer_norm(const NormArgs& a, bool bwd) {
-  if (a.bf16) return a.vec ? by_width<__bf16, true>(a, bwd) : by_width<__bf16, false>(a, bwd);
-  return a.vec ? by_width<float, true>(a, bwd) : by_width<float, false>(a, bwd);
+  if (!a.bf16) return a.piece == 4 ? by_width<float, 4>(a, bwd) : by_width<float, 1>(a, bwd);
+  if (a.piece == 8) return by_width<__bf16, 8>(a, bwd);
+  return a.piece == 2 ? by_width<__bf16, 2>(a, bwd) : by_width<__bf16, 1>(a, bwd);
 }
 
 }  // namespace ringx

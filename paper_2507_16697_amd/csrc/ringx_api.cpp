@@ -1191,8 +1191,9 @@ ringx::NormArgs norm_args(const void* x, int64_t row_stride, int64_t rows, int64
   a.x = x, a.rows = rows, a.C = static_cast<int>(C), a.weight = weight;
   a.stride = rows > 1 ? row_stride : C;
   a.bf16 = dtype == RINGX_BF16;
-  const int64_t piece = 16 / esize(dtype);
-  a.vec = C % piece == 0 && a.stride % piece == 0;
+  const int whole = static_cast<int>(16 / esize(dtype));
+  const auto fits = [&](int piece) { return C % piece == 0 && a.stride % piece == 0; };
+  a.piece = fits(whole) ? whole : a.bf16 && fits(2) ? 2 : 1;
   a.stream = stream;
   return a;
 }

@@ -446,7 +446,8 @@ struct NormArgs {
   float* part = nullptr;                       // backward: the workgroups' parts [.., 2, C], or null
   int C = 0;
   float eps = 0.f;
-  bool bf16 = false, vec = true;               // vec: rows in 16-byte pieces
+  bool bf16 = false;
+  int piece = 1;                               // values of a piece that rows come in: 16 bytes, 4 of bf16, or one
   bool dy_f32 = false;                         // dy in fp32 whatever x is
   hipStream_t stream = nullptr;
 };

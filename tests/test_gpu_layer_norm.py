@@ -82,6 +82,9 @@ SHAPES = [
     ((2, 19, 520), 0), ((21, 960), 0), ((19, 1024), 0), ((18, 1032), 0), ((2, 3, 5, 2048), 0),
     ((11, 2047), 1), ((9, 2056), 0), ((7, 4096), 8), ((6, 4099), 0), ((5, 8192), 0), ((4, 8200), 0),
     ((3, 16384), 0), ((3, 16383), 2),
+    # rows in pairs of values, and even ones whose stride is odd
+    ((7, 2), 0), ((33, 66), 0), ((35, 300), 36), ((40, 258), 0), ((21, 962), 4), ((11, 2046), 2), ((6, 4098), 0),
+    ((5, 8190), 0), ((3, 16382), 0), ((9, 66), 3),
 ]
 
 
@@ -112,7 +115,7 @@ def test_without_some(store, weight, bias, res):
 
 @pytest.mark.parametrize("shape,pad", [((1, 8), 0), ((33, 65), 0), ((65, 136), 0), ((41, 375), 3), ((2, 19, 520), 0),
                                        ((18, 1032), 8), ((9, 2056), 0), ((6, 4099), 0), ((4, 8200), 0),
-                                       ((3, 16383), 0)])
+                                       ((3, 16383), 0), ((35, 302), 0), ((18, 1034), 6), ((4, 8198), 0)])
 def test_gradient_in_32_bits(shape, pad):
     x, w, b, dy, dres = make(sum(shape) + 1, shape, "bf16", pad)
     dy = torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
@@ -128,7 +131,8 @@ def test_gradient_in_32_bits(shape, pad):
 @pytest.mark.parametrize("store,rows,C", [("bf16", 5003, 192), ("fp32", 4501, 384), ("bf16", 3001, 2048),
                                           ("fp32", 1201, 4096), ("bf16", 20011, 40), ("bf16", 1301, 3000),
                                           ("bf16", 1203, 2051), ("bf16", 1201, 4104), ("bf16", 603, 8200),
-                                          ("fp32", 601, 5001), ("fp32", 401, 9001)])
+                                          ("fp32", 601, 5001), ("fp32", 401, 9001), ("bf16", 5003, 300),
+                                          ("bf16", 1203, 2050)])
 def test_many_rows(store, rows, C):
     # more rows than workgroups take at once, the last ones short
     x, w, b, dy, dres = make(rows, (rows, C), store)
