@@ -158,6 +158,8 @@ def test_activations_at_their_ends(act):
     (1500, 1501, 700, 0),      # and of both gradients in one launch
     (2100, 1601, 1400, 0),     # and of each by itself
     (8190, 1101, 8200, 0),     # tiles of 128, ragged
+    (4000, 601, 302, 0),       # tiles of 64 and of 32 in one backward
+    (9000, 1001, 130, 0),      # of 128 and of 32
 ])
 def test_large(M, K, O, heads, store):
     lead = (2, M // 2) if heads else (M,)
