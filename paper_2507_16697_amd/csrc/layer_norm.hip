@@ -344,7 +344,8 @@ hipError_t launch_as(const NormArgs& a, bool bwd) {
 
 template <class T, int V, int E, int TPR>
 hipError_t launch(const NormArgs& a, bool bwd) {
-  return bwd && a.dy_f32 ? launch_as<T, float, V, E, TPR>(a, bwd) : launch_as<T, T, V, E, TPR>(a, bwd);
+  if (bwd && a.dy_f32) return launch_as<T, float, V, E, TPR>(a, bwd);
+  return launch_as<T, T, V, E, TPR>(a, bwd);
 }
 
 template <class T, int V>
@@ -354,13 +355,14 @@ hipError_t by_width(const NormArgs& a, bool bwd) {
   if (a.C <= 256) return launch<T, V, 8, 32>(a, bwd);
   if (a.C <= 512) return launch<T, V, 8, 64>(a, bwd);
   if (a.C <= 1024) return launch<T, V, 16, 64>(a, bwd);
-  // 32 values to a thread only in 16-byte pieces of bf16: the others' backward would not keep them in registers (with 16,
-  // only the widest rows' does not, of 1024 threads)
-  constexpr int E = V == 8 ? 32 : 16;
+  // 32 values to a thread in 16-byte pieces of bf16, and past 8192 columns also in pairs (4096 x 12002 backward 82 us,
+  // with 16 118; 16384 x 3002 forward 45, 40).  The others' backward would not keep them in registers; with 16, only
+  // the widest rows' does not, of 1024 threads.
+  constexpr int E = V == 8 ? 32 : 16, W = V > 1 && std::is_same_v<T, __bf16> ? 32 : 16;
   if (a.C <= 2048) return launch<T, V, E, 2048 / E>(a, bwd);
   if (a.C <= 4096) return launch<T, V, E, 4096 / E>(a, bwd);
   if (a.C <= 8192) return launch<T, V, E, 8192 / E>(a, bwd);
-  return launch<T, V, E, 16384 / E>(a, bwd);
+  return launch<T, V, W, 16384 / W>(a, bwd);
 }
 
 }  // namespace

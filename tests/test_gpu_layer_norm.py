@@ -115,7 +115,8 @@ def test_without_some(store, weight, bias, res):
 
 @pytest.mark.parametrize("shape,pad", [((1, 8), 0), ((33, 65), 0), ((65, 136), 0), ((41, 375), 3), ((2, 19, 520), 0),
                                        ((18, 1032), 8), ((9, 2056), 0), ((6, 4099), 0), ((4, 8200), 0),
-                                       ((3, 16383), 0), ((35, 302), 0), ((18, 1034), 6), ((4, 8198), 0)])
+                                       ((3, 16383), 0), ((35, 302), 0), ((18, 1034), 6), ((4, 8198), 0),
+                                       ((5, 5002), 0)])
 def test_gradient_in_32_bits(shape, pad):
     x, w, b, dy, dres = make(sum(shape) + 1, shape, "bf16", pad)
     dy = torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
