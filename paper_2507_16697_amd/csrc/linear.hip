@@ -81,8 +81,11 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(GemmArgs a) {
   };
   constexpr int kTurns = WAVES * 32 * kSteps;   // of K, from a wave's turn to its next
   int at = 0;                                   // the turn's buffer
-  if constexpr (VEC) load(wave * 32 * kSteps, base);
-  for (int k0 = wave * 32 * kSteps; k0 < K; k0 += kTurns) {
+  const int first = wave * 32 * kSteps;
+  if constexpr (VEC) {
+    if (first < K) load(first, base);           // a short K leaves waves without a turn
+  }
+  for (int k0 = first; k0 < K; k0 += kTurns) {
     if constexpr (VEC) {
       if (k0 + kTurns < K) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what lies there has been read
@@ -120,6 +123,9 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(GemmArgs a) {
     at = kTurn - at;
   }
   f32x4* const sums = reinterpret_cast<f32x4*>(lds) + lane;   // [wave][block][lane]
+  // The sums lie where every wave's loads go: none may be in flight, whichever way the wave came here.  The compiler
+  // does not wait for loads that are inline assembly.
+  if constexpr (VEC) wait_vmem_all();
   __syncthreads();
 #pragma unroll
   for (int m = 0; m < MB * NB; ++m) sums[(wave * MB * NB + m) * 64] = acc[m];
