@@ -74,3 +74,41 @@ def test_few_rows_has_no_load_in_flight_at_a_barrier(asm):
     assert len(with_loads) == 14     # seven forms of blocks, four waves and eight
     for name in with_loads:
         assert not reached_in_flight(some[name]), name
+
+
+@pytest.mark.parametrize("src,load", [
+    ("linear.hip", r"global_load_lds_dwordx4 v\[\d+:\d+\], off$"),
+    ("gemm_bf16.hip", r"buffer_load_dwordx4 v\d+, s\[\d+:\d+\], 0 offen lds$"),
+    ("gemm_f32.hip", r"buffer_load_dwordx4 v\d+, s\[\d+:\d+\], 0 offen lds$")])
+def test_m0_only_feeds_direct_loads(src, load, asm):
+    code = [l.split(";")[0].strip() for l in asm(src).splitlines()]
+    code = [l for l in code if l and not l.startswith(".")]
+    uses = [i for i, l in enumerate(code) if re.search(r"\bm0\b", l)]
+    assert uses and len(uses) == sum(bool(re.match(load, l)) for l in code)
+    for i in uses:
+        assert re.match(r"s_mov_b32 m0, s\d+$", code[i]), code[i]
+        assert code[i + 1] == "s_nop 0", code[i + 1]
+        assert re.match(load, code[i + 2]), code[i + 2]
+
+
+# (source, part of the kernel's name, kernels, products along r that each holds)
+PRODUCTS = [("gemm_bf16.hip", "gemm_bf16_kernel", 9, 1), ("gemm_bf16.hip", "gemm_pair_kernel", 2, 2),
+            ("gemm_f32.hip", r"gemm_f32_kernel\S*Li(?:128|64)E", 6, 1), ("gemm_f32.hip", r"gemm_f32_pair_kernel\S*Li64E", 1, 2)]
+
+
+@pytest.mark.parametrize("src,fragment,count,products", PRODUCTS)
+def test_a_step_waits_for_its_loads_once(src, fragment, count, products, asm):
+    """The loop of a product of tiles, from its first matrix instruction to its last, waits for vector memory once,
+    right before its barrier: a wait beside the products would be one for the loads of a later step."""
+    some = kernels(asm(src), fragment)
+    assert len(some) == count
+    for name, lines in some.items():
+        at = [i for i, l in enumerate(lines) if l.startswith("v_mfma")]
+        # a kernel of two products has two loops, far apart
+        cuts = [0] + [k for k in range(1, len(at)) if at[k] - at[k - 1] > 300] + [len(at)]
+        loops = [lines[at[a]:at[b - 1]] for a, b in zip(cuts, cuts[1:])]
+        assert len(loops) == products, name
+        for loop in loops:
+            waits = [i for i, l in enumerate(loop) if l.startswith("s_waitcnt") and "vmcnt" in l]
+            assert len(waits) == 1 and "vmcnt(0)" in loop[waits[0]], name
+            assert any(l == "s_barrier" for l in loop[waits[0]:waits[0] + 4]), name
