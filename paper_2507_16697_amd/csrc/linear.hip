@@ -9,8 +9,6 @@
 namespace ringx {
 namespace {
 
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
-
 // -------------------------------------------------------------------------------------------------
 // A few rows (a token at a time, or some of them), bf16.  Bound by the weights' bytes: every weight is
 // loaded once, for v_mfma_f32_16x16x32_bf16 (lane l: row l % 16, r = 8 (l / 16) .. + 7), NB blocks of 16 features
