@@ -446,7 +446,8 @@ size_t ringx_qkv_norm_rope_bwd_workspace_bytes(int64_t B, int64_t N, int64_t H, 
  *   mean = sum_c x_c / C;  r = (sum_c (x_c - mean)^2 / C + eps)^(-1/2);  y_c = (x_c - mean) r weight_c + bias_c.
  *   x [rows, C] (dtype), row n at element n row_stride (not looked at for one row); a row is contiguous.
  *   y [rows, C] (dtype), contiguous.  weight, bias [C] fp32, either or both NULL for 1 and 0.
- *   stats [2, rows] fp32 or NULL: mean and r of every row, the backward's input.
+ *   stats [2, rows] fp32 or NULL: mean and r of every row, the backward's input; NaN, as the whole row of y,
+ *   where the row holds an infinity or NaN.
  * fp32 arithmetic, one rounding at the end; the squares' sum has to stay in fp32's range.
  * RINGX_E_NORM unless 1 <= C <= 16384, row_stride >= C, eps >= 0 and finite.
  */

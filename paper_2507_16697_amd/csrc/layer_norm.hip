@@ -217,8 +217,8 @@ __global__ __launch_bounds__((kGroup<TPR, false>)) void layer_norm_kernel(NormAr
     }
     const f32x2 ss = sum(s1, s2, slot);
     const float m1 = ss[0] * inv;   // what m0 is off by
-    const float var = fmaxf(__builtin_fmaf(-m1, m1, ss[1] * inv), 0.f);
-    const float r = 1.f / sqrtf(var + a.eps);
+    const float var = __builtin_fmaf(-m1, m1, ss[1] * inv);
+    const float r = 1.f / sqrtf((var < 0.f ? 0.f : var) + a.eps);   // a row that holds NaN has none
 #pragma unroll
     for (int e = 0; e < E; ++e) d[e] = __builtin_fmaf((d[e] - m1) * r, w[e], b[e]);
     if (row < a.rows) {
