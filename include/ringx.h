@@ -80,7 +80,7 @@ typedef enum ringx_dtype RINGX_ENUM_BASE { RINGX_FP32 = 0, RINGX_BF16 = 1 } ring
 /* Activations of ringx_linear. */
 typedef enum ringx_act RINGX_ENUM_BASE {
   RINGX_ACT_NONE = 0,
-  RINGX_ACT_GELU = 1,       /* z Phi(z), Phi the normal distribution                       */
+  RINGX_ACT_GELU = 1,       /* z Phi(z), Phi the normal distribution (to 2.3e-7 below 0)   */
   RINGX_ACT_GELU_TANH = 2,  /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2           */
   RINGX_ACT_SILU = 3        /* z / (1 + exp(-z))                                           */
 } ringx_act;
@@ -491,8 +491,8 @@ size_t ringx_layer_norm_bwd_workspace_bytes(int64_t rows, int64_t C, ringx_dtype
  *   workspace: ringx_linear_workspace_bytes(...) bytes (0 for many shapes), 16-byte aligned, contents ignored:
  *   parts of products whose rows and features are few, operands whose rows do not come in 16-byte pieces.
  * RINGX_E_LINEAR unless 1 <= K, O <= 2^20, M <= 2^31 - 1024, x_stride >= K (heads = 0), heads divides K and
- * tokens M (heads > 0), and act is one of ringx_act; RINGX_E_SHAPE for products of more than 2^24 tiles of
- * 128 x 128 (bf16) or 32 x 32 (fp32).
+ * tokens M (heads > 0), and act is one of ringx_act; RINGX_E_SHAPE where M x O, M x K or O x K is 2^24 tiles of
+ * 128 x 128 (bf16) or 32 x 32 (fp32) or more, in either direction.
  */
 ringx_status ringx_linear(const void* x, int64_t x_stride, int64_t heads, int64_t tokens,
                           const void* w, const float* bias, const void* residual, void* y, void* pre,

@@ -17,8 +17,10 @@ namespace {
 //
 // VEC: both go through the wave's own LDS, since a fragment's load touches 16 lines at a time and takes four times
 // as long as one of whole 64-byte pieces: lane l loads row l / 4 of a block, piece l % 4, XORed with (row / 4) so
-// that 16 rows' same piece lies in 16 places.  Two buffers: the next turn's loads are in flight while a turn is
-// multiplied.
+// that 16 rows' same piece lies in 16 places.  (Bank conflicts are 3.8 cycles to an LDS instruction all the same; with
+// the row's two bits the other way round the times were equal.  LDS is not what it waits for.)  Two buffers: the next
+// turn's loads are in flight while a turn is multiplied.  One row of 2048 to 8192: 5.8 us where the memory-side cache
+// holds the weights, 9.9 where they come from HBM.
 
 template <int MB, int NB, int WAVES, bool VEC>
 __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(GemmArgs a) {

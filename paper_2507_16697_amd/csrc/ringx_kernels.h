@@ -680,9 +680,16 @@ struct LinearPlan {
 };
 constexpr int64_t kLinearMaxWidth = int64_t(1) << 20;   // of K and O
 constexpr int64_t kLinearMaxRows = (int64_t(1) << 31) - 1024;   // 32-bit positions, a step of headroom
-// bf16 rows up to which the kernel for a few of them is taken.  us of it and of the tiles, K 2048 to O 2048: one row
-// 4.7 / 14.8, 64 6.8 / 14.9; 4096 to 4096: 6.7 / 18.8, 13.7 / 18.9; 4096 to 16384: 23.3 / 31.5, 35.0 / 32.7;
-// 8192 to 2048: 8.7 / 19.5, 21.0 / 19.7.
+// bf16 rows up to which the kernel for a few of them is taken.  us of it and of the tiles, in a graph, weights from HBM
+// (in brackets: held by the memory-side cache):
+//                     1 row                   16                      32                      64
+//   2048 to 2048       4.9 / 15.1 (3.9 / 14)   5.2 / 15.2 (4.1 / 14)   6.4 / 15.3 (5.1 / 14)   7.7 / 15.2 (5.8 / 14)
+//   2048 to 8192       9.9 / 20.1 (5.8 / 18)  11.2 / 20.4 (7.0 / 18)  12.3 / 20.4 (8.5 / 18)  14.5 / 20.6 (10 / 18)
+//   4096 to 4096       9.3 / 19.7 (5.8 / 18)  11.0 / 19.8 (7.3 / 18)  14.0 / 19.8 (9.7 / 18)  19.3 / 20.0 (13 / 18)
+//   4096 to 16384     26.8 / 41.0 (22 / 31)   32.2 / 40.5 (24 / 31)   37.7 / 41.1 (31 / 32)   47.5 / 41.2 (34 / 32)
+//   8192 to 2048      12.2 / 20.8 (7.8 / 19)  15.5 / 20.7 (10 / 19)   22.0 / 20.7 (14 / 19)   32.2 / 20.7 (20 / 19)
+// The rows alone decide, which is right but for much of K and more than 16 rows: there the tiles would take up to a
+// third less time (K 8192, 64 rows), at the price of a workspace for the parts of r.
 constexpr int64_t kFewRows = 64;
 // Offsets of an operand's tile are 31 bits: rows of at most 2^21 values, heads whose batch has at most 2^29.
 inline bool linear_near(const LinearShape& s) {
