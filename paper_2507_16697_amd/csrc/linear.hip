@@ -151,10 +151,13 @@ hipError_t launch_few_rows_as(const GemmArgs& a) {
   const dim3 grid((uint32_t)((a.J + 16 * NB - 1) / (16 * NB)));
   // 4 waves; 8 where there are few workgroups and much of K (us of 8 / 4: one row of 8192 to 2048 8.7 / 10.6, of 2048
   // to 8192 7.8 / 6.5; 64 rows of 2048 to 2048 6.8 / 9.2)
-  if (grid.x <= 256 && a.R >= 1024)
-    hipLaunchKernelGGL((few_rows_kernel<MB, NB, 8, VEC>), grid, dim3(512), 0, a.stream, a);
-  else
-    hipLaunchKernelGGL((few_rows_kernel<MB, NB, 4, VEC>), grid, dim3(256), 0, a.stream, a);
+  if constexpr (VEC || MB == 1) {   // others have less of K (linear_few)
+    if (grid.x <= 256 && a.R >= 1024) {
+      hipLaunchKernelGGL((few_rows_kernel<MB, NB, 8, VEC>), grid, dim3(512), 0, a.stream, a);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((few_rows_kernel<MB, NB, 4, VEC>), grid, dim3(256), 0, a.stream, a);
   return hipGetLastError();
 }
 
@@ -428,10 +431,7 @@ hipError_t forward(const LinearArgs& a) {
   g.o.out = a.y, g.o.pre = a.pre, g.o.residual = a.residual, g.o.bias = a.bias, g.o.J = a.s.O;
   g.o.act = a.act;
   if constexpr (std::is_same_v<T, __bf16>) {
-    if (p.few) {
-      const bool vec = a.s.K % 8 == 0 && (a.s.heads ? a.s.K / a.s.heads % 8 == 0 : a.s.ldx % 8 == 0);
-      return vec ? launch_few_rows<true>(g) : launch_few_rows<false>(g);
-    }
+    if (p.few) return linear_few_pieces(a.s) ? launch_few_rows<true>(g) : launch_few_rows<false>(g);
   }
   const hipError_t e = pack<T>(&g.P, p.x, p.ldx, &g.Q, p.w, p.ldw, a.workspace, a.stream);
   if (e != hipSuccess) return e;

@@ -680,17 +680,34 @@ struct LinearPlan {
 };
 constexpr int64_t kLinearMaxWidth = int64_t(1) << 20;   // of K and O
 constexpr int64_t kLinearMaxRows = (int64_t(1) << 31) - 1024;   // 32-bit positions, a step of headroom
-// bf16 rows up to which the kernel for a few of them is taken.  us of it and of the tiles, in a graph, weights from HBM
-// (in brackets: held by the memory-side cache):
-//                     1 row                   16                      32                      64
-//   2048 to 2048       4.9 / 15.1 (3.9 / 14)   5.2 / 15.2 (4.1 / 14)   6.4 / 15.3 (5.1 / 14)   7.7 / 15.2 (5.8 / 14)
-//   2048 to 8192       9.9 / 20.1 (5.8 / 18)  11.2 / 20.4 (7.0 / 18)  12.3 / 20.4 (8.5 / 18)  14.5 / 20.6 (10 / 18)
-//   4096 to 4096       9.3 / 19.7 (5.8 / 18)  11.0 / 19.8 (7.3 / 18)  14.0 / 19.8 (9.7 / 18)  19.3 / 20.0 (13 / 18)
-//   4096 to 16384     26.8 / 41.0 (22 / 31)   32.2 / 40.5 (24 / 31)   37.7 / 41.1 (31 / 32)   47.5 / 41.2 (34 / 32)
-//   8192 to 2048      12.2 / 20.8 (7.8 / 19)  15.5 / 20.7 (10 / 19)   22.0 / 20.7 (14 / 19)   32.2 / 20.7 (20 / 19)
-// The rows alone decide, which is right but for much of K and more than 16 rows: there the tiles would take up to a
-// third less time (K 8192, 64 rows), at the price of a workspace for the parts of r.
+// Whether a bf16 layer takes the kernel for a few rows, and whether its operands come there in 16-byte pieces.  That
+// kernel reads the rows again for every 16 features and splits K over one workgroup's waves alone, so it is for up to
+// 64 rows and not much of K for each 16 of them: 16384; 2048 where the weights' rows are no whole pieces, which the
+// tiles copy first, 1024 where only those of x are not.  us of it and of the tiles, in a graph, weights from HBM:
+//                      1 row         16            32            64
+//   2048 to 2048        4.9 / 15.1    5.2 / 15.2    6.4 / 15.3    7.7 / 15.2
+//   4096 to 4096        9.3 / 19.7   11.0 / 19.8   14.0 / 19.8   19.3 / 20.0
+//   4096 to 16384      26.7 / 41.2   32.1 / 41.1   38.1 / 41.0   46.8 / 41.5
+//   8192 to 2048       11.6 / 20.5   15.2 / 20.6   21.9 / 20.7   32.7 / 20.7
+//   8192 to 8192       28.4 / 42.3   32.7 / 43.8   39.2 / 44.1   49.4 / 44.9
+//   16384 to 1024      17.3 / 23.4   26.0 / 23.5   39.5 / 23.5   62.3 / 23.5
+//   65536 to 64        33.5 / 26.2   55.9 / 26.5   98.4 / 26.6    162 / 26.6
+//   375 to 2048         5.1 / 12.1    5.8 / 12.2    7.4 / 12.2   11.2 / 12.6
+//   1023 to 8192       16.4 / 27.1   20.8 / 27.1   27.2 / 27.0   53.0 / 27.5
+//   2047 to 2048       15.3 / 24.3   19.7 / 24.8   26.1 / 25.0   51.5 / 25.0
+//   4095 to 1024       26.8 / 25.6   35.5 / 26.5   47.5 / 26.6   76.9 / 26.5
+//   4097 to 4096       26.9 / 43.0   39.9 / 43.7   51.4 / 43.8   79.8 / 44.1
+//   512, stride 513, to 2048   7.1 / 10.5    6.9 / 11.0    9.0 / 11.1   14.5 / 11.4
+//   1024, 1025, to 1024       11.4 / 14.1   11.1 / 14.5   14.1 / 14.5   25.1 / 14.4
+//   2048, 2049, to 8192       41.8 / 23.4   41.1 / 23.8   56.0 / 23.7   95.6 / 23.9
 constexpr int64_t kFewRows = 64;
+inline bool linear_few_pieces(const LinearShape& s) {
+  return s.K % 8 == 0 && (s.heads ? s.K / s.heads % 8 == 0 : s.ldx % 8 == 0);
+}
+inline bool linear_few(const LinearShape& s) {
+  const int64_t most = linear_few_pieces(s) ? 16384 : s.K % 8 ? 2048 : 1024;
+  return s.M <= kFewRows && (s.M + 15) / 16 * s.K <= most;
+}
 // Offsets of an operand's tile are 31 bits: rows of at most 2^21 values, heads whose batch has at most 2^29.
 inline bool linear_near(const LinearShape& s) {
   return s.heads ? s.tokens * s.K <= (int64_t(1) << 29) : s.ldx <= (int64_t(1) << 21);
@@ -700,7 +717,7 @@ inline LinearPlan linear_plan(const LinearShape& s) {
   const int64_t Kp = (s.K + 7) / 8 * 8;
   p.R = s.K;
   if (s.bf16) {
-    p.few = s.M <= kFewRows;
+    p.few = linear_few(s);
     if (p.few) return p;
     p.R = Kp;
     const bool fits = s.K % 8 == 0 && linear_near(s) && (s.heads ? s.K / s.heads % 64 == 0 : s.ldx % 8 == 0);

@@ -93,7 +93,8 @@ def test_m0_only_feeds_direct_loads(src, load, asm):
 
 # (source, part of the kernel's name, kernels, products along r that each holds)
 PRODUCTS = [("gemm_bf16.hip", "gemm_bf16_kernel", 9, 1), ("gemm_bf16.hip", "gemm_pair_kernel", 2, 2),
-            ("gemm_f32.hip", r"gemm_f32_kernel\S*Li(?:128|64)E", 6, 1), ("gemm_f32.hip", r"gemm_f32_pair_kernel\S*Li64E", 1, 2)]
+            ("gemm_f32.hip", r"gemm_f32_kernel\S*Li(?:128|64)E", 6, 1),
+            ("gemm_f32.hip", r"gemm_f32_pair_kernel\S*Li64E", 1, 2)]
 
 
 @pytest.mark.parametrize("src,fragment,count,products", PRODUCTS)
