@@ -11,8 +11,8 @@
 // 1.9 to 1.4 GHz (it does for the library's product too); zeros take 20% less time.  And what stands beside the
 // products: the cores are busy for 73% of the cycles (1390 TFLOP/s; the library's product 87%, 1630), for 62% of them
 // at 32768 x 2048 to 6144 with its twelve starts and ends of tiles (75%), with 0.38 LDS instructions to a product
-// (0.25); by rocprofv3's counters.  Launches without the barriers took 4% less, deeper buffers (four of 32 of r) 6% more,
-// wave tiles of 128 x 128 from four waves as much.
+// (0.25); by rocprofv3's counters.  Launches without the barriers took 4% less, deeper buffers (four of 32 of r) 6%
+// more, wave tiles of 128 x 128 from four waves as much.
 
 #include "gemm_feed.h"
 #include "linear.h"

@@ -684,7 +684,7 @@ constexpr int64_t kLinearMaxRows = (int64_t(1) << 31) - 1024;   // 32-bit positi
 // kernel reads the rows again for every 16 features and splits K over one workgroup's waves alone, so it is for up to
 // 64 rows and not much of K for each 16 of them: 16384; 2048 where the weights' rows are no whole pieces, which the
 // tiles copy first, 1024 where only those of x are not.  us of it and of the tiles, in a graph, weights from HBM:
-//                      1 row         16            32            64
+//                      1 row (2)     16            32            64      (2: where rows are no whole pieces)
 //   2048 to 2048        4.9 / 15.1    5.2 / 15.2    6.4 / 15.3    7.7 / 15.2
 //   4096 to 4096        9.3 / 19.7   11.0 / 19.8   14.0 / 19.8   19.3 / 20.0
 //   4096 to 16384      26.7 / 41.2   32.1 / 41.1   38.1 / 41.0   46.8 / 41.5
